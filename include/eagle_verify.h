@@ -459,6 +459,182 @@ int eagle_tree_commit_paged(const eagle_commit_desc* desc, const eagle_paged_kv*
 int eagle_tree_build_mask(const int32_t* tree_parent, const int32_t* tree_sizes, int32_t batch, int32_t max_tree,
                           uint64_t* anc_mask, uint8_t* depth, int32_t* status, eagle_stream_t stream);
 
+/*
+ * ---------------------------------------------------------------------------------------------------------------------
+ * Around the verification step: rotary positions written into the cache, attention of a prompt's chunk, and penalties,
+ * biases and grammar masks on the rows that acceptance reads.
+ */
+
+/*
+ * A cache as the calls below take it, in any of its storage forms (see eagle_tree_verify_attn, eagle_paged_kv and
+ * eagle_tree_verify_attn_fp8 for the layouts).
+ */
+typedef struct eagle_kv_store {
+  void* k;                      /* device bf16, or uint8 e4m3 codes when the scales are set; 16-byte aligned:
+                                   [B, Hkv, kv_capacity, D], or [num_pages, Hkv, page_size, D] with a block table */
+  void* v;
+  const float* k_scale;         /* device fp32 [B, Hkv], both or neither: the cache holds codes (head_dim 128) */
+  const float* v_scale;
+  int32_t kv_capacity;          /* slots per (sequence, KV head); ignored with a block table */
+  const int32_t* block_table;   /* device int32 [B, max_pages_per_seq], or NULL: contiguous */
+  int32_t num_pages;            /* pages in the pool, >= 1 */
+  int32_t page_size;            /* a power of two, >= 16 */
+  int32_t max_pages_per_seq;
+} eagle_kv_store;
+
+/* How rotary frequencies are stretched for contexts beyond the trained one. */
+enum {
+  EAGLE_ROPE_PLAIN = 0,         /* f_m = base^(-2m / R) */
+  EAGLE_ROPE_LINEAR = 1,        /* f_m / factor */
+  EAGLE_ROPE_NTK = 2,           /* base replaced by base * factor^(R / (R - 2)) */
+  EAGLE_ROPE_YARN = 3,          /* f_m / factor below a band of wavelengths, f_m above it, a ramp between; amplitude 0.1 ln(factor) + 1 */
+  EAGLE_ROPE_BANDED = 4         /* f_m / factor for wavelengths over context / low, f_m under context / high, blended between */
+};
+typedef struct eagle_rope_scaling {
+  int32_t kind;                 /* EAGLE_ROPE_* */
+  int32_t rotary_dim;           /* R: even, >= 2 (NTK: >= 4) */
+  double base;                  /* > 1 */
+  double factor;                /* >= 1 (all kinds but PLAIN) */
+  double context;               /* the trained context, > 0 (YARN, BANDED) */
+  double low, high;             /* YARN: turns over the trained context at the band's ends, high > low > 0 (32 and 1 are usual: high = 32,
+                                   low = 1); BANDED: 0 < low < high (1 and 4 are usual) */
+} eagle_rope_scaling;
+
+/*
+ * Rotary frequencies (host function, no CUDA work): freqs, host double [R / 2], in radians per position, and the amplitude
+ * that sines and cosines are to be multiplied by (1 for all kinds but YARN).
+ *   YARN: with d(t) = R ln(context / (2 pi t)) / (2 ln base), lo = max(floor(d(high)), 0), hi = min(ceil(d(low)), R - 1) (hi = lo + 0.001
+ *   if they are equal), ramp = clamp((m - lo) / (hi - lo), 0, 1): f_m (1 - ramp) + f_m / factor * ramp.
+ *   BANDED: with the wavelength w = 2 pi / f_m and s = (context / w - low) / (high - low) between the two borders: (1 - s) f_m / factor + s f_m.
+ * EAGLE_ERR_NULL / EAGLE_ERR_SHAPE on bad arguments.
+ */
+int eagle_rope_frequencies(const eagle_rope_scaling* scaling, double* freqs, float* amplitude);
+
+typedef struct eagle_rope_desc {
+  int32_t batch;                /* B, 0 .. 65535 */
+  int32_t num_tokens;           /* N >= 0: rows of q, k, v and q_out (chunk form) */
+  int32_t max_tree;             /* T_max <= 64 (tree form; q, k, v and q_out have B * T_max rows) */
+  int32_t num_q_heads;          /* Hq >= 0 (0: only the cache is written) */
+  int32_t num_kv_heads;         /* Hkv >= 1 */
+  int32_t head_dim;             /* D: 64 or 128 */
+  int32_t rotary_dim;           /* R: a multiple of 16, <= D: the first R elements of each head turn, the others stay */
+  int32_t interleaved;          /* 0: element m turns with m + R/2; nonzero: element 2m with 2m + 1 */
+  float amplitude;              /* factor on sines and cosines; 0 means 1 */
+  int64_t q_stride, k_stride, v_stride;   /* elements from one row to the next: multiples of 8, at least heads * D (slices of one
+                                   projection's output need no copy); 0 means heads * D.  A row's heads are dense. */
+  const double* freqs;          /* device double [R / 2], radians per position */
+  const int32_t* positions;     /* chunk form: device int32 [N], or NULL: a token's position is its slot */
+  const int32_t* tree_sizes;    /* tree form: device int32 [B] ([1] when shared_tree is set), or NULL */
+  int32_t shared_tree;          /* tree form, nonzero: tree_parent is int32 [T_max], one tree for every sequence */
+  int32_t* status;              /* device int32 or NULL */
+} eagle_rope_desc;
+
+/*
+ * Rotary positions of new tokens, and their keys and values into the cache, in one launch.
+ *
+ *   q, k, v     device bf16 [N, Hq, D], [N, Hkv, D], [N, Hkv, D] with the descriptor's strides, 16-byte aligned
+ *   seq_lens    device int32 [B]      L_b: slots of the cache that are in use already
+ *   token_start device int32 [B + 1]  ascending: rows token_start[b] .. token_start[b + 1] - 1 are sequence b's new tokens, in order
+ *   q_out       device bf16 [N, Hq, D] dense, 16-byte aligned; may be q itself when q is dense
+ *
+ * Token i of sequence b turns by position L_b + i (or positions[row]) and goes to slot L_b + i.  Pair (x, y) of frequency f at
+ * position p becomes amplitude * (x cos pf - y sin pf, y cos pf + x sin pf); the angle is reduced in fp64, the rotation is
+ * fp32, rounded once.  Keys of an fp8 cache are stored as the nearest e4m3 code of key / k_scale[b, h] (magnitudes above
+ * 448 become 448), values likewise.  Nothing else in the cache changes.  Rows outside every sequence (behind the last one) are
+ * neither read nor written.  A sequence with L_b < 0 or more tokens than its slots reports EAGLE_ERR_SEQ: its rows of q_out
+ * are zeros and nothing of it is stored; starts that descend or leave [0, N] report it too, and rows that they do not place
+ * are left alone.  A token whose page is outside the pool reports EAGLE_ERR_PAGE and is not stored.
+ */
+int eagle_rope_append(const eagle_rope_desc* desc, const void* q, const void* k, const void* v, void* q_out, const eagle_kv_store* kv,
+                      const int32_t* seq_lens, const int32_t* token_start, eagle_stream_t stream);
+
+/*
+ * The same for the nodes of draft trees, in the layout of eagle_tree_verify_attn: q, k, v and q_out have rows [B, T_max], node i
+ * of sequence b turns by position L_b + depth(i) - 1 (top-level nodes have depth 1: siblings share a position) and goes to slot
+ * L_b + i.  Rows of nodes >= tree size are left alone.  An invalid tree reports EAGLE_ERR_TREE, a tree that does not fit
+ * EAGLE_ERR_SEQ: the sequence's rows of q_out are zeros and nothing of it is stored.
+ */
+int eagle_tree_rope_append(const eagle_rope_desc* desc, const void* q, const void* k, const void* v, void* q_out, const eagle_kv_store* kv,
+                           const int32_t* seq_lens, const int32_t* tree_parent, eagle_stream_t stream);
+
+typedef struct eagle_chunk_desc {
+  int32_t batch;                /* B, 0 .. 65535 */
+  int32_t num_tokens;           /* N >= 0: rows of q and out */
+  int32_t num_q_heads;          /* Hq; Hq % Hkv == 0, group size G = Hq / Hkv <= 16 */
+  int32_t num_kv_heads;         /* Hkv */
+  int32_t head_dim;             /* D: 64 or 128 */
+  float sm_scale;               /* softmax scale, > 0; 0 means 1/sqrt(D) */
+  void* workspace;              /* device, 256-byte aligned, >= eagle_chunk_attn_workspace() bytes */
+  size_t workspace_bytes;
+  int32_t* status;              /* device int32 or NULL */
+} eagle_chunk_desc;
+
+/* Bytes of scratch one call with this descriptor needs (host function, no CUDA work); 0 if the shape is unsupported. */
+size_t eagle_chunk_attn_workspace(const eagle_chunk_desc* desc);
+
+/*
+ * Causal attention of one layer for chunks of new tokens: a prompt, a part of one, or single tokens, any mix in one call.
+ *
+ *   q           device bf16 [N, Hq, D], 16-byte aligned   queries, already position-encoded (q_out of eagle_rope_append)
+ *   kv          the cache, bf16, contiguous or paged, with the chunk's own keys and values in it
+ *   seq_lens    device int32 [B]      L_b: slots in use before the chunk
+ *   token_start device int32 [B + 1]  as for eagle_rope_append
+ *   out         device bf16 [N, Hq, D], 32-byte aligned   out[t,h,:] = sum_j softmax_j(scale * q[t,h]·k[b,h/G,j]) v[b,h/G,j], j <= L_b + i
+ *                                     for token t = token_start[b] + i of sequence b
+ *
+ * A cache of fp8 codes is EAGLE_ERR_SHAPE.  bf16 inputs, fp32 scores / softmax / accumulation, probabilities rounded to bf16
+ * for the tensor cores, bf16 output.  Slots past the chunk may hold anything.  The values of slots in use have to be finite:
+ * one that is not may reach rows of the same sequence that do not see it (its probability there is 0, and 0 * inf is NaN).
+ * Rows outside every sequence are left as they were.  A sequence with L_b < 0 or L_b + n_b over its slots reports EAGLE_ERR_SEQ,
+ * one with a block-table entry in use outside [0, num_pages) EAGLE_ERR_PAGE: its rows are zeros.  Starts that descend or
+ * leave [0, N] report EAGLE_ERR_SEQ and no row is computed.  Three launches (planner, attention, merge), asynchronous on
+ * `stream`; calls that share a workspace must not overlap on the GPU.
+ */
+int eagle_chunk_attn(const eagle_chunk_desc* desc, const void* q, const eagle_kv_store* kv, const int32_t* seq_lens,
+                     const int32_t* token_start, void* out, eagle_stream_t stream);
+
+#define EAGLE_MAX_BIAS 1024
+
+typedef struct eagle_logits_desc {
+  int32_t batch;                /* B, 0 .. 65535 */
+  int32_t max_tree;             /* T_max <= 64; 0: one row per sequence, no trees */
+  int32_t vocab;                /* V, 1 .. 2^30 */
+  int32_t bf16;                 /* 0: logits are fp32; nonzero: bf16 */
+  const int32_t* tree_sizes;    /* device int32 [B] ([1] when shared_tree is set), or NULL: T_max nodes each */
+  int32_t shared_tree;          /* one tree for every sequence: tree_parent is [T_max] (draft_tokens stay per sequence) */
+  int32_t history_cap;          /* row length of history */
+  const int32_t* history;       /* device int32 [B, history_cap]: the sequence's tokens, prompt first; or NULL: nothing was there before */
+  const int32_t* history_len;   /* device int32 [B] (with history) */
+  const int32_t* prompt_len;    /* device int32 [B], or NULL: all of the history was generated */
+  const float* repetition;      /* device fp32 [B] or NULL (1): rho > 0 */
+  const float* presence;        /* device fp32 [B] or NULL (0): pi */
+  const float* frequency;       /* device fp32 [B] or NULL (0): phi */
+  int32_t max_bias;             /* row length of the bias lists, <= EAGLE_MAX_BIAS */
+  const int32_t* bias_tokens;   /* device int32 [B, max_bias] or NULL */
+  const float* bias_values;     /* device fp32 [B, max_bias] (with bias_tokens); a token listed twice gets the sum */
+  const int32_t* bias_len;      /* device int32 [B], or NULL: max_bias entries each */
+  const uint32_t* allowed;      /* device uint32 [B, T_max + 1, ceil(V / 32)] or NULL: bit v % 32 of word v / 32 is set where token v may follow */
+  int32_t* status;              /* device int32 or NULL */
+} eagle_logits_desc;
+
+/*
+ * Penalties for repeated tokens, biases and grammar masks on the target's rows of a draft tree (T_max = 0: on one row per
+ * sequence, plain decoding), into the fp32 rows that eagle_tree_accept_logits reads.
+ *
+ *   logits       device fp32 or bf16 [B, T_max + 1, V]   row 0: after the context; row i + 1: after tree node i
+ *   draft_tokens device int32 [B, T_max], tree_parent device int32 [B, T_max] ([T_max] when shared_tree is set); unused with T_max = 0
+ *   out          device fp32 [B, T_max + 1, V]; may be `logits` itself when that is fp32
+ *
+ * With c the number of times token v was generated (in the history past the prompt, and on the path from the root to the row's
+ * node, that node included) and seen = c > 0 or v in the prompt:
+ *     z <- seen ? (z > 0 ? z / rho : z * rho) : z;   z <- z - phi c - (c > 0 ? pi : 0);   z <- z + bias(v);   not allowed: -inf
+ * in fp32.  A row whose mask allows nothing is all -inf.  Rows of nodes >= tree size are neither read nor written.  Lengths are clamped to
+ * their rows; a token outside the vocabulary (history, bias list, draft) is ignored and reports EAGLE_ERR_TOKEN; an invalid
+ * tree reports EAGLE_ERR_TREE and all T_max + 1 rows of its sequence become zeros.  One launch; no workspace.
+ */
+int eagle_tree_logits_adjust(const eagle_logits_desc* desc, const void* logits, const int32_t* draft_tokens, const int32_t* tree_parent,
+                             float* out, eagle_stream_t stream);
+
 /* Human-readable name of a return / status code (host function; never NULL). */
 const char* eagle_status_string(int code);
 

@@ -23,7 +23,9 @@ EXPORTS = ["eagle_tree_verify_attn_workspace", "eagle_tree_verify_attn", "eagle_
            "eagle_tree_verify_plan", "eagle_tree_verify_attn_planned", "eagle_tree_verify_attn_planned_paged",
            "eagle_tree_verify_plan_masks", "eagle_set_wait_limit_ns", "eagle_test_stall_kv_producer",
            "eagle_tree_verify_attn_fp8", "eagle_tree_verify_attn_planned_fp8", "eagle_tree_verify_attn_paged_fp8",
-           "eagle_tree_verify_attn_planned_paged_fp8", "eagle_tree_accept_cluster_width_greedy"]
+           "eagle_tree_verify_attn_planned_paged_fp8", "eagle_tree_accept_cluster_width_greedy", "eagle_rope_frequencies",
+           "eagle_rope_append", "eagle_tree_rope_append", "eagle_chunk_attn_workspace", "eagle_chunk_attn",
+           "eagle_tree_logits_adjust"]
 _lib = None
 
 
@@ -66,6 +68,37 @@ class HostStep(ctypes.Structure):
                 [(n, ctypes.c_void_p) for n in ("q", "k_cache", "v_cache", "seq_lens", "tree_sizes", "tree_parent", "target_probs",
                                                 "draft_probs", "draft_tokens", "uniforms", "greedy", "out", "accepted_path",
                                                 "bonus_token", "accept_len", "status", "arena")] + [("arena_bytes", ctypes.c_size_t)])
+
+
+class KVStoreDesc(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("kv_capacity", ctypes.c_int32), ("block_table", ctypes.c_void_p), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32)]
+
+
+class RopeScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("rotary_dim", ctypes.c_int32)] + [(n, ctypes.c_double) for n in ("base", "factor", "context", "low", "high")]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("batch", "num_tokens", "max_tree", "num_q_heads", "num_kv_heads", "head_dim", "rotary_dim",
+                                               "interleaved")] + [("amplitude", ctypes.c_float)] +
+                [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")] +
+                [("freqs", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("tree_sizes", ctypes.c_void_p), ("shared_tree", ctypes.c_int32),
+                 ("status", ctypes.c_void_p)])
+
+
+class ChunkDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("batch", "num_tokens", "num_q_heads", "num_kv_heads", "head_dim")] +
+                [("sm_scale", ctypes.c_float), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("status", ctypes.c_void_p)])
+
+
+class LogitsDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("max_tree", ctypes.c_int32), ("vocab", ctypes.c_int32), ("bf16", ctypes.c_int32),
+                ("tree_sizes", ctypes.c_void_p), ("shared_tree", ctypes.c_int32), ("history_cap", ctypes.c_int32), ("history", ctypes.c_void_p),
+                ("history_len", ctypes.c_void_p), ("prompt_len", ctypes.c_void_p), ("repetition", ctypes.c_void_p), ("presence", ctypes.c_void_p),
+                ("frequency", ctypes.c_void_p), ("max_bias", ctypes.c_int32), ("bias_tokens", ctypes.c_void_p), ("bias_values", ctypes.c_void_p),
+                ("bias_len", ctypes.c_void_p), ("allowed", ctypes.c_void_p), ("status", ctypes.c_void_p)]
 
 
 def load():
@@ -129,6 +162,17 @@ def load():
         lib.eagle_tree_commit_paged.restype = ctypes.c_int
         lib.eagle_tree_build_mask.argtypes = [vp, vp, i32, i32, vp, vp, vp, vp]
         lib.eagle_tree_build_mask.restype = ctypes.c_int
+        lib.eagle_rope_frequencies.argtypes = [ctypes.POINTER(RopeScaling), vp, vp]
+        lib.eagle_rope_frequencies.restype = ctypes.c_int
+        for fn in (lib.eagle_rope_append, lib.eagle_tree_rope_append):
+            fn.argtypes = [ctypes.POINTER(RopeDesc), vp, vp, vp, vp, ctypes.POINTER(KVStoreDesc), vp, vp, vp]
+            fn.restype = ctypes.c_int
+        lib.eagle_chunk_attn_workspace.argtypes = [ctypes.POINTER(ChunkDesc)]
+        lib.eagle_chunk_attn_workspace.restype = ctypes.c_size_t
+        lib.eagle_chunk_attn.argtypes = [ctypes.POINTER(ChunkDesc), vp, ctypes.POINTER(KVStoreDesc), vp, vp, vp, vp]
+        lib.eagle_chunk_attn.restype = ctypes.c_int
+        lib.eagle_tree_logits_adjust.argtypes = [ctypes.POINTER(LogitsDesc), vp, vp, vp, vp, vp]
+        lib.eagle_tree_logits_adjust.restype = ctypes.c_int
         lib.eagle_status_string.argtypes = [ctypes.c_int]
         lib.eagle_status_string.restype = ctypes.c_char_p
         lib.eagle_launch_count.restype = ctypes.c_uint64
@@ -561,6 +605,174 @@ def eagle_tree_commit_paged(k_pages, v_pages, block_table, seq_lens, accepted_pa
                                      _dev(new_seq_lens, torch.int32, "new_seq_lens"), _stream())
     _check(rc, "eagle_tree_commit_paged")
     return new_seq_lens, features_out
+
+
+def _here(t, dtype, name, device, shape=None):
+    """Address of a dense tensor on ``device`` (the current one); None passes through."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise EagleError(f"{name} must be a contiguous {dtype} tensor on {device}" + (f" of shape {tuple(shape)}" if shape is not None else ""))
+    return t.data_ptr()
+
+
+def _current(t, name):
+    """The device of ``t``, which has to be the current one: the call is enqueued on its current stream."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise EagleError(f"{name} must be on the current CUDA device")
+    return t.device
+
+
+class KVStore:
+    """A cache as the calls around verification take it: k / v [B,Hkv,S,D], or [num_pages,Hkv,page_size,D] with ``block_table``
+    [B,max_pages_per_seq] int32; bf16, or uint8 e4m3 codes with ``k_scale`` / ``v_scale`` fp32 [B,Hkv].  Holds the tensors."""
+
+    def __init__(self, k, v, *, block_table=None, k_scale=None, v_scale=None):
+        if k.dim() != 4 or k.shape != v.shape or (k_scale is None) != (v_scale is None) or (block_table is not None and block_table.dim() != 2):
+            raise EagleError("bad cache: k and v of one 4-d shape, both scales or neither, a 2-d block table")
+        self.k, self.v, self.block_table, self.k_scale, self.v_scale = k, v, block_table, k_scale, v_scale
+        self.num_kv_heads, self.head_dim, self.fp8 = k.shape[1], k.shape[3], k_scale is not None
+        self.batch = k.shape[0] if block_table is None else block_table.shape[0]
+        dtype, dev = torch.uint8 if self.fp8 else torch.bfloat16, k.device
+        scales = torch.Size((self.batch, self.num_kv_heads))
+        paged = block_table is not None
+        self.desc = KVStoreDesc(_here(k, dtype, "k", dev), _here(v, dtype, "v", dev), _here(k_scale, torch.float32, "k_scale", dev, scales),
+                                _here(v_scale, torch.float32, "v_scale", dev, scales), 0 if paged else k.shape[2],
+                                _here(block_table, torch.int32, "block_table", dev), k.shape[0] if paged else 0, k.shape[2] if paged else 0,
+                                block_table.shape[1] if paged else 0)
+
+
+ROPE_KINDS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "banded": 4}
+
+
+def eagle_rope_frequencies(rotary_dim, base=10000.0, kind="plain", factor=1.0, context=0.0, low=1.0, high=32.0, device=None):
+    """Rotary frequencies (fp64 [rotary_dim / 2], radians per position, on ``device`` or the host) and the amplitude."""
+    if kind not in ROPE_KINDS:
+        raise EagleError(f"unknown kind of scaling {kind!r}")
+    freqs, amplitude = torch.empty(max(int(rotary_dim), 0) // 2, dtype=torch.float64), ctypes.c_float(0.0)
+    s = RopeScaling(ROPE_KINDS[kind], int(rotary_dim), float(base), float(factor), float(context), float(low), float(high))
+    _check(load().eagle_rope_frequencies(ctypes.byref(s), freqs.data_ptr() or None, ctypes.byref(amplitude)), "eagle_rope_frequencies")
+    return (freqs if device is None else freqs.to(device)), float(amplitude.value)
+
+
+def _rope_rows(t, name, lead, dev):
+    """(address, elements from row to row) of [..., heads, D] bf16 whose rows lie a constant stride apart, heads dense within."""
+    D = t.shape[-1]
+    if t.dtype != torch.bfloat16 or t.device != dev or t.shape[:-2] != lead or t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != D):
+        raise EagleError(f"{name} must be bf16 [..., heads, D] on {dev} with dense heads, rows as the other tensors")
+    row = t.stride(-3)
+    if len(lead) == 2 and lead[0] > 1 and lead[1] > 0 and t.stride(0) != lead[1] * row:
+        if lead[1] > 1:
+            raise EagleError(f"{name} must have its rows a constant stride apart")
+        row = t.stride(0)
+    return t.data_ptr(), row
+
+
+def _rope_append(name, tree, q, k, v, kv, seq_lens, order, freqs, q_out, interleaved, amplitude, positions, tree_sizes, shared_tree, status):
+    dev, lead = _current(q, "q"), q.shape[:-2]
+    if q.dim() != (4 if tree else 3) or k.dim() != q.dim() or v.dim() != q.dim():
+        raise EagleError("q, k, v must be " + ("[B, T, heads, D]" if tree else "[N, heads, D]"))
+    B, Hq, Hkv, D = seq_lens.numel(), q.shape[-2], k.shape[-2], q.shape[-1]
+    if k.shape[-1] != D or v.shape[-2:] != k.shape[-2:] or kv.head_dim != D or kv.num_kv_heads != Hkv or kv.batch != B or kv.k.device != dev or \
+            freqs.dim() != 1 or (tree and lead[0] != B):
+        raise EagleError("inconsistent shapes")
+    T = lead[1] if tree else 0
+    if tree:
+        _check_tree(order, tree_sizes, B, T, shared_tree)
+    elif order.shape != (B + 1,):
+        raise EagleError("token_start must be [B + 1]")
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+    qp, qs = _rope_rows(q, "q", lead, dev)
+    kp, ks = _rope_rows(k, "k", lead, dev)
+    vp, vs = _rope_rows(v, "v", lead, dev)
+    d = RopeDesc(B, 0 if tree else lead[0], T, Hq, Hkv, D, 2 * freqs.shape[0], 1 if interleaved else 0, float(amplitude), qs, ks, vs,
+                 _here(freqs, torch.float64, "freqs", dev), _here(positions, torch.int32, "positions", dev, lead),
+                 _here(tree_sizes, torch.int32, "tree_sizes", dev), 1 if shared_tree else 0, _here(status, torch.int32, "status", dev))
+    rc = getattr(load(), name)(ctypes.byref(d), qp, kp, vp, _here(q_out, torch.bfloat16, "q_out", dev, q.shape), ctypes.byref(kv.desc),
+                               _here(seq_lens, torch.int32, "seq_lens", dev), _here(order, torch.int32, "tree_parent" if tree else "token_start", dev),
+                               _stream())
+    _check(rc, name)
+    return q_out
+
+
+def eagle_rope_append(q, k, v, kv, seq_lens, token_start, freqs, q_out=None, *, interleaved=False, amplitude=1.0, positions=None, status=None):
+    """Rotary positions of packed new tokens, keys and values into the cache ``kv`` (a ``KVStore``) IN PLACE.  q [N,Hq,D], k / v
+    [N,Hkv,D] bf16 (slices of one projection's rows are taken as they are); token_start [B+1] int32; freqs fp64 [R/2].
+    Returns q_out [N,Hq,D]; rows outside every sequence are left as they are."""
+    return _rope_append("eagle_rope_append", False, q, k, v, kv, seq_lens, token_start, freqs, q_out, interleaved, amplitude, positions, None, False,
+                        status)
+
+
+def eagle_tree_rope_append(q, k, v, kv, seq_lens, tree_parent, freqs, q_out=None, *, tree_sizes=None, interleaved=False, amplitude=1.0,
+                           status=None, shared_tree=False):
+    """The same for the nodes of draft trees: q [B,T,Hq,D], k / v [B,T,Hkv,D]; a node's position is its sequence's length plus
+    its depth - 1, its slot the length plus its index."""
+    return _rope_append("eagle_tree_rope_append", True, q, k, v, kv, seq_lens, tree_parent, freqs, q_out, interleaved, amplitude, None, tree_sizes,
+                        shared_tree, status)
+
+
+def eagle_chunk_attn_workspace(batch, num_tokens, num_q_heads, num_kv_heads, head_dim) -> int:
+    d = ChunkDesc(batch, num_tokens, num_q_heads, num_kv_heads, head_dim, 0.0, None, 0, None)
+    n = load().eagle_chunk_attn_workspace(ctypes.byref(d))
+    if n == 0:
+        raise EagleError("unsupported attention shape")
+    return int(n)
+
+
+def eagle_chunk_attn(q, kv, seq_lens, token_start, out=None, *, sm_scale=0.0, workspace=None, status=None):
+    """Causal attention of packed chunks of new tokens over the cache ``kv`` (a bf16 ``KVStore``) that holds them.  q [N,Hq,D] bf16,
+    seq_lens [B] (before the chunk), token_start [B+1] int32.  Returns out [N,Hq,D]; rows outside every sequence are left as they are."""
+    dev = _current(q, "q")
+    if q.dim() != 3 or kv.fp8 or kv.head_dim != q.shape[2] or kv.batch != seq_lens.numel() or token_start.shape != (kv.batch + 1,) or kv.k.device != dev:
+        raise EagleError("inconsistent shapes (q [N, Hq, D], a bf16 cache of as many sequences as seq_lens, token_start [B + 1])")
+    N, Hq, D = q.shape
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = torch.empty(eagle_chunk_attn_workspace(kv.batch, N, Hq, kv.num_kv_heads, D), dtype=torch.uint8, device=dev)
+    d = ChunkDesc(kv.batch, N, Hq, kv.num_kv_heads, D, float(sm_scale), _here(workspace, torch.uint8, "workspace", dev), workspace.numel(),
+                  _here(status, torch.int32, "status", dev))
+    rc = load().eagle_chunk_attn(ctypes.byref(d), _here(q, torch.bfloat16, "q", dev), ctypes.byref(kv.desc), _here(seq_lens, torch.int32, "seq_lens", dev),
+                                 _here(token_start, torch.int32, "token_start", dev), _here(out, torch.bfloat16, "out", dev, q.shape), _stream())
+    _check(rc, "eagle_chunk_attn")
+    return out
+
+
+def eagle_tree_logits_adjust(logits, draft_tokens=None, tree_parent=None, out=None, *, tree_sizes=None, history=None, history_len=None,
+                             prompt_len=None, repetition=None, presence=None, frequency=None, bias_tokens=None, bias_values=None,
+                             bias_len=None, allowed=None, shared_tree=False, status=None):
+    """Penalties, biases and grammar masks on the target's rows: logits [B,T+1,V] fp32 or bf16 (T = 0: one row per sequence, no
+    trees); history [B,H] int32 with history_len / prompt_len [B]; repetition / presence / frequency fp32 [B]; bias_tokens int32 and
+    bias_values fp32 [B,n]; allowed int32 [B,T+1,ceil(V/32)] bits.  Returns out fp32 [B,T+1,V] (may be ``logits`` itself)."""
+    dev = _current(logits, "logits")
+    if logits.dim() != 3 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise EagleError("logits must be fp32 or bf16 [B, T + 1, V]")
+    B, T, V = logits.shape[0], logits.shape[1] - 1, logits.shape[2]
+    if T < 0:
+        raise EagleError("logits must have a row for the context")
+    per_seq, f32, i32 = torch.Size((B,)), torch.float32, torch.int32
+    if T > 0:
+        if draft_tokens is None or tree_parent is None:
+            raise EagleError("draft_tokens and tree_parent are required with trees")
+        _check_tree(tree_parent, tree_sizes, B, T, shared_tree)
+    if (history is not None and (history.dim() != 2 or history.shape[0] != B)) or (bias_tokens is not None and (bias_tokens.dim() != 2 or bias_tokens.shape[0] != B)):
+        raise EagleError("history and bias lists must be [B, n]")
+    if out is None:
+        out = torch.empty(logits.shape, dtype=f32, device=dev)
+    d = LogitsDesc(B, T, V, 1 if logits.dtype == torch.bfloat16 else 0, _here(tree_sizes, i32, "tree_sizes", dev), 1 if shared_tree else 0,
+                   0 if history is None else history.shape[1], _here(history, i32, "history", dev), _here(history_len, i32, "history_len", dev, per_seq),
+                   _here(prompt_len, i32, "prompt_len", dev, per_seq), _here(repetition, f32, "repetition", dev, per_seq),
+                   _here(presence, f32, "presence", dev, per_seq), _here(frequency, f32, "frequency", dev, per_seq),
+                   0 if bias_tokens is None else bias_tokens.shape[1], _here(bias_tokens, i32, "bias_tokens", dev),
+                   _here(bias_values, f32, "bias_values", dev, None if bias_tokens is None else bias_tokens.shape),
+                   _here(bias_len, i32, "bias_len", dev, per_seq), _here(allowed, i32, "allowed", dev, torch.Size((B, T + 1, (V + 31) // 32))),
+                   _here(status, i32, "status", dev))
+    rc = load().eagle_tree_logits_adjust(ctypes.byref(d), _here(logits, logits.dtype, "logits", dev),
+                                         _here(draft_tokens, i32, "draft_tokens", dev, torch.Size((B, T))) if T else None,
+                                         _here(tree_parent, i32, "tree_parent", dev) if T else None, _here(out, f32, "out", dev, logits.shape), _stream())
+    _check(rc, "eagle_tree_logits_adjust")
+    return out
 
 
 class HostStepRunner:

@@ -68,6 +68,16 @@ DeviceInfo* device_info(int* err) {
 
 void count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 
+int usable_device(int* sm_count) {
+  int err = EAGLE_OK;
+  const DeviceInfo* dev = device_info(&err);
+  if (!dev) return err;
+  *sm_count = dev->sm_count;
+  return EAGLE_OK;
+}
+
+unsigned long long wait_limit_ns() { return g_wait_limit_ns.load(std::memory_order_relaxed); }
+
 }  // namespace eagle
 
 using namespace eagle;

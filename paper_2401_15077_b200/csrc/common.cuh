@@ -238,5 +238,8 @@ int accept_cluster_width(int batch, int vocab, int sm_count, bool all_greedy = f
 cudaError_t launch_commit(const CommitParams& p, cudaStream_t stream);
 cudaError_t launch_expand(const ExpandParams& p, int sm_count, cudaStream_t stream);
 void count_launch();
+// The current device's number of SMs; EAGLE_ERR_DEVICE when it is not an sm_100 device.
+int usable_device(int* sm_count);
+unsigned long long wait_limit_ns();
 
 }  // namespace eagle

@@ -1,0 +1,270 @@
+"""Attention of packed chunks over the cache, against the 64-bit definition.
+
+Tolerance, element by element: the output is rounded to bf16 (2^-8 of it) and every probability before it is multiplied
+with its value (2^-8 of sum p |v|, which the oracle returns); scores, exponentials (one pair in a few is a cubic good to 1.2e-4) and sums are
+fp32, for which 5e-4 of the same sum is ample: a score of 128 products of unit-variance inputs is good to about 1e-5 and its
+exponential relatively to the same."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving as S
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+
+
+@pytest.fixture(scope="module")
+def E():
+    from paper_2401_15077_b200 import binding, build
+    build.build()
+    binding.load()
+    assert torch.cuda.is_available()
+    return binding
+
+
+def _ints(v):
+    return torch.tensor(v, dtype=torch.int32)
+
+
+class Case:
+    """Keys and values only where the sequences are: every other slot is NaN."""
+
+    def __init__(self, n, lens, hq, hkv, d, page=0, seed=0, pad=37):
+        g = torch.Generator().manual_seed(seed)
+        self.n, self.lens, self.page = n, lens, page
+        B, need = len(n), [a + b for a, b in zip(n, lens)]
+        self.start = _ints(np.concatenate([[0], np.cumsum(n)]).tolist())
+        self.q = torch.randn(sum(n) + 3, hq, d, generator=g).bfloat16()
+        if page:
+            used = [-(-x // page) for x in need]
+            order = torch.randperm(sum(used) + 2, generator=g).tolist()
+            self.table = torch.full((B, max(max(used), 1) + 1), -1, dtype=torch.int32)
+            for b, u in enumerate(used):
+                self.table[b, :u] = _ints([order.pop() for _ in range(u)])
+            shape = (sum(used) + 2, hkv, page, d)
+        else:
+            self.table, shape = None, (B, hkv, max(need) + pad, d)
+        self.k, self.v = (torch.full(shape, float("nan"), dtype=torch.bfloat16) for _ in range(2))
+        for b, m in enumerate(need):
+            kk, vv = (torch.randn(hkv, m, d, generator=g).bfloat16() for _ in range(2))
+            if page:
+                for i in range(-(-m // page)):
+                    w = min(page, m - i * page)
+                    self.k[self.table[b, i], :, :w], self.v[self.table[b, i], :, :w] = kk[:, i * page:i * page + w], vv[:, i * page:i * page + w]
+            else:
+                self.k[b, :, :m], self.v[b, :, :m] = kk, vv
+
+    def run(self, E, **kw):
+        up = lambda t: None if t is None else t.to(DEV)  # noqa: E731
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        out = torch.full(self.q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+        E.eagle_chunk_attn(up(self.q), E.KVStore(up(self.k), up(self.v), block_table=up(self.table)), up(_ints(self.lens)), up(self.start), out,
+                           status=status, **kw)
+        torch.cuda.synchronize()
+        return out.cpu(), int(status.item())
+
+    def want(self, **kw):
+        return S.chunk_attn(self.q, self.k, self.v, self.lens, self.start, block_table=self.table, **kw)
+
+
+def _check(out, want, spread):
+    got = out.double().numpy()
+    rows = ~np.isnan(want[:, 0, 0])
+    assert (got[~rows] == 7.0).all(), "rows outside the sequences have changed"
+    assert np.isfinite(got).all()
+    err, tol = np.abs(got - want)[rows], (2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 5e-4) * spread)[rows]
+    assert (err <= tol).all(), (err.max(), (err / tol).max())
+
+
+CASES = {
+    "one_token_empty_cache": dict(n=[1], lens=[0], hq=1, hkv=1, d=64),
+    "one_token": dict(n=[1], lens=[300], hq=8, hkv=2, d=128),
+    "two_tokens_at_a_tile_edge": dict(n=[2, 2, 2, 1], lens=[126, 127, 128, 127], hq=4, hkv=4, d=128),
+    "single_tokens_lone_head": dict(n=[1, 1, 1], lens=[5, 1000, 255], hq=4, hkv=1, d=64),
+    "three_heads": dict(n=[40, 1, 0, 130], lens=[0, 700, 9, 60], hq=12, hkv=3, d=128),
+    "group_of_five": dict(n=[61, 26], lens=[10, 0], hq=10, hkv=2, d=64),
+    "group_of_seven": dict(n=[100], lens=[33], hq=7, hkv=1, d=128),
+    "group_of_sixteen": dict(n=[19, 8, 1], lens=[0, 200, 4000], hq=16, hkv=1, d=128),
+    "no_group": dict(n=[257, 3], lens=[0, 127], hq=3, hkv=3, d=64),
+    "prompt_in_tiles": dict(n=[512], lens=[0], hq=2, hkv=1, d=128),
+    "prompt_behind_a_prefix": dict(n=[300], lens=[1000], hq=4, hkv=1, d=128),
+    "ragged_many": dict(n=[(i * 7) % 23 for i in range(40)], lens=[(i * 53) % 411 for i in range(40)], hq=4, hkv=2, d=64),
+    "all_empty": dict(n=[0, 0], lens=[3, 0], hq=4, hkv=2, d=64),
+}
+
+
+@pytest.mark.parametrize("page", [0, 16, 64, 256])
+@pytest.mark.parametrize("name", list(CASES))
+def test_matches_the_definition(E, name, page):
+    c = Case(**CASES[name], page=page, seed=len(name))
+    out, status = c.run(E)
+    assert status == 0
+    _check(out, *c.want())
+
+
+def test_one_long_context_is_split_and_merged(E):
+    """One token over a long context: every CTA takes a piece (even and odd numbers of KV heads: twins and lone tiles)."""
+    for hq, hkv in ((4, 2), (3, 1), (6, 3)):
+        c = Case([1], [30011], hq, hkv, 64, page=128, seed=hq)
+        out, status = c.run(E)
+        assert status == 0
+        _check(out, *c.want())
+
+
+def test_many_single_tokens_are_whole_units_and_pieces(E):
+    """More units than CTAs, of very different lengths: whole ones are dealt out, the rest is cut."""
+    lens = [(i * 977) % 2600 for i in range(90)]
+    c = Case([1] * 90, lens, 8, 4, 64, page=32, seed=3)
+    out, status = c.run(E)
+    assert status == 0
+    _check(out, *c.want())
+
+
+def test_the_softmax_scale_and_growing_scores(E):
+    c = Case([130], [200], 2, 1, 64, seed=4)
+    for scale in (0.01, 1.0):
+        out, status = c.run(E, sm_scale=scale)
+        want, spread = c.want(sm_scale=scale)
+        # a score's fp32 error grows with the scale: 64 products of up to ~16 each, 2^-24 apiece, times the scale
+        assert status == 0
+        _check(out, want, spread)
+    # keys that grow along the sequence move the running maximum again and again
+    c.k *= torch.linspace(0.01, 6.0, c.k.shape[2]).bfloat16()[:, None]
+    out, status = c.run(E)
+    assert status == 0
+    _check(out, *c.want())
+
+
+def test_masked_slots_may_hold_anything(E):
+    """Keys that a row does not see may be infinite or NaN; past the chunk, values too (the cases above have NaN there)."""
+    c = Case([140], [20], 4, 2, 128, seed=6)
+    c.k[0, :, 159] = float("nan")
+    c.k[0, :, 158] = float("inf")
+    out, status = c.run(E)
+    want, spread = c.want()
+    assert status == 0
+    got = out.double().numpy()
+    err = np.abs(got - want)[:138]
+    assert (err <= (2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 5e-4) * spread)[:138]).all()
+    assert np.isnan(got[139]).all()
+
+
+def test_paged_equals_contiguous_bit_for_bit_and_repeats(E):
+    kw = dict(n=[70, 1, 200, 0, 1], lens=[300, 2000, 5, 8, 61], hq=8, hkv=2, d=128, seed=7)
+    a = Case(**kw)
+    want = a.run(E)[0]
+    for page in (16, 128):
+        c = Case(**kw, page=page)
+        for b, m in enumerate([x + y for x, y in zip(c.n, c.lens)]):
+            for j in range(m):
+                at = int(c.table[b, j // page]), slice(None), j % page
+                c.k[at], c.v[at] = a.k[b, :, j], a.v[b, :, j]
+        c.q = a.q
+        for _ in range(3):
+            same = torch.equal(want.view(torch.int16), c.run(E)[0].view(torch.int16))
+            assert same
+
+
+def test_a_workspace_full_of_leftovers(E):
+    c = Case([33, 1, 5], [100, 900, 0], 6, 3, 64, seed=8)
+    ws = torch.full((E.eagle_chunk_attn_workspace(3, c.q.shape[0], 6, 3, 64),), 255, dtype=torch.uint8, device=DEV)
+    out, status = c.run(E, workspace=ws)
+    _check(out, *c.want())
+    other = Case([1, 1, 1], [3000, 10, 10], 6, 3, 64, seed=9)
+    other.q = other.q[:c.q.shape[0]]
+    out, status = other.run(E, workspace=ws)
+    assert status == 0
+    _check(out, *other.want())
+
+
+# ---------------------------------------------------------------------------------------------------------------- bad inputs
+def test_a_sequence_that_does_not_fit_is_zeroed(E):
+    c = Case([5, 6, 3], [10, 20, 30], 4, 2, 64, seed=10)
+    want, spread = c.want()
+    for bad in (-2, c.k.shape[2] - 5):
+        c.lens = [10, bad, 30]
+        out, status = c.run(E)
+        assert status == -6 and (out[5:11] == 0).all()
+        w, sp = want.copy(), spread.copy()
+        w[5:11], sp[5:11] = 0, 0
+        _check(out, w, sp)
+
+
+def test_a_page_outside_the_pool_is_reported_and_the_sequence_zeroed(E):
+    c = Case([5, 6, 3], [10, 200, 30], 4, 2, 64, page=16, seed=11)
+    want, spread = c.want()
+    for bad in (-1, c.k.shape[0], 2 ** 31 - 1, -(2 ** 31)):
+        c.table[1, 12] = bad                 # the last page in use
+        out, status = c.run(E)
+        assert status == -11 and (out[5:11] == 0).all()
+        w, sp = want.copy(), spread.copy()
+        w[5:11], sp[5:11] = 0, 0
+        _check(out, w, sp)
+    assert c.table[1, 13] == -1              # an entry past the pages in use is never looked at
+
+
+def test_starts_that_descend_or_leave_the_rows_are_refused(E):
+    c = Case([5, 6, 3], [10, 20, 30], 4, 2, 64, seed=12)
+    good = c.start.clone()
+    for i, v in ((1, 12), (3, 18), (0, -1), (2, 4)):
+        c.start = good.clone()
+        c.start[i] = v
+        assert c.run(E)[1] == -6
+    c.start = good
+    out, status = c.run(E)
+    assert status == 0
+    _check(out, *c.want())
+
+
+def test_a_limit_on_waits_that_none_needs_changes_nothing(E):
+    c = Case([64, 1], [500, 700], 4, 2, 128, seed=13)
+    E.set_wait_limit_ns(200_000_000)
+    try:
+        out, status = c.run(E)
+    finally:
+        E.set_wait_limit_ns(0)
+    assert status == 0
+    _check(out, *c.want())
+
+
+def test_replayed_from_a_graph_with_other_lengths(E):
+    """The plan is made on the device: a captured call follows the lengths it finds when it is replayed."""
+    a, b = Case([20, 1, 30], [100, 50, 0], 4, 2, 128, page=16, seed=14), Case([1, 49, 1], [3, 60, 400], 4, 2, 128, page=16, seed=15)
+    pages, per = max(a.k.shape[0], b.k.shape[0]), max(a.table.shape[1], b.table.shape[1])
+    dev = dict(q=torch.empty_like(a.q, device=DEV), k=torch.empty(pages, 2, 16, 128, dtype=torch.bfloat16, device=DEV),
+               v=torch.empty(pages, 2, 16, 128, dtype=torch.bfloat16, device=DEV), table=torch.full((3, per), -1, dtype=torch.int32, device=DEV),
+               lens=torch.zeros(3, dtype=torch.int32, device=DEV), start=torch.zeros(4, dtype=torch.int32, device=DEV))
+    out, status = torch.full(a.q.shape, 7.0, dtype=torch.bfloat16, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    kv = E.KVStore(dev["k"], dev["v"], block_table=dev["table"])
+    ws = torch.empty(E.eagle_chunk_attn_workspace(3, a.q.shape[0], 4, 2, 128), dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    E.eagle_chunk_attn(dev["q"], kv, dev["lens"], dev["start"], out, workspace=ws, status=status)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        E.eagle_chunk_attn(dev["q"], kv, dev["lens"], dev["start"], out, workspace=ws, status=status)
+    for c in (a, b, a):
+        out.fill_(7.0)
+        dev["q"].copy_(c.q)
+        dev["k"][:c.k.shape[0]].copy_(c.k)
+        dev["v"][:c.v.shape[0]].copy_(c.v)
+        dev["table"][:, :c.table.shape[1]].copy_(c.table)
+        dev["lens"].copy_(_ints(c.lens))
+        dev["start"].copy_(c.start)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0
+        _check(out.cpu(), *c.want())
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_shapes(E, seed):
+    r = np.random.default_rng(seed)
+    hkv, G, d = int(r.integers(1, 5)), int(r.integers(1, 17)), int(r.choice([64, 128]))
+    B = int(r.integers(1, 12))
+    n = [int(x) for x in r.integers(0, int(r.choice([2, 40, 200])), B)]
+    lens = [int(x) for x in r.integers(0, int(r.choice([5, 300, 3001])), B)]
+    c = Case(n, lens, G * hkv, hkv, d, page=int(r.choice([0, 16, 32, 64, 128])), seed=seed + 100)
+    out, status = c.run(E)
+    assert status == 0
+    _check(out, *c.want())
