@@ -541,7 +541,7 @@ typedef struct eagle_rope_desc {
  * position p becomes amplitude * (x cos pf - y sin pf, y cos pf + x sin pf); the angle is reduced in fp64, the rotation is
  * fp32, rounded once.  Keys of an fp8 cache are stored as the nearest e4m3 code of key / k_scale[b, h] (magnitudes above
  * 448 become 448), values likewise.  Nothing else in the cache changes.  Rows outside every sequence (behind the last one) are
- * neither read nor written.  A sequence with L_b < 0 or more tokens than its slots reports EAGLE_ERR_SEQ: its rows of q_out
+ * not written.  A sequence with L_b < 0 or more tokens than its slots reports EAGLE_ERR_SEQ: its rows of q_out
  * are zeros and nothing of it is stored; starts that descend or leave [0, N] report it too, and rows that they do not place
  * are left alone.  A token whose page is outside the pool reports EAGLE_ERR_PAGE and is not stored.
  */
@@ -628,7 +628,7 @@ typedef struct eagle_logits_desc {
  * With c the number of times token v was generated (in the history past the prompt, and on the path from the root to the row's
  * node, that node included) and seen = c > 0 or v in the prompt:
  *     z <- seen ? (z > 0 ? z / rho : z * rho) : z;   z <- z - phi c - (c > 0 ? pi : 0);   z <- z + bias(v);   not allowed: -inf
- * in fp32.  A row whose mask allows nothing is all -inf.  Rows of nodes >= tree size are neither read nor written.  Lengths are clamped to
+ * in fp32.  A row whose mask allows nothing is all -inf.  Rows of nodes >= tree size are not written.  Lengths are clamped to
  * their rows; a token outside the vocabulary (history, bias list, draft) is ignored and reports EAGLE_ERR_TOKEN; an invalid
  * tree reports EAGLE_ERR_TREE and all T_max + 1 rows of its sequence become zeros.  One launch; no workspace.
  */

@@ -7,12 +7,15 @@
 // the cache, values to the cache as they are; an fp8 cache takes e4m3 codes of x / scale.
 //
 // The angle is taken in turns: pos * (freqs[m] / 2 pi) in fp64, its whole turns dropped there, the rest rounded to fp32 (error
-// 2^-25 of a turn at any position) for sincospi.  It depends on the token and the pair only: a CTA takes a few tokens, computes
-// their sines and cosines once into shared memory and uses them for every head.
+// 2^-25 of a turn at any position) for sincospi.
 //
-// A unit of work is two 16-byte vectors of one head of one token, the two that a rotation of eight pairs in halves needs; a
-// thread keeps its place in the head and walks over (token, head), two units in flight.  The kernel moves
-// (2 Hq + 2 Hkv + 2 Hkv) * D elements a token and is bound by HBM for long chunks, by launch and memory latency for short ones.
+// A warp takes one token (or some of its heads, when there are few tokens) and needs no other warp: it finds the token's sequence,
+// computes the token's sines and cosines, two pairs a lane, and shares them out so that a lane holds the eight pairs that its
+// place in a head needs, for every head.  A unit of work is two 16-byte vectors of one head, the two that a rotation of eight
+// pairs in halves needs; units of the heads to come are on their way while one is turned.  (With tokens spread over a CTA and the
+// sines read from shared memory for each unit, those reads, four-way bank conflicts among them, cost as much as the loads.)
+// The kernel moves (2 Hq + 2 Hkv + 2 Hkv) * D elements a token and is bound by HBM for long chunks, by launch and memory
+// latency for short ones.
 #include <cuda_fp8.h>
 
 #include "rope.cuh"
@@ -22,11 +25,7 @@ namespace eagle {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeTokens = 4;         // tokens per CTA
-
-struct Vec2 {
-  uint4 a, b;
-};
+constexpr int kRopeWarps = kRopeThreads / 32;
 
 __device__ __forceinline__ void widen(const uint4& v, float* f) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -45,13 +44,14 @@ __device__ __forceinline__ uint4 narrow(const float* f) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// eight e4m3 codes (round to nearest even, magnitudes above 448 become 448, NaN stays NaN)
-__device__ __forceinline__ uint2 codes(const float* f, float scale) {
+// Eight e4m3 codes of f * inv (round to nearest even, magnitudes above 448 become 448, NaN stays NaN).  `inv` is the reciprocal
+// of the scale within one fp32 step: a product can be two steps off the quotient, which matters only within 2^-22 of a tie.
+__device__ __forceinline__ uint2 codes(const float* f, float inv) {
   uint32_t w[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const float2 lo = make_float2(__fdiv_rn(f[4 * i], scale), __fdiv_rn(f[4 * i + 1], scale));
-    const float2 hi = make_float2(__fdiv_rn(f[4 * i + 2], scale), __fdiv_rn(f[4 * i + 3], scale));
+    const float2 lo = make_float2(f[4 * i] * inv, f[4 * i + 1] * inv);
+    const float2 hi = make_float2(f[4 * i + 2] * inv, f[4 * i + 3] * inv);
     w[i] = __nv_cvt_float2_to_fp8x2(lo, __NV_SATFINITE, __NV_E4M3) | (static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(hi, __NV_SATFINITE, __NV_E4M3)) << 16);
   }
   return make_uint2(w[0], w[1]);
@@ -70,208 +70,200 @@ __device__ __forceinline__ int owner_of(const int32_t* start, int B, int t, int 
   return lo;
 }
 
-template <bool TREE, bool FP8>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeParams p) {
-  __shared__ float2 s_cs[kRopeTokens][64];               // (cos, sin) of every pair of every token of the CTA
-  __shared__ long long s_row[kRopeTokens];               // first cache row of the token's slot (KV head 0), -1: not stored
-  __shared__ int s_seq[kRopeTokens], s_pos[kRopeTokens]; // sequence (-1: nothing to do), position
-  __shared__ int s_zero[kRopeTokens];                    // its sequence is refused: the queries become zeros
-  __shared__ int s_parent[kMaxTree];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int t0;                                                // first token (row of q, k, v) of this CTA
-  int n_tok = kRopeTokens;
+template <bool TREE, bool FP8, bool INTERLEAVED, int D>
+__global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(RopeParams p) {
+  __shared__ float2 s_cs[kRopeWarps][D / 2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long job = static_cast<long long>(blockIdx.x) * kRopeWarps + warp;
+  const int chunks = p.head_chunks, H = p.Hq + 2 * p.Hkv, tokens = TREE ? p.B * p.T : p.N;
+  const long long token_of = job / chunks;
+  const int h_lo = static_cast<int>(job - token_of * chunks) * p.heads_per_warp, h_hi = min(H, h_lo + p.heads_per_warp);
 
-  if constexpr (TREE) {
-    const int groups = (p.T + kRopeTokens - 1) / kRopeTokens;
-    const int b = blockIdx.x / groups, i0 = (blockIdx.x - b * groups) * kRopeTokens;
-    t0 = b * p.T + i0;
-    const int32_t* parent = p.tree_parent + (p.shared_tree ? 0 : static_cast<size_t>(b) * p.T);
-    const int n = p.tree_sizes ? p.tree_sizes[p.shared_tree ? 0 : b] : p.T;
-    const int L = p.seq_lens[b];
-    const bool size_ok = n >= 0 && n <= p.T;
-    int bad = !size_ok;
-    if (size_ok && tid < n) {
-      const int m = parent[tid];
-      s_parent[tid] = m;
-      bad = m < -1 || m >= tid;
+  if (!TREE && blockIdx.x == 0) {                          // the list of starts has to ascend within the tensor
+    int bad = 0;
+    for (int i = threadIdx.x; i <= p.B; i += kRopeThreads) {
+      const int s = p.token_start[i];
+      if (s < 0 || s > p.N || (i < p.B && p.token_start[i + 1] < s)) bad = 1;
     }
-    bad = __syncthreads_or(bad);
-    const bool no_room = L < 0 || static_cast<long long>(L) + n > p.capacity;
-    if (tid == 0 && i0 == 0 && (bad || (no_room && n > 0))) report_status(p.status, bad ? EAGLE_ERR_TREE : EAGLE_ERR_SEQ);
-    if (tid < kRopeTokens) {
-      const int i = i0 + tid, nodes = size_ok ? n : p.T;
-      const bool here = i < nodes && i < p.T, refused = bad || no_room;
+    if (bad) report_status(p.status, EAGLE_ERR_SEQ);
+  }
+  if (token_of >= tokens) return;
+  const int t = static_cast<int>(token_of);
+
+  // ---- units: lane `l` has place l % U in the heads l / U, l / U + 32 / U, ...
+  constexpr int U = D / 16, kStep = 32 / U;
+  const int u = lane & (U - 1), half = p.R / 2;
+  const bool turn = 16 * u < p.R;                          // its two vectors hold eight whole pairs
+  const int va = !turn ? 16 * u : (INTERLEAVED ? 16 * u : 8 * u);
+  const int vb = !turn ? 16 * u + 8 : (INTERLEAVED ? 16 * u + 8 : half + 8 * u);
+  const __nv_bfloat16 *q_row = p.q + t * p.q_stride, *k_row = p.k + t * p.k_stride, *v_row = p.v + t * p.v_stride;
+  struct Unit {
+    uint4 a, b;
+    float scale;
+  };
+  auto fetch = [&](Unit& x, int h) __attribute__((always_inline)) {
+    if (h >= h_hi) return;
+    const __nv_bfloat16* s = h < p.Hq ? q_row + h * D : (h < p.Hq + p.Hkv ? k_row + (h - p.Hq) * D : v_row + (h - p.Hq - p.Hkv) * D);
+    x.a = *reinterpret_cast<const uint4*>(s + va);
+    x.b = *reinterpret_cast<const uint4*>(s + vb);
+  };
+  Unit now, then;
+  int h = h_lo + lane / U;
+  fetch(now, h);                                           // sets out before anything is known about the token
+
+  // ---- the token: sequence, position, cache row; a token without a sequence is left alone
+  int seq, pos = 0;
+  bool zero = false;                                       // its sequence is refused: the queries become zeros
+  long long row = -1;                                      // cache row of its slot (KV head 0), -1: not stored
+  if constexpr (TREE) {
+    seq = t / p.T;
+    const int i = t - seq * p.T;
+    const int32_t* parent = p.tree_parent + (p.shared_tree ? 0 : static_cast<size_t>(seq) * p.T);
+    const int n = p.tree_sizes ? p.tree_sizes[p.shared_tree ? 0 : seq] : p.T, L = p.seq_lens[seq];
+    const bool size_ok = n >= 0 && n <= p.T;
+    const int p0 = size_ok && lane < n ? parent[lane] : -1, p1 = size_ok && lane + 32 < n ? parent[lane + 32] : -1;
+    const bool bad = __any_sync(0xffffffffu, !size_ok || p0 < -1 || p0 >= lane || p1 < -1 || p1 >= lane + 32);
+    const bool no_room = n > 0 && (L < 0 || static_cast<long long>(L) + n > p.capacity);
+    if (lane == 0 && i == 0 && (bad || no_room)) report_status(p.status, bad ? EAGLE_ERR_TREE : EAGLE_ERR_SEQ);
+    if (size_ok && i >= n) return;
+    zero = bad || no_room;
+    if (!zero) {
       int depth = 0;
-      if (here && !refused)
-        for (int m = i; m >= 0; m = s_parent[m]) ++depth;
-      s_seq[tid] = here ? b : -1;
-      s_zero[tid] = refused;
-      s_pos[tid] = L + depth - 1;
-      s_row[tid] = here && !refused ? rope_row(p, b, L + i) : -1;
+      for (int m = i; m >= 0; ++depth) m = m < 32 ? __shfl_sync(0xffffffffu, p0, m) : __shfl_sync(0xffffffffu, p1, m - 32);
+      pos = L + depth - 1;
+      row = rope_row(p, seq, L + i);
     }
   } else {
-    t0 = blockIdx.x * kRopeTokens;
-    if (warp < kRopeTokens) {
-      const int t = t0 + warp;
-      int b = -1, zero = 0, pos = 0;
-      long long row = -1;
-      if (t < p.N) {
-        const int o = owner_of(p.token_start, p.B, t, lane);
-        const int s = p.token_start[o], e = p.token_start[o + 1];
-        if (s >= 0 && s <= t && t < e && e <= p.N) {
-          const int L = p.seq_lens[o];
-          b = o;
-          zero = L < 0 || static_cast<long long>(L) + (e - s) > p.capacity;
-          if (zero && lane == 0) report_status(p.status, EAGLE_ERR_SEQ);
-          pos = p.positions ? p.positions[t] : L + (t - s);
-          if (!zero) row = rope_row(p, o, L + (t - s));
-        }
-      }
-      if (lane == 0) {
-        s_seq[warp] = b;
-        s_zero[warp] = zero;
-        s_pos[warp] = pos;
-        s_row[warp] = row;
-      }
-    } else if (blockIdx.x == 0 && blockIdx.y == 0) {
-      // the list of starts has to ascend within the tensor
-      int bad = 0;
-      for (int b = tid - 32 * kRopeTokens; b <= p.B; b += kRopeThreads - 32 * kRopeTokens) {
-        const int s = p.token_start[b];
-        if (s < 0 || s > p.N || (b < p.B && p.token_start[b + 1] < s)) bad = 1;
-      }
-      if (bad) report_status(p.status, EAGLE_ERR_SEQ);
+    seq = owner_of(p.token_start, p.B, t, lane);
+    const int s = p.token_start[seq], e = p.token_start[seq + 1], L = p.seq_lens[seq];
+    if (s < 0 || s > t || t >= e || e > p.N) return;
+    zero = L < 0 || static_cast<long long>(L) + (e - s) > p.capacity;
+    if (zero && lane == 0) report_status(p.status, EAGLE_ERR_SEQ);
+    if (!zero) {
+      pos = p.positions ? p.positions[t] : L + (t - s);
+      row = rope_row(p, seq, L + (t - s));
     }
   }
-  __syncthreads();
 
-  const int half = p.R / 2;
-  for (int i = tid; i < kRopeTokens * half; i += kRopeThreads) {
-    const int t = i / half, m = i - t * half;
-    double turns = static_cast<double>(s_pos[t]) * (p.freqs[m] * 0.15915494309189535);      // 1 / (2 pi)
+  // ---- sines and cosines, times the amplitude
+  for (int m = lane; m < half; m += 32) {
+    double turns = static_cast<double>(pos) * (p.freqs[m] * 0.15915494309189535);      // 1 / (2 pi)
     turns -= rint(turns);
     float sn, cs;
     sincospif(2.0f * static_cast<float>(turns), &sn, &cs);
-    s_cs[t][m] = make_float2(cs * p.amplitude, sn * p.amplitude);
+    s_cs[warp][m] = make_float2(cs * p.amplitude, sn * p.amplitude);
   }
-  __syncthreads();
-
-  // ---- units: `u` is the place within a head, fixed for the thread; (token, head) advances by `step` heads
-  const int U = p.D / 16, u = tid & (U - 1), step = kRopeThreads / U;
-  const int h_lo = blockIdx.y * p.heads_per_block, H = p.Hq + 2 * p.Hkv;
-  const int heads = min(p.heads_per_block, H - h_lo);
-  // element offsets of the unit's two vectors; `turn`: they hold eight whole pairs
-  const bool turn = 16 * u < p.R;
-  const int va = !turn ? 16 * u : (p.interleaved ? 16 * u : 8 * u);
-  const int vb = !turn ? 16 * u + 8 : (p.interleaved ? 16 * u + 8 : half + 8 * u);
-  int tok = 0, h = tid / U;
-  while (h >= heads && tok < n_tok) { h -= heads; ++tok; }
-
-  auto source = [&](int t, int head) -> const uint4* {
-    const __nv_bfloat16* s = head < p.Hq              ? p.q + (t0 + t) * p.q_stride + static_cast<long long>(head) * p.D
-                             : head < p.Hq + p.Hkv    ? p.k + (t0 + t) * p.k_stride + static_cast<long long>(head - p.Hq) * p.D
-                                                      : p.v + (t0 + t) * p.v_stride + static_cast<long long>(head - p.Hq - p.Hkv) * p.D;
-    return reinterpret_cast<const uint4*>(s);
-  };
-  auto live = [&](int t, int head) { return s_seq[t] >= 0 && (head < p.Hq || s_row[t] >= 0); };
-  auto finish = [&](int t, int head, const Vec2& in) {
-    const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.Hkv;
-    float x[8], y[8];
-    Vec2 out = in;
-    if (turn && !is_v) {
-      widen(in.a, x);
-      widen(in.b, y);
-      if (p.interleaved) {
+  __syncwarp();
+  float cs[8], sn[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 c = s_cs[t][8 * u + e], d = s_cs[t][8 * u + 4 + e];
-          const float x0 = x[2 * e], x1 = x[2 * e + 1], y0 = y[2 * e], y1 = y[2 * e + 1];
-          x[2 * e] = x0 * c.x - x1 * c.y;
-          x[2 * e + 1] = x1 * c.x + x0 * c.y;
-          y[2 * e] = y0 * d.x - y1 * d.y;
-          y[2 * e + 1] = y1 * d.x + y0 * d.y;
-        }
-      } else {
+  for (int e = 0; e < 8; ++e) {
+    const float2 c = turn ? s_cs[warp][8 * u + e] : make_float2(1.f, 0.f);
+    cs[e] = c.x;
+    sn[e] = c.y;
+  }
+
+  auto rotate = [&](float (&x)[8], float (&y)[8]) __attribute__((always_inline)) {
+    if constexpr (INTERLEAVED) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 c = s_cs[t][8 * u + e];
-          const float x0 = x[e], y0 = y[e];
-          x[e] = x0 * c.x - y0 * c.y;
-          y[e] = y0 * c.x + x0 * c.y;
-        }
+      for (int e = 0; e < 4; ++e) {
+        const float x0 = x[2 * e], x1 = x[2 * e + 1], y0 = y[2 * e], y1 = y[2 * e + 1];
+        x[2 * e] = x0 * cs[e] - x1 * sn[e];
+        x[2 * e + 1] = x1 * cs[e] + x0 * sn[e];
+        y[2 * e] = y0 * cs[4 + e] - y1 * sn[4 + e];
+        y[2 * e + 1] = y1 * cs[4 + e] + y0 * sn[4 + e];
       }
-      if (is_q || !FP8) {
-        out.a = narrow(x);
-        out.b = narrow(y);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x0 = x[e], y0 = y[e];
+        x[e] = x0 * cs[e] - y0 * sn[e];
+        y[e] = y0 * cs[e] + x0 * sn[e];
       }
-    } else if (FP8 && !is_q) {
-      widen(in.a, x);
-      widen(in.b, y);
     }
-    if (is_q) {
-      if (s_zero[t]) out.a = out.b = make_uint4(0u, 0u, 0u, 0u);
-      __nv_bfloat16* dst = p.q_out + (static_cast<long long>(t0 + t) * p.Hq + head) * p.D;
-      *reinterpret_cast<uint4*>(dst + va) = out.a;
-      *reinterpret_cast<uint4*>(dst + vb) = out.b;
+  };
+  auto work = [&](const Unit& in, int head) __attribute__((always_inline)) {
+    if (head >= h_hi) return;
+    const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.Hkv;
+    const int g = is_v ? head - p.Hq - p.Hkv : head - p.Hq;
+    if (FP8 && !is_q) {
+      if (row < 0) return;
+      uint8_t* dst = static_cast<uint8_t*>(is_v ? p.v_cache : p.k_cache) + (row + g * p.head_rows) * D;
+      float x[8], y[8], inv;
+      asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(in.scale));
+      widen(in.a, x);
+      widen(in.b, y);
+      if (turn && !is_v) rotate(x, y);
+      *reinterpret_cast<uint2*>(dst + va) = codes(x, inv);
+      *reinterpret_cast<uint2*>(dst + vb) = codes(y, inv);
       return;
     }
-    const int g = is_v ? head - p.Hq - p.Hkv : head - p.Hq;
-    const long long row = s_row[t] + g * p.head_rows;
-    if constexpr (FP8) {
-      const float scale = (is_v ? p.v_scale : p.k_scale)[static_cast<size_t>(s_seq[t]) * p.Hkv + g];
-      uint8_t* dst = static_cast<uint8_t*>(is_v ? p.v_cache : p.k_cache) + row * p.D;
-      *reinterpret_cast<uint2*>(dst + va) = codes(x, scale);
-      *reinterpret_cast<uint2*>(dst + vb) = codes(y, scale);
+    uint4 out_a = in.a, out_b = in.b;
+    if (turn && !is_v) {
+      float x[8], y[8];
+      widen(in.a, x);
+      widen(in.b, y);
+      rotate(x, y);
+      out_a = narrow(x);
+      out_b = narrow(y);
+    }
+    __nv_bfloat16* dst;
+    if (is_q) {
+      if (zero) out_a = out_b = make_uint4(0u, 0u, 0u, 0u);
+      dst = p.q_out + (static_cast<long long>(t) * p.Hq + head) * D;
     } else {
-      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(is_v ? p.v_cache : p.k_cache) + row * p.D;
-      *reinterpret_cast<uint4*>(dst + va) = out.a;
-      *reinterpret_cast<uint4*>(dst + vb) = out.b;
+      if (row < 0) return;
+      dst = static_cast<__nv_bfloat16*>(is_v ? p.v_cache : p.k_cache) + (row + g * p.head_rows) * D;
+    }
+    *reinterpret_cast<uint4*>(dst + va) = out_a;
+    *reinterpret_cast<uint4*>(dst + vb) = out_b;
+  };
+  // (the scales need the sequence, so they follow the first unit's vectors and travel with those after it)
+  auto scale_of = [&](Unit& x, int h) __attribute__((always_inline)) {
+    if constexpr (FP8) {
+      if (h >= p.Hq && h < h_hi) x.scale = __ldg((h < p.Hq + p.Hkv ? p.k_scale - p.Hq : p.v_scale - p.Hq - p.Hkv) + static_cast<size_t>(seq) * p.Hkv + h);
     }
   };
-  auto advance = [&]() {
-    h += step;
-    while (h >= heads && tok < n_tok) { h -= heads; ++tok; }
-  };
-  while (tok < n_tok) {
-    int ts[2], hs[2];
-    bool on[2];
-    Vec2 in[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      ts[i] = tok;
-      hs[i] = h_lo + h;
-      on[i] = tok < n_tok && live(tok, hs[i]);
-      if (on[i]) {
-        const uint4* s = source(ts[i], hs[i]);
-        in[i].a = s[va / 8];
-        in[i].b = s[vb / 8];
-      }
-      if (tok < n_tok) advance();
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (on[i]) finish(ts[i], hs[i], in[i]);
+  scale_of(now, h);
+  // (two units in turn, not moved along: a move would wait for the loads that have just set out)
+  for (; h < h_hi; h += 2 * kStep) {
+    fetch(then, h + kStep);
+    scale_of(then, h + kStep);
+    work(now, h);
+    fetch(now, h + 2 * kStep);
+    scale_of(now, h + 2 * kStep);
+    work(then, h + kStep);
   }
+}
+
+template <bool TREE, bool FP8, int D>
+void launch_kernel(const RopeParams& p, unsigned blocks, cudaStream_t stream) {
+  if (p.interleaved) rope_kernel<TREE, FP8, true, D><<<blocks, kRopeThreads, 0, stream>>>(p);
+  else rope_kernel<TREE, FP8, false, D><<<blocks, kRopeThreads, 0, stream>>>(p);
 }
 
 }  // namespace
 
 cudaError_t launch_rope(const RopeParams& p_in, bool tree, int sm_count, cudaStream_t stream) {
   RopeParams p = p_in;
-  const int H = p.Hq + 2 * p.Hkv;
-  const long long groups = tree ? static_cast<long long>(p.B) * ((p.T + kRopeTokens - 1) / kRopeTokens) : (static_cast<long long>(p.N) + kRopeTokens - 1) / kRopeTokens;
-  // few tokens: the heads are split over several CTAs (each computes the same sines again) until there are two CTAs per SM
-  int splits = 1;
-  while (groups * splits < 2ll * sm_count && H > splits * (kRopeThreads / (p.D / 16)) / kRopeTokens && splits < 64) splits *= 2;
-  p.heads_per_block = (H + splits - 1) / splits;
-  const dim3 grid(static_cast<unsigned>(groups), static_cast<unsigned>((H + p.heads_per_block - 1) / p.heads_per_block));
-  const bool fp8 = p.k_scale != nullptr;
-  if (tree) {
-    if (fp8) rope_kernel<true, true><<<grid, kRopeThreads, 0, stream>>>(p);
-    else rope_kernel<true, false><<<grid, kRopeThreads, 0, stream>>>(p);
+  const int H = p.Hq + 2 * p.Hkv, step = 32 / (p.D / 16);
+  const long long tokens = tree ? static_cast<long long>(p.B) * p.T : p.N;
+  // few tokens: a token's heads are split over several warps (each computes the same sines again) until there are
+  // sixteen warps per SM, or a warp has a single step of heads
+  int chunks = 1;
+  while (tokens * chunks < 16ll * sm_count && H > chunks * step) chunks *= 2;
+  p.heads_per_warp = ((H + chunks - 1) / chunks + step - 1) / step * step;
+  p.head_chunks = (H + p.heads_per_warp - 1) / p.heads_per_warp;
+  const long long jobs = tokens * p.head_chunks;
+  const unsigned blocks = static_cast<unsigned>((jobs + kRopeWarps - 1) / kRopeWarps);
+  if (p.k_scale) {                                         // codes: head_dim 128 only
+    if (tree) launch_kernel<true, true, 128>(p, blocks, stream);
+    else launch_kernel<false, true, 128>(p, blocks, stream);
+  } else if (p.D == 128) {
+    if (tree) launch_kernel<true, false, 128>(p, blocks, stream);
+    else launch_kernel<false, false, 128>(p, blocks, stream);
   } else {
-    if (fp8) rope_kernel<false, true><<<grid, kRopeThreads, 0, stream>>>(p);
-    else rope_kernel<false, false><<<grid, kRopeThreads, 0, stream>>>(p);
+    if (tree) launch_kernel<true, false, 64>(p, blocks, stream);
+    else launch_kernel<false, false, 64>(p, blocks, stream);
   }
   count_launch();
   return cudaGetLastError();

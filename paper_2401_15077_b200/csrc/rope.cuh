@@ -27,7 +27,7 @@ struct RopeParams {
   float amplitude;
   int32_t B, N, T, Hq, Hkv, D, R;
   int32_t interleaved, shared_tree;
-  int32_t heads_per_block;
+  int32_t heads_per_warp, head_chunks;
   int32_t* status;
 };
 
