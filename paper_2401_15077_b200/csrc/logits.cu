@@ -6,12 +6,13 @@
 //     z <- seen ? (z > 0 ? z / rho : z * rho) : z;   z <- z - phi c - pi [c > 0];   z <- z + bias(v);   masked: -inf.
 //
 // A CTA takes 2048 tokens of the vocabulary and some rows of one sequence.  It counts the history's tokens that fall into its
-// range in shared memory (the list is short next to the rows: 16 KB against 8 KB * rows at 4096 tokens), keeps the counts and
-// biases of its eight tokens per thread in registers and then streams the rows: one read and one write of each logit, nothing
-// else of that size, no workspace.  Draft tokens on a row's path are rare in a CTA's range (a bit set says which nodes matter),
-// so they cost a test per row.  Token tid + 256 k belongs to a thread: every access is coalesced whatever the vocabulary's
-// alignment, and a warp's 32 tokens share one word of the grammar's mask.  Counts are integers and a token's biases are added
-// up by one thread in list order, so a call gives the same bits every time.
+// range in shared memory (the list is short next to the rows: 16 KB against 8 KB * rows at 4096 tokens), turns them into a
+// factor choice and an addend for each of its eight tokens per thread, kept in registers, and then streams the rows: one read
+// and one write of each logit, nothing else of that size, no workspace.  Draft tokens on a row's path are rare in a CTA's
+// range: a bit set says which nodes matter, and the thread that owns such a token computes it again.  A warp has 256
+// consecutive tokens, 32 at a time: every access is coalesced whatever the vocabulary's alignment, and lane l holds word l & 7
+// of the grammar's mask for all of them.  Logits and mask of the rows to come are on their way while one is worked on.
+// Counts are integers and a token's biases are added up by one thread in list order, so a call gives the same bits every time.
 #include "logits.cuh"
 
 namespace eagle {
@@ -21,16 +22,17 @@ namespace {
 constexpr int kLogThreads = 256;
 constexpr int kPerThread = 8;
 constexpr int kRange = kLogThreads * kPerThread;
+constexpr int kRowsPerCta = 16;
 constexpr uint32_t kInPrompt = 0x80000000u;
 
 template <bool BF16>
 __device__ __forceinline__ float load_logit(const void* base, size_t i) {
   if constexpr (BF16) return __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(base)[i]) << 16);
-  else return static_cast<const float*>(base)[i];
+  else return __ldcs(static_cast<const float*>(base) + i);
 }
 
 template <bool BF16>
-__global__ void __launch_bounds__(kLogThreads) logits_kernel(LogitsParams p) {
+__global__ void __launch_bounds__(kLogThreads, 4) logits_kernel(LogitsParams p) {
   __shared__ uint32_t s_count[kRange];
   __shared__ float s_bias[kRange];
   __shared__ int s_btok[kMaxBias];
@@ -67,6 +69,26 @@ __global__ void __launch_bounds__(kLogThreads) logits_kernel(LogitsParams p) {
   }
   if (r_lo >= r_hi) return;
 
+  // ---- the first rows set out before anything else is looked at
+  const int lane = tid & 31, v_warp = (tid >> 5) * (32 * kPerThread), words = (p.V + 31) / 32;
+  const int n_here = min(max(p.V - v0 - v_warp - lane, 0) + 31, 32 * kPerThread) >> 5;     // this lane's tokens that exist
+  const int w_at = (v0 + v_warp) / 32 + (lane & (kPerThread - 1));                         // this lane's word of the mask
+  const bool has_word = p.allowed && w_at < words;
+  auto fetch = [&](int r, float (&z)[kPerThread], uint32_t& mask) __attribute__((always_inline)) {
+    if (r >= r_hi) return;
+    const size_t at = row0 + static_cast<size_t>(r) * p.V + v0 + v_warp + lane;
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k)
+      if (k < n_here) z[k] = load_logit<BF16>(p.logits, at + k * 32);
+    if (has_word) mask = __ldg(p.allowed + (static_cast<size_t>(b) * (p.T + 1) + r) * words + w_at);
+  };
+  float z0[kPerThread], z1[kPerThread];
+  uint32_t m0 = 0u, m1 = 0u;
+#pragma unroll
+  for (int k = 0; k < kPerThread; ++k) z0[k] = z1[k] = 0.f;
+  fetch(r_lo, z0, m0);
+  fetch(r_lo + 1, z1, m1);
+
   // ---- history: counts of the tokens in the range
   for (int i = tid; i < kRange; i += kLogThreads) { s_count[i] = 0u; s_bias[i] = 0.f; }
   if (tid < n) {
@@ -81,12 +103,19 @@ __global__ void __launch_bounds__(kLogThreads) logits_kernel(LogitsParams p) {
   if (p.history) {
     const int len = min(max(p.history_len[b], 0), p.H), prompt = p.prompt_len ? p.prompt_len[b] : 0;
     const int32_t* h = p.history + static_cast<size_t>(b) * p.H;
-    for (int i = tid; i < len; i += kLogThreads) {
-      const int t = h[i];
-      if (t < 0 || t >= p.V) { if (blockIdx.x == 0 && blockIdx.z == 0) report_status(p.status, EAGLE_ERR_TOKEN); }
-      else if (t >= v0 && t < v0 + kRange) {
-        if (i < prompt) atomicOr(&s_count[t - v0], kInPrompt);
-        else atomicAdd(&s_count[t - v0], 1u);
+    for (int i0 = tid; i0 < len; i0 += 8 * kLogThreads) {
+      int t[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[j] = i0 + j * kLogThreads < len ? __ldg(h + i0 + j * kLogThreads) : 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int i = i0 + j * kLogThreads;
+        if (i >= len) break;
+        if (t[j] < 0 || t[j] >= p.V) { if (blockIdx.x == 0 && blockIdx.z == 0) report_status(p.status, EAGLE_ERR_TOKEN); }
+        else if (t[j] >= v0 && t[j] < v0 + kRange) {
+          if (i < prompt) atomicOr(&s_count[t[j] - v0], kInPrompt);
+          else atomicAdd(&s_count[t[j] - v0], 1u);
+        }
       }
     }
   }
@@ -104,55 +133,59 @@ __global__ void __launch_bounds__(kLogThreads) logits_kernel(LogitsParams p) {
   }
   __syncthreads();
 
-  uint32_t count[kPerThread];
-  float bias[kPerThread];
+  // z' = (z > 0 ? z / rho : z * rho) + add for a token that is there already, z + add for any other
+  const float rho = p.repetition ? p.repetition[b] : 1.f, pi = p.presence ? p.presence[b] : 0.f, phi = p.frequency ? p.frequency[b] : 0.f;
+  const float inv_rho = 1.f / rho;
+  float add[kPerThread];
+  uint32_t seen = 0;
 #pragma unroll
   for (int k = 0; k < kPerThread; ++k) {
-    count[k] = s_count[tid + k * kLogThreads];
-    bias[k] = s_bias[tid + k * kLogThreads];
+    const int off = v_warp + k * 32 + lane;
+    const uint32_t c = s_count[off];
+    seen |= (c != 0u ? 1u : 0u) << k;
+    add[k] = s_bias[off];
+    if (c & ~kInPrompt) add[k] -= phi * static_cast<float>(c & ~kInPrompt) + pi;
   }
-  const float rho = p.repetition ? p.repetition[b] : 1.f, pi = p.presence ? p.presence[b] : 0.f, phi = p.frequency ? p.frequency[b] : 0.f;
-  const int words = (p.V + 31) / 32;
 
-  // ---- rows, the next one's logits on their way while one is worked on
-  float z[kPerThread], next[kPerThread];
-  auto fetch = [&](int r, float* to) {
-    const size_t at = row0 + static_cast<size_t>(r) * p.V + v0 + tid;
-#pragma unroll
-    for (int k = 0; k < kPerThread; ++k)
-      if (v0 + tid + k * kLogThreads < p.V) to[k] = load_logit<BF16>(p.logits, at + k * kLogThreads);
-  };
-  fetch(r_lo, z);
-  for (int r = r_lo; r < r_hi; ++r) {
-    if (r + 1 < r_hi) fetch(r + 1, next);
-    uint32_t extra[kPerThread];
-#pragma unroll
-    for (int k = 0; k < kPerThread; ++k) extra[k] = 0u;
-    for (unsigned long long path = r > 0 ? s_path[r - 1] : 0ull; path; path &= path - 1) {
-      const int off = s_off[__ffsll(static_cast<long long>(path)) - 1];
-      if ((off & (kLogThreads - 1)) == tid) {
-#pragma unroll
-        for (int k = 0; k < kPerThread; ++k) extra[k] += (off >> 8) == k;
-      }
-    }
-    const size_t at = row0 + static_cast<size_t>(r) * p.V + v0 + tid;
-    const uint32_t* mask = p.allowed ? p.allowed + (static_cast<size_t>(b) * (p.T + 1) + r) * words : nullptr;
+  // ---- rows
+  auto work = [&](int r, const float (&z0)[kPerThread], uint32_t m0) __attribute__((always_inline)) {
+    if (r >= r_hi) return;
+    float x[kPerThread];
 #pragma unroll
     for (int k = 0; k < kPerThread; ++k) {
-      const int v = v0 + tid + k * kLogThreads;
-      if (v >= p.V) continue;
-      float x = z[k];
-      const uint32_t c = (count[k] & ~kInPrompt) + extra[k];
-      if (c | (count[k] & kInPrompt)) {
-        x = x > 0.f ? __fdiv_rn(x, rho) : x * rho;
-        if (c) x = x - phi * static_cast<float>(c) - pi;
-      }
-      x += bias[k];
-      if (mask && !((__ldg(mask + (v >> 5)) >> (v & 31)) & 1u)) x = -INFINITY;
-      p.out[at + k * kLogThreads] = x;
+      const float f = z0[k] > 0.f ? inv_rho : rho;
+      x[k] = (seen >> k) & 1u ? fmaf(z0[k], f, add[k]) : z0[k] + add[k];
     }
+    const unsigned long long path = r > 0 ? s_path[r - 1] : 0ull;
+    for (unsigned long long left = path; left; left &= left - 1) {
+      const int off = s_off[__ffsll(static_cast<long long>(left)) - 1], mine = off - v_warp - lane;
+      if (mine < 0 || mine >= 32 * kPerThread || (mine & 31)) continue;      // another lane's token
+      int c = static_cast<int>(s_count[off] & ~kInPrompt);
+      for (unsigned long long q = path; q; q &= q - 1) c += s_off[__ffsll(static_cast<long long>(q)) - 1] == off;
+      const uint32_t hit = 1u << (mine >> 5);        // (a bit per token: a comparison with k would put the rows into local memory)
+      const float plus = s_bias[off] - (phi * static_cast<float>(c) + pi);
 #pragma unroll
-    for (int k = 0; k < kPerThread; ++k) z[k] = next[k];
+      for (int k = 0; k < kPerThread; ++k)
+        if ((hit >> k) & 1u) x[k] = fmaf(z0[k], z0[k] > 0.f ? inv_rho : rho, plus);
+    }
+    if (p.allowed) {
+#pragma unroll
+      for (int k = 0; k < kPerThread; ++k) {
+        const uint32_t word = __shfl_sync(0xffffffffu, m0, k);
+        if (!((word >> lane) & 1u)) x[k] = -INFINITY;
+      }
+    }
+    float* to = p.out + row0 + static_cast<size_t>(r) * p.V + v0 + v_warp + lane;
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k)
+      if (k < n_here) __stcs(to + k * 32, x[k]);
+  };
+  // (two buffers in turn, not moved along: a move would wait for the loads that have just set out)
+  for (int r = r_lo; r < r_hi; r += 2) {
+    work(r, z0, m0);
+    fetch(r + 2, z0, m0);
+    work(r + 1, z1, m1);
+    fetch(r + 3, z1, m1);
   }
 }
 
@@ -161,9 +194,11 @@ __global__ void __launch_bounds__(kLogThreads) logits_kernel(LogitsParams p) {
 cudaError_t launch_logits(const LogitsParams& p_in, int sm_count, cudaStream_t stream) {
   LogitsParams p = p_in;
   const int ranges = (p.V + kRange - 1) / kRange, rows = p.T + 1;
-  // rows are shared out over several CTAs (which count the history again each) while there are too few to fill the machine
-  int splits = 1;
-  while (static_cast<long long>(ranges) * p.B * splits < 8ll * sm_count && splits < rows) ++splits;
+  // Rows are shared out over several CTAs (each counts the history again): at most 16 to one, so that trees of 16 and of 64
+  // nodes end together (147 us for 64 trees x 32000 tokens; 156 us with 33 rows, 158 us with 8), fewer while the CTAs do not fill
+  // the machine.
+  int splits = (rows + kRowsPerCta - 1) / kRowsPerCta;
+  while (static_cast<long long>(ranges) * p.B * splits < 4ll * sm_count && splits < rows) ++splits;
   p.rows_per_block = (rows + splits - 1) / splits;
   const dim3 grid(static_cast<unsigned>(ranges), static_cast<unsigned>(p.B), static_cast<unsigned>((rows + p.rows_per_block - 1) / p.rows_per_block));
   if (p.bf16) logits_kernel<true><<<grid, kLogThreads, 0, stream>>>(p);
