@@ -169,7 +169,7 @@ int eagle_tree_rope_append(const eagle_rope_desc* desc, const void* q, const voi
 
 size_t eagle_chunk_attn_workspace(const eagle_chunk_desc* desc) {
   ChunkWork w;
-  if (!desc || !carve_chunk_work(*desc, nullptr, kMaxPlanCtas, &w)) return 0;
+  if (!desc || !carve_chunk_work(*desc, nullptr, kMaxPairs, &w)) return 0;
   return w.bytes;
 }
 
@@ -179,7 +179,7 @@ int eagle_chunk_attn(const eagle_chunk_desc* desc, const void* q, const eagle_kv
   const eagle_chunk_desc& d = *desc;
   ChunkParams p = {};
   ChunkWork need;
-  if (!(d.sm_scale >= 0.f) || !(d.sm_scale < 3.0e38f) || !carve_chunk_work(d, nullptr, kMaxPlanCtas, &need) || kv->k_scale || kv->v_scale) return EAGLE_ERR_SHAPE;
+  if (!(d.sm_scale >= 0.f) || !(d.sm_scale < 3.0e38f) || !carve_chunk_work(d, nullptr, kMaxPairs, &need) || kv->k_scale || kv->v_scale) return EAGLE_ERR_SHAPE;
   const int rc = check_store(*kv, d.head_dim, d.num_kv_heads, &p.capacity);
   if (rc != EAGLE_OK) return rc;
   if (d.batch == 0 || d.num_tokens == 0) return EAGLE_OK;
@@ -190,8 +190,8 @@ int eagle_chunk_attn(const eagle_chunk_desc* desc, const void* q, const eagle_kv
   const int dev = usable_device(&sms);
   if (dev != EAGLE_OK) return dev;
   if (!prepared(d.head_dim)) return EAGLE_ERR_DEVICE;
-  p.num_ctas = sms < kMaxPlanCtas ? sms : kMaxPlanCtas;
-  carve_chunk_work(d, d.workspace, p.num_ctas, &p.work);
+  p.num_pairs = sms / 2 < kMaxPairs ? sms / 2 : kMaxPairs;
+  carve_chunk_work(d, d.workspace, p.num_pairs, &p.work);
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.k = static_cast<const __nv_bfloat16*>(kv->k);
   p.v = static_cast<const __nv_bfloat16*>(kv->v);

@@ -2,15 +2,13 @@
 //
 //   out[t] = sum_j softmax_j(scale * q[t].k[j]) v[j],  j <= L_b + i, for token t = token_start[b] + i of sequence b.
 //
-// Three launches: a planner (one CTA), the attention kernel (one persistent CTA per SM) and the merge of what was cut.
+// Three launches: a planner (one CTA), the attention kernel (persistent, one cluster of two CTAs on every two SMs) and the merge
+// of what was cut.
 //
-// A query tile is 128 rows of one (sequence, KV head): TPT = 128 / G tokens (rounded down) times the G heads of the group.
-// A CTA runs two *streams* side by side, each with its own query tile, score buffer, accumulator and softmax warps:
-//   - a pair: query tiles 2p and 2p + 1 of one (sequence, KV head) over the same K/V tiles, which are loaded once;
-//   - a twin: the odd last query tile of two neighbouring KV heads, each with its own K/V tiles;
-//   - a lone tile (odd number of KV heads): one query tile, the streams take the two halves of its keys.
-// While one stream's softmax works on its scores the tensor pipe runs the other stream's products, so neither waits for the
-// other as long as a softmax step is shorter than two products of 128 x 128 x D.
+// A query tile is 128 rows of one (sequence, KV head): TPT = 128 / G tokens (rounded down) times the G heads of the group.  The two
+// CTAs of a pair take neighbouring query tiles over the same K/V tiles, and the tensor cores of both work on one MMA of 256
+// rows (cta_group::2): each CTA holds half of every K tile (64 keys) and half of every V tile (D / 2 columns), so a tile is
+// loaded once for both, and each SM reads half of the operand from its shared memory.
 #include "chunk.cuh"
 #include "tc.cuh"
 
@@ -22,14 +20,9 @@ using namespace tc;
 
 // ================================================================================================================ planner
 constexpr int kPlanThreads = 1024;
+constexpr int kNearSeqs = 512, kNearUnits = 4096;      // tables of calls this small stay in shared memory as well
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
-
-// Keys that query tile `qt` of a sequence sees at the most: the prefix and the tile's last token.
-__device__ __forceinline__ long long tile_keys(int L, int n, int qt, int tpt) {
-  const long long last = static_cast<long long>(qt + 1) * tpt;
-  return L + (last < n ? last : n);
-}
 
 // Inclusive prefix sums of (a, b) over the block; every thread gets its own, `tot` the block's.
 struct Sum2 {
@@ -74,70 +67,76 @@ __device__ __forceinline__ int last_le(const T* a, int n, T v) {
   return lo;
 }
 
-// K/V tile (of the unit's rounds) at which position `pos` of the work line cuts a unit that starts at `x`.
-__device__ __forceinline__ int cut_round(long long pos, long long x, int rounds) {
+// K/V tile at which position `pos` of the work line cuts a unit of `tiles` tiles that starts at `x`.
+__device__ __forceinline__ int cut_tile(long long pos, long long x, int tiles) {
   const long long t = (pos - x - kChunkItemKeys + kChunkTile / 2) >> 7;
   if (t < kChunkSnap) return 0;
-  return t > rounds - kChunkSnap ? rounds : static_cast<int>(t);
+  return t > tiles - kChunkSnap ? tiles : static_cast<int>(t);
 }
 
-// Work is counted in keys: a unit (pair, twin, lone) costs the keys of its longer stream plus a constant for starting it.
-// All units lie end to end on one line.  Whole units are dealt to the CTAs in rounds (CTA c gets units c, c + P, ...) while
-// every CTA's sum stays within its equal share W / P: CTAs then start neighbouring units at the same time, walk the same
-// keys at the same pace and share them through L2.  The units that are left are cut in contiguous shares that fill each
-// CTA up to W / P exactly, so the split needs at most P - 1 cuts whatever the lengths are.
+// Work is counted in keys: a unit costs the keys that its last token sees plus a constant for starting it.  All units lie end
+// to end on one line.  Whole units are dealt to the CTA pairs in rounds (pair c gets units c, c + P, ...) while every pair's sum
+// stays within its equal share W / P: pairs then start neighbouring units at the same time, walk the same keys at the same
+// pace and share them through L2.  The units that are left are cut in contiguous shares that fill each CTA pair up to W / P exactly,
+// so the split needs at most P - 1 cuts whatever the lengths are.
 __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p) {
   __shared__ Sum2 s_warp[kPlanThreads / 32];
-  __shared__ long long s_pos[kMaxPlanCtas + 1];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, P = p.num_ctas, B = p.B, Hkv = p.Hkv;
+  __shared__ long long s_pos[kMaxPairs + 1], s_cost[kNearSeqs], s_x[kNearUnits + 1];
+  __shared__ int s_base[kNearSeqs];
+  __shared__ ChunkSeq s_seq[kNearSeqs];
+  const int tid = threadIdx.x, P = p.num_pairs, B = p.B, Hkv = p.Hkv, tpt = p.tpt;
   ChunkWork& w = p.work;
+  ChunkSeq* seqs = B <= kNearSeqs ? s_seq : w.seq;
+  int* base_of = B <= kNearSeqs ? s_base : w.unit_base;
+  long long* cost_of = B <= kNearSeqs ? s_cost : w.cost_base;
 
+  launch_dependents();
   // the packed layout has to be an ascending list of starts inside the tensor: everything below relies on it
   int bad = 0;
-  for (int b = tid; b <= B; b += kPlanThreads) {
-    const int s = p.token_start[b];
-    if (s < 0 || s > p.N || (b < B && p.token_start[b + 1] < s)) bad = 1;
+  for (int b = tid; b < B; b += kPlanThreads) {
+    const int s = p.token_start[b], e = p.token_start[b + 1];
+    if (s < 0 || e < s || e > p.N) bad = 1;
+    if (b < kNearSeqs) s_seq[b] = ChunkSeq{s, e - s, p.seq_lens[b], 0};
   }
   bad = __syncthreads_or(bad);
   if (bad && tid == 0) report_status(p.status, EAGLE_ERR_SEQ);
 
   // ---- sequences: validity, units and cost, and where both start
-  const int singles = (Hkv + 1) / 2;                 // units of an odd last query tile: twins and, if Hkv is odd, a lone one
   Sum2 carry = {0, 0};
   for (int base = 0; base < B; base += kPlanThreads) {
     const int b = base + tid;
     ChunkSeq q = {0, 0, 0, 0};
     Sum2 v = {0, 0};
     if (b < B) {
-      const int s = p.token_start[b], e = p.token_start[b + 1];
-      q.L = p.seq_lens[b];
-      q.start = s;
-      if (!bad && e > s) {
-        if (q.L < 0 || static_cast<long long>(q.L) + (e - s) > p.capacity) report_status(p.status, EAGLE_ERR_SEQ);
-        else q.n = e - s;
+      int n;
+      if (B <= kNearSeqs) {
+        q = s_seq[b];
+        n = q.n;
+      } else {
+        q.start = p.token_start[b];
+        q.L = p.seq_lens[b];
+        n = p.token_start[b + 1] - q.start;
+      }
+      q.n = 0;
+      if (!bad && n > 0) {
+        if (q.L < 0 || static_cast<long long>(q.L) + n > p.capacity) report_status(p.status, EAGLE_ERR_SEQ);
+        else q.n = n;
       }
       if (q.n > 0) {
-        q.qtiles = ceil_div(q.n, p.tpt);
-        const long long np = q.qtiles / 2, keys = static_cast<long long>(q.L) + q.n;
+        q.pairs = ceil_div(ceil_div(q.n, tpt), 2);
+        const long long np = q.pairs;
         v.a = static_cast<int>(np) * Hkv;
-        // sum over the pairs of L + (2p + 2) TPT, the last one's end being n
-        long long pairs = np * (q.L + kChunkItemKeys) + p.tpt * np * (np + 1);
-        if (np > 0 && !(q.qtiles & 1)) pairs -= static_cast<long long>(q.qtiles) * p.tpt - q.n;
-        v.b = pairs * Hkv;
-        if (q.qtiles & 1) {
-          v.a += singles;
-          v.b += (Hkv / 2) * (keys + kChunkItemKeys);
-          if (Hkv & 1) v.b += (keys + 1) / 2 + kChunkItemKeys;
-        }
+        // sum over the pairs of L + (2p + 2) TPT, but the last one ends at n
+        v.b = (np * (q.L + kChunkItemKeys) + tpt * np * (np + 1) - (2 * np * tpt - q.n)) * Hkv;
       }
     }
     Sum2 tot;
     const Sum2 inc = block_scan(v, s_warp, &tot);
     if (b < B) {
-      w.seq[b] = q;
-      w.unit_base[b] = carry.a + inc.a - v.a;
-      w.cost_base[b] = carry.b + inc.b - v.b;
-      w.cut[P + b].unit = -1;
+      seqs[b] = q;
+      if (seqs != w.seq) w.seq[b] = q;
+      base_of[b] = carry.a + inc.a - v.a;
+      cost_of[b] = carry.b + inc.b - v.b;
     }
     carry.a += tot.a;
     carry.b += tot.b;
@@ -145,129 +144,89 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
   }
   const int U = carry.a;
   const long long W = carry.b;
-  for (int c = tid; c < P; c += kPlanThreads) w.cut[c].unit = -1;
+  if (tid < P) w.cut[tid].unit = -1;
   if (U == 0) {
-    for (int c = tid; c < P; c += kPlanThreads) w.cta[c] = make_int4(0, 0, 0, 0);
+    if (tid < P) w.cta[tid] = make_int4(0, 0, 0, 0);
     return;
   }
+  long long* x_of = U <= kNearUnits ? s_x : w.x;
   __syncthreads();
 
-  // ---- units: the odd last query tile first, then the pairs from the longest to the shortest, KV heads innermost
-  for (int u = tid; u < U; u += kPlanThreads) {
-    const int b = last_le(w.unit_base, B, u);
-    const ChunkSeq q = w.seq[b];
-    int i = u - w.unit_base[b];
-    long long x = w.cost_base[b];
-    const long long keys = static_cast<long long>(q.L) + q.n;
+  // ---- units: a sequence's pairs from the longest to the shortest, KV heads innermost
+  auto unit_of = [&](int u, long long* x) {
+    const int b = last_le(base_of, B, u);
+    const ChunkSeq q = seqs[b];
+    const int i = u - base_of[b], r = i / Hkv, pr = q.pairs - 1 - r;      // r longer pairs come before
     ChunkUnit un;
     un.b = b;
-    un.pad = 0;
-    const int first = q.qtiles & 1 ? singles : 0;
-    if (i < first) {
-      un.g = 2 * i;
-      un.qt = q.qtiles - 1;
-      un.kind = 2 * i + 1 < Hkv ? kChunkTwin : kChunkLone;
-      x += i * (keys + kChunkItemKeys);
-    } else {
-      i -= first;
-      const int np = q.qtiles / 2, r = i / Hkv, pr = np - 1 - r;     // pairs pr + 1 .. np - 1 come before
-      un.g = i - r * Hkv;
-      un.qt = 2 * pr;
-      un.kind = kChunkPair;
-      if (first) x += (Hkv / 2) * (keys + kChunkItemKeys) + (Hkv & 1 ? (keys + 1) / 2 + kChunkItemKeys : 0);
-      long long before = static_cast<long long>(r) * (q.L + kChunkItemKeys) +
-                         p.tpt * (static_cast<long long>(np) * (np + 1) - static_cast<long long>(pr + 1) * (pr + 2));
-      const long long over = q.qtiles & 1 ? 0 : static_cast<long long>(q.qtiles) * p.tpt - q.n;   // the last pair is that much shorter
-      if (r > 0) before -= over;
-      long long one = q.L + kChunkItemKeys + static_cast<long long>(2 * pr + 2) * p.tpt;
-      if (r == 0) one -= over;
-      x += before * Hkv + un.g * one;
+    un.g = i - r * Hkv;
+    un.pair = pr;
+    const long long over = 2ll * q.pairs * tpt - q.n;                      // the last pair is that much shorter
+    const long long keys = q.L + (2ll * pr + 2) * tpt - (r == 0 ? over : 0);
+    un.tiles = static_cast<int>((keys + kChunkTile - 1) / kChunkTile);
+    if (x) {
+      const long long before = static_cast<long long>(r) * (q.L + kChunkItemKeys) +
+                               tpt * (static_cast<long long>(q.pairs) * (q.pairs + 1) - static_cast<long long>(pr + 1) * (pr + 2)) - (r > 0 ? over : 0);
+      *x = cost_of[b] + before * Hkv + un.g * (keys + kChunkItemKeys);
     }
-    un.nt[0] = static_cast<int>((tile_keys(q.L, q.n, un.qt, p.tpt) + kChunkTile - 1) / kChunkTile);
-    un.nt[1] = un.kind == kChunkPair ? static_cast<int>((tile_keys(q.L, q.n, un.qt + 1, p.tpt) + kChunkTile - 1) / kChunkTile) : un.nt[0];
-    w.unit[u] = un;
-    w.x[u] = x;
+    return un;
+  };
+  for (int u = tid; u < U; u += kPlanThreads) {
+    long long x;
+    w.unit[u] = unit_of(u, &x);
+    x_of[u] = x;
   }
-  if (tid == 0) w.x[U] = W;
+  if (tid == 0) x_of[U] = W;
   __syncthreads();
 
-  // ---- whole units while they fit every CTA's share
+  // ---- whole units while they fit every CTA pair's share
   const long long T = (W + P - 1) / P;
   long long S = 0;
   int k = 0;
   for (; (k + 1) * P <= U; ++k) {
     long long cost = 0;
-    if (tid < P) cost = w.x[k * P + tid + 1] - w.x[k * P + tid];
+    if (tid < P) cost = x_of[k * P + tid + 1] - x_of[k * P + tid];
     if (__syncthreads_or(S + cost > T)) break;
     S += cost;
   }
   const int F = k * P;
-  // ---- what is left is shared out so that every CTA comes to T
+  // ---- what is left is shared out so that every pair comes to T
   {
     Sum2 v = {0, tid < P ? T - S : 0}, tot;
     const Sum2 inc = block_scan(v, s_warp, &tot);
     if (tid <= P) {
-      const long long at = w.x[F] + inc.b - v.b;
+      const long long at = x_of[F] + inc.b - v.b;
       s_pos[tid] = tid == P || at > W ? W : at;
     }
   }
   __syncthreads();
 
-  auto emit = [&](int slot_index, int u, int r0, int r1, int part) {   // rounds [r0, r1) of unit u; part < 0: all of it
-    const ChunkUnit un = w.unit[u];
-    const ChunkSeq q = w.seq[un.b];
-    ChunkItem it;
-    it.b = un.b;
-    it.kind = un.kind;
-    it.start = q.start;
-    it.n = q.n;
-    it.L = q.L;
-    it.pad = 0;
-    it.g[0] = un.g;
-    it.g[1] = un.kind == kChunkTwin ? un.g + 1 : un.g;
-    it.qt[0] = un.qt;
-    it.qt[1] = un.kind == kChunkPair ? un.qt + 1 : un.qt;
-    const int half = un.kind == kChunkLone ? (un.nt[0] + 1) / 2 : 0;
-    const int end0 = un.kind == kChunkLone ? half : un.nt[0], end1 = un.nt[1];
-    it.t0[0] = r0;
-    it.t1[0] = r1 < end0 ? r1 : end0;
-    it.t0[1] = half + r0;
-    it.t1[1] = half + r1 < end1 ? half + r1 : end1;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      if (it.t1[s] < it.t0[s]) it.t1[s] = it.t0[s];
-      it.slot[s] = part < 0 ? -1 : 2 * part + s;
-    }
-    w.items[slot_index] = it;
+  auto emit = [&](int at, const ChunkUnit& un, int t0, int t1, int slot) {
+    const ChunkSeq q = seqs[un.b];
+    int4* it = reinterpret_cast<int4*>(w.items + at);
+    it[0] = make_int4(un.b, un.g, un.pair, q.start);
+    it[1] = make_int4(q.n, q.L, t0, t1);
+    it[2] = make_int4(slot, 0, 0, 0);
   };
-  auto rounds_of = [&](const ChunkUnit& un) { return un.kind == kChunkLone ? (un.nt[0] + 1) / 2 : un.nt[1]; };
-  // a lone tile that is not cut is merged from its two halves all the same (unless there is only one K/V tile)
-  auto whole_part = [&](int u, const ChunkUnit& un) {
-    if (un.kind != kChunkLone || un.nt[0] < 2) return -1;
-    w.cut[P + un.b] = ChunkCut{u, -1, 2 * P + un.b, 0};
-    return 2 * P + un.b;
-  };
-
   for (int u = tid; u < F; u += kPlanThreads) {
-    const ChunkUnit un = w.unit[u];
-    emit((u % P) * k + u / P, u, 0, rounds_of(un), whole_part(u, un));
+    const ChunkUnit un = unit_of(u, nullptr);
+    emit((u % P) * k + u / P, un, 0, un.tiles, -1);
   }
-  // the shares: piece (u, c) of unit u in CTA c's share is item u + c
-  for (int u = F + warp; u < U; u += kPlanThreads / 32) {
-    const ChunkUnit un = w.unit[u];
-    const long long x0 = w.x[u], x1 = w.x[u + 1];
-    const int c_lo = last_le(s_pos, P, x0), c_hi = last_le(s_pos, P, x1 - 1), rounds = rounds_of(un);
-    for (int c = c_lo + lane; c <= c_hi; c += 32) {
-      const int r0 = c == c_lo ? 0 : cut_round(s_pos[c], x0, rounds), r1 = c == c_hi ? rounds : cut_round(s_pos[c + 1], x0, rounds);
-      if (r0 == 0 && r1 == rounds) emit(u + c, u, r0, r1, whole_part(u, un));
-      else emit(u + c, u, r0, r1 > r0 ? r1 : r0, 2 * c + (r0 > 0 ? 0 : 1));
+  // the shares: piece (u, c) of unit u in pair c's share is item u + c
+  for (int u = F + (tid >> 3); u < U; u += kPlanThreads / 8) {           // eight lanes to a unit
+    const ChunkUnit un = unit_of(u, nullptr);
+    const long long x0 = x_of[u], x1 = x_of[u + 1];
+    const int c_lo = last_le(s_pos, P, x0), c_hi = last_le(s_pos, P, x1 - 1);
+    for (int c = c_lo + (tid & 7); c <= c_hi; c += 8) {
+      const int t0 = c == c_lo ? 0 : cut_tile(s_pos[c], x0, un.tiles), t1 = c == c_hi ? un.tiles : cut_tile(s_pos[c + 1], x0, un.tiles);
+      emit(u + c, un, t0, t1 > t0 ? t1 : t0, t0 == 0 && t1 == un.tiles ? -1 : 4 * c + (t0 > 0 ? 0 : 2));
     }
-    if (lane == 0 && c_hi > c_lo) w.cut[c_lo] = ChunkCut{u, c_lo, c_hi, 0};
+    if ((tid & 7) == 0 && c_hi > c_lo) w.cut[c_lo] = ChunkCut{u, c_lo, c_hi, 0};
   }
   if (tid < P) {
     int first = 0, count = 0;
     if (s_pos[tid + 1] > s_pos[tid] && F < U) {
-      const int u0 = last_le(w.x, U, s_pos[tid]), u1 = last_le(w.x, U, s_pos[tid + 1] - 1);
+      const int u0 = last_le(x_of, U, s_pos[tid]), u1 = last_le(x_of, U, s_pos[tid + 1] - 1);
       first = u0 + tid;
       count = u1 - u0 + 1;
     }
@@ -276,11 +235,12 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
 }
 
 // ============================================================================================================== attention
-constexpr int kThreads = 384;            // two softmax groups of four warps, producer, two MMA issuers, query loader
-constexpr int kGroupThreads = 128;
-constexpr int kWarpProducer = 8, kWarpMma = 9, kWarpQuery = 11;
-constexpr int kSlots = 4;                // K/V ring: a pair uses slots 0, 1 for K and 2, 3 for V; a twin's stream s slots s and 2 + s
-constexpr uint32_t kTmemCols = 512;      // S0 S1 | O0 O1; P (packed bf16, 64 columns) overwrites the front of its S
+constexpr int kThreads = 384;            // two softmax groups of four warps, K/V producer, relay, two MMA issuers (idle in the second CTA)
+constexpr int kWarpProducer = 8, kWarpRelay = 9, kWarpQK = 10, kWarpPV = 11;
+constexpr int kSBufs = 3;                // score buffers in tensor memory; step g uses buffer g % 3
+constexpr int kKSlots = 5, kVSlots = 4;  // rings of half tiles; step g's tiles lie in slots g % 5 and g % 4
+constexpr uint32_t kTmemCols = 512;      // S0 S1 S2 | O; P (packed bf16, 64 columns) overwrites the front of its S
+constexpr uint32_t kColO = 384;
 constexpr float kRescaleThreshold = 8.0f;   // log2 units: the accumulator is rescaled when the row maximum outgrows its reference by more
 #ifndef EAGLE_CHUNK_POLY
 #define EAGLE_CHUNK_POLY 3
@@ -290,71 +250,81 @@ constexpr int kPolyStride = EAGLE_CHUNK_POLY;   // one pair of exponentials in s
 template <int D>
 struct Smem {
   static constexpr int kSlabs = D / 64;                      // 64 bf16 = one 128-byte swizzled row
-  static constexpr int kSlabBytes = kChunkTile * 128;
-  static constexpr int kTileBytes = kSlabs * kSlabBytes;
-  static constexpr int kQ = 0;                               // one query tile per stream
-  static constexpr int kRing = 2 * kTileBytes;
-  static constexpr int kBar = kRing + kSlots * kTileBytes;
-  static constexpr int kNumBars = 3 * kSlots + 12;
+  static constexpr int kQSlab = 128 * 128, kQBytes = kSlabs * kQSlab;
+  static constexpr int kKSlab = 64 * 128, kKBytes = kSlabs * kKSlab;     // half a K tile: 64 keys
+  static constexpr int kVBytes = 128 * D;                    // half a V tile: 128 keys x D / 2 columns
+  static constexpr int kQ = 0;                               // two query tiles: the current item's and the next one's
+  static constexpr int kK = 2 * kQBytes;
+  static constexpr int kV = kK + kKSlots * kKBytes;
+  static constexpr int kTag = kV + kVSlots * kVBytes;        // uint32 [128 rows]: reference maximum | step number
+  static constexpr int kLfin = kTag + 128 * 4;               // float [2][128 rows]: row sums on their way to the output, by items in turn
+  static constexpr int kBar = kLfin + 2 * 128 * 4;
+  static constexpr int kNumBars = 2 * (kKSlots + 2) + 3 * kVSlots + 3 * kSBufs + 1;
   static constexpr int kMisc = kBar + 8 * kNumBars;          // tensor-memory base, abort flag, wait limit (8 bytes)
   static constexpr int kBytes = kMisc + 16;
 };
 
-// A slot has one "empty" barrier and two "full" ones, for its uses in pairs and in twins.  A waiter tells the phases of a
-// barrier apart by parity only, so it has to see every one of them: both issuers see every load of a pair (the stream with
-// fewer tiles walks past those it does not need), and the loads of a twin are seen by the one stream that owns the slot.
+// The same places in both CTAs.  ready: a tile has landed in both (first CTA only); full: this CTA's half of a V tile has
+// landed; empty: the MMAs have finished with the slot (both CTAs).
 struct Bars {
   uint32_t base;
-  __device__ __forceinline__ uint32_t full(bool shared, uint32_t i) const { return base + 8u * ((shared ? 0 : kSlots) + i); }
-  __device__ __forceinline__ uint32_t empty(uint32_t i) const { return base + 8u * (2 * kSlots + i); }
-  __device__ __forceinline__ uint32_t q_full(uint32_t s) const { return base + 8u * (3 * kSlots + s); }
-  __device__ __forceinline__ uint32_t q_empty(uint32_t s) const { return base + 8u * (3 * kSlots + 2 + s); }
-  __device__ __forceinline__ uint32_t s_full(uint32_t s) const { return base + 8u * (3 * kSlots + 4 + s); }   // scores are there
-  __device__ __forceinline__ uint32_t p_full(uint32_t s) const { return base + 8u * (3 * kSlots + 6 + s); }   // probabilities are there
-  __device__ __forceinline__ uint32_t o_full(uint32_t s) const { return base + 8u * (3 * kSlots + 8 + s); }   // an item's last PV has finished
-  __device__ __forceinline__ uint32_t o_free(uint32_t s) const { return base + 8u * (3 * kSlots + 10 + s); }  // its accumulator has been read
+  static constexpr uint32_t kVAt = 2 * kKSlots, kQAt = kVAt + 3 * kVSlots, kSAt = kQAt + 4;
+  __device__ __forceinline__ uint32_t at(uint32_t i) const { return base + 8u * i; }
+  __device__ __forceinline__ uint32_t k_ready(uint32_t i) const { return at(i); }
+  __device__ __forceinline__ uint32_t k_empty(uint32_t i) const { return at(kKSlots + i); }
+  __device__ __forceinline__ uint32_t v_full(uint32_t i) const { return at(kVAt + i); }
+  __device__ __forceinline__ uint32_t v_ready(uint32_t i) const { return at(kVAt + kVSlots + i); }
+  __device__ __forceinline__ uint32_t v_empty(uint32_t i) const { return at(kVAt + 2 * kVSlots + i); }
+  __device__ __forceinline__ uint32_t q_ready(uint32_t i) const { return at(kQAt + i); }
+  __device__ __forceinline__ uint32_t q_empty(uint32_t i) const { return at(kQAt + 2 + i); }
+  __device__ __forceinline__ uint32_t s_full(uint32_t i) const { return at(kSAt + i); }                  // scores of a step (both CTAs)
+  __device__ __forceinline__ uint32_t p_full(uint32_t i) const { return at(kSAt + kSBufs + i); }         // its probabilities (first CTA only)
+  __device__ __forceinline__ uint32_t o_done(uint32_t i) const { return at(kSAt + 2 * kSBufs + i); }     // its PV has finished (both CTAs)
+  __device__ __forceinline__ uint32_t o_free() const { return at(kSAt + 3 * kSBufs); }                   // an item's accumulators have been read (first CTA only)
 };
 
-// How often the items so far have used slots 0 and 1 (slots 2 and 3: the same), in pairs and in twins; and where round j of
-// stream s finds its K tile (the V tile is two slots further): the slot and the number of that use among those of its kind.
-struct Place {
-  uint32_t slot, use;
+// Counts steps through a ring: slot and parity of the use after next calls of step().
+template <int N>
+struct Ring {
+  uint32_t slot = 0, par = 0;
+  __device__ __forceinline__ void step() {
+    if (++slot == N) { slot = 0; par ^= 1u; }
+  }
 };
-struct Uses {
-  uint32_t pair[2] = {0, 0}, twin[2] = {0, 0};
-  __device__ __forceinline__ Place place(bool shared, int s, int j) const {
-    if (shared) return {static_cast<uint32_t>(j & 1), ((j & 1) ? pair[1] : pair[0]) + static_cast<uint32_t>(j >> 1)};
-    return {static_cast<uint32_t>(s), (s ? twin[1] : twin[0]) + static_cast<uint32_t>(j)};
-  }
-  // parity to wait for before the slot is filled again: uses of either kind count
-  __device__ __forceinline__ uint32_t free_parity(bool shared, const Place& pl) const {
-    const uint32_t before = pl.use + (shared ? (pl.slot ? twin[1] : twin[0]) : (pl.slot ? pair[1] : pair[0]));
-    return (before & 1u) ^ 1u;
-  }
-  __device__ __forceinline__ void add(bool shared, int len0, int len1) {
-    if (shared) {
-      const uint32_t len = static_cast<uint32_t>(len0 > len1 ? len0 : len1);
-      pair[0] += (len + 1) >> 1;
-      pair[1] += len >> 1;
-    } else {
-      twin[0] += static_cast<uint32_t>(len0);
-      twin[1] += static_cast<uint32_t>(len1);
+
+// Bounded wait for a tagged word in shared memory (low byte == want): the word, with bit 32 set; 0 when the CTA was aborted or
+// the time limit passed.
+__device__ __noinline__ unsigned long long tag_wait_slow(volatile uint32_t* slot, uint32_t want, volatile int* abort_flag) {
+  const unsigned long long t0 = global_timer(), limit = *reinterpret_cast<volatile unsigned long long*>(abort_flag + 1);
+  for (uint32_t spins = 1;; ++spins) {
+    const uint32_t t = *slot;
+    if ((t & 0xffu) == want) return (1ull << 32) | t;
+    if ((spins & 63u) == 0) {
+      if (*abort_flag) return 0ull;
+      if (global_timer() - t0 > limit) {
+        *abort_flag = 1;
+        return 0ull;
+      }
     }
+    __nanosleep(20);
   }
-};
-
-// (a runtime index into the item's arrays would put it into local memory)
-__device__ __forceinline__ int of_stream(const int32_t (&a)[2], int s) { return s ? a[1] : a[0]; }
+}
+__device__ __forceinline__ unsigned long long tag_wait(volatile uint32_t* slot, uint32_t want, volatile int* abort_flag) {
+  const uint32_t t = *slot;
+  if ((t & 0xffu) == want) return (1ull << 32) | t;
+  return tag_wait_slow(slot, want, abort_flag);
+}
 
 template <int D, bool PAGED>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ CUtensorMap map_q) {
   using S = Smem<D>;
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t sbase = smem_u32(smem);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (sbase & 1023u) {   // the swizzled tiles need a 1024-byte aligned base; uniform over the CTA
+  const uint32_t rank = cluster_rank();
+  if (sbase & 1023u) {   // the swizzled tiles need a 1024-byte aligned base; uniform over the launch
     if (tid == 0) report_status(p.status, EAGLE_ERR_DEVICE);
     return;
   }
@@ -367,225 +337,252 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     prefetch_map(&map_k);
     prefetch_map(&map_v);
     prefetch_map(&map_q);
-    for (int i = 0; i < kSlots; ++i) {
-      mbar_init(B.full(false, i), 1);
-      mbar_init(B.full(true, i), 1);
-      mbar_init(B.empty(i), 2);          // both streams of a pair, or twice the one that uses it
+    for (int i = 0; i < kKSlots; ++i) { mbar_init(B.k_ready(i), 1); mbar_init(B.k_empty(i), 1); }
+    for (int i = 0; i < kVSlots; ++i) { mbar_init(B.v_full(i), 1); mbar_init(B.v_ready(i), 2); mbar_init(B.v_empty(i), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(B.q_ready(i), 1); mbar_init(B.q_empty(i), 1); }
+    for (int i = 0; i < kSBufs; ++i) {
+      mbar_init(B.s_full(i), 1);
+      mbar_init(B.p_full(i), 8);           // a group's four warps, in both CTAs
+      mbar_init(B.o_done(i), 1);
     }
-    for (int s = 0; s < 2; ++s) {
-      mbar_init(B.q_full(s), 1);
-      mbar_init(B.q_empty(s), 1);
-      mbar_init(B.s_full(s), 1);
-      mbar_init(B.p_full(s), kGroupThreads);
-      mbar_init(B.o_full(s), 1);
-      mbar_init(B.o_free(s), kGroupThreads);
-    }
+    mbar_init(B.o_free(), 8);
     *s_abort = 0;
     *reinterpret_cast<volatile unsigned long long*>(smem + S::kMisc + 8) = p.wait_limit_ns;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == kWarpMma) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sbase + S::kMisc), "r"(kTmemCols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  if (tid < 128) reinterpret_cast<volatile uint32_t*>(smem + S::kTag)[tid] = 0xffffffffu;   // no step carries this tag yet
+  if (warp == kWarpQK) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sbase + S::kMisc), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   fence_before();
   __syncthreads();
+  cluster_sync();                          // both CTAs' barriers exist before either is arrived at from across
   fence_after();
   const uint32_t tmem = *s_tmem;
 
-  const int4 mine = p.work.cta[blockIdx.x];              // whole units first, then this CTA's share of the rest
+  launch_dependents();
+  wait_for_prerequisites();                // the plan is there
+  const int4 mine = p.work.cta[blockIdx.x >> 1];         // whole units first, then this pair's share of the rest
   const int n_items = mine.y + mine.w;
-  auto item = [&](int i) { return p.work.items[i < mine.y ? mine.x + i : mine.z + (i - mine.y)]; };
+  struct Item {
+    int b, g, pair, start, n, L, t0, t1, slot;
+  };
+  auto item = [&](int i) {
+    const int4* at = reinterpret_cast<const int4*>(p.work.items + (i < mine.y ? mine.x + i : mine.z + (i - mine.y)));
+    const int4 a = at[0], b = at[1];
+    return Item{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, at[2].x};
+  };
 
-  if (warp == kWarpMma || warp == kWarpMma + 1) {
-    // =========================================================================== MMA issuer of one stream
-    // The tensor pipe runs one thread's MMAs in the order they were issued: S(j + 1) may overwrite P(j) without a wait, and
-    // the arrival that reports S(j + 1) reports PV(j) too.
-    if (lane == 0) {
-      const int s = warp - kWarpMma;
-      constexpr uint32_t idesc_qk = instr_desc(128, kChunkTile, false), idesc_pv = instr_desc(128, D, true);
-      const uint32_t q_lo = desc_lo(sbase + S::kQ + s * S::kTileBytes, 16);
-      const uint32_t k_lo = desc_lo(sbase + S::kRing, 16), v_lo = desc_lo(sbase + S::kRing, S::kSlabBytes);
-      constexpr uint32_t kTileStep = S::kTileBytes >> 4, kSlabStep = S::kSlabBytes >> 4;
-      const uint32_t t_s = tmem + s * 128, t_o = tmem + 256 + s * 128;
-      Uses uses;
+  if (warp == kWarpProducer) {
+    // =========================================================================== copies
+    // Order: K(0), K(1), K(2), then V(g), K(g + 3), g counting this pair's steps over all items (the score MMA runs up to three
+    // steps ahead of the PV MMA); an item's query tile goes with its first K tile.  Each CTA's producer fetches its own halves; K
+    // and query tiles report to the first CTA's barrier, V tiles to the relay of their own CTA.  A lane per box (a page, or a
+    // 64-column half); the page of a lane's next box is looked up while the box before it is on its way.
+    struct Cursor {
+      Item it;
+      int i, tile, end;
+      int y, page;                         // this lane's next box: row in its page (or in the sequence), page (or sequence)
+      bool valid, fresh;
+    };
+    const int k_rows = PAGED ? min(p.page_size, 64) : 64, v_rows = PAGED ? min(p.page_size, kChunkTile) : kChunkTile;
+    const int k_r0 = (lane / S::kSlabs) * k_rows, v_r0 = lane * v_rows, half = static_cast<int>(rank);
+    auto advance = [&](Cursor& c, bool is_v) {        // to the next K/V tile of the work list
+      c.fresh = false;
+      if (++c.tile >= c.end) {
+        for (++c.i; c.i < n_items; ++c.i) {
+          c.it = item(c.i);
+          if (c.it.t1 > c.it.t0) break;
+        }
+        if (c.i >= n_items) {
+          c.valid = false;
+          return;
+        }
+        c.tile = c.it.t0;
+        c.end = c.it.t1;
+        c.fresh = true;
+      }
+      const int r0 = is_v ? v_r0 : k_r0, key = c.tile * kChunkTile + (is_v ? 0 : half * 64) + r0;
+      c.y = key;
+      c.page = c.it.b;
+      if (PAGED && r0 < (is_v ? kChunkTile : 64)) {
+        // a box past the sequence's last page fetches that page again (its rows are masked), so that a tile's byte count never changes
+        const int last = (c.it.L + c.it.n - 1) >> p.page_shift, pi = key >> p.page_shift;
+        c.page = __ldg(p.block_table + static_cast<size_t>(c.it.b) * p.max_pages + (pi < last ? pi : last));
+        c.y = key & (p.page_size - 1);
+      }
+    };
+    // an entry outside the pool reads page 0 (the merge kernel reports it and zeroes the sequence)
+    auto place = [&](const Cursor& c) { return (PAGED && (c.page < 0 || c.page >= p.num_pages) ? 0 : c.page) * p.Hkv + c.it.g; };
+    const uint32_t to_first = map_to_rank(sbase, 0) - sbase;       // added to a barrier's address: the first CTA's
+    bool ok = true;
+    Ring<kKSlots> kr;
+    Ring<kVSlots> vr;
+    uint32_t q_items = 0;
+    Cursor ck, cv;
+    ck.i = cv.i = -1;
+    ck.tile = ck.end = cv.tile = cv.end = 0;
+    ck.valid = cv.valid = true;
+    advance(ck, false);
+    advance(cv, true);
+    auto next_key = [&]() {
+      if (!ck.valid || !ok) return;
+      if (ck.fresh) {
+        // box of TPT tokens x G heads x 64 columns: rows land in (token, head) order; rows of the next sequence (or zeros past
+        // the tensor) that come along are computed and never written
+        const uint32_t qb = q_items & 1u;
+        ok = mbar_wait_warp(B.q_empty(qb), ((q_items >> 1) & 1u) ^ 1u, s_abort);
+        if (!ok) return;
+        if (lane == 0) {
+          if (rank == 0) mbar_expect_tx(B.q_ready(qb), 2 * S::kSlabs * p.tpt * p.G * 128);
+#pragma unroll
+          for (int sl = 0; sl < S::kSlabs; ++sl)
+            tma_load_3d_pair(sbase + S::kQ + qb * S::kQBytes + sl * S::kQSlab, &map_q, sl * 64, ck.it.g * p.G,
+                             ck.it.start + (2 * ck.it.pair + half) * p.tpt, B.q_ready(qb) + to_first);
+        }
+        ++q_items;
+      }
+      ok = mbar_wait_warp(B.k_empty(kr.slot), kr.par ^ 1u, s_abort);
+      if (!ok) return;
+      if (lane == 0 && rank == 0) mbar_expect_tx(B.k_ready(kr.slot), 2 * S::kKBytes);
+      const int sl = lane % S::kSlabs;
+      if (k_r0 < 64)
+        tma_load_3d_pair(sbase + S::kK + kr.slot * S::kKBytes + sl * S::kKSlab + k_r0 * 128, &map_k, sl * 64, ck.y, place(ck),
+                         B.k_ready(kr.slot) + to_first);
+      kr.step();
+      advance(ck, false);
+    };
+    for (int i = 0; i < 3; ++i) next_key();
+    while (cv.valid && ok) {
+      ok = mbar_wait_warp(B.v_empty(vr.slot), vr.par ^ 1u, s_abort);
+      if (!ok) break;
+      if (lane == 0) mbar_expect_tx(B.v_full(vr.slot), S::kVBytes);
+      __syncwarp();
+      if (v_r0 < kChunkTile)
+        tma_load_3d(sbase + S::kV + vr.slot * S::kVBytes + v_r0 * D, &map_v, half * (D / 2), cv.y, place(cv), B.v_full(vr.slot));
+      vr.step();
+      advance(cv, true);
+      next_key();
+    }
+  } else if (warp == kWarpRelay) {
+    // =========================================================================== V tiles that have landed
+    // The rows of V past the sequence may hold anything, and 0 * garbage must not reach O: they are zeroed here before the first
+    // CTA's issuer hears of the tile.
+    bool ok = true;
+    Ring<kVSlots> vr;
+    const uint32_t to_first = map_to_rank(sbase, 0) - sbase;
+    for (int i = 0; i < n_items && ok; ++i) {
+      const Item it = item(i);
+      for (int t = it.t0; t < it.t1; ++t, vr.step()) {
+        ok = mbar_wait_warp(B.v_full(vr.slot), vr.par, s_abort);
+        if (!ok) break;
+        const int valid = it.L + it.n - t * kChunkTile;            // keys of the tile that belong to the sequence
+        if (valid < kChunkTile) {
+          for (int j = valid * (D / 16) + lane; j < kChunkTile * (D / 16); j += 32)        // whole rows of D bytes, so the swizzle does not matter
+            *reinterpret_cast<uint4*>(smem + S::kV + vr.slot * S::kVBytes + j * 16) = make_uint4(0u, 0u, 0u, 0u);
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_release_pair(B.v_ready(vr.slot) + to_first);
+        } else if (lane == 0) {
+          mbar_arrive_pair(B.v_ready(vr.slot) + to_first);
+        }
+      }
+    }
+  } else if (warp == kWarpQK) {
+    // =========================================================================== S = Q K^T, up to three steps ahead of the softmax
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = instr_desc(256, kChunkTile, false);
+      const uint32_t q_lo = desc_lo(sbase + S::kQ), k_lo = desc_lo(sbase + S::kK);
+      Ring<kKSlots> kr;
+      Ring<kSBufs> sr;
       uint32_t steps = 0, items = 0;
       bool ok = true;
       for (int i = 0; i < n_items && ok; ++i) {
-        const ChunkItem it = item(i);
-        const bool shared = it.kind == kChunkPair;
-        const int len0 = it.t1[0] - it.t0[0], len1 = it.t1[1] - it.t0[1], len = s ? len1 : len0;
-        auto release = [&](uint32_t bar) {
-          commit(bar);
-          if (!shared) commit(bar);          // nobody else uses the slot
-        };
-        auto score = [&](int j) {
-          const Place pl = uses.place(shared, s, j);
-          ok = mbar_wait(B.full(shared, pl.slot), pl.use & 1u, s_abort);
-          if (!ok) return;
+        const Item it = item(i);
+        if (it.t1 <= it.t0) continue;
+        const uint32_t qb = items & 1u;
+        ok = mbar_wait(B.q_ready(qb), (items >> 1) & 1u, s_abort);
+        for (int t = it.t0; t < it.t1 && ok; ++t, ++steps) {
+          ok = mbar_wait(B.k_ready(kr.slot), kr.par, s_abort);
+          if (ok && steps >= kSBufs) ok = mbar_wait(B.o_done(sr.slot), sr.par ^ 1u, s_abort);   // the buffer's last P has been used
+          if (!ok) break;
           fence_after();
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            const uint32_t step = (kk >> 2) * kSlabStep + (kk & 3) * 2;
-            mma_ss(t_s, desc(q_lo + step), desc(k_lo + pl.slot * kTileStep + step), idesc_qk, kk != 0);
-          }
-          commit(B.s_full(s));
-          release(B.empty(pl.slot));
-          if (j == len - 1) commit(B.q_empty(s));
-        };
-        if (len > 0) {
-          ok = mbar_wait(B.q_full(s), items & 1u, s_abort);
-          if (!ok) break;
-          score(0);
-          for (int j = 0; j < len && ok; ++j, ++steps) {
-            const Place pl = uses.place(shared, s, j);
-            ok = mbar_wait(B.full(shared, 2 + pl.slot), pl.use & 1u, s_abort);
-            if (!ok) break;
-            if (j == 0 && items > 0) {
-              ok = mbar_wait(B.o_free(s), (items - 1) & 1u, s_abort);
-              if (!ok) break;
-            }
-            ok = mbar_wait(B.p_full(s), steps & 1u, s_abort);
-            if (!ok) break;
-            fence_after();
-#pragma unroll
-            for (int kk = 0; kk < kChunkTile / 16; ++kk)
-              mma_ts(t_o, t_s + kk * 8, desc(v_lo + (2 + pl.slot) * kTileStep + kk * 128), idesc_pv, (j | kk) != 0);
-            release(B.empty(2 + pl.slot));
-            if (j == len - 1) commit(B.o_full(s));
-            else score(j + 1);
-          }
-          ++items;
+          issue_qk_pair<D>(tmem + sr.slot * 128, q_lo + qb * (S::kQBytes >> 4), k_lo + kr.slot * (S::kKBytes >> 4), idesc);
+          commit_pair(B.s_full(sr.slot));
+          commit_pair(B.k_empty(kr.slot));
+          if (t == it.t1 - 1) commit_pair(B.q_empty(qb));
+          kr.step();
+          sr.step();
         }
-        if (shared) {
-          for (int j = len; j < len1 && ok; ++j) {   // the first stream of a pair may have fewer tiles: it lets the others pass
-            const Place pl = uses.place(true, 0, j);
-            ok = mbar_wait(B.full(true, pl.slot), pl.use & 1u, s_abort);
-            if (!ok) break;
-            mbar_arrive(B.empty(pl.slot));
-            ok = mbar_wait(B.full(true, 2 + pl.slot), pl.use & 1u, s_abort);
-            if (!ok) break;
-            mbar_arrive(B.empty(2 + pl.slot));
-          }
-        }
-        uses.add(shared, len0, len1);
+        ++items;
       }
     }
-  } else if (warp == kWarpQuery) {
-    // =========================================================================== query tiles
-    // Box of TPT tokens x G heads x 64 columns: rows land in (token, head) order.  A tile that reaches past the sequence's
-    // last token brings rows of the next sequence (or zeros past the tensor) along; they are computed and never written.
-    if (lane == 0) {
-      uint32_t items[2] = {0, 0};
+  } else if (warp == kWarpPV) {
+    // =========================================================================== O += P V
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = instr_desc(256, D, true);
+      const uint32_t v_lo = desc_lo(sbase + S::kV);
+      Ring<kVSlots> vr;
+      Ring<kSBufs> sr;
+      uint32_t items = 0;
       bool ok = true;
       for (int i = 0; i < n_items && ok; ++i) {
-        const ChunkItem it = item(i);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          if (it.t1[s] <= it.t0[s] || !ok) continue;
-          ok = mbar_wait(B.q_empty(s), (items[s] & 1u) ^ 1u, s_abort);
+        const Item it = item(i);
+        if (it.t1 <= it.t0) continue;
+        for (int t = it.t0; t < it.t1 && ok; ++t) {
+          ok = mbar_wait(B.v_ready(vr.slot), vr.par, s_abort);
+          if (ok && t == it.t0 && items > 0) ok = mbar_wait(B.o_free(), (items - 1) & 1u, s_abort);   // the last item's output has been read
+          ok = ok && mbar_wait(B.p_full(sr.slot), sr.par, s_abort);
           if (!ok) break;
-          mbar_expect_tx(B.q_full(s), S::kSlabs * p.tpt * p.G * 128);
-#pragma unroll
-          for (int sl = 0; sl < S::kSlabs; ++sl)
-            tma_load_3d(sbase + S::kQ + s * S::kTileBytes + sl * S::kSlabBytes, &map_q, sl * 64, it.g[s] * p.G, it.start + it.qt[s] * p.tpt,
-                        B.q_full(s));
-          ++items[s];
+          fence_after();
+          issue_pv_pair<D>(tmem + kColO, tmem + sr.slot * 128, v_lo + vr.slot * (S::kVBytes >> 4), idesc, t == it.t0 ? 0u : 1u);
+          commit_pair(B.o_done(sr.slot));
+          commit_pair(B.v_empty(vr.slot));
+          vr.step();
+          sr.step();
         }
-      }
-    }
-  } else if (warp == kWarpProducer) {
-    // =========================================================================== K/V tiles
-    // Paged cache: the whole warp walks the list in step and each lane fetches one box (a page, or a page's 64-column half).
-    if (lane == 0 || PAGED) {
-      Uses uses;
-      bool ok = true;
-      for (int i = 0; i < n_items && ok; ++i) {
-        const ChunkItem it = item(i);
-        const bool shared = it.kind == kChunkPair;
-        const int len0 = it.t1[0] - it.t0[0], len1 = it.t1[1] - it.t0[1], len = len0 > len1 ? len0 : len1;
-        const int32_t* pages = PAGED ? p.block_table + static_cast<size_t>(it.b) * p.max_pages : nullptr;
-        const int last_page = PAGED ? (it.L + it.n - 1) >> p.page_shift : 0;
-        auto load = [&](uint32_t slot, uint32_t parity, const CUtensorMap* map, int g, int tile) {
-          const uint32_t dst = sbase + S::kRing + slot * S::kTileBytes;
-          if constexpr (PAGED) {
-            // The box past the sequence's last page fetches that page again (its rows are masked), so that a tile's byte
-            // count never changes; an entry outside the pool reads page 0 (the merge kernel reports and zeroes the sequence).
-            const int rows = p.page_size < kChunkTile ? p.page_size : kChunkTile;
-            const int sl = lane % S::kSlabs, r0 = (lane / S::kSlabs) * rows;
-            const int key = tile * kChunkTile + r0;
-            int page = 0;
-            if (r0 < kChunkTile) {
-              const int pi = key >> p.page_shift;
-              page = __ldg(pages + (pi < last_page ? pi : last_page));
-              if (page < 0 || page >= p.num_pages) page = 0;
-            }
-            ok = mbar_wait_warp(B.empty(slot), parity, s_abort);
-            if (!ok) return;
-            if (lane == 0) mbar_expect_tx(B.full(shared, slot), S::kTileBytes);
-            __syncwarp();
-            if (r0 < kChunkTile)
-              tma_load_3d(dst + sl * S::kSlabBytes + r0 * 128, map, sl * 64, key & (p.page_size - 1), page * p.Hkv + g, B.full(shared, slot));
-          } else {
-            ok = mbar_wait(B.empty(slot), parity, s_abort);
-            if (!ok) return;
-            mbar_expect_tx(B.full(shared, slot), S::kTileBytes);
-#pragma unroll
-            for (int sl = 0; sl < S::kSlabs; ++sl)
-              tma_load_3d(dst + sl * S::kSlabBytes, map, sl * 64, tile * kChunkTile, it.b * p.Hkv + g, B.full(shared, slot));
-          }
-        };
-        for (int j = 0; j < len && ok; ++j) {
-          if (shared) {
-            const Place pl = uses.place(true, 0, j);
-            const int tile = it.t0[1] + j;               // (the second stream of a pair is never the shorter one)
-            const uint32_t parity = uses.free_parity(true, pl);
-            load(pl.slot, parity, &map_k, it.g[0], tile);
-            if (ok) load(2 + pl.slot, parity, &map_v, it.g[0], tile);
-          } else {
-#pragma unroll
-            for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-              for (int s = 0; s < 2; ++s) {
-                if (!ok || j >= (s ? len1 : len0)) continue;
-                const Place pl = uses.place(false, s, j);
-                load(2 * kv + pl.slot, uses.free_parity(false, pl), kv ? &map_v : &map_k, it.g[s], it.t0[s] + j);
-              }
-          }
-        }
-        uses.add(shared, len0, len1);
+        ++items;
       }
     }
   } else {
-    // =========================================================================== softmax and output of one stream
-    // Thread r owns query row r (tensor-memory lane r), all 128 score columns.  fp32 throughout, in the log2 domain; the
-    // probabilities are rounded to bf16 for the tensor cores (relative 2^-8 each, half of the inputs' own spacing), the sum
-    // that divides them is kept from the unrounded ones.
-    const int s = warp >> 2;
-    const int r = tid & (kGroupThreads - 1);
+    // =========================================================================== softmax and output
+    // Two groups of four warps take alternate steps, so that one computes while the other waits.  Thread r of a group owns query
+    // row r (tensor-memory lane r), all 128 score columns.  The two threads of a row share one reference maximum: the one
+    // that handled step g publishes it, tagged with g, before it takes its exponentials, and the other picks it up at step g + 1;
+    // each keeps its own part of the row sum.  fp32 throughout, in the log2 domain; the probabilities are rounded to bf16 for
+    // the tensor cores (relative 2^-8 each, half of the inputs' own spacing), the sum that divides them is kept from the
+    // unrounded ones.  A warp without a row that belongs to the sequence only passes its turns on.
+    const uint32_t grp = static_cast<uint32_t>(warp >> 2);
+    const int r = tid & 127;
     const uint32_t lane_addr = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_addr = tmem + lane_addr + s * 128, o_addr = tmem + lane_addr + 256 + s * 128;
+    volatile uint32_t* tag = reinterpret_cast<volatile uint32_t*>(smem + S::kTag) + r;
+    volatile float* lfin = reinterpret_cast<volatile float*>(smem + S::kLfin) + r;
+    const uint32_t o_addr = tmem + lane_addr + kColO;
+    const uint32_t p_to = map_to_rank(B.p_full(0), 0), o_free_to = map_to_rank(B.o_free(), 0);
     const int tok_r = r / p.G, head_r = r - tok_r * p.G;   // token and head within the tile
-    const bool row_used = tok_r < p.tpt;
     const float scale_log2 = p.scale_log2;
-    Uses uses;
-    uint32_t steps = 0, items = 0;
+    uint32_t sg = 0, items = 0;                            // steps and items before the current item
     bool ok = true;
     for (int i = 0; i < n_items && ok; ++i) {
-      const ChunkItem it = item(i);
-      const bool shared = it.kind == kChunkPair;
-      const int len0 = it.t1[0] - it.t0[0], len1 = it.t1[1] - it.t0[1], len = s ? len1 : len0;
-      if (len > 0) {
-        const int tile0 = of_stream(it.t0, s), kv_end = it.L + it.n;
-        const int first = of_stream(it.qt, s) * p.tpt, token = first + tok_r;                  // place in the chunk
-        const bool row_valid = row_used && token < it.n;
-        const int limit = it.L + (token < it.n ? token : it.n - 1);                 // the last key this row sees
-        float m_ref = -INFINITY, l_sum = 0.f;
-        for (int j = 0; j < len; ++j, ++steps) {
-          const int key0 = (tile0 + j) * kChunkTile;
-          ok = mbar_wait_warp(B.s_full(s), steps & 1u, s_abort);
-          if (!ok) break;
+      const Item it = item(i);
+      const int steps = it.t1 - it.t0;
+      if (steps <= 0) continue;
+      const int first = (2 * it.pair + static_cast<int>(rank)) * p.tpt, token = first + tok_r;    // place in the chunk
+      const bool row_valid = tok_r < p.tpt && token < it.n;
+      const bool warp_rests = !__any_sync(0xffffffffu, row_valid);
+      const int limit = it.L + (token < it.n ? token : it.n - 1);                 // the last key this row sees
+      float m_ref = -INFINITY;   // reference this thread's row sum is relative to
+      float m_in = -INFINITY;    // reference the other group left behind at the step before this group's latest one
+      float l_sum = 0.f;
+      for (int s = static_cast<int>((sg ^ grp) & 1u); s < steps; s += 2) {
+        const uint32_t gs = sg + s, sb = gs % kSBufs, sph = (gs / kSBufs) & 1u;
+        const uint32_t s_addr = tmem + lane_addr + sb * 128;
+        ok = mbar_wait_warp(B.s_full(sb), sph, s_abort);
+        if (!ok) break;
+        if (!warp_rests) {
           fence_after();
+          const int key0 = (it.t0 + s) * kChunkTile;
           if (key0 + kChunkTile - 1 > it.L + first) {
             // a tile that some row of this query tile does not see whole: -inf over the invisible scores, in place
             const int lim = limit - key0;                  // last visible column of this row
@@ -603,20 +600,6 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
               st32(s_addr + c * 32, t);
             }
             wait_st();
-          }
-          if (key0 + kChunkTile > kv_end) {
-            // slots past the sequence may hold anything: their V rows are zeroed so that 0 * garbage cannot reach O.  Both
-            // streams of a pair do it, each before it hands over its own probabilities.
-            const Place pl = uses.place(shared, s, j);
-            ok = mbar_wait_warp(B.full(shared, 2 + pl.slot), pl.use & 1u, s_abort);
-            if (!ok) break;
-            if (key0 + r >= kv_end) {
-#pragma unroll
-              for (int c = 0; c < 8 * S::kSlabs; ++c)
-                *reinterpret_cast<uint4*>(smem + S::kRing + (2 + pl.slot) * S::kTileBytes + (c >> 3) * S::kSlabBytes + r * 128 + (c & 7) * 16) =
-                    make_uint4(0u, 0u, 0u, 0u);
-            }
-            fence_proxy_async();
           }
           // ---- row maximum.  Chunks 0 and 1 stay in registers, chunks 2 and 3 are fetched again for the exponentials.
           uint32_t ra[32], rb[32];
@@ -637,15 +620,35 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
             }
           }
           const float tmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale_log2;   // scale > 0
+
+          // the reference the other group settled on at the previous step (waited for at an item's first step too, where its value
+          // is not used: the other group must have read the tag of step gs - 2 before it is replaced)
+          float m_prev = -INFINITY;
+          if (gs > 0) {
+            const unsigned long long t = tag_wait(tag, (gs - 1u) & 0xffu, s_abort);
+            ok = __all_sync(0xffffffffu, (t >> 32) != 0ull);
+            if (!ok) break;
+            if (s > 0) m_prev = __uint_as_float(static_cast<uint32_t>(t) & 0xffffff00u);
+          }
+          if (m_prev != m_ref) {
+            l_sum *= fast_exp2(m_ref - m_prev);     // m_ref = -inf: nothing summed yet, the factor is 0
+            m_ref = m_prev;
+          }
+          m_in = m_prev;
           const bool grow = tmax > m_ref + kRescaleThreshold || (m_ref == -INFINITY && tmax > -INFINITY);
           float factor = 1.f;
           if (grow) {
-            factor = fast_exp2(m_ref - tmax);            // 0 when there was no reference yet
-            m_ref = tmax;
+            const float m_new = __uint_as_float(__float_as_uint(tmax) & 0xffffff00u);   // the low byte carries the step's tag
+            factor = fast_exp2(m_ref - m_new);     // 0 when there was no reference yet
+            m_ref = m_new;
             l_sum *= factor;
           }
-          if (j > 0 && __any_sync(0xffffffffu, grow)) {
-            // the PV of the step before has finished (it was issued before the scores that have just arrived)
+          *tag = __float_as_uint(m_ref) | (gs & 0xffu);
+          if (s > 0 && __any_sync(0xffffffffu, grow)) {
+            // the previous step accumulated into O and may still be running
+            ok = mbar_wait_warp(B.o_done((gs - 1) % kSBufs), ((gs - 1) / kSBufs) & 1u, s_abort);
+            if (!ok) break;
+            fence_after();
             uint32_t o[32];
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
@@ -693,78 +696,100 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
             unpack2(ls2[1], c, d);
             l_sum += (a + b) + (c + d);
           }
+          if (s == steps - 2) {
+            // This group's last step of the item, but not the item's: hand the row sum to the group that writes the output.  (That
+            // group reads it before it publishes a tag of the next item, and this place is written again two items on.)
+            lfin[(items & 1u) * 128] = l_sum;
+          }
           wait_st();
           fence_before();
-          mbar_arrive(B.p_full(s));
-        }
-        if (!ok) break;
-        // ---- output: a bf16 row, or the unnormalised fp32 partial of a cut tile, laid out [4 columns][row] so that the
-        // lanes of a store write consecutive 16-byte pieces
-        ok = mbar_wait_warp(B.o_full(s), items & 1u, s_abort);
-        if (!ok) break;
-        fence_after();
-        const float inv = l_sum > 0.f ? 1.f / l_sum : (l_sum == 0.f ? 0.f : l_sum);    // a NaN sum stays one
-        const int slot = of_stream(it.slot, s), g = of_stream(it.g, s);
-        uint32_t oa[32], ob[32];
-        auto store_chunk = [&](uint32_t (&o)[32], int c) {
-          if (!row_valid) return;
-          if (slot < 0) {
-            __nv_bfloat16* out_row = p.out + (static_cast<size_t>(it.start + token) * p.Hq + g * p.G + head_r) * D;
-#pragma unroll
-            for (int e = 0; e < 32; e += 16) {
-              uint32_t v[8];
-#pragma unroll
-              for (int k = 0; k < 8; ++k) v[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
-              st_global_v8(out_row + c * 32 + e, v);
-            }
-          } else {
-            float* part = p.work.part_o + (static_cast<size_t>(slot) * (D / 4) + c * 8) * (128 * 4) + r * 4;
-#pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<uint4*>(part + (e / 4) * (128 * 4)) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        } else {
+          // (the chain of tags goes on: the next item's rows may be in use)
+          if (gs > 0) {
+            ok = __all_sync(0xffffffffu, (tag_wait(tag, (gs - 1u) & 0xffu, s_abort) >> 32) != 0ull);
+            if (!ok) break;
           }
-        };
-        ld32(o_addr, oa);
-#pragma unroll
-        for (int c = 0; c < D / 32; c += 2) {
-          wait_ld();
-          ld32(o_addr + (c + 1) * 32, ob);
-          store_chunk(oa, c);
-          wait_ld();
-          if (c + 2 < D / 32) ld32(o_addr + (c + 2) * 32, oa);
-          store_chunk(ob, c + 1);
+          *tag = 0xff800000u | (gs & 0xffu);
         }
-        if (row_valid && slot >= 0) p.work.part_ml[static_cast<size_t>(slot) * 128 + r] = make_float2(m_ref, l_sum);
-        fence_before();
-        mbar_arrive(B.o_free(s));
-        ++items;
+        __syncwarp();
+        if (lane == 0) mbar_arrive_pair(p_to + 8u * sb);
+
+        if (s == steps - 1) {
+          // ---- this group took the item's last step: it writes the item's output
+          ok = mbar_wait_warp(B.o_done(sb), sph, s_abort);      // PVs complete in order
+          if (!ok) break;
+          if (!warp_rests) {
+            fence_after();
+            float l_row = l_sum;
+            if (steps > 1) l_row = fmaf(lfin[(items & 1u) * 128], m_in == m_ref ? 1.f : fast_exp2(m_in - m_ref), l_row);   // the other's sum is relative to the reference it last saw
+            const float inv = l_row > 0.f ? 1.f / l_row : (l_row == 0.f ? 0.f : l_row);                 // a NaN sum stays one
+            const int slot = it.slot < 0 ? -1 : it.slot + static_cast<int>(rank);
+            uint32_t oa[32], ob[32];
+            auto store_chunk = [&](uint32_t (&o)[32], int c) {
+              if (!row_valid) return;
+              if (slot < 0) {
+                __nv_bfloat16* out_row = p.out + (static_cast<size_t>(it.start + token) * p.Hq + it.g * p.G + head_r) * D;
+#pragma unroll
+                for (int e = 0; e < 32; e += 16) {
+                  uint32_t v[8];
+#pragma unroll
+                  for (int k = 0; k < 8; ++k) v[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
+                  st_global_v8(out_row + c * 32 + e, v);
+                }
+              } else {
+                // an fp32 partial is laid out [4 columns][row], so that the lanes of a store write consecutive 16-byte pieces
+                float* part = p.work.part_o + (static_cast<size_t>(slot) * (D / 4) + c * 8) * (128 * 4) + r * 4;
+#pragma unroll
+                for (int e = 0; e < 32; e += 4)
+                  *reinterpret_cast<uint4*>(part + (e / 4) * (128 * 4)) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+              }
+            };
+            ld32(o_addr, oa);
+#pragma unroll
+            for (int c = 0; c < D / 32; c += 2) {
+              wait_ld();
+              ld32(o_addr + (c + 1) * 32, ob);
+              store_chunk(oa, c);
+              wait_ld();
+              if (c + 2 < D / 32) ld32(o_addr + (c + 2) * 32, oa);
+              store_chunk(ob, c + 1);
+            }
+            if (row_valid && slot >= 0) p.work.part_ml[static_cast<size_t>(slot) * 128 + r] = make_float2(m_ref, l_row);
+            fence_before();
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive_pair(o_free_to);
+        }
       }
-      uses.add(shared, len0, len1);
+      sg += steps;
+      ++items;
     }
   }
 
-  // ---- teardown: everyone arrives here, normally or after an abort
+  // ---- teardown: everyone arrives here, normally or after an abort; neither CTA leaves while the other may still reach into it
   fence_before();
   __syncthreads();
   if (tid == 0 && *s_abort) report_status(p.status, EAGLE_ERR_TIMEOUT);
-  if (warp == kWarpMma) {
+  cluster_sync();
+  if (warp == kWarpQK) {
     __syncwarp();
     fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
   }
 }
 
 // ================================================================================================================== merge
-// Cut query tiles: m* = max m_i, l* = sum l_i 2^(m_i - m*), out = sum o_i 2^(m_i - m*) / l*.  A block takes 8 rows of one
-// stream of one record (a warp: 8 rows x 4 groups of 4 columns, so that its loads are runs of 128 bytes).  The blocks behind
-// them look at one sequence each: rows of a sequence that does not fit its cache, or whose block table names a page outside
-// the pool, become zeros.
+// Cut query tiles: m* = max m_i, l* = sum l_i 2^(m_i - m*), out = sum o_i 2^(m_i - m*) / l*.  A block takes 8 rows of one query
+// tile of one record (a warp: 8 rows x 4 groups of 4 columns, so that its loads are runs of 128 bytes); the slots of the
+// pieces are looked up together, and four pieces' loads are in flight at a time.  The blocks behind them look at one sequence
+// each: rows of a sequence that does not fit its cache, or whose block table names a page outside the pool, become zeros.
 constexpr int kMergeThreads = 256;
 
 template <int D>
-__global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams p, int records, int row_blocks) {
+__global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams p, int row_blocks) {
+  wait_for_prerequisites();                              // partials and outputs of the attention kernel are there
   const ChunkWork& w = p.work;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, records = p.num_pairs;
   if (static_cast<int>(blockIdx.x) >= records * 2 * row_blocks) {
     const int b = blockIdx.x - records * 2 * row_blocks;
     const ChunkSeq q = w.seq[b];
@@ -788,77 +813,108 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams 
     for (size_t i = tid; i < vecs; i += kMergeThreads) out[i] = make_uint4(0u, 0u, 0u, 0u);
     return;
   }
-  const int rec = blockIdx.x / (2 * row_blocks), rest = blockIdx.x - rec * 2 * row_blocks, s = rest / row_blocks, rb = rest - s * row_blocks;
+  __shared__ int s_slot[kMaxPairs];                      // slots of the pieces that are not empty, in order
+  __shared__ int s_count;
+  const int rec = blockIdx.x / (2 * row_blocks), rest = blockIdx.x - rec * 2 * row_blocks, half = rest / row_blocks, rb = rest - half * row_blocks;
   const ChunkCut cut = w.cut[rec];
   if (cut.unit < 0) return;
   const ChunkUnit un = w.unit[cut.unit];
-  const bool lone = un.kind == kChunkLone;
-  if (lone && s) return;                                 // its two streams are halves of one tile
   const ChunkSeq q = w.seq[un.b];
-  const int qt = un.kind == kChunkPair ? un.qt + s : un.qt, g = un.kind == kChunkTwin ? un.g + s : un.g;
+  const int first = (2 * un.pair + half) * p.tpt;
+  if (first + rb * 8 / p.G >= q.n || rb * 8 / p.G >= p.tpt) return;      // no row of this block belongs to the sequence
+  if (tid < 32) {
+    int count = 0;
+    for (int i = cut.c_lo; i <= cut.c_hi; i += 32) {
+      const int c = i + tid;
+      int slot = -1;
+      if (c <= cut.c_hi) {
+        const ChunkItem* it = w.items + cut.unit + c;
+        if (it->t1 > it->t0) slot = it->slot;
+      }
+      const unsigned has = __ballot_sync(0xffffffffu, slot >= 0);
+      if (slot >= 0) s_slot[count + __popc(has & ((1u << tid) - 1u))] = slot + half;
+      count += __popc(has);
+    }
+    if (tid == 0) s_count = count;
+  }
+  __syncthreads();
+  const int pieces = s_count;                            // 0: the cuts snapped to the unit's edges, its output is there already
   const int row = rb * 8 + ((tid >> 2) & 7), cols = (tid >> 5) * 4 + (tid & 3);      // row of the tile, group of 4 columns
-  const int tok = row / p.G, head = row - tok * p.G, token = qt * p.tpt + tok;
-  if (tok >= p.tpt || token >= q.n || cols >= D / 4) return;
-  const int pieces = cut.c_lo < 0 ? 1 : cut.c_hi - cut.c_lo + 1, streams = lone ? 2 : 1;
+  const int tok = row / p.G, head = row - tok * p.G, token = first + tok;
+  if (pieces == 0 || tok >= p.tpt || token >= q.n || cols >= D / 4) return;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = 0; i < pieces; ++i) {
-    for (int t = 0; t < streams; ++t) {
-      const int st = lone ? t : s;
-      int slot;
-      if (cut.c_lo < 0) {
-        slot = 2 * cut.c_hi + st;                        // both halves of a lone tile that was not cut
-      } else {
-        const ChunkItem* it = w.items + cut.unit + cut.c_lo + i;
-        if (it->t1[st] <= it->t0[st]) continue;
-        slot = it->slot[st];
-        if (slot < 0) return;                            // its cuts snapped to the edges: the output is there already
-        if (lone && it->slot[st] >= 4 * p.num_ctas) return;   // the same, merged from the halves by the record of its sequence
+  for (int i = 0; i < pieces; i += 4) {
+    float2 ml[4];
+    float4 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      ml[k] = make_float2(-INFINITY, 0.f);
+      v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i + k < pieces) {
+        const size_t slot = s_slot[i + k];
+        ml[k] = w.part_ml[slot * 128 + row];
+        v[k] = *reinterpret_cast<const float4*>(w.part_o + (slot * (D / 4) + cols) * (128 * 4) + row * 4);
       }
-      const float2 ml = w.part_ml[static_cast<size_t>(slot) * 128 + row];
-      const float4 v = *reinterpret_cast<const float4*>(w.part_o + (static_cast<size_t>(slot) * (D / 4) + cols) * (128 * 4) + row * 4);
-      if (ml.x == -INFINITY && ml.y == 0.f) continue;    // nothing visible in this piece
-      const float top = fmaxf(m, ml.x);
-      const float a = m == -INFINITY ? 0.f : exp2f(m - top), c = exp2f(ml.x - top);
-      m = top;
-      l = l * a + ml.y * c;
-      o = make_float4(o.x * a + v.x * c, o.y * a + v.y * c, o.z * a + v.z * c, o.w * a + v.w * c);
     }
+    const float top = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
+    const float base = top == -INFINITY ? 0.f : top;     // (nothing visible so far: every weight is 2^-inf)
+    const float a = exp2f(m - base);
+    l *= a;
+    o = make_float4(o.x * a, o.y * a, o.z * a, o.w * a);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      // a piece in which the row sees nothing has m = -inf and l = 0, and an accumulator that the weight 0 keeps out
+      const float c = exp2f(ml[k].x - base);
+      l = fmaf(ml[k].y, c, l);
+      o = make_float4(fmaf(v[k].x, c, o.x), fmaf(v[k].y, c, o.y), fmaf(v[k].z, c, o.z), fmaf(v[k].w, c, o.w));
+    }
+    m = top;
   }
   const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
   uint2 out;
   out.x = pack_bf16(o.x * inv, o.y * inv);
   out.y = pack_bf16(o.z * inv, o.w * inv);
-  *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(q.start + token) * p.Hq + g * p.G + head) * D + cols * 4) = out;
+  *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(q.start + token) * p.Hq + un.g * p.G + head) * D + cols * 4) = out;
 }
 
 template <int D>
 cudaError_t launch_all(const ChunkParams& p, cudaStream_t stream) {
   CUtensorMap mk, mv, mq;
   const bool paged = p.block_table != nullptr;
-  if (paged) {
-    const int rows = p.page_size < kChunkTile ? p.page_size : kChunkTile;
-    const long long ph = static_cast<long long>(p.num_pages) * p.Hkv;
-    if (!map_bf16_3d(&mk, p.k, D, p.page_size, ph, rows, 1) || !map_bf16_3d(&mv, p.v, D, p.page_size, ph, rows, 1)) return cudaErrorInvalidValue;
-  } else {
-    const long long bh = static_cast<long long>(p.B) * p.Hkv, cap = p.capacity > 0 ? p.capacity : 1;
-    if (!map_bf16_3d(&mk, p.k, D, cap, bh, kChunkTile, 1) || !map_bf16_3d(&mv, p.v, D, cap, bh, kChunkTile, 1)) return cudaErrorInvalidValue;
-  }
-  if (!map_bf16_3d(&mq, p.q, D, p.Hq, p.N, p.G, p.tpt)) return cudaErrorInvalidValue;
+  const int k_rows = paged && p.page_size < 64 ? p.page_size : 64, v_rows = paged && p.page_size < 128 ? p.page_size : 128;
+  const long long n1 = paged ? p.page_size : (p.capacity > 0 ? p.capacity : 1);
+  const long long n2 = paged ? static_cast<long long>(p.num_pages) * p.Hkv : static_cast<long long>(p.B) * p.Hkv;
+  if (!map_bf16_3d(&mk, p.k, D, n1, n2, 64, k_rows, 1) || !map_bf16_3d(&mv, p.v, D, n1, n2, D / 2, v_rows, 1) ||
+      !map_bf16_3d(&mq, p.q, D, p.Hq, p.N, 64, p.G, p.tpt))
+    return cudaErrorInvalidValue;
   chunk_plan_kernel<<<1, kPlanThreads, 0, stream>>>(p);
   count_launch();
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  if (paged) chunk_attn_kernel<D, true><<<p.num_ctas, kThreads, Smem<D>::kBytes, stream>>>(p, mk, mv, mq);
-  else chunk_attn_kernel<D, false><<<p.num_ctas, kThreads, Smem<D>::kBytes, stream>>>(p, mk, mv, mq);
-  count_launch();
-  e = cudaGetLastError();
+  // Both kernels after the planner are launched programmatically: their prologues (and the launches themselves) overlap the
+  // kernel before, whose results they wait for.
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t config = {};
+  config.stream = stream;
+  config.attrs = &attr;
+  config.numAttrs = 1;
+  config.gridDim = dim3(2 * p.num_pairs);
+  config.blockDim = dim3(kThreads);
+  config.dynamicSmemBytes = Smem<D>::kBytes;
+  e = cudaLaunchKernelEx(&config, paged ? chunk_attn_kernel<D, true> : chunk_attn_kernel<D, false>, p, mk, mv, mq);
   if (e != cudaSuccess) return e;
-  const int records = p.num_ctas + ((p.Hkv & 1) ? p.B : 0);
-  const int rows = p.max_rows < 128 ? p.max_rows : 128, row_blocks = (rows + 7) / 8;
-  chunk_merge_kernel<D><<<records * 2 * row_blocks + p.B, kMergeThreads, 0, stream>>>(p, records, row_blocks);
   count_launch();
-  return cudaGetLastError();
+  const int rows = p.max_rows < 128 ? p.max_rows : 128, row_blocks = (rows + 7) / 8;
+  config.gridDim = dim3(p.num_pairs * 2 * row_blocks + p.B);
+  config.blockDim = dim3(kMergeThreads);
+  config.dynamicSmemBytes = 0;
+  e = cudaLaunchKernelEx(&config, chunk_merge_kernel<D>, p, row_blocks);
+  if (e != cudaSuccess) return e;
+  count_launch();
+  return cudaSuccess;
 }
 
 }  // namespace

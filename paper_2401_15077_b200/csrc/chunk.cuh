@@ -9,25 +9,22 @@ constexpr int kChunkTile = 128;        // keys per K/V tile
 // unit's edge a cut moves to the edge.
 constexpr int kChunkItemKeys = 256;
 constexpr int kChunkSnap = 2;
+constexpr int kMaxPairs = kMaxPlanCtas / 2;
 
-enum ChunkKind { kChunkPair = 0, kChunkTwin = 1, kChunkLone = 2 };
-
+// A unit is a pair of neighbouring query tiles of one (sequence, KV head); an item is what a pair of CTAs does of it in one go.
 struct ChunkSeq {        // n = 0: empty or refused
-  int32_t start, n, L, qtiles;
+  int32_t start, n, L, pairs;
 };
 struct ChunkUnit {
-  int32_t b, g, qt, kind;
-  int32_t nt[2];         // K/V tiles of the two streams
-  int32_t pad, pad1;
+  int32_t b, g, pair, tiles;     // K/V tiles
 };
-// What a CTA does in one go: for each of its two streams a query tile and a range of K/V tiles (empty: the stream rests).
 struct alignas(16) ChunkItem {
-  int32_t b, kind, start, n;
-  int32_t L, pad;
-  int32_t g[2], qt[2], t0[2], t1[2], slot[2];    // slot: of the partial, or -1: write the output
+  int32_t b, g, pair, start;     // start: the sequence's first row
+  int32_t n, L, t0, t1;          // K/V tiles [t0, t1)
+  int32_t slot;                  // partial slot of the first CTA's query tile (the second's is the next one), -1: write the output
+  int32_t pad[3];
 };
-// A unit whose output is merged: pieces (unit, c), c_lo <= c <= c_hi, or (c_lo < 0) the two halves of an uncut lone tile,
-// whose slots are 2 * c_hi and 2 * c_hi + 1.
+// A unit whose output is merged from the pieces (unit, c), c_lo <= c <= c_hi; unit < 0: none.
 struct ChunkCut {
   int32_t unit, c_lo, c_hi, pad;
 };
@@ -38,9 +35,9 @@ struct ChunkWork {
   long long* cost_base;    // [B]
   long long* x;            // [units + 1]: where each unit starts on the work line
   ChunkUnit* unit;         // [units]
-  ChunkItem* items;        // [units + CTAs]
-  int4* cta;               // [CTAs]: whole units (first, count), pieces (first, count)
-  ChunkCut* cut;           // [CTAs + B]
+  ChunkItem* items;        // [units + CTA pairs]
+  int4* cta;               // [CTA pairs]: whole units (first, count), pieces (first, count)
+  ChunkCut* cut;           // [CTA pairs]
   float2* part_ml;         // [slots, 128]
   float* part_o;           // [slots, D / 4, 128, 4]
   size_t bytes;
@@ -59,23 +56,22 @@ struct ChunkParams {
   int32_t max_rows;              // query rows of a (sequence, KV head) at the most
   long long capacity;            // slots per sequence
   int32_t page_size, page_shift, max_pages, num_pages;
-  int32_t num_ctas;
+  int32_t num_pairs;             // pairs of CTAs of the attention kernel
   float scale_log2;
   int32_t* status;
   unsigned long long wait_limit_ns;
   ChunkWork work;
 };
 
-// Partial slots: a CTA's share of the cut units begins and ends inside a unit at the most (two pieces of two streams), and
-// with an odd number of KV heads a sequence's lone tile is merged from its two halves.
-inline bool carve_chunk_work(const eagle_chunk_desc& d, void* base, int num_ctas, ChunkWork* w) {
+// Partial slots: a pair of CTAs' share of the cut units begins and ends inside a unit at the most: two pieces of two query tiles.
+inline bool carve_chunk_work(const eagle_chunk_desc& d, void* base, int num_pairs, ChunkWork* w) {
   if (d.batch < 0 || d.num_tokens < 0 || d.num_kv_heads <= 0 || d.num_q_heads <= 0 || d.num_q_heads % d.num_kv_heads) return false;
   const int G = d.num_q_heads / d.num_kv_heads;
   if (G > kMaxGroup || (d.head_dim != 64 && d.head_dim != 128) || d.batch > 65535) return false;
   const size_t B = static_cast<size_t>(d.batch), tpt = 128 / G;
-  const size_t units = static_cast<size_t>(d.num_kv_heads) * (d.num_tokens / (2 * tpt)) + B * (d.num_kv_heads + 1);
+  const size_t units = static_cast<size_t>(d.num_kv_heads) * (d.num_tokens / (2 * tpt) + B);
   if (units > (1u << 28)) return false;
-  const size_t slots = 4 * static_cast<size_t>(num_ctas) + 2 * B * (d.num_kv_heads & 1);
+  const size_t slots = 4 * static_cast<size_t>(num_pairs);
   char* p = static_cast<char*>(base);
   size_t off = 0;
   auto take = [&](size_t n) { char* r = p ? p + off : nullptr; off += align256(n > 0 ? n : 1); return r; };
@@ -84,9 +80,9 @@ inline bool carve_chunk_work(const eagle_chunk_desc& d, void* base, int num_ctas
   w->cost_base = reinterpret_cast<long long*>(take(sizeof(long long) * B));
   w->x = reinterpret_cast<long long*>(take(sizeof(long long) * (units + 1)));
   w->unit = reinterpret_cast<ChunkUnit*>(take(sizeof(ChunkUnit) * units));
-  w->items = reinterpret_cast<ChunkItem*>(take(sizeof(ChunkItem) * (units + num_ctas)));
-  w->cta = reinterpret_cast<int4*>(take(sizeof(int4) * num_ctas));
-  w->cut = reinterpret_cast<ChunkCut*>(take(sizeof(ChunkCut) * (num_ctas + B)));
+  w->items = reinterpret_cast<ChunkItem*>(take(sizeof(ChunkItem) * (units + num_pairs)));
+  w->cta = reinterpret_cast<int4*>(take(sizeof(int4) * num_pairs));
+  w->cut = reinterpret_cast<ChunkCut*>(take(sizeof(ChunkCut) * num_pairs));
   w->part_ml = reinterpret_cast<float2*>(take(sizeof(float2) * slots * 128));
   w->part_o = reinterpret_cast<float*>(take(sizeof(float) * slots * 128 * d.head_dim));
   w->bytes = off;
