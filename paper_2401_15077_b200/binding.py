@@ -8,6 +8,7 @@ shared library is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import math
 from pathlib import Path
 
 import torch
@@ -618,9 +619,15 @@ def _here(t, dtype, name, device, shape=None):
 
 def _current(t, name):
     """The device of ``t``, which has to be the current one: the call is enqueued on its current stream."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    dev = t.device
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
         raise EagleError(f"{name} must be on the current CUDA device")
-    return t.device
+    return dev
+
+
+def _stream_of(dev):
+    """The current stream's handle (without the Stream object that costs as much as the rest of a small call's marshalling)."""
+    return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
 class KVStore:
@@ -634,7 +641,7 @@ class KVStore:
         self.num_kv_heads, self.head_dim, self.fp8 = k.shape[1], k.shape[3], k_scale is not None
         self.batch = k.shape[0] if block_table is None else block_table.shape[0]
         dtype, dev = torch.uint8 if self.fp8 else torch.bfloat16, k.device
-        scales = torch.Size((self.batch, self.num_kv_heads))
+        scales = torch.Size((self.batch, self.num_kv_heads)) if self.fp8 else None
         paged = block_table is not None
         self.desc = KVStoreDesc(_here(k, dtype, "k", dev), _here(v, dtype, "v", dev), _here(k_scale, torch.float32, "k_scale", dev, scales),
                                 _here(v_scale, torch.float32, "v_scale", dev, scales), 0 if paged else k.shape[2],
@@ -657,14 +664,18 @@ def eagle_rope_frequencies(rotary_dim, base=10000.0, kind="plain", factor=1.0, c
 
 def _rope_rows(t, name, lead, dev):
     """(address, elements from row to row) of [..., heads, D] bf16 whose rows lie a constant stride apart, heads dense within."""
-    D = t.shape[-1]
-    if t.dtype != torch.bfloat16 or t.device != dev or t.shape[:-2] != lead or t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != D):
+    shape, stride = t.shape, t.stride()
+    if t.dtype != torch.bfloat16 or t.device != dev or shape[:-2] != lead or stride[-1] != 1 or (shape[-2] > 1 and stride[-2] != shape[-1]):
         raise EagleError(f"{name} must be bf16 [..., heads, D] on {dev} with dense heads, rows as the other tensors")
-    row = t.stride(-3)
-    if len(lead) == 2 and lead[0] > 1 and lead[1] > 0 and t.stride(0) != lead[1] * row:
+    row = stride[-3]
+    if len(lead) == 2 and lead[0] > 1 and lead[1] > 0 and stride[0] != lead[1] * row:
         if lead[1] > 1:
             raise EagleError(f"{name} must have its rows a constant stride apart")
-        row = t.stride(0)
+        row = stride[0]
+    if row <= 0:                       # one row may have any stride; 0 stands for dense rows in the descriptor
+        if math.prod(lead) > 1:
+            raise EagleError(f"{name} must have rows of its own (it is expanded)")
+        row = 0
     return t.data_ptr(), row
 
 
@@ -691,7 +702,7 @@ def _rope_append(name, tree, q, k, v, kv, seq_lens, order, freqs, q_out, interle
                  _here(tree_sizes, torch.int32, "tree_sizes", dev), 1 if shared_tree else 0, _here(status, torch.int32, "status", dev))
     rc = getattr(load(), name)(ctypes.byref(d), qp, kp, vp, _here(q_out, torch.bfloat16, "q_out", dev, q.shape), ctypes.byref(kv.desc),
                                _here(seq_lens, torch.int32, "seq_lens", dev), _here(order, torch.int32, "tree_parent" if tree else "token_start", dev),
-                               _stream())
+                               _stream_of(dev))
     _check(rc, name)
     return q_out
 
@@ -734,7 +745,7 @@ def eagle_chunk_attn(q, kv, seq_lens, token_start, out=None, *, sm_scale=0.0, wo
     d = ChunkDesc(kv.batch, N, Hq, kv.num_kv_heads, D, float(sm_scale), _here(workspace, torch.uint8, "workspace", dev), workspace.numel(),
                   _here(status, torch.int32, "status", dev))
     rc = load().eagle_chunk_attn(ctypes.byref(d), _here(q, torch.bfloat16, "q", dev), ctypes.byref(kv.desc), _here(seq_lens, torch.int32, "seq_lens", dev),
-                                 _here(token_start, torch.int32, "token_start", dev), _here(out, torch.bfloat16, "out", dev, q.shape), _stream())
+                                 _here(token_start, torch.int32, "token_start", dev), _here(out, torch.bfloat16, "out", dev, q.shape), _stream_of(dev))
     _check(rc, "eagle_chunk_attn")
     return out
 
@@ -770,7 +781,7 @@ def eagle_tree_logits_adjust(logits, draft_tokens=None, tree_parent=None, out=No
                    _here(status, i32, "status", dev))
     rc = load().eagle_tree_logits_adjust(ctypes.byref(d), _here(logits, logits.dtype, "logits", dev),
                                          _here(draft_tokens, i32, "draft_tokens", dev, torch.Size((B, T))) if T else None,
-                                         _here(tree_parent, i32, "tree_parent", dev) if T else None, _here(out, f32, "out", dev, logits.shape), _stream())
+                                         _here(tree_parent, i32, "tree_parent", dev) if T else None, _here(out, f32, "out", dev, logits.shape), _stream_of(dev))
     _check(rc, "eagle_tree_logits_adjust")
     return out
 

@@ -286,3 +286,20 @@ def test_replayed_from_a_graph_on_another_stream(E):
     c.q, c.k, c.v = fresh.split((c.hq, c.hkv, c.hkv), dim=-2)
     want, stored = S.rope_append(c.q, c.k, c.v, c.lens, c.freqs.numpy(), token_start=c.start)
     _check(c, q_out, kv, want, stored, 1.0, before, {(t,) for t in range(14)})
+
+
+def test_rows_of_their_own_are_asked_for(E):
+    c = Case([3, 2], [1, 4], 4, 2, 64, seed=14, rows=5)
+    q, k, v, kv, lens, start, freqs = c.q.to(DEV), c.k.to(DEV), c.v.to(DEV), c.store(E), _ints(c.lens).to(DEV), c.start.to(DEV), c.freqs.to(DEV)
+    for bad in (q[:1].expand(5, -1, -1), q.transpose(0, 1).contiguous().transpose(0, 1), q[:, :, ::2], q.float(), q[:4]):
+        with pytest.raises(E.EagleError):
+            E.eagle_rope_append(bad, k, v, kv, lens, start, freqs)
+    with pytest.raises(E.EagleError):
+        E.eagle_rope_append(q, k, v[:, :1], kv, lens, start, freqs)
+    with pytest.raises(E.EagleError):
+        E.eagle_rope_append(q, k, v, kv, lens, start, freqs.float())
+    # every other row of a larger tensor is a constant stride
+    wide = torch.randn(10, 4, 64, device=DEV).bfloat16()
+    wide[::2] = q
+    a = E.eagle_rope_append(wide[::2], k, v, kv, lens, start, freqs)
+    assert torch.equal(a, E.eagle_rope_append(q.contiguous(), k, v, kv, lens, start, freqs))
