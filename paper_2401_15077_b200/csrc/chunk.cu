@@ -19,8 +19,8 @@ namespace {
 using namespace tc;
 
 // ================================================================================================================ planner
-constexpr int kPlanThreads = 1024;
-constexpr int kNearSeqs = 512, kNearUnits = 4096;      // tables of calls this small stay in shared memory as well
+constexpr int kPlanThreads = 512;
+constexpr int kNearSeqs = 256, kNearUnits = 4096;      // tables of calls this small stay in shared memory as well
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
@@ -41,14 +41,14 @@ __device__ Sum2 block_scan(Sum2 v, Sum2* warp_tot, Sum2* tot) {
   if (lane == 31) warp_tot[w] = v;
   __syncthreads();
   if (w == 0) {
-    Sum2 t = warp_tot[lane];
+    Sum2 t = lane < kPlanThreads / 32 ? warp_tot[lane] : Sum2{0, 0};
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int a = __shfl_up_sync(0xffffffffu, t.a, o);
       const long long b = __shfl_up_sync(0xffffffffu, t.b, o);
       if (lane >= o) { t.a += a; t.b += b; }
     }
-    warp_tot[lane] = t;
+    if (lane < kPlanThreads / 32) warp_tot[lane] = t;
   }
   __syncthreads();
   if (w > 0) { v.a += warp_tot[w - 1].a; v.b += warp_tot[w - 1].b; }
@@ -82,7 +82,7 @@ __device__ __forceinline__ int cut_tile(long long pos, long long x, int tiles) {
 __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p) {
   __shared__ Sum2 s_warp[kPlanThreads / 32];
   __shared__ long long s_pos[kMaxPairs + 1], s_cost[kNearSeqs], s_x[kNearUnits + 1];
-  __shared__ int s_base[kNearSeqs];
+  __shared__ int s_base[kNearSeqs], s_first[kMaxPairs], s_last[kMaxPairs];
   __shared__ ChunkSeq s_seq[kNearSeqs];
   const int tid = threadIdx.x, P = p.num_pairs, B = p.B, Hkv = p.Hkv, tpt = p.tpt;
   ChunkWork& w = p.work;
@@ -171,9 +171,14 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
     }
     return un;
   };
+  ChunkUnit own = {};                                                      // this thread's first unit, looked up once
+  long long own_x = 0;
+  if (tid < U) own = unit_of(tid, &own_x);
   for (int u = tid; u < U; u += kPlanThreads) {
-    long long x;
-    w.unit[u] = unit_of(u, &x);
+    ChunkUnit un = own;
+    long long x = own_x;
+    if (u != tid) un = unit_of(u, &x);
+    w.unit[u] = un;
     x_of[u] = x;
   }
   if (tid == 0) x_of[U] = W;
@@ -208,29 +213,33 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
     it[1] = make_int4(q.n, q.L, t0, t1);
     it[2] = make_int4(slot, 0, 0, 0);
   };
-  for (int u = tid; u < F; u += kPlanThreads) {
-    const ChunkUnit un = unit_of(u, nullptr);
-    emit((u % P) * k + u / P, un, 0, un.tiles, -1);
-  }
-  // the shares: piece (u, c) of unit u in pair c's share is item u + c
-  for (int u = F + (tid >> 3); u < U; u += kPlanThreads / 8) {           // eight lanes to a unit
-    const ChunkUnit un = unit_of(u, nullptr);
+  // Whole units are items c * k + round.  Of the shares, piece (u, c) of unit u in pair c's share is item u + c; the units in
+  // which a share begins and ends are noted for the pair.
+  for (int u = tid; u < U; u += kPlanThreads) {
+    const ChunkUnit un = u == tid ? own : unit_of(u, nullptr);
+    if (u < F) {
+      emit((u % P) * k + u / P, un, 0, un.tiles, -1);
+      continue;
+    }
     const long long x0 = x_of[u], x1 = x_of[u + 1];
-    const int c_lo = last_le(s_pos, P, x0), c_hi = last_le(s_pos, P, x1 - 1);
-    for (int c = c_lo + (tid & 7); c <= c_hi; c += 8) {
-      const int t0 = c == c_lo ? 0 : cut_tile(s_pos[c], x0, un.tiles), t1 = c == c_hi ? un.tiles : cut_tile(s_pos[c + 1], x0, un.tiles);
-      emit(u + c, un, t0, t1 > t0 ? t1 : t0, t0 == 0 && t1 == un.tiles ? -1 : 4 * c + (t0 > 0 ? 0 : 2));
+    const int c_lo = last_le(s_pos, P, x0);
+    int c = c_lo, t0 = 0;
+    if (s_pos[c] == x0) s_first[c] = u;
+    for (;; ++c) {
+      const bool ends = x1 <= s_pos[c + 1];
+      const int cut = ends ? un.tiles : cut_tile(s_pos[c + 1], x0, un.tiles), t1 = cut > t0 ? cut : t0;
+      emit(u + c, un, t0, t1, t0 == 0 && t1 == un.tiles ? -1 : 4 * c + (t0 > 0 ? 0 : 2));
+      if (x1 >= s_pos[c + 1]) s_last[c] = u;
+      if (ends) break;
+      s_first[c + 1] = u;
+      t0 = t1;
     }
-    if ((tid & 7) == 0 && c_hi > c_lo) w.cut[c_lo] = ChunkCut{u, c_lo, c_hi, 0};
+    if (c > c_lo) w.cut[c_lo] = ChunkCut{u, c_lo, c, 0};
   }
+  __syncthreads();
   if (tid < P) {
-    int first = 0, count = 0;
-    if (s_pos[tid + 1] > s_pos[tid] && F < U) {
-      const int u0 = last_le(x_of, U, s_pos[tid]), u1 = last_le(x_of, U, s_pos[tid + 1] - 1);
-      first = u0 + tid;
-      count = u1 - u0 + 1;
-    }
-    w.cta[tid] = make_int4(tid * k, k, first, count);
+    const bool some = s_pos[tid + 1] > s_pos[tid];
+    w.cta[tid] = make_int4(tid * k, k, some ? s_first[tid] + tid : 0, some ? s_last[tid] - s_first[tid] + 1 : 0);
   }
 }
 
@@ -586,17 +595,22 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
           if (key0 + kChunkTile - 1 > it.L + first) {
             // a tile that some row of this query tile does not see whole: -inf over the invisible scores, in place
             const int lim = limit - key0;                  // last visible column of this row
-            const int lim_lo = __reduce_min_sync(0xffffffffu, lim);
+            const int lim_lo = __reduce_min_sync(0xffffffffu, lim), lim_hi = __reduce_max_sync(0xffffffffu, lim);
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
               if (lim_lo >= c * 32 + 31) continue;         // uniform: every row of the warp sees the whole chunk
               const int v = lim - c * 32;
               const uint32_t see = v >= 31 ? 0xffffffffu : (v < 0 ? 0u : (2u << v) - 1u);
               uint32_t t[32];
-              ld32(s_addr + c * 32, t);
-              wait_ld();
+              if (lim_hi >= c * 32) {                      // (uniform too: some row sees some of it)
+                ld32(s_addr + c * 32, t);
+                wait_ld();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) t[e] = (see >> e) & 1u ? t[e] : 0xff800000u;
+                for (int e = 0; e < 32; ++e) t[e] = (see >> e) & 1u ? t[e] : 0xff800000u;
+              } else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) t[e] = 0xff800000u;
+              }
               st32(s_addr + c * 32, t);
             }
             wait_st();
@@ -724,41 +738,34 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
             if (steps > 1) l_row = fmaf(lfin[(items & 1u) * 128], m_in == m_ref ? 1.f : fast_exp2(m_in - m_ref), l_row);   // the other's sum is relative to the reference it last saw
             const float inv = l_row > 0.f ? 1.f / l_row : (l_row == 0.f ? 0.f : l_row);                 // a NaN sum stays one
             const int slot = it.slot < 0 ? -1 : it.slot + static_cast<int>(rank);
-            uint32_t oa[32], ob[32];
-            auto store_chunk = [&](uint32_t (&o)[32], int c) {
-              if (!row_valid) return;
-              if (slot < 0) {
-                __nv_bfloat16* out_row = p.out + (static_cast<size_t>(it.start + token) * p.Hq + it.g * p.G + head_r) * D;
+            // The accumulator is given back as soon as it is in registers: the next item's first PV waits for that.
+            uint32_t o[D];
 #pragma unroll
-                for (int e = 0; e < 32; e += 16) {
-                  uint32_t v[8];
+            for (int c = 0; c < D / 32; ++c) ld32(o_addr + c * 32, o + c * 32);
+            wait_ld();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_pair(o_free_to);
+            if (row_valid && slot < 0) {
+              __nv_bfloat16* out_row = p.out + (static_cast<size_t>(it.start + token) * p.Hq + it.g * p.G + head_r) * D;
 #pragma unroll
-                  for (int k = 0; k < 8; ++k) v[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
-                  st_global_v8(out_row + c * 32 + e, v);
-                }
-              } else {
-                // an fp32 partial is laid out [4 columns][row], so that the lanes of a store write consecutive 16-byte pieces
-                float* part = p.work.part_o + (static_cast<size_t>(slot) * (D / 4) + c * 8) * (128 * 4) + r * 4;
+              for (int e = 0; e < D; e += 16) {
+                uint32_t v[8];
 #pragma unroll
-                for (int e = 0; e < 32; e += 4)
-                  *reinterpret_cast<uint4*>(part + (e / 4) * (128 * 4)) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                for (int k = 0; k < 8; ++k) v[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
+                st_global_v8(out_row + e, v);
               }
-            };
-            ld32(o_addr, oa);
+            } else if (row_valid) {
+              // an fp32 partial is laid out [4 columns][row], so that the lanes of a store write consecutive 16-byte pieces
+              float* part = p.work.part_o + static_cast<size_t>(slot) * (D / 4) * (128 * 4) + r * 4;
 #pragma unroll
-            for (int c = 0; c < D / 32; c += 2) {
-              wait_ld();
-              ld32(o_addr + (c + 1) * 32, ob);
-              store_chunk(oa, c);
-              wait_ld();
-              if (c + 2 < D / 32) ld32(o_addr + (c + 2) * 32, oa);
-              store_chunk(ob, c + 1);
+              for (int e = 0; e < D; e += 4)
+                *reinterpret_cast<uint4*>(part + (e / 4) * (128 * 4)) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
             }
             if (row_valid && slot >= 0) p.work.part_ml[static_cast<size_t>(slot) * 128 + r] = make_float2(m_ref, l_row);
-            fence_before();
+          } else if (lane == 0) {
+            mbar_arrive_pair(o_free_to);
           }
-          __syncwarp();
-          if (lane == 0) mbar_arrive_pair(o_free_to);
         }
       }
       sg += steps;
