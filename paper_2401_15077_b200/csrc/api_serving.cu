@@ -106,7 +106,7 @@ bool prepared(int head_dim) {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
   std::lock_guard<std::mutex> lock(g_prepared_mutex);
   bool& done = g_prepared[dev][head_dim == 128];
-  if (!done) done = chunk_prepare(head_dim) == cudaSuccess;
+  if (!done) done = chunk_prepare(head_dim) == cudaSuccess && chunk_rows_prepare(head_dim) == cudaSuccess;
   return done;
 }
 
@@ -169,7 +169,8 @@ int eagle_tree_rope_append(const eagle_rope_desc* desc, const void* q, const voi
 
 size_t eagle_chunk_attn_workspace(const eagle_chunk_desc* desc) {
   ChunkWork w;
-  if (!desc || !carve_chunk_work(*desc, nullptr, kMaxPairs, &w)) return 0;
+  int workers = 0;
+  if (!desc || !carve_chunk_work(*desc, nullptr, kMaxPlanCtas, &w, &workers)) return 0;
   return w.bytes;
 }
 
@@ -179,7 +180,7 @@ int eagle_chunk_attn(const eagle_chunk_desc* desc, const void* q, const eagle_kv
   const eagle_chunk_desc& d = *desc;
   ChunkParams p = {};
   ChunkWork need;
-  if (!(d.sm_scale >= 0.f) || !(d.sm_scale < 3.0e38f) || !carve_chunk_work(d, nullptr, kMaxPairs, &need) || kv->k_scale || kv->v_scale) return EAGLE_ERR_SHAPE;
+  if (!(d.sm_scale >= 0.f) || !(d.sm_scale < 3.0e38f) || !carve_chunk_work(d, nullptr, kMaxPlanCtas, &need, &p.num_workers) || kv->k_scale || kv->v_scale) return EAGLE_ERR_SHAPE;
   const int rc = check_store(*kv, d.head_dim, d.num_kv_heads, &p.capacity);
   if (rc != EAGLE_OK) return rc;
   if (d.batch == 0 || d.num_tokens == 0) return EAGLE_OK;
@@ -190,8 +191,7 @@ int eagle_chunk_attn(const eagle_chunk_desc* desc, const void* q, const eagle_kv
   const int dev = usable_device(&sms);
   if (dev != EAGLE_OK) return dev;
   if (!prepared(d.head_dim)) return EAGLE_ERR_DEVICE;
-  p.num_pairs = sms / 2 < kMaxPairs ? sms / 2 : kMaxPairs;
-  carve_chunk_work(d, d.workspace, p.num_pairs, &p.work);
+  carve_chunk_work(d, d.workspace, sms, &p.work, &p.num_workers);
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.k = static_cast<const __nv_bfloat16*>(kv->k);
   p.v = static_cast<const __nv_bfloat16*>(kv->v);
@@ -205,7 +205,10 @@ int eagle_chunk_attn(const eagle_chunk_desc* desc, const void* q, const eagle_kv
   p.Hkv = d.num_kv_heads;
   p.G = d.num_q_heads / d.num_kv_heads;
   p.D = d.head_dim;
-  p.tpt = 128 / p.G;
+  p.few = chunk_takes_rows(d);
+  p.rows = p.few ? kFewRows : kTileRows;
+  p.tpt = p.rows / p.G;
+  p.ut = p.few ? p.tpt : 2 * p.tpt;
   p.max_rows = static_cast<int>(std::fmin(1.0e9, static_cast<double>(d.num_tokens) * p.G));
   p.page_size = kv->page_size;
   p.page_shift = kv->block_table ? page_shift_of(kv->page_size) : 0;

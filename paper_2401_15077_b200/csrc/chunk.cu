@@ -2,8 +2,8 @@
 //
 //   out[t] = sum_j softmax_j(scale * q[t].k[j]) v[j],  j <= L_b + i, for token t = token_start[b] + i of sequence b.
 //
-// Three launches: a planner (one CTA), the attention kernel (persistent, one cluster of two CTAs on every two SMs) and the merge
-// of what was cut.
+// Three launches: a planner (one CTA), an attention kernel (persistent) and the merge of what was cut.  The attention kernel of
+// this file is one cluster of two CTAs on every two SMs; calls of single tokens take the one of chunk_rows.cu.
 //
 // A query tile is 128 rows of one (sequence, KV head): TPT = 128 / G tokens (rounded down) times the G heads of the group.  The two
 // CTAs of a pair take neighbouring query tiles over the same K/V tiles, and the tensor cores of both work on one MMA of 256
@@ -75,16 +75,16 @@ __device__ __forceinline__ int cut_tile(long long pos, long long x, int tiles) {
 }
 
 // Work is counted in keys: a unit costs the keys that its last token sees plus a constant for starting it.  All units lie end
-// to end on one line.  Whole units are dealt to the CTA pairs in rounds (pair c gets units c, c + P, ...) while every pair's sum
-// stays within its equal share W / P: pairs then start neighbouring units at the same time, walk the same keys at the same
-// pace and share them through L2.  The units that are left are cut in contiguous shares that fill each CTA pair up to W / P exactly,
+// to end on one line.  Whole units are dealt to the workers in rounds (worker c gets units c, c + P, ...) while every worker's sum
+// stays within its equal share W / P: they then start neighbouring units at the same time, walk the same keys at the same
+// pace and share them through L2.  The units that are left are cut in contiguous shares that fill each worker up to W / P exactly,
 // so the split needs at most P - 1 cuts whatever the lengths are.
 __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p) {
   __shared__ Sum2 s_warp[kPlanThreads / 32];
-  __shared__ long long s_pos[kMaxPairs + 1], s_cost[kNearSeqs], s_x[kNearUnits + 1];
-  __shared__ int s_base[kNearSeqs], s_first[kMaxPairs], s_last[kMaxPairs];
+  __shared__ long long s_pos[kMaxPlanCtas + 1], s_cost[kNearSeqs], s_x[kNearUnits + 1];
+  __shared__ int s_base[kNearSeqs], s_first[kMaxPlanCtas], s_last[kMaxPlanCtas];
   __shared__ ChunkSeq s_seq[kNearSeqs];
-  const int tid = threadIdx.x, P = p.num_pairs, B = p.B, Hkv = p.Hkv, tpt = p.tpt;
+  const int tid = threadIdx.x, P = p.num_workers, B = p.B, Hkv = p.Hkv, ut = p.ut;
   ChunkWork& w = p.work;
   ChunkSeq* seqs = B <= kNearSeqs ? s_seq : w.seq;
   int* base_of = B <= kNearSeqs ? s_base : w.unit_base;
@@ -123,11 +123,11 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
         else q.n = n;
       }
       if (q.n > 0) {
-        q.pairs = ceil_div(ceil_div(q.n, tpt), 2);
-        const long long np = q.pairs;
+        q.parts = ceil_div(q.n, ut);
+        const long long np = q.parts;
         v.a = static_cast<int>(np) * Hkv;
-        // sum over the pairs of L + (2p + 2) TPT, but the last one ends at n
-        v.b = (np * (q.L + kChunkItemKeys) + tpt * np * (np + 1) - (2 * np * tpt - q.n)) * Hkv;
+        // sum over the parts of L + (p + 1) UT, but the last one ends at n
+        v.b = (np * (q.L + kChunkItemKeys) + ut * (np * (np + 1) / 2) - (np * ut - q.n)) * Hkv;
       }
     }
     Sum2 tot;
@@ -152,21 +152,21 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
   long long* x_of = U <= kNearUnits ? s_x : w.x;
   __syncthreads();
 
-  // ---- units: a sequence's pairs from the longest to the shortest, KV heads innermost
+  // ---- units: a sequence's parts from the longest to the shortest, KV heads innermost
   auto unit_of = [&](int u, long long* x) {
     const int b = last_le(base_of, B, u);
     const ChunkSeq q = seqs[b];
-    const int i = u - base_of[b], r = i / Hkv, pr = q.pairs - 1 - r;      // r longer pairs come before
+    const int i = u - base_of[b], r = i / Hkv, pr = q.parts - 1 - r;      // r longer parts come before
     ChunkUnit un;
     un.b = b;
     un.g = i - r * Hkv;
-    un.pair = pr;
-    const long long over = 2ll * q.pairs * tpt - q.n;                      // the last pair is that much shorter
-    const long long keys = q.L + (2ll * pr + 2) * tpt - (r == 0 ? over : 0);
+    un.part = pr;
+    const long long over = static_cast<long long>(q.parts) * ut - q.n;     // the last part is that much shorter
+    const long long keys = q.L + (pr + 1ll) * ut - (r == 0 ? over : 0);
     un.tiles = static_cast<int>((keys + kChunkTile - 1) / kChunkTile);
     if (x) {
       const long long before = static_cast<long long>(r) * (q.L + kChunkItemKeys) +
-                               tpt * (static_cast<long long>(q.pairs) * (q.pairs + 1) - static_cast<long long>(pr + 1) * (pr + 2)) - (r > 0 ? over : 0);
+                               ut * ((static_cast<long long>(q.parts) * (q.parts + 1) - static_cast<long long>(pr + 1) * (pr + 2)) / 2) - (r > 0 ? over : 0);
       *x = cost_of[b] + before * Hkv + un.g * (keys + kChunkItemKeys);
     }
     return un;
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
   if (tid == 0) x_of[U] = W;
   __syncthreads();
 
-  // ---- whole units while they fit every CTA pair's share
+  // ---- whole units while they fit every worker's share
   const long long T = (W + P - 1) / P;
   long long S = 0;
   int k = 0;
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
     S += cost;
   }
   const int F = k * P;
-  // ---- what is left is shared out so that every pair comes to T
+  // ---- what is left is shared out so that every worker comes to T
   {
     Sum2 v = {0, tid < P ? T - S : 0}, tot;
     const Sum2 inc = block_scan(v, s_warp, &tot);
@@ -206,15 +206,16 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
   }
   __syncthreads();
 
+  const int tiles = p.few ? 1 : 2;                                         // query tiles of a unit, a partial slot each
   auto emit = [&](int at, const ChunkUnit& un, int t0, int t1, int slot) {
     const ChunkSeq q = seqs[un.b];
     int4* it = reinterpret_cast<int4*>(w.items + at);
-    it[0] = make_int4(un.b, un.g, un.pair, q.start);
+    it[0] = make_int4(un.b, un.g, un.part, q.start);
     it[1] = make_int4(q.n, q.L, t0, t1);
     it[2] = make_int4(slot, 0, 0, 0);
   };
-  // Whole units are items c * k + round.  Of the shares, piece (u, c) of unit u in pair c's share is item u + c; the units in
-  // which a share begins and ends are noted for the pair.
+  // Whole units are items c * k + round.  Of the shares, piece (u, c) of unit u in worker c's share is item u + c; the units in
+  // which a share begins and ends are noted for the worker.
   for (int u = tid; u < U; u += kPlanThreads) {
     const ChunkUnit un = u == tid ? own : unit_of(u, nullptr);
     if (u < F) {
@@ -228,7 +229,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
     for (;; ++c) {
       const bool ends = x1 <= s_pos[c + 1];
       const int cut = ends ? un.tiles : cut_tile(s_pos[c + 1], x0, un.tiles), t1 = cut > t0 ? cut : t0;
-      emit(u + c, un, t0, t1, t0 == 0 && t1 == un.tiles ? -1 : 4 * c + (t0 > 0 ? 0 : 2));
+      emit(u + c, un, t0, t1, t0 == 0 && t1 == un.tiles ? -1 : (2 * c + (t0 > 0 ? 0 : 1)) * tiles);
       if (x1 >= s_pos[c + 1]) s_last[c] = u;
       if (ends) break;
       s_first[c + 1] = u;
@@ -290,15 +291,6 @@ struct Bars {
   __device__ __forceinline__ uint32_t p_full(uint32_t i) const { return at(kSAt + kSBufs + i); }         // its probabilities (first CTA only)
   __device__ __forceinline__ uint32_t o_done(uint32_t i) const { return at(kSAt + 2 * kSBufs + i); }     // its PV has finished (both CTAs)
   __device__ __forceinline__ uint32_t o_free() const { return at(kSAt + 3 * kSBufs); }                   // an item's accumulators have been read (first CTA only)
-};
-
-// Counts steps through a ring: slot and parity of the use after next calls of step().
-template <int N>
-struct Ring {
-  uint32_t slot = 0, par = 0;
-  __device__ __forceinline__ void step() {
-    if (++slot == N) { slot = 0; par ^= 1u; }
-  }
 };
 
 // Bounded wait for a tagged word in shared memory (low byte == want): the word, with bit 32 set; 0 when the CTA was aborted or
@@ -375,7 +367,7 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
   const int4 mine = p.work.cta[blockIdx.x >> 1];         // whole units first, then this pair's share of the rest
   const int n_items = mine.y + mine.w;
   struct Item {
-    int b, g, pair, start, n, L, t0, t1, slot;
+    int b, g, part, start, n, L, t0, t1, slot;
   };
   auto item = [&](int i) {
     const int4* at = reinterpret_cast<const int4*>(p.work.items + (i < mine.y ? mine.x + i : mine.z + (i - mine.y)));
@@ -448,7 +440,7 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
 #pragma unroll
           for (int sl = 0; sl < S::kSlabs; ++sl)
             tma_load_3d_pair(sbase + S::kQ + qb * S::kQBytes + sl * S::kQSlab, &map_q, sl * 64, ck.it.g * p.G,
-                             ck.it.start + (2 * ck.it.pair + half) * p.tpt, B.q_ready(qb) + to_first);
+                             ck.it.start + (2 * ck.it.part + half) * p.tpt, B.q_ready(qb) + to_first);
         }
         ++q_items;
       }
@@ -577,7 +569,7 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
       const Item it = item(i);
       const int steps = it.t1 - it.t0;
       if (steps <= 0) continue;
-      const int first = (2 * it.pair + static_cast<int>(rank)) * p.tpt, token = first + tok_r;    // place in the chunk
+      const int first = (2 * it.part + static_cast<int>(rank)) * p.tpt, token = first + tok_r;    // place in the chunk
       const bool row_valid = tok_r < p.tpt && token < it.n;
       const bool warp_rests = !__any_sync(0xffffffffu, row_valid);
       const int limit = it.L + (token < it.n ? token : it.n - 1);                 // the last key this row sees
@@ -796,9 +788,9 @@ template <int D>
 __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams p, int row_blocks) {
   wait_for_prerequisites();                              // partials and outputs of the attention kernel are there
   const ChunkWork& w = p.work;
-  const int tid = threadIdx.x, records = p.num_pairs;
-  if (static_cast<int>(blockIdx.x) >= records * 2 * row_blocks) {
-    const int b = blockIdx.x - records * 2 * row_blocks;
+  const int tid = threadIdx.x, records = p.num_workers, halves = p.few ? 1 : 2;
+  if (static_cast<int>(blockIdx.x) >= records * halves * row_blocks) {
+    const int b = blockIdx.x - records * halves * row_blocks;
     const ChunkSeq q = w.seq[b];
     const int s = p.token_start[b], e = p.token_start[b + 1];
     if (s < 0 || e <= s || e > p.N) return;
@@ -820,14 +812,14 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams 
     for (size_t i = tid; i < vecs; i += kMergeThreads) out[i] = make_uint4(0u, 0u, 0u, 0u);
     return;
   }
-  __shared__ int s_slot[kMaxPairs];                      // slots of the pieces that are not empty, in order
+  __shared__ int s_slot[kMaxPlanCtas];                      // slots of the pieces that are not empty, in order
   __shared__ int s_count;
-  const int rec = blockIdx.x / (2 * row_blocks), rest = blockIdx.x - rec * 2 * row_blocks, half = rest / row_blocks, rb = rest - half * row_blocks;
+  const int rec = blockIdx.x / (halves * row_blocks), rest = blockIdx.x - rec * halves * row_blocks, half = rest / row_blocks, rb = rest - half * row_blocks;
   const ChunkCut cut = w.cut[rec];
   if (cut.unit < 0) return;
   const ChunkUnit un = w.unit[cut.unit];
   const ChunkSeq q = w.seq[un.b];
-  const int first = (2 * un.pair + half) * p.tpt;
+  const int first = un.part * p.ut + half * p.tpt;
   if (first + rb * 8 / p.G >= q.n || rb * 8 / p.G >= p.tpt) return;      // no row of this block belongs to the sequence
   if (tid < 32) {
     int count = 0;
@@ -860,8 +852,8 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams 
       v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (i + k < pieces) {
         const size_t slot = s_slot[i + k];
-        ml[k] = w.part_ml[slot * 128 + row];
-        v[k] = *reinterpret_cast<const float4*>(w.part_o + (slot * (D / 4) + cols) * (128 * 4) + row * 4);
+        ml[k] = w.part_ml[slot * p.rows + row];
+        v[k] = *reinterpret_cast<const float4*>(w.part_o + (slot * (D / 4) + cols) * (p.rows * 4) + row * 4);
       }
     }
     const float top = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
@@ -886,7 +878,7 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams 
 }
 
 template <int D>
-cudaError_t launch_all(const ChunkParams& p, cudaStream_t stream) {
+cudaError_t launch_tiles(const ChunkParams& p, cudaStream_t stream) {
   CUtensorMap mk, mv, mq;
   const bool paged = p.block_table != nullptr;
   const int k_rows = paged && p.page_size < 64 ? p.page_size : 64, v_rows = paged && p.page_size < 128 ? p.page_size : 128;
@@ -895,30 +887,24 @@ cudaError_t launch_all(const ChunkParams& p, cudaStream_t stream) {
   if (!map_bf16_3d(&mk, p.k, D, n1, n2, 64, k_rows, 1) || !map_bf16_3d(&mv, p.v, D, n1, n2, D / 2, v_rows, 1) ||
       !map_bf16_3d(&mq, p.q, D, p.Hq, p.N, 64, p.G, p.tpt))
     return cudaErrorInvalidValue;
-  chunk_plan_kernel<<<1, kPlanThreads, 0, stream>>>(p);
-  count_launch();
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
+  BehindLaunch at(2 * p.num_workers, kThreads, Smem<D>::kBytes, stream);
+  return cudaLaunchKernelEx(&at.config, paged ? chunk_attn_kernel<D, true> : chunk_attn_kernel<D, false>, p, mk, mv, mq);
+}
+
+template <int D>
+cudaError_t launch_all(const ChunkParams& p, cudaStream_t stream) {
   // Both kernels after the planner are launched programmatically: their prologues (and the launches themselves) overlap the
   // kernel before, whose results they wait for.
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t config = {};
-  config.stream = stream;
-  config.attrs = &attr;
-  config.numAttrs = 1;
-  config.gridDim = dim3(2 * p.num_pairs);
-  config.blockDim = dim3(kThreads);
-  config.dynamicSmemBytes = Smem<D>::kBytes;
-  e = cudaLaunchKernelEx(&config, paged ? chunk_attn_kernel<D, true> : chunk_attn_kernel<D, false>, p, mk, mv, mq);
+  chunk_plan_kernel<<<1, kPlanThreads, 0, stream>>>(p);
+  cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   count_launch();
-  const int rows = p.max_rows < 128 ? p.max_rows : 128, row_blocks = (rows + 7) / 8;
-  config.gridDim = dim3(p.num_pairs * 2 * row_blocks + p.B);
-  config.blockDim = dim3(kMergeThreads);
-  config.dynamicSmemBytes = 0;
-  e = cudaLaunchKernelEx(&config, chunk_merge_kernel<D>, p, row_blocks);
+  e = p.few ? launch_chunk_rows(p, stream) : launch_tiles<D>(p, stream);
+  if (e != cudaSuccess) return e;
+  count_launch();
+  const int rows = p.max_rows < p.rows ? p.max_rows : p.rows, row_blocks = (rows + 7) / 8;
+  BehindLaunch at(p.num_workers * (p.few ? 1 : 2) * row_blocks + p.B, kMergeThreads, 0, stream);
+  e = cudaLaunchKernelEx(&at.config, chunk_merge_kernel<D>, p, row_blocks);
   if (e != cudaSuccess) return e;
   count_launch();
   return cudaSuccess;

@@ -1,4 +1,4 @@
-// Plan records, workspace and parameters of the chunk attention (chunk.cu).
+// Plan records, workspace and parameters of the chunk attention (chunk.cu, chunk_rows.cu).
 #pragma once
 #include "common.cuh"
 
@@ -9,19 +9,28 @@ constexpr int kChunkTile = 128;        // keys per K/V tile
 // unit's edge a cut moves to the edge.
 constexpr int kChunkItemKeys = 256;
 constexpr int kChunkSnap = 2;
-constexpr int kMaxPairs = kMaxPlanCtas / 2;
 
-// A unit is a pair of neighbouring query tiles of one (sequence, KV head); an item is what a pair of CTAs does of it in one go.
+// Two attention kernels share the planner and the merge.  The tile kernel's workers are pairs of CTAs, with two query tiles of
+// 128 rows on the tensor cores of both; the row kernel's are single CTAs, with one query tile of 16 rows.  A query tile is
+// TPT tokens times the G heads of a group.  Calls with no more rows than sequences (single tokens) take the row kernel: there
+// the keys and values are streamed once for a few rows, and what counts is how steadily they come.  64 single tokens over 512 to
+// 8192 slots, 32 heads over 8: 208 us, the tile kernel 249 us; one token over 65536, 64 heads over 8: 61 us against
+// 77 us.  The row kernel is right for more tokens too, but reads the cache again for every 16 / G of them.
+constexpr int kTileRows = 128, kFewRows = 16;
+inline bool chunk_takes_rows(const eagle_chunk_desc& d) { return d.num_tokens <= d.batch; }
+
+// A unit is what a worker holds at once (one or two neighbouring query tiles) of one (sequence, KV head); an item is what a
+// worker does of it in one go.
 struct ChunkSeq {        // n = 0: empty or refused
-  int32_t start, n, L, pairs;
+  int32_t start, n, L, parts;    // units per KV head
 };
 struct ChunkUnit {
-  int32_t b, g, pair, tiles;     // K/V tiles
+  int32_t b, g, part, tiles;     // K/V tiles
 };
 struct alignas(16) ChunkItem {
-  int32_t b, g, pair, start;     // start: the sequence's first row
+  int32_t b, g, part, start;     // start: the sequence's first row
   int32_t n, L, t0, t1;          // K/V tiles [t0, t1)
-  int32_t slot;                  // partial slot of the first CTA's query tile (the second's is the next one), -1: write the output
+  int32_t slot;                  // partial slot of the first query tile (the second's is the next one), -1: write the output
   int32_t pad[3];
 };
 // A unit whose output is merged from the pieces (unit, c), c_lo <= c <= c_hi; unit < 0: none.
@@ -35,11 +44,11 @@ struct ChunkWork {
   long long* cost_base;    // [B]
   long long* x;            // [units + 1]: where each unit starts on the work line
   ChunkUnit* unit;         // [units]
-  ChunkItem* items;        // [units + CTA pairs]
-  int4* cta;               // [CTA pairs]: whole units (first, count), pieces (first, count)
-  ChunkCut* cut;           // [CTA pairs]
-  float2* part_ml;         // [slots, 128]
-  float* part_o;           // [slots, D / 4, 128, 4]
+  ChunkItem* items;        // [units + workers]
+  int4* cta;               // [workers]: whole units (first, count), pieces (first, count)
+  ChunkCut* cut;           // [workers]
+  float2* part_ml;         // [slots, rows of a query tile]
+  float* part_o;           // [slots, D / 4, rows, 4]
   size_t bytes;
 };
 
@@ -52,26 +61,31 @@ struct ChunkParams {
   const int32_t* token_start;    // [B + 1]
   const int32_t* block_table;    // paged cache, or null
   int32_t B, N, Hq, Hkv, G, D;
-  int32_t tpt;                   // tokens per query tile
+  int32_t few;                   // the row kernel's call
+  int32_t rows, tpt, ut;         // rows and tokens of a query tile, tokens of a unit
   int32_t max_rows;              // query rows of a (sequence, KV head) at the most
   long long capacity;            // slots per sequence
   int32_t page_size, page_shift, max_pages, num_pages;
-  int32_t num_pairs;             // pairs of CTAs of the attention kernel
+  int32_t num_workers;           // CTAs of the row kernel, pairs of CTAs of the tile kernel
   float scale_log2;
   int32_t* status;
   unsigned long long wait_limit_ns;
   ChunkWork work;
 };
 
-// Partial slots: a pair of CTAs' share of the cut units begins and ends inside a unit at the most: two pieces of two query tiles.
-inline bool carve_chunk_work(const eagle_chunk_desc& d, void* base, int num_pairs, ChunkWork* w) {
+// Partial slots: a worker's share of the cut units begins and ends inside a unit at the most, with the query tiles of both.
+// `sms` bounds the workers.
+inline bool carve_chunk_work(const eagle_chunk_desc& d, void* base, int sms, ChunkWork* w, int* num_workers) {
   if (d.batch < 0 || d.num_tokens < 0 || d.num_kv_heads <= 0 || d.num_q_heads <= 0 || d.num_q_heads % d.num_kv_heads) return false;
   const int G = d.num_q_heads / d.num_kv_heads;
   if (G > kMaxGroup || (d.head_dim != 64 && d.head_dim != 128) || d.batch > 65535) return false;
-  const size_t B = static_cast<size_t>(d.batch), tpt = 128 / G;
-  const size_t units = static_cast<size_t>(d.num_kv_heads) * (d.num_tokens / (2 * tpt) + B);
+  const bool few = chunk_takes_rows(d);
+  const int rows = few ? kFewRows : kTileRows, tiles = few ? 1 : 2, workers = (sms < kMaxPlanCtas ? sms : kMaxPlanCtas) / tiles;
+  const size_t B = static_cast<size_t>(d.batch), ut = tiles * (rows / G);
+  const size_t units = static_cast<size_t>(d.num_kv_heads) * (d.num_tokens / ut + B);
   if (units > (1u << 28)) return false;
-  const size_t slots = 4 * static_cast<size_t>(num_pairs);
+  const size_t slots = 2 * static_cast<size_t>(tiles) * workers;
+  *num_workers = workers;
   char* p = static_cast<char*>(base);
   size_t off = 0;
   auto take = [&](size_t n) { char* r = p ? p + off : nullptr; off += align256(n > 0 ? n : 1); return r; };
@@ -80,16 +94,18 @@ inline bool carve_chunk_work(const eagle_chunk_desc& d, void* base, int num_pair
   w->cost_base = reinterpret_cast<long long*>(take(sizeof(long long) * B));
   w->x = reinterpret_cast<long long*>(take(sizeof(long long) * (units + 1)));
   w->unit = reinterpret_cast<ChunkUnit*>(take(sizeof(ChunkUnit) * units));
-  w->items = reinterpret_cast<ChunkItem*>(take(sizeof(ChunkItem) * (units + num_pairs)));
-  w->cta = reinterpret_cast<int4*>(take(sizeof(int4) * num_pairs));
-  w->cut = reinterpret_cast<ChunkCut*>(take(sizeof(ChunkCut) * num_pairs));
-  w->part_ml = reinterpret_cast<float2*>(take(sizeof(float2) * slots * 128));
-  w->part_o = reinterpret_cast<float*>(take(sizeof(float) * slots * 128 * d.head_dim));
+  w->items = reinterpret_cast<ChunkItem*>(take(sizeof(ChunkItem) * (units + workers)));
+  w->cta = reinterpret_cast<int4*>(take(sizeof(int4) * workers));
+  w->cut = reinterpret_cast<ChunkCut*>(take(sizeof(ChunkCut) * workers));
+  w->part_ml = reinterpret_cast<float2*>(take(sizeof(float2) * slots * rows));
+  w->part_o = reinterpret_cast<float*>(take(sizeof(float) * slots * rows * d.head_dim));
   w->bytes = off;
   return true;
 }
 
 cudaError_t chunk_prepare(int head_dim);
+cudaError_t chunk_rows_prepare(int head_dim);
+cudaError_t launch_chunk_rows(const ChunkParams& p, cudaStream_t stream);      // the row kernel alone, behind the planner
 cudaError_t launch_chunk(const ChunkParams& p, cudaStream_t stream);
 
 }  // namespace eagle

@@ -57,7 +57,7 @@ __device__ __forceinline__ unsigned long long global_timer() {
 }
 // Every wait gives up after the limit that the host set (it sits in shared memory right behind the abort flag), raises
 // the flag and returns false; so does every other wait of the CTA from then on.
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   const unsigned long long t0 = global_timer(), limit = *reinterpret_cast<volatile unsigned long long*>(abort_flag + 1);
   for (uint32_t spins = 1;; ++spins) {
     if (mbar_try_wait(bar, parity)) return true;
@@ -78,6 +78,15 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
 }
+
+// Counts steps through a ring of N slots: the slot of the next step, and the parity of its use.
+template <int N>
+struct Ring {
+  uint32_t slot = 0, par = 0;
+  __device__ __forceinline__ void step() {
+    if (++slot == N) { slot = 0; par ^= 1u; }
+  }
+};
 
 // ------------------------------------------------------------------------------------------------ fences, commits, copies
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -324,6 +333,23 @@ inline bool map_bf16_3d(CUtensorMap* map, const void* base, int D, long long n1,
             cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+// Configuration of a programmatic launch: the kernel may start before the one in front of it in the stream has finished.
+struct BehindLaunch {
+  cudaLaunchConfig_t config = {};
+  cudaLaunchAttribute attr;
+  BehindLaunch(int blocks, int threads, size_t smem, cudaStream_t stream) {
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    config.gridDim = dim3(blocks);
+    config.blockDim = dim3(threads);
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    config.attrs = &attr;
+    config.numAttrs = 1;
+  }
+  BehindLaunch(const BehindLaunch&) = delete;
+};
 
 }  // namespace tc
 }  // namespace eagle

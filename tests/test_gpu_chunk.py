@@ -30,12 +30,12 @@ def _ints(v):
 class Case:
     """Keys and values only where the sequences are: every other slot is NaN."""
 
-    def __init__(self, n, lens, hq, hkv, d, page=0, seed=0, pad=37):
+    def __init__(self, n, lens, hq, hkv, d, page=0, seed=0, pad=37, spare=3):
         g = torch.Generator().manual_seed(seed)
         self.n, self.lens, self.page = n, lens, page
         B, need = len(n), [a + b for a, b in zip(n, lens)]
         self.start = _ints(np.concatenate([[0], np.cumsum(n)]).tolist())
-        self.q = torch.randn(sum(n) + 3, hq, d, generator=g).bfloat16()
+        self.q = torch.randn(sum(n) + spare, hq, d, generator=g).bfloat16()
         if page:
             used = [-(-x // page) for x in need]
             order = torch.randperm(sum(used) + 2, generator=g).tolist()
@@ -268,3 +268,147 @@ def test_random_shapes(E, seed):
     out, status = c.run(E)
     assert status == 0
     _check(out, *c.want())
+
+
+# ---- no more rows than sequences: the kernel for single tokens (it takes several tokens of a sequence too, 16 / G at a time)
+ROWS = {
+    "lone": dict(n=[1], lens=[0], hq=1, hkv=1, d=64),
+    "tile_edges": dict(n=[1] * 8, lens=[62, 63, 64, 126, 127, 128, 191, 255], hq=4, hkv=2, d=128),
+    "group_of_three": dict(n=[1, 1, 1], lens=[700, 1, 90], hq=12, hkv=4, d=128),
+    "group_of_seven": dict(n=[1, 0, 1, 0], lens=[33, 8, 1500, 0], hq=7, hkv=1, d=64),
+    "group_of_sixteen": dict(n=[1, 1], lens=[4000, 64], hq=32, hkv=2, d=128),
+    "no_group": dict(n=[1] * 5, lens=[0, 1, 2, 300, 500], hq=3, hkv=3, d=64),
+    "sixteen_tokens_in_a_tile": dict(n=[16, 0, 1] + [0] * 20, lens=[50, 3, 700] + [1] * 20, hq=2, hkv=2, d=128),
+    "more_tokens_than_a_tile": dict(n=[20] + [0] * 21 + [2], lens=[117] + [9] * 21 + [0], hq=10, hkv=2, d=64),
+    "a_tile_for_each_token": dict(n=[0, 9, 1, 3] + [0] * 12, lens=[0, 60, 127, 126] + [40] * 12, hq=16, hkv=1, d=128),
+    "one_long": dict(n=[1], lens=[30011], hq=6, hkv=3, d=128),
+    "long_and_short": dict(n=[1] * 90, lens=[(i * 977) % 2600 for i in range(90)], hq=8, hkv=4, d=64),
+    "all_empty": dict(n=[0, 0], lens=[3, 0], hq=4, hkv=2, d=64),
+}
+
+
+@pytest.mark.parametrize("page", [0, 16, 32, 64, 256])
+@pytest.mark.parametrize("name", list(ROWS))
+def test_single_tokens_match_the_definition(E, name, page):
+    c = Case(**ROWS[name], page=page, seed=len(name), spare=0)
+    assert c.q.shape[0] <= len(c.n)
+    out, status = c.run(E)
+    assert status == 0
+    _check(out, *c.want())
+
+
+def test_single_tokens_with_a_row_behind_the_last_sequence(E):
+    c = Case([1, 0, 0, 1, 0], [200, 5, 0, 77, 1], 8, 2, 128, page=16, seed=21, spare=2)
+    out, status = c.run(E)
+    assert status == 0
+    _check(out, *c.want())
+
+
+def test_single_tokens_and_what_they_cannot_see(E):
+    """Infinite and NaN keys of later tokens, growing scores, a NaN that is seen: as for chunks."""
+    c = Case([3, 0, 0, 0], [200, 0, 0, 0], 4, 2, 128, seed=22, spare=0)
+    c.k[0, :, 202] = float("nan")
+    c.k[0, :, 201] = float("inf")
+    out, status = c.run(E)
+    want, spread = c.want()
+    assert status == 0
+    got = out.double().numpy()
+    err = np.abs(got - want)[:1]
+    assert (err <= (2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 5e-4) * spread)[:1]).all()
+    assert np.isnan(got[2]).all()
+    c = Case([1, 1], [900, 310], 4, 1, 64, seed=23, spare=0)
+    c.k *= torch.linspace(0.01, 6.0, c.k.shape[2]).bfloat16()[:, None]
+    out, status = c.run(E)
+    assert status == 0
+    _check(out, *c.want())
+
+
+def test_single_tokens_repeat_bit_for_bit_over_any_cache(E):
+    kw = dict(n=[1] * 9, lens=[300, 2000, 5, 8, 61, 64, 63, 4000, 0], hq=8, hkv=2, d=128, seed=24, spare=0)
+    a = Case(**kw)
+    want = a.run(E)[0]
+    for page in (16, 128):
+        c = Case(**kw, page=page)
+        for b, m in enumerate([x + y for x, y in zip(c.n, c.lens)]):
+            for j in range(m):
+                at = int(c.table[b, j // page]), slice(None), j % page
+                c.k[at], c.v[at] = a.k[b, :, j], a.v[b, :, j]
+        c.q = a.q
+        for _ in range(3):
+            assert torch.equal(want.view(torch.int16), c.run(E)[0].view(torch.int16))
+
+
+def test_single_tokens_of_bad_sequences_are_zeroed(E):
+    c = Case([1, 1, 1], [40, 70, 20], 4, 2, 64, page=16, seed=25, spare=0)
+    want = c.want()[0]
+    c.table[1, 2] = c.k.shape[0]
+    out, status = c.run(E)
+    assert status == -11 and (out[1] == 0).all()
+    for b in (0, 2):
+        assert np.abs(out[b].double().numpy() - want[b]).max() < 0.05
+    c.table[1, 2] = 0
+    c.lens[1] = c.table.shape[1] * 16
+    out, status = c.run(E)
+    assert status == -6 and (out[1] == 0).all()
+    for b in (0, 2):
+        assert np.abs(out[b].double().numpy() - want[b]).max() < 0.05
+
+
+@pytest.mark.parametrize("spare", [0, 3])
+def test_more_sequences_and_units_than_the_planner_keeps_at_hand(E, spare):
+    n = [i % 3 % 2 for i in range(300)] if spare == 0 else [(i * 5) % 4 for i in range(300)]
+    for hq, hkv in ((4, 2), (16, 16)):
+        c = Case(n, [(i * 37) % 90 for i in range(300)], hq, hkv, 64, page=16 if hq == 4 else 0, seed=26, spare=spare)
+        out, status = c.run(E)
+        assert status == 0
+        _check(out, *c.want())
+    # (5000 units and more)
+    c = Case([1] * 320 if spare == 0 else [2] * 320, [(i * 11) % 30 for i in range(320)], 16, 16, 64, seed=27, spare=spare)
+    out, status = c.run(E)
+    assert status == 0
+    _check(out, *c.want())
+
+
+@pytest.mark.parametrize("spare", [0, 3])
+@pytest.mark.parametrize("page", [0, 256])
+def test_caches_of_more_than_2_31_elements(E, page, spare):
+    """The same sequences at the far end of a large cache: the outputs agree bit for bit."""
+    c = Case([1, 1, 1] if spare == 0 else [1, 40, 130], [500, 3, 777], 16, 8, 128, page=page, seed=28, spare=spare)
+    want, status = c.run(E)
+    assert status == 0
+    k, v = c.k, c.v
+    if page:
+        shape = (9000, 8, page, 128)                     # 2.4e9 elements
+        far = 9000 - k.shape[0]
+        c.k, c.v = (torch.empty(shape, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        c.k[far:], c.v[far:] = k.to(DEV), v.to(DEV)
+        c.table = torch.where(c.table >= 0, c.table + far, c.table)
+    else:
+        c.k, c.v = (torch.empty(3, 8, 1000000, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        c.k[:, :, :k.shape[2]], c.v[:, :, :k.shape[2]] = k.to(DEV), v.to(DEV)
+    out, status = c.run(E)
+    assert status == 0 and torch.equal(out.view(torch.int16), want.view(torch.int16))
+    del c
+    torch.cuda.empty_cache()
+
+
+def test_single_tokens_of_long_streams(E):
+    """Every SM streams megabytes through its ring, call after call: the same bits each time, and the tile kernel's answer (which
+    it takes when rows behind the last sequence make them more than the sequences).  The tolerance is twice the one above;
+    sum p |v| is the tile kernel's too, of absolute values, 1% up for its own error."""
+    g = torch.Generator(device=DEV).manual_seed(29)
+    lens = [512 + (i * 2311) % 7600 for i in range(48)]
+    for d, hq, hkv, page in ((128, 32, 8, 64), (64, 16, 8, 16), (128, 16, 16, 0)):
+        per = 8192 // page if page else 0
+        shape = (48 * per, hkv, page, d) if page else (48, hkv, 8192, d)
+        q = torch.randn(51, hq, d, generator=g, device=DEV).bfloat16()
+        k, v = (torch.randn(shape, generator=g, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+        table = torch.randperm(48 * per, generator=g, device=DEV).int().view(48, per) if page else None
+        sl, start = _ints(lens).to(DEV), torch.arange(49, dtype=torch.int32, device=DEV)
+        runs = [E.eagle_chunk_attn(q[:48], E.KVStore(k, v, block_table=table), sl, start) for _ in range(6)]
+        tile = E.eagle_chunk_attn(q, E.KVStore(k, v, block_table=table), sl, start)[:48].double()
+        spread = 1.01 * E.eagle_chunk_attn(q, E.KVStore(k, v.abs(), block_table=table), sl, start)[:48].double()
+        torch.cuda.synchronize()
+        assert all(torch.equal(runs[0].view(torch.int16), r.view(torch.int16)) for r in runs[1:])
+        err = (runs[0].double() - tile).abs()
+        assert bool((err <= 2 * (2.0 ** -8 * tile.abs() + (2.0 ** -8 + 5e-4) * spread)).all())
