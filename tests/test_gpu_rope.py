@@ -303,3 +303,37 @@ def test_rows_of_their_own_are_asked_for(E):
     wide[::2] = q
     a = E.eagle_rope_append(wide[::2], k, v, kv, lens, start, freqs)
     assert torch.equal(a, E.eagle_rope_append(q.contiguous(), k, v, kv, lens, start, freqs))
+
+
+def test_thousands_of_sequences(E):
+    """(The search for a token's sequence takes a third round beyond 1024 of them.)"""
+    c = Case([(i * 7 + i // 900) % 3 for i in range(2500)], [(i * 13) % 29 for i in range(2500)], 1, 1, 64, page=16, seed=31)
+    want, stored = S.rope_append(c.q, c.k, c.v, c.lens, c.freqs.numpy(), token_start=c.start)
+    q_out, kv, status, before = _run_chunk(E, c)
+    assert status == 0
+    _check(c, q_out, kv, want, stored, 1.0, before, {(t,) for t in range(sum(c.n))})
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("page", [0, 256])
+def test_caches_of_more_than_2_31_elements(E, page, fp8):
+    """The same tokens at the far end of a large cache: the same bits there."""
+    c = Case([2, 40, 3], [300, 7, 511], 4, 8, 128, page=page, fp8=fp8, seed=32)
+    q_small, kv, status, _ = _run_chunk(E, c)
+    assert status == 0
+    up = lambda t: None if t is None else t.to(DEV)  # noqa: E731
+    if page:
+        far, shape = 9000 - c.kc.shape[0], (9000, 8, page, 128)          # 2.4e9 elements
+    else:
+        far, shape = 0, (3, 8, 1000000, 128)
+    big_k, big_v = (torch.zeros(shape, dtype=c.kc.dtype, device=DEV) for _ in range(2))
+    part = (slice(far, None),) if page else (slice(None), slice(None), slice(0, c.kc.shape[2]))
+    big_k[part], big_v[part] = up(c.kc), up(c.vc)
+    table = up(torch.where(c.table >= 0, c.table + far, c.table)) if page else None
+    big = E.KVStore(big_k, big_v, block_table=table, k_scale=up(c.ks), v_scale=up(c.vs))
+    q_big, _, status, _ = _run_chunk(E, c, kv=big)
+    bits = lambda t: t.contiguous().view(torch.uint8)  # noqa: E731
+    assert status == 0 and torch.equal(bits(q_small), bits(q_big))
+    assert torch.equal(bits(kv.k), bits(big_k[part])) and torch.equal(bits(kv.v), bits(big_v[part]))
+    rest = (slice(0, far),) if page else (slice(None), slice(None), slice(c.kc.shape[2], None))
+    assert not bool(big_k[rest].any()) and not bool(big_v[rest].any())
