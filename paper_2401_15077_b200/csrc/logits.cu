@@ -13,6 +13,11 @@
 // consecutive tokens, 32 at a time: every access is coalesced whatever the vocabulary's alignment, and lane l holds word l & 7
 // of the grammar's mask for all of them.  Logits and mask of the rows to come are on their way while one is worked on.
 // Counts are integers and a token's biases are added up by one thread in list order, so a call gives the same bits every time.
+//
+// Bound by HBM for a batch of trees, and there by what a CTA does before its first row: all its loads set out together as soon as
+// the sequence's lengths are known.  64 trees of 16 to 64 nodes x 32000 tokens, 4096 tokens of history, biases and masks (699 MB): 135 us,
+// 5.2 of the 6.6 TB/s that a plain copy reaches (147 us with the loads where they are used).  16 bf16 rows of 129537 tokens: 8.3 us,
+// of which 1.9 us would be the bytes: two rounds of CTAs, a launch and three trips to memory.
 #include "logits.cuh"
 
 namespace eagle {
@@ -33,43 +38,29 @@ __device__ __forceinline__ float load_logit(const void* base, size_t i) {
 
 template <bool BF16>
 __global__ void __launch_bounds__(kLogThreads, 4) logits_kernel(LogitsParams p) {
-  __shared__ uint32_t s_count[kRange];
-  __shared__ float s_bias[kRange];
+  __shared__ __align__(16) uint32_t s_count[kRange];
+  __shared__ __align__(16) float s_bias[kRange];
   __shared__ int s_btok[kMaxBias];
   __shared__ unsigned long long s_path[kMaxTree];   // nodes on the path of node i whose token lies in this CTA's range
   __shared__ int s_parent[kMaxTree], s_off[kMaxTree];   // parent; place of the node's token in the range, -1: outside
   const int tid = threadIdx.x, b = blockIdx.y, v0 = blockIdx.x * kRange, r_lo = blockIdx.z * p.rows_per_block;
   const bool first = blockIdx.x == 0 && blockIdx.z == 0 && tid == 0;      // reports for the sequence
 
-  // ---- the tree
+  // ---- what the sequence has: everything below sets out as soon as its lengths are there
   const int n = p.tree_sizes ? p.tree_sizes[p.shared_tree ? 0 : b] : p.T;
-  bool bad = n < 0 || n > p.T;
-  {
-    int wrong = 0, off = -1;
-    if (!bad && tid < n) {
-      const int m = p.tree_parent[(p.shared_tree ? 0 : static_cast<size_t>(b) * p.T) + tid], t = p.draft_tokens[static_cast<size_t>(b) * p.T + tid];
-      wrong = m < -1 || m >= tid;
-      if (t < 0 || t >= p.V) { if (blockIdx.x == 0 && blockIdx.z == 0) report_status(p.status, EAGLE_ERR_TOKEN); }
-      else if (t >= v0 && t < v0 + kRange) off = t - v0;
-      s_parent[tid] = m;
-      s_off[tid] = off;
-    }
-    bad = __syncthreads_or(bad || wrong);
+  int len = p.history ? min(max(p.history_len[b], 0), p.H) : 0;
+  const int prompt = p.history && p.prompt_len ? p.prompt_len[b] : 0;
+  const int nb = p.bias_tokens ? min(max(p.bias_len ? p.bias_len[b] : p.max_bias, 0), p.max_bias) : 0;
+  const float rho = p.repetition ? p.repetition[b] : 1.f, pi = p.presence ? p.presence[b] : 0.f, phi = p.frequency ? p.frequency[b] : 0.f;
+#pragma unroll
+  for (int i = 4 * tid; i < kRange; i += 4 * kLogThreads) {
+    *reinterpret_cast<uint4*>(s_count + i) = make_uint4(0u, 0u, 0u, 0u);
+    *reinterpret_cast<float4*>(s_bias + i) = make_float4(0.f, 0.f, 0.f, 0.f);
   }
+  bool bad = n < 0 || n > p.T;
   const int rows = bad ? p.T + 1 : n + 1, r_hi = min(rows, r_lo + p.rows_per_block);
   const size_t row0 = static_cast<size_t>(b) * (p.T + 1) * p.V;
-  if (bad) {
-    if (first) report_status(p.status, EAGLE_ERR_TREE);
-    for (int r = r_lo; r < r_hi; ++r)
-      for (int k = 0; k < kPerThread; ++k) {
-        const int v = v0 + tid + k * kLogThreads;
-        if (v < p.V) p.out[row0 + static_cast<size_t>(r) * p.V + v] = 0.f;
-      }
-    return;
-  }
-  if (r_lo >= r_hi) return;
-
-  // ---- the first rows set out before anything else is looked at
+  if (r_lo >= r_hi) len = 0;                         // (no row of this CTA exists: it only looks whether the tree is valid)
   const int lane = tid & 31, v_warp = (tid >> 5) * (32 * kPerThread), words = (p.V + 31) / 32;
   const int n_here = min(max(p.V - v0 - v_warp - lane, 0) + 31, 32 * kPerThread) >> 5;     // this lane's tokens that exist
   const int w_at = (v0 + v_warp) / 32 + (lane & (kPerThread - 1));                         // this lane's word of the mask
@@ -82,6 +73,18 @@ __global__ void __launch_bounds__(kLogThreads, 4) logits_kernel(LogitsParams p) 
       if (k < n_here) z[k] = load_logit<BF16>(p.logits, at + k * 32);
     if (has_word) mask = __ldg(p.allowed + (static_cast<size_t>(b) * (p.T + 1) + r) * words + w_at);
   };
+  const int32_t* h = p.history + static_cast<size_t>(b) * p.H;
+  int t[8];                                          // this thread's next tokens of the history
+  auto fetch_history = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = i0 + j * kLogThreads < len ? __ldg(h + i0 + j * kLogThreads) : 0;
+  };
+  fetch_history(tid);
+  int parent = -1, token = 0;
+  if (!bad && tid < n) {
+    parent = p.tree_parent[(p.shared_tree ? 0 : static_cast<size_t>(b) * p.T) + tid];
+    token = p.draft_tokens[static_cast<size_t>(b) * p.T + tid];
+  }
   float z0[kPerThread], z1[kPerThread];
   uint32_t m0 = 0u, m1 = 0u;
 #pragma unroll
@@ -89,52 +92,65 @@ __global__ void __launch_bounds__(kLogThreads, 4) logits_kernel(LogitsParams p) 
   fetch(r_lo, z0, m0);
   fetch(r_lo + 1, z1, m1);
 
+  for (int i = tid; i < nb; i += kLogThreads) s_btok[i] = p.bias_tokens[static_cast<size_t>(b) * p.max_bias + i];
+  // ---- the tree
+  {
+    int wrong = 0, off = -1;
+    if (!bad && tid < n) {
+      wrong = parent < -1 || parent >= tid;
+      if (token < 0 || token >= p.V) { if (blockIdx.x == 0 && blockIdx.z == 0) report_status(p.status, EAGLE_ERR_TOKEN); }
+      else if (token >= v0 && token < v0 + kRange) off = token - v0;
+      s_parent[tid] = parent;
+      s_off[tid] = off;
+    }
+    bad = __syncthreads_or(bad || wrong);
+  }
+  if (bad) {
+    if (first) report_status(p.status, EAGLE_ERR_TREE);
+    for (int r = r_lo; r < min(p.T + 1, r_lo + p.rows_per_block); ++r)
+      for (int k = 0; k < kPerThread; ++k) {
+        const int v = v0 + tid + k * kLogThreads;
+        if (v < p.V) p.out[row0 + static_cast<size_t>(r) * p.V + v] = 0.f;
+      }
+    return;
+  }
+  if (r_lo >= r_hi) return;
+
   // ---- history: counts of the tokens in the range
-  for (int i = tid; i < kRange; i += kLogThreads) { s_count[i] = 0u; s_bias[i] = 0.f; }
   if (tid < n) {
     unsigned long long path = 0ull;
     for (int m = tid; m >= 0; m = s_parent[m])
       if (s_off[m] >= 0) path |= 1ull << m;
     s_path[tid] = path;
   }
-  const int nb = p.bias_tokens ? min(max(p.bias_len ? p.bias_len[b] : p.max_bias, 0), p.max_bias) : 0;
-  for (int i = tid; i < nb; i += kLogThreads) s_btok[i] = p.bias_tokens[static_cast<size_t>(b) * p.max_bias + i];
-  __syncthreads();
-  if (p.history) {
-    const int len = min(max(p.history_len[b], 0), p.H), prompt = p.prompt_len ? p.prompt_len[b] : 0;
-    const int32_t* h = p.history + static_cast<size_t>(b) * p.H;
-    for (int i0 = tid; i0 < len; i0 += 8 * kLogThreads) {
-      int t[8];
+  for (int i0 = tid; i0 < len; i0 += 8 * kLogThreads) {
+    if (i0 != tid) fetch_history(i0);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[j] = i0 + j * kLogThreads < len ? __ldg(h + i0 + j * kLogThreads) : 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int i = i0 + j * kLogThreads;
-        if (i >= len) break;
-        if (t[j] < 0 || t[j] >= p.V) { if (blockIdx.x == 0 && blockIdx.z == 0) report_status(p.status, EAGLE_ERR_TOKEN); }
-        else if (t[j] >= v0 && t[j] < v0 + kRange) {
-          if (i < prompt) atomicOr(&s_count[t[j] - v0], kInPrompt);
-          else atomicAdd(&s_count[t[j] - v0], 1u);
-        }
+    for (int j = 0; j < 8; ++j) {
+      const int i = i0 + j * kLogThreads;
+      if (i >= len) break;
+      if (t[j] < 0 || t[j] >= p.V) { if (blockIdx.x == 0 && blockIdx.z == 0) report_status(p.status, EAGLE_ERR_TOKEN); }
+      else if (t[j] >= v0 && t[j] < v0 + kRange) {
+        if (i < prompt) atomicOr(&s_count[t[j] - v0], kInPrompt);
+        else atomicAdd(&s_count[t[j] - v0], 1u);
       }
     }
   }
   for (int i = tid; i < nb; i += kLogThreads) {
-    const int t = s_btok[i];
-    if (t < 0 || t >= p.V) { if (blockIdx.x == 0 && blockIdx.z == 0) report_status(p.status, EAGLE_ERR_TOKEN); continue; }
-    if (t < v0 || t >= v0 + kRange) continue;
+    const int tok = s_btok[i];
+    if (tok < 0 || tok >= p.V) { if (blockIdx.x == 0 && blockIdx.z == 0) report_status(p.status, EAGLE_ERR_TOKEN); continue; }
+    if (tok < v0 || tok >= v0 + kRange) continue;
     bool mine = true;                                // the first entry of a token adds up all of them
-    for (int j = 0; j < i; ++j) mine = mine && s_btok[j] != t;
+    for (int j = 0; j < i; ++j) mine = mine && s_btok[j] != tok;
     if (!mine) continue;
     float sum = 0.f;
     for (int j = i; j < nb; ++j)
-      if (s_btok[j] == t) sum += p.bias_values[static_cast<size_t>(b) * p.max_bias + j];
-    s_bias[t - v0] = sum;
+      if (s_btok[j] == tok) sum += p.bias_values[static_cast<size_t>(b) * p.max_bias + j];
+    s_bias[tok - v0] = sum;
   }
   __syncthreads();
 
   // z' = (z > 0 ? z / rho : z * rho) + add for a token that is there already, z + add for any other
-  const float rho = p.repetition ? p.repetition[b] : 1.f, pi = p.presence ? p.presence[b] : 0.f, phi = p.frequency ? p.frequency[b] : 0.f;
   const float inv_rho = 1.f / rho;
   float add[kPerThread];
   uint32_t seen = 0;
@@ -195,7 +211,7 @@ cudaError_t launch_logits(const LogitsParams& p_in, int sm_count, cudaStream_t s
   LogitsParams p = p_in;
   const int ranges = (p.V + kRange - 1) / kRange, rows = p.T + 1;
   // Rows are shared out over several CTAs (each counts the history again): at most 16 to one, so that trees of 16 and of 64
-  // nodes end together (147 us for 64 trees x 32000 tokens; 156 us with 33 rows, 158 us with 8), fewer while the CTAs do not fill
+  // nodes end together (135 us for 64 trees x 32000 tokens; 139 us with 33 rows, 143 us with 8), fewer while the CTAs do not fill
   // the machine.
   int splits = (rows + kRowsPerCta - 1) / kRowsPerCta;
   while (static_cast<long long>(ranges) * p.B * splits < 4ll * sm_count && splits < rows) ++splits;
