@@ -588,7 +588,8 @@ size_t eagle_chunk_attn_workspace(const eagle_chunk_desc* desc);
  * Rows outside every sequence are left as they were.  A sequence with L_b < 0 or L_b + n_b over its slots reports EAGLE_ERR_SEQ,
  * one with a block-table entry in use outside [0, num_pages) EAGLE_ERR_PAGE: its rows are zeros.  Starts that descend or
  * leave [0, N] report EAGLE_ERR_SEQ and no row is computed.  Three launches (planner, attention, merge), asynchronous on
- * `stream`; calls that share a workspace must not overlap on the GPU.
+ * `stream`; calls that share a workspace must not overlap on the GPU.  Calls with N <= B run a kernel made for single tokens (it is
+ * right for any lengths, but reads a sequence's cache once for every 16 / G of its tokens).
  */
 int eagle_chunk_attn(const eagle_chunk_desc* desc, const void* q, const eagle_kv_store* kv, const int32_t* seq_lens,
                      const int32_t* token_start, void* out, eagle_stream_t stream);
@@ -628,7 +629,8 @@ typedef struct eagle_logits_desc {
  * With c the number of times token v was generated (in the history past the prompt, and on the path from the root to the row's
  * node, that node included) and seen = c > 0 or v in the prompt:
  *     z <- seen ? (z > 0 ? z / rho : z * rho) : z;   z <- z - phi c - (c > 0 ? pi : 0);   z <- z + bias(v);   not allowed: -inf
- * in fp32.  A row whose mask allows nothing is all -inf.  Rows of nodes >= tree size are not written.  Lengths are clamped to
+ * in fp32.  A row whose mask allows nothing is all -inf (an acceptance walk that ends there still returns a token of the
+ * vocabulary, which then means nothing).  Rows of nodes >= tree size are not written.  Lengths are clamped to
  * their rows; a token outside the vocabulary (history, bias list, draft) is ignored and reports EAGLE_ERR_TOKEN; an invalid
  * tree reports EAGLE_ERR_TREE and all T_max + 1 rows of its sequence become zeros.  One launch; no workspace.
  */

@@ -9,6 +9,11 @@
 // CTAs of a pair take neighbouring query tiles over the same K/V tiles, and the tensor cores of both work on one MMA of 256
 // rows (cta_group::2): each CTA holds half of every K tile (64 keys) and half of every V tile (D / 2 columns), so a tile is
 // loaded once for both, and each SM reads half of the operand from its shared memory.
+//
+// What bounds it is the way of one score buffer around the loop (score MMA, softmax, PV MMA, and a wait between each two): about 4700
+// cycles, with three buffers on it 1550 per 128 keys, of which the tensor cores need 1036.  A prompt of 4096 tokens, 32 heads, D = 128
+// (137 GFLOP, causal): 160 us, 860 TFLOP/s; two chunks of 2048 tokens behind 16384 (1.17 TFLOP in 0.97 to 1.10 ms, by the clock that
+// the power limit leaves): 1.06 to 1.2 PFLOP/s of the 1.65 (1.40 sustained) that a large matrix product reaches.
 #include "chunk.cuh"
 #include "tc.cuh"
 
