@@ -412,3 +412,61 @@ def test_single_tokens_of_long_streams(E):
         assert all(torch.equal(runs[0].view(torch.int16), r.view(torch.int16)) for r in runs[1:])
         err = (runs[0].double() - tile).abs()
         assert bool((err <= 2 * (2.0 ** -8 * tile.abs() + (2.0 ** -8 + 5e-4) * spread)).all())
+
+
+def test_calls_on_two_streams_at_once(E):
+    """Both kernels, back to back on two streams with workspaces of their own: each gives what it gives alone."""
+    cases = [Case([1] * 40, [(i * 331) % 3000 for i in range(40)], 8, 2, 128, page=32, seed=41, spare=0),
+             Case([150, 1, 77], [300, 4000, 0], 8, 2, 128, page=16, seed=42),
+             Case([1, 0, 1], [9000, 5, 20], 16, 4, 64, seed=43, spare=0)]
+    want = [c.run(E)[0] for c in cases]
+    args = [(c.q.to(DEV), E.KVStore(c.k.to(DEV), c.v.to(DEV), block_table=None if c.table is None else c.table.to(DEV)), _ints(c.lens).to(DEV), c.start.to(DEV))
+            for c in cases]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = []
+    for rep in range(12):
+        for i, s in enumerate(streams):
+            which = (rep + i) % 3
+            with torch.cuda.stream(s):
+                out = torch.full(cases[which].q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+                E.eagle_chunk_attn(*args[which], out)
+            outs.append((which, out))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o.cpu().view(torch.int16), want[w].view(torch.int16)) for w, o in outs)
+
+
+def test_thousands_of_single_tokens(E):
+    c = Case([1] * 3000, [(i * 7) % 50 for i in range(3000)], 2, 1, 64, page=16, seed=44, spare=0)
+    out, status = c.run(E)
+    assert status == 0
+    _check(out, *c.want())
+
+
+def test_single_tokens_replayed_from_a_graph_with_other_lengths(E):
+    """A serving loop's decode graph: a fixed number of rows, sequences that grow, end (their rows stay as they are) and begin."""
+    steps = [Case([1, 1, 0, 1], [40, 700, 3, 0], 8, 2, 128, page=16, seed=45, spare=1), Case([0, 1, 1, 1], [9, 701, 333, 1], 8, 2, 128, page=16, seed=46, spare=1),
+             Case([0, 0, 0, 0], [1, 2, 3, 4], 8, 2, 128, page=16, seed=47, spare=4)]
+    pages, per = max(c.k.shape[0] for c in steps), max(c.table.shape[1] for c in steps)
+    k, v = (torch.empty(pages, 2, 16, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    table, lens, start = torch.full((4, per), -1, dtype=torch.int32, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV), torch.zeros(5, dtype=torch.int32, device=DEV)
+    q, out, status = torch.zeros(4, 8, 128, dtype=torch.bfloat16, device=DEV), torch.empty(4, 8, 128, dtype=torch.bfloat16, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    kv, ws = E.KVStore(k, v, block_table=table), torch.empty(E.eagle_chunk_attn_workspace(4, 4, 8, 2, 128), dtype=torch.uint8, device=DEV)
+    E.eagle_chunk_attn(q, kv, lens, start, out, workspace=ws, status=status)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        E.eagle_chunk_attn(q, kv, lens, start, out, workspace=ws, status=status)
+    for c in steps + steps[:1]:
+        out.fill_(7.0)
+        q.copy_(c.q)
+        k[:c.k.shape[0]].copy_(c.k)
+        v[:c.v.shape[0]].copy_(c.v)
+        table.fill_(-1)
+        table[:, :c.table.shape[1]].copy_(c.table)
+        lens.copy_(_ints(c.lens))
+        start.copy_(c.start)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0
+        _check(out.cpu(), *c.want())

@@ -188,3 +188,30 @@ def test_replayed_from_a_graph(E):
     graph.replay()
     torch.cuda.synchronize()
     check(out.cpu(), z2, kw2)
+
+
+def test_the_largest_vocabulary(E):
+    """Rows whose elements pass 2^31, in place: every untouched logit keeps its bits, the others are what the formula says."""
+    V, B = (1 << 30) - 1, 3
+    z = torch.empty(B, 1, V, device=DEV)
+    for b in range(B):
+        z[b, 0] = torch.arange(b, b + V, dtype=torch.int32, device=DEV).remainder_(8191).sub_(4000)
+    at = _ints([[0, V - 1, V - 2047], [V - 1, 5, V // 2], [V - 1, V - 2, 2048]]).to(DEV)
+    allowed = torch.full((B, 1, (V + 31) // 32), -1, dtype=torch.int32, device=DEV)
+    allowed[2, 0, -1] = ~(1 << 3)                         # token V - 28
+    rho, phi, pi = (torch.tensor(x, device=DEV) for x in ([1.5, 2.0, 0.5], [0.25, 0.5, 1.0], [0.125, 0.0, 2.0]))
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    want = z.clone()
+    for b in range(B):
+        for t in at[b].tolist():
+            x = float(z[b, 0, t])
+            want[b, 0, t] = (x / float(rho[b]) if x > 0 else x * float(rho[b])) - float(phi[b]) - float(pi[b])
+    want[2, 0, (V // 32) * 32 + 3] = -float("inf")
+    E.eagle_tree_logits_adjust(z, out=z, history=at, history_len=_ints([3, 3, 3]).to(DEV), repetition=rho, frequency=phi, presence=pi, allowed=allowed,
+                               status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    wrong = (z != want).nonzero()
+    assert all(abs(float(z[i, j, k]) - float(want[i, j, k])) <= 1e-6 * 16500 for i, j, k in wrong[:16].tolist()) and len(wrong) <= 9
+    del z, want, allowed
+    torch.cuda.empty_cache()
