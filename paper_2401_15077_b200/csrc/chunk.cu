@@ -257,10 +257,9 @@ constexpr int kKSlots = 5, kVSlots = 4;  // rings of half tiles; step g's tiles 
 constexpr uint32_t kTmemCols = 512;      // S0 S1 S2 | O; P (packed bf16, 64 columns) overwrites the front of its S
 constexpr uint32_t kColO = 384;
 constexpr float kRescaleThreshold = 8.0f;   // log2 units: the accumulator is rescaled when the row maximum outgrows its reference by more
-#ifndef EAGLE_CHUNK_POLY
-#define EAGLE_CHUNK_POLY 3
-#endif
-constexpr int kPolyStride = EAGLE_CHUNK_POLY;   // one pair of exponentials in so many is a polynomial on the FMA pipe (0: none)
+// One pair of exponentials in so many is a polynomial on the FMA pipe, beside the special-function unit (a prompt of 4096 tokens x 32
+// heads: 172 us with none, 160 us with one in 3).
+constexpr int kPolyStride = 3;
 
 template <int D>
 struct Smem {
@@ -624,13 +623,15 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
             wait_ld();
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              mx[0] = max3(mx[0], __uint_as_float(rc[e]), __uint_as_float(rc[e + 1]));
-              mx[1] = max3(mx[1], __uint_as_float(rd[e]), __uint_as_float(rd[e + 1]));
-              mx[2] = max3(mx[2], __uint_as_float(ra[e]), __uint_as_float(ra[e + 1]));
-              mx[3] = max3(mx[3], __uint_as_float(rb[e]), __uint_as_float(rb[e + 1]));
+              mx[0] = max3_nan(mx[0], __uint_as_float(rc[e]), __uint_as_float(rc[e + 1]));
+              mx[1] = max3_nan(mx[1], __uint_as_float(rd[e]), __uint_as_float(rd[e + 1]));
+              mx[2] = max3_nan(mx[2], __uint_as_float(ra[e]), __uint_as_float(ra[e + 1]));
+              mx[3] = max3_nan(mx[3], __uint_as_float(rb[e]), __uint_as_float(rb[e + 1]));
             }
           }
-          const float tmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale_log2;   // scale > 0
+          const float tmax = max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], -INFINITY) * scale_log2;   // scale > 0
+          // a visible score that is NaN or +inf makes the row NaN (through its sum: not every exponential below passes one on)
+          if (!(tmax < INFINITY)) l_sum = __uint_as_float(0x7fffffffu);
 
           // the reference the other group settled on at the previous step (waited for at an item's first step too, where its value
           // is not used: the other group must have read the tag of step gs - 2 before it is replaced)
@@ -681,7 +682,7 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
             for (int e = 0; e < 16; ++e) {
               const uint64_t x2 = fma2(pack2(__uint_as_float(raw[2 * e]), __uint_as_float(raw[2 * e + 1])), scale2, base2);
               float p0, p1;
-              if (kPolyStride > 0 && e % (kPolyStride > 0 ? kPolyStride : 1) == (kPolyStride > 0 ? kPolyStride : 1) - 1) {
+              if (e % kPolyStride == kPolyStride - 1) {
                 poly_exp2_pair(x2, p0, p1);
               } else {
                 float a, b;

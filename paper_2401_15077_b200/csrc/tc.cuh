@@ -283,9 +283,15 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+// The same, but NaN when one of them is.
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 // 2^x of a pair on the FMA and integer pipes (x <= ~8): x = n + f with n whole and f in [-1/2, 1/2] (adding and taking off
 // 1.5 * 2^23 rounds to a whole number), a cubic for 2^f fitted over that interval (relative error 1e-4, well below the bf16
-// rounding of what it is used for), n added to the exponent field.
+// rounding of what it is used for), n added to the exponent field.  A NaN comes out as 2^-126: the caller looks for those.
 __device__ __forceinline__ void poly_exp2_pair(uint64_t x2, float& p0, float& p1) {
   float a, b;
   unpack2(x2, a, b);

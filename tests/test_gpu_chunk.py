@@ -470,3 +470,32 @@ def test_single_tokens_replayed_from_a_graph_with_other_lengths(E):
         torch.cuda.synchronize()
         assert int(status.item()) == 0
         _check(out.cpu(), *c.want())
+
+
+@pytest.mark.parametrize("single", [False, True])
+@pytest.mark.parametrize("what", ["nan", "inf"])
+def test_a_visible_nan_or_infinite_score_makes_its_row_nan_wherever_it_is(E, what, single):
+    """At every place of a tile's first 32 columns and some later ones: rows that see the key, and only those (a key with one infinite
+    component scores +inf or -inf by the query's sign; -inf is a weight of 0)."""
+    for at in list(range(33)) + [63, 64, 97, 127, 130]:
+        c = Case([1, 1] if single else [3, 1, 40], [131, 50] if single else [131, 50, 100], 4, 2, 128, seed=51, spare=0 if single else 3)
+        c.k[0, :, at] = float("nan") if what == "nan" else 0.0
+        if what == "inf":
+            c.k[0, :, at, 5] = float("inf")
+        out, status = c.run(E)
+        assert status == 0
+        got = out.double().numpy()
+        hit = np.zeros(got.shape[:2], bool)
+        n0 = c.n[0]
+        hit[:n0] = True if what == "nan" else (c.q[:n0, :, 5].double().numpy() > 0)
+        if what == "inf":
+            c.k[0, :, at] = 0.0                        # score 0 in place of -inf: one weight more, so those rows are only looked at for NaN
+        want, spread = c.want() if what == "inf" else (None, None)
+        assert np.isnan(got[hit]).all()
+        rest = ~hit
+        rest[sum(c.n):] = False
+        assert np.isfinite(got[rest]).all()
+        if what == "inf":
+            err, tol = np.abs(got - want), 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 5e-4) * spread
+            rest[:n0] = False
+            assert (err <= tol)[rest].all()
