@@ -12,7 +12,7 @@
 //
 // What bounds it is the way of one score buffer around the loop (score MMA, softmax, PV MMA, and a wait between each two): about 4700
 // cycles, with three buffers on it 1550 per 128 keys, of which the tensor cores need 1036.  A prompt of 4096 tokens, 32 heads, D = 128
-// (137 GFLOP, causal): 160 us, 860 TFLOP/s; two chunks of 2048 tokens behind 16384 (1.17 TFLOP in 0.97 to 1.10 ms, by the clock that
+// (137 GFLOP, causal): 154 us, 890 TFLOP/s; two chunks of 2048 tokens behind 16384 (1.17 TFLOP in 0.97 to 1.10 ms, by the clock that
 // the power limit leaves): 1.06 to 1.2 PFLOP/s of the 1.65 (1.40 sustained) that a large matrix product reaches.
 #include "chunk.cuh"
 #include "tc.cuh"
@@ -258,8 +258,8 @@ constexpr uint32_t kTmemCols = 512;      // S0 S1 S2 | O; P (packed bf16, 64 col
 constexpr uint32_t kColO = 384;
 constexpr float kRescaleThreshold = 8.0f;   // log2 units: the accumulator is rescaled when the row maximum outgrows its reference by more
 // One pair of exponentials in so many is a polynomial on the FMA pipe, beside the special-function unit (a prompt of 4096 tokens x 32
-// heads: 172 us with none, 160 us with one in 3).
-constexpr int kPolyStride = 3;
+// heads: 172 us with none, 158 us with one in 3, 154 us with one in 2).
+constexpr int kPolyStride = 2;
 
 template <int D>
 struct Smem {
