@@ -569,7 +569,7 @@ typedef struct eagle_chunk_desc {
   int32_t* status;              /* device int32 or NULL */
 } eagle_chunk_desc;
 
-/* Bytes of scratch one call with this descriptor needs (host function, no CUDA work); 0 if the shape is unsupported. */
+/* Bytes of scratch one call with this descriptor, or with fewer tokens, needs (host function, no CUDA work); 0 if the shape is unsupported. */
 size_t eagle_chunk_attn_workspace(const eagle_chunk_desc* desc);
 
 /*

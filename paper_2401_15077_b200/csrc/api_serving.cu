@@ -171,7 +171,13 @@ size_t eagle_chunk_attn_workspace(const eagle_chunk_desc* desc) {
   ChunkWork w;
   int workers = 0;
   if (!desc || !carve_chunk_work(*desc, nullptr, kMaxPlanCtas, &w, &workers)) return 0;
-  return w.bytes;
+  size_t bytes = w.bytes;
+  if (!chunk_takes_rows(*desc)) {          // enough for fewer tokens too, single ones among them
+    eagle_chunk_desc d = *desc;
+    d.num_tokens = d.batch;
+    if (carve_chunk_work(d, nullptr, kMaxPlanCtas, &w, &workers) && w.bytes > bytes) bytes = w.bytes;
+  }
+  return bytes;
 }
 
 int eagle_chunk_attn(const eagle_chunk_desc* desc, const void* q, const eagle_kv_store* kv, const int32_t* seq_lens,

@@ -222,3 +222,15 @@ def test_binding_refuses_host_tensors(E):
             E.KVStore(k, k.clone(), **bad)
     with pytest.raises(E.EagleError):
         E.KVStore(k, k[:, :, :8])
+
+
+def test_chunk_workspace_covers_calls_with_fewer_tokens(E):
+    """A workspace sized for a call's most tokens serves every smaller one: the size never falls as tokens are added."""
+    for batch in (1, 7, 300, 65535):
+        for hq, hkv, d in ((32, 8, 128), (16, 1, 64), (40, 40, 64), (128, 8, 128)):
+            counts = sorted({0, 1, batch // 2, batch - 1, batch, batch + 1, 2 * batch, 10 * batch, 100000})
+            sizes = [E.eagle_chunk_attn_workspace(batch, n, hq, hkv, d) for n in counts]
+            # (calls with no more tokens than sequences run another kernel with other needs)
+            few = [s for n, s in zip(counts, sizes) if n <= batch]
+            assert few == sorted(few) and all(s >= few[-1] for n, s in zip(counts, sizes) if n > batch)
+            assert sizes == sorted(sizes)
