@@ -258,7 +258,8 @@ constexpr uint32_t kTmemCols = 512;      // S0 S1 S2 | O; P (packed bf16, 64 col
 constexpr uint32_t kColO = 384;
 constexpr float kRescaleThreshold = 8.0f;   // log2 units: the accumulator is rescaled when the row maximum outgrows its reference by more
 // One pair of exponentials in so many is a polynomial on the FMA pipe, beside the special-function unit (a prompt of 4096 tokens x 32
-// heads: 172 us with none, 160 us with one in 3 or two in 3, 154 us with one in 2, 206 us with all).
+// heads: 172 us with none, 160 us with one in 3 or two in 3, 154 us with one in 2, 206 us with all; where the power limit sets the clock,
+// one in 2 and one in 3 are within 0.5 %).
 constexpr int kPolyStride = 2;
 
 template <int D>
