@@ -775,7 +775,10 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
   // ---- teardown: everyone arrives here, normally or after an abort; neither CTA leaves while the other may still reach into it
   fence_before();
   __syncthreads();
-  if (tid == 0 && *s_abort) report_status(p.status, EAGLE_ERR_TIMEOUT);
+  if (*s_abort) {
+    if (tid == 0) report_status(p.status, EAGLE_ERR_TIMEOUT);
+    let_work_land();
+  }
   cluster_sync();
   if (warp == kWarpQK) {
     __syncwarp();

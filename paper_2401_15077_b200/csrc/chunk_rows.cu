@@ -318,7 +318,10 @@ chunk_rows_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     }
   }
   __syncthreads();
-  if (tid == 0 && *s_abort) report_status(p.status, EAGLE_ERR_TIMEOUT);
+  if (*s_abort) {
+    if (tid == 0) report_status(p.status, EAGLE_ERR_TIMEOUT);
+    let_work_land();
+  }
 }
 
 template <int D>

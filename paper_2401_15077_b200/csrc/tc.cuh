@@ -74,7 +74,13 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   if (mbar_try_wait(bar, parity)) return true;     // (a suspended wait: polling would take issue slots from the warps that work)
   return mbar_wait_slow(bar, parity, abort_flag);
 }
-// The same with a verdict that is uniform over the warp (the callers go on to warp-collective instructions).
+// After an abort: copies and MMAs that the CTA has issued may still be at work on its shared and tensor memory.  They take
+// microseconds; this waits a hundred before it may leave.
+static __device__ __noinline__ void let_work_land() {
+  const unsigned long long t0 = global_timer();
+  while (global_timer() - t0 < 100000ull) __nanosleep(1000);
+}
+// mbar_wait with a verdict that is uniform over the warp (the callers go on to warp-collective instructions).
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
 }
