@@ -140,6 +140,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
     if (b < B) {
       seqs[b] = q;
       if (seqs != w.seq) w.seq[b] = q;
+      w.bad_page[b] = 0;
       base_of[b] = carry.a + inc.a - v.a;
       cost_of[b] = carry.b + inc.b - v.b;
     }
@@ -391,12 +392,15 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
       int i, tile, end;
       int y, page;                         // this lane's next box: row in its page (or in the sequence), page (or sequence)
       bool valid, fresh;
+      bool wrong;                          // some entry of the item was outside the pool
     };
     const int k_rows = PAGED ? min(p.page_size, 64) : 64, v_rows = PAGED ? min(p.page_size, kChunkTile) : kChunkTile;
     const int k_r0 = (lane / S::kSlabs) * k_rows, v_r0 = lane * v_rows, half = static_cast<int>(rank);
     auto advance = [&](Cursor& c, bool is_v) {        // to the next K/V tile of the work list
       c.fresh = false;
       if (++c.tile >= c.end) {
+        if (PAGED && c.wrong) p.work.bad_page[c.it.b] = 1;
+        c.wrong = false;
         for (++c.i; c.i < n_items; ++c.i) {
           c.it = item(c.i);
           if (c.it.t1 > c.it.t0) break;
@@ -419,8 +423,12 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
         c.y = key & (p.page_size - 1);
       }
     };
-    // an entry outside the pool reads page 0 (the merge kernel reports it and zeroes the sequence)
-    auto place = [&](const Cursor& c) { return (PAGED && (c.page < 0 || c.page >= p.num_pages) ? 0 : c.page) * p.Hkv + c.it.g; };
+    // an entry outside the pool reads page 0, and marks its sequence when the item ends (the merge kernel reports it and zeroes the rows)
+    auto place = [&](Cursor& c) {
+      const bool wrong = PAGED && static_cast<uint32_t>(c.page) >= static_cast<uint32_t>(p.num_pages);
+      c.wrong |= wrong;
+      return (wrong ? 0 : c.page) * p.Hkv + c.it.g;
+    };
     const uint32_t to_first = map_to_rank(sbase, 0) - sbase;       // added to a barrier's address: the first CTA's
     bool ok = true;
     Ring<kKSlots> kr;
@@ -430,6 +438,7 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     ck.i = cv.i = -1;
     ck.tile = ck.end = cv.tile = cv.end = 0;
     ck.valid = cv.valid = true;
+    ck.wrong = cv.wrong = false;
     advance(ck, false);
     advance(cv, true);
     auto next_key = [&]() {
@@ -791,7 +800,9 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
 // Cut query tiles: m* = max m_i, l* = sum l_i 2^(m_i - m*), out = sum o_i 2^(m_i - m*) / l*.  A block takes 8 rows of one query
 // tile of one record (a warp: 8 rows x 4 groups of 4 columns, so that its loads are runs of 128 bytes); the slots of the
 // pieces are looked up together, and four pieces' loads are in flight at a time.  The blocks behind them look at one sequence
-// each: rows of a sequence that does not fit its cache, or whose block table names a page outside the pool, become zeros.
+// each: rows of a sequence that does not fit its cache, or whose block table names a page outside the pool, become zeros.  Nothing
+// orders the two kinds of blocks, so those of a cut unit leave the rows of such a sequence alone; every page in use has been copied
+// from by some worker, so the attention kernel has looked at all of them.
 constexpr int kMergeThreads = 256;
 
 template <int D>
@@ -804,19 +815,9 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams 
     const ChunkSeq q = w.seq[b];
     const int s = p.token_start[b], e = p.token_start[b + 1];
     if (s < 0 || e <= s || e > p.N) return;
-    bool bad = q.n == 0;                                 // the planner refused it (and reported it)
-    if (p.block_table && q.n > 0) {
-      int wrong = 0;
-      const int pages = ((q.L + q.n - 1) >> p.page_shift) + 1;
-      for (int i = tid; i < pages; i += kMergeThreads) {
-        const int pg = p.block_table[static_cast<size_t>(b) * p.max_pages + i];
-        if (pg < 0 || pg >= p.num_pages) wrong = 1;
-      }
-      wrong = __syncthreads_or(wrong);
-      if (wrong && tid == 0) report_status(p.status, EAGLE_ERR_PAGE);
-      bad = bad || wrong;
-    }
-    if (!bad) return;
+    const bool wrong = w.bad_page[b] != 0;
+    if (wrong && tid == 0) report_status(p.status, EAGLE_ERR_PAGE);
+    if (q.n > 0 && !wrong) return;                       // (n = 0: the planner refused it, and reported it)
     uint4* out = reinterpret_cast<uint4*>(p.out + static_cast<size_t>(s) * p.Hq * D);
     const size_t vecs = static_cast<size_t>(e - s) * p.Hq * (D / 8);
     for (size_t i = tid; i < vecs; i += kMergeThreads) out[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -831,6 +832,7 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams 
   const ChunkSeq q = w.seq[un.b];
   const int first = un.part * p.ut + half * p.tpt;
   if (first + rb * 8 / p.G >= q.n || rb * 8 / p.G >= p.tpt) return;      // no row of this block belongs to the sequence
+  if (w.bad_page[un.b]) return;
   if (tid < 32) {
     int count = 0;
     for (int i = cut.c_lo; i <= cut.c_hi; i += 32) {

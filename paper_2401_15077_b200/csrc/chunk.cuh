@@ -47,6 +47,7 @@ struct ChunkWork {
   ChunkItem* items;        // [units + workers]
   int4* cta;               // [workers]: whole units (first, count), pieces (first, count)
   ChunkCut* cut;           // [workers]
+  int32_t* bad_page;       // [B]: cleared by the planner, set by whoever copies from a page that is not in the pool
   float2* part_ml;         // [slots, rows of a query tile]
   float* part_o;           // [slots, D / 4, rows, 4]
   size_t bytes;
@@ -97,6 +98,7 @@ inline bool carve_chunk_work(const eagle_chunk_desc& d, void* base, int sms, Chu
   w->items = reinterpret_cast<ChunkItem*>(take(sizeof(ChunkItem) * (units + workers)));
   w->cta = reinterpret_cast<int4*>(take(sizeof(int4) * workers));
   w->cut = reinterpret_cast<ChunkCut*>(take(sizeof(ChunkCut) * workers));
+  w->bad_page = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * B));
   w->part_ml = reinterpret_cast<float2*>(take(sizeof(float2) * slots * rows));
   w->part_o = reinterpret_cast<float*>(take(sizeof(float) * slots * rows * d.head_dim));
   w->bytes = off;

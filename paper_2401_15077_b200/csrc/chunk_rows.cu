@@ -106,16 +106,19 @@ chunk_rows_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     // =========================================================================== copies
     // A lane per box (a page's rows x 64 columns, of K or of V); the page of a lane's next box is looked up while the box before it
     // is on its way.  A box past the sequence's last page fetches that page again (its rows are masked), so that a tile's byte count
-    // never changes; an entry outside the pool reads page 0 (the merge kernel reports it and zeroes the sequence).
+    // never changes; an entry outside the pool reads page 0, and marks its sequence when the item ends (the merge kernel reports it and
+    // zeroes the rows).
     const int box_rows = PAGED ? min(p.page_size, kRowKeys) : kRowKeys, per = S::kSlabs * (kRowKeys / box_rows);
     const bool is_v = lane >= per, active = lane < 2 * per;
     const int r0 = ((lane - (is_v ? per : 0)) / S::kSlabs) * box_rows, sl = lane % S::kSlabs;      // (per is a multiple of kSlabs)
     const uint32_t dst = sbase + (is_v ? S::kTile : 0) + sl * S::kSlab + r0 * 128;
     Item it = {};
     int i = -1, step = 0, y = 0, z = 0;
-    bool more = true;
+    bool more = true, wrong = false;                       // wrong: some entry of the item was outside the pool
     auto advance = [&]() {
       if (++step >= it.steps) {
+        if (PAGED && wrong) p.work.bad_page[it.b] = 1;
+        wrong = false;
         for (++i; i < n_items; ++i) {
           it = item(i);
           if (it.steps > 0) break;
@@ -140,7 +143,9 @@ chunk_rows_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
       if (!mbar_wait_warp(empty(ring.slot), ring.par ^ 1u, s_abort)) break;
       if (lane == 0) mbar_expect_tx(full(ring.slot), S::kStage);
       __syncwarp();
-      const int page = PAGED && (z < 0 || z >= p.num_pages) ? 0 : z;
+      const bool out_of_pool = PAGED && active && static_cast<uint32_t>(z) >= static_cast<uint32_t>(p.num_pages);
+      const int page = out_of_pool ? 0 : z;
+      wrong |= out_of_pool;
       if (active) tma_load_3d(dst + ring.slot * S::kStage, is_v ? &map_v : &map_k, sl * 64, y, page * p.Hkv + it.g, full(ring.slot));
       ring.step();
       advance();

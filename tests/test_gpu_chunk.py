@@ -499,3 +499,24 @@ def test_a_visible_nan_or_infinite_score_makes_its_row_nan_wherever_it_is(E, wha
             err, tol = np.abs(got - want), 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 5e-4) * spread
             rest[:n0] = False
             assert (err <= tol)[rest].all()
+
+
+# ---------------------------------------------------------------------------------- cut units of bad sequences, extreme values
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+@pytest.mark.parametrize("single", [False, True])
+def test_a_page_outside_the_pool_in_a_sequence_whose_units_are_cut(E, single, where):
+    """Its rows are zeros although pieces of them come to be merged, and the other sequences' are what they are without it."""
+    c = Case(*(([1, 1], [30011, 500], 6, 3) if single else ([140, 1, 9], [30000, 40, 300], 4, 2)), 128, page=16, seed=61, spare=0 if single else 3)
+    want, spread = c.want()
+    used = -(-(c.n[0] + c.lens[0]) // 16)
+    c.table[0, {"first": 0, "middle": used // 2, "last": used - 1}[where]] = c.k.shape[0]
+    want[:c.n[0]], spread[:c.n[0]] = 0, 0
+    q, kv, lens, start = c.q.to(DEV), E.KVStore(c.k.to(DEV), c.v.to(DEV), block_table=c.table.to(DEV)), _ints(c.lens).to(DEV), c.start.to(DEV)
+    outs, status = [torch.full(c.q.shape, 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(20)], torch.zeros(1, dtype=torch.int32, device=DEV)
+    for out in outs:
+        E.eagle_chunk_attn(q, kv, lens, start, out, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == -11
+    for out in outs:
+        assert (out[:c.n[0]] == 0).all()
+        _check(out.cpu(), want, spread)
