@@ -486,10 +486,12 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     // CTA's issuer hears of the tile.
     bool ok = true;
     Ring<kVSlots> vr;
+    uint32_t steps = 0, items = 0;
     const uint32_t to_first = map_to_rank(sbase, 0) - sbase;
     for (int i = 0; i < n_items && ok; ++i) {
       const Item it = item(i);
-      for (int t = it.t0; t < it.t1; ++t, vr.step()) {
+      items += it.t1 > it.t0 ? 1u : 0u;
+      for (int t = it.t0; t < it.t1; ++t, ++steps, vr.step()) {
         ok = mbar_wait_warp(B.v_full(vr.slot), vr.par, s_abort);
         if (!ok) break;
         const int valid = it.L + it.n - t * kChunkTile;            // keys of the tile that belong to the sequence
@@ -504,6 +506,16 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
         }
       }
     }
+    // The MMAs report to the barriers of both CTAs, also where nobody waits for it: all reports of the last uses have to be in before
+    // the CTA may leave its shared memory to another.
+#pragma unroll 1
+    for (uint32_t g = steps > kKSlots ? steps - kKSlots : 0u; g < steps && ok; ++g) {
+      ok = mbar_wait_warp(B.k_empty(g % kKSlots), (g / kKSlots) & 1u, s_abort);
+      if (ok && g + kVSlots >= steps) ok = mbar_wait_warp(B.v_empty(g % kVSlots), (g / kVSlots) & 1u, s_abort);
+      if (ok && g + kSBufs >= steps) ok = mbar_wait_warp(B.o_done(g % kSBufs), (g / kSBufs) & 1u, s_abort);
+    }
+#pragma unroll 1
+    for (uint32_t i = items > 2 ? items - 2 : 0u; i < items && ok; ++i) ok = mbar_wait_warp(B.q_empty(i & 1u), (i >> 1) & 1u, s_abort);
   } else if (warp == kWarpQK) {
     // =========================================================================== S = Q K^T, up to three steps ahead of the softmax
     if (lane == 0 && rank == 0) {
