@@ -583,7 +583,8 @@ size_t eagle_chunk_attn_workspace(const eagle_chunk_desc* desc);
  *                                     for token t = token_start[b] + i of sequence b
  *
  * A cache of fp8 codes is EAGLE_ERR_SHAPE.  bf16 inputs, fp32 scores / softmax / accumulation, probabilities rounded to bf16
- * for the tensor cores, bf16 output.  Slots past the chunk may hold anything.  The values of slots in use have to be finite:
+ * for the tensor cores, bf16 output.  |scale * q.k| has to stay below 2^29 (beyond, a step of fp32 is wider than what an exponential spans:
+ * a row may come out NaN).  Slots past the chunk may hold anything.  The values of slots in use have to be finite:
  * one that is not may reach rows of the same sequence that do not see it (its probability there is 0, and 0 * inf is NaN).
  * Rows outside every sequence are left as they were.  A sequence with L_b < 0 or L_b + n_b over its slots reports EAGLE_ERR_SEQ,
  * one with a block-table entry in use outside [0, num_pages) EAGLE_ERR_PAGE: its rows are zeros.  Starts that descend or

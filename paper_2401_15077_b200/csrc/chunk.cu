@@ -272,8 +272,8 @@ struct Smem {
   static constexpr int kQ = 0;                               // two query tiles: the current item's and the next one's
   static constexpr int kK = 2 * kQBytes;
   static constexpr int kV = kK + kKSlots * kKBytes;
-  static constexpr int kTag = kV + kVSlots * kVBytes;        // uint32 [128 rows]: reference maximum | step number
-  static constexpr int kLfin = kTag + 128 * 4;               // float [2][128 rows]: row sums on their way to the output, by items in turn
+  static constexpr int kTag = kV + kVSlots * kVBytes;        // uint64 [128 rows]: step number | reference maximum
+  static constexpr int kLfin = kTag + 128 * 8;               // float [2][128 rows]: row sums on their way to the output, by items in turn
   static constexpr int kBar = kLfin + 2 * 128 * 4;
   static constexpr int kNumBars = 2 * (kKSlots + 2) + 3 * kVSlots + 3 * kSBufs + 1;
   static constexpr int kMisc = kBar + 8 * kNumBars;          // tensor-memory base, abort flag, wait limit (8 bytes)
@@ -299,26 +299,30 @@ struct Bars {
   __device__ __forceinline__ uint32_t o_free() const { return at(kSAt + 3 * kSBufs); }                   // an item's accumulators have been read (first CTA only)
 };
 
-// Bounded wait for a tagged word in shared memory (low byte == want): the word, with bit 32 set; 0 when the CTA was aborted or
-// the time limit passed.
-__device__ __noinline__ unsigned long long tag_wait_slow(volatile uint32_t* slot, uint32_t want, volatile int* abort_flag) {
+// A float with a number, written and read in one piece.
+__device__ __forceinline__ unsigned long long tagged(uint32_t number, float x) { return static_cast<unsigned long long>(number) << 32 | __float_as_uint(x); }
+__device__ __forceinline__ float value_of(unsigned long long t) { return __uint_as_float(static_cast<uint32_t>(t)); }
+__device__ __forceinline__ bool has_tag(unsigned long long t, uint32_t want) { return static_cast<uint32_t>(t >> 32) == want; }
+// Bounded wait for the word with number `want` in shared memory; one with another number when the CTA was aborted or the time
+// limit passed.
+__device__ __noinline__ unsigned long long tag_wait_slow(volatile unsigned long long* slot, uint32_t want, volatile int* abort_flag) {
   const unsigned long long t0 = global_timer(), limit = *reinterpret_cast<volatile unsigned long long*>(abort_flag + 1);
   for (uint32_t spins = 1;; ++spins) {
-    const uint32_t t = *slot;
-    if ((t & 0xffu) == want) return (1ull << 32) | t;
+    const unsigned long long t = *slot;
+    if (has_tag(t, want)) return t;
     if ((spins & 63u) == 0) {
-      if (*abort_flag) return 0ull;
+      if (*abort_flag) return tagged(~want, 0.f);
       if (global_timer() - t0 > limit) {
         *abort_flag = 1;
-        return 0ull;
+        return tagged(~want, 0.f);
       }
     }
     __nanosleep(20);
   }
 }
-__device__ __forceinline__ unsigned long long tag_wait(volatile uint32_t* slot, uint32_t want, volatile int* abort_flag) {
-  const uint32_t t = *slot;
-  if ((t & 0xffu) == want) return (1ull << 32) | t;
+__device__ __forceinline__ unsigned long long tag_wait(volatile unsigned long long* slot, uint32_t want, volatile int* abort_flag) {
+  const unsigned long long t = *slot;
+  if (has_tag(t, want)) return t;
   return tag_wait_slow(slot, want, abort_flag);
 }
 
@@ -357,7 +361,7 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     *reinterpret_cast<volatile unsigned long long*>(smem + S::kMisc + 8) = p.wait_limit_ns;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (tid < 128) reinterpret_cast<volatile uint32_t*>(smem + S::kTag)[tid] = 0xffffffffu;   // no step carries this tag yet
+  if (tid < 128) reinterpret_cast<volatile unsigned long long*>(smem + S::kTag)[tid] = ~0ull;   // no step has this number
   if (warp == kWarpQK) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sbase + S::kMisc), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -577,13 +581,14 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     // Two groups of four warps take alternate steps, so that one computes while the other waits.  Thread r of a group owns query
     // row r (tensor-memory lane r), all 128 score columns.  The two threads of a row share one reference maximum: the one
     // that handled step g publishes it, tagged with g, before it takes its exponentials, and the other picks it up at step g + 1;
-    // each keeps its own part of the row sum.  fp32 throughout, in the log2 domain; the probabilities are rounded to bf16 for
+    // each keeps its own part of the row sum.  The reference is a whole fp32 number: what is left between it and the product that it
+    // stands for is within half a step for all of a row's exponentials alike, so it cancels, however large the scores are.  fp32 throughout, in the log2 domain; the probabilities are rounded to bf16 for
     // the tensor cores (relative 2^-8 each, half of the inputs' own spacing), the sum that divides them is kept from the
     // unrounded ones.  A warp without a row that belongs to the sequence only passes its turns on.
     const uint32_t grp = static_cast<uint32_t>(warp >> 2);
     const int r = tid & 127;
     const uint32_t lane_addr = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    volatile uint32_t* tag = reinterpret_cast<volatile uint32_t*>(smem + S::kTag) + r;
+    volatile unsigned long long* tag = reinterpret_cast<volatile unsigned long long*>(smem + S::kTag) + r;
     volatile float* lfin = reinterpret_cast<volatile float*>(smem + S::kLfin) + r;
     const uint32_t o_addr = tmem + lane_addr + kColO;
     const uint32_t p_to = map_to_rank(B.p_full(0), 0), o_free_to = map_to_rank(B.o_free(), 0);
@@ -659,10 +664,10 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
           // is not used: the other group must have read the tag of step gs - 2 before it is replaced)
           float m_prev = -INFINITY;
           if (gs > 0) {
-            const unsigned long long t = tag_wait(tag, (gs - 1u) & 0xffu, s_abort);
-            ok = __all_sync(0xffffffffu, (t >> 32) != 0ull);
+            const unsigned long long t = tag_wait(tag, gs - 1u, s_abort);
+            ok = __all_sync(0xffffffffu, has_tag(t, gs - 1u));
             if (!ok) break;
-            if (s > 0) m_prev = __uint_as_float(static_cast<uint32_t>(t) & 0xffffff00u);
+            if (s > 0) m_prev = value_of(t);
           }
           if (m_prev != m_ref) {
             l_sum *= fast_exp2(m_ref - m_prev);     // m_ref = -inf: nothing summed yet, the factor is 0
@@ -672,12 +677,11 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
           const bool grow = tmax > m_ref + kRescaleThreshold || (m_ref == -INFINITY && tmax > -INFINITY);
           float factor = 1.f;
           if (grow) {
-            const float m_new = __uint_as_float(__float_as_uint(tmax) & 0xffffff00u);   // the low byte carries the step's tag
-            factor = fast_exp2(m_ref - m_new);     // 0 when there was no reference yet
-            m_ref = m_new;
+            factor = fast_exp2(m_ref - tmax);      // 0 when there was no reference yet
+            m_ref = tmax;
             l_sum *= factor;
           }
-          *tag = __float_as_uint(m_ref) | (gs & 0xffu);
+          *tag = tagged(gs, m_ref);
           if (s > 0 && __any_sync(0xffffffffu, grow)) {
             // the previous step accumulated into O and may still be running
             ok = mbar_wait_warp(B.o_done((gs - 1) % kSBufs), ((gs - 1) / kSBufs) & 1u, s_abort);
@@ -740,10 +744,10 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
         } else {
           // (the chain of tags goes on: the next item's rows may be in use)
           if (gs > 0) {
-            ok = __all_sync(0xffffffffu, (tag_wait(tag, (gs - 1u) & 0xffu, s_abort) >> 32) != 0ull);
+            ok = __all_sync(0xffffffffu, has_tag(tag_wait(tag, gs - 1u, s_abort), gs - 1u));
             if (!ok) break;
           }
-          *tag = 0xff800000u | (gs & 0xffu);
+          *tag = tagged(gs, -INFINITY);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive_pair(p_to + 8u * sb);

@@ -552,3 +552,22 @@ def test_short_calls_one_right_behind_another(E):
             differ += sum((x.view(torch.int16) != w.view(torch.int16)).sum() for x in o)
     torch.cuda.synchronize()
     assert int(status.item()) == 0 and int(differ.item()) == 0
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("single", [False, True])
+def test_scores_of_large_magnitude(E, single, sign):
+    """Every score is a multiple of 2048 between 2^22 and 2^24 (or its negative) plus a whole number of at most 5, all of them exact
+    in fp32, so the weights are exact as well up to the errors of any other row: what the large part adds to all of a row cancels."""
+    g = torch.Generator().manual_seed(62)
+    c = Case(*(([1, 1], [900, 301]) if single else ([40, 3, 1], [200, 700, 2000])), 16, 1, 128, seed=62, spare=0 if single else 3)
+    for t in (c.q, c.k):
+        t[:] = torch.where(t.isnan(), t, 0)
+    i = torch.arange(c.q.shape[0] * 16).view(-1, 16)
+    c.q[..., 0], c.q[..., 1] = 2048.0 * (1 + (i % 128) / 128) * (1 + i // 128 % 2), 1.0
+    for b, m in enumerate([x + y for x, y in zip(c.n, c.lens)]):
+        c.k[b, :, :m, 0] = 2048.0 * sign
+        c.k[b, :, :m, 1] = torch.randint(-5, 6, (m,), generator=g).bfloat16()
+    out, status = c.run(E, sm_scale=1.0)
+    assert status == 0
+    _check(out, *c.want(sm_scale=1.0))
