@@ -273,8 +273,8 @@ struct Smem {
   static constexpr int kK = 2 * kQBytes;
   static constexpr int kV = kK + kKSlots * kKBytes;
   static constexpr int kTag = kV + kVSlots * kVBytes;        // uint64 [128 rows]: step number | reference maximum
-  static constexpr int kLfin = kTag + 128 * 8;               // float [2][128 rows]: row sums on their way to the output, by items in turn
-  static constexpr int kBar = kLfin + 2 * 128 * 4;
+  static constexpr int kLfin = kTag + 128 * 8;               // uint64 [2][128 rows]: item number | row sum on its way to the output, by items in turn
+  static constexpr int kBar = kLfin + 2 * 128 * 8;
   static constexpr int kNumBars = 2 * (kKSlots + 2) + 3 * kVSlots + 3 * kSBufs + 1;
   static constexpr int kMisc = kBar + 8 * kNumBars;          // tensor-memory base, abort flag, wait limit (8 bytes)
   static constexpr int kBytes = kMisc + 16;
@@ -361,7 +361,7 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     *reinterpret_cast<volatile unsigned long long*>(smem + S::kMisc + 8) = p.wait_limit_ns;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (tid < 128) reinterpret_cast<volatile unsigned long long*>(smem + S::kTag)[tid] = ~0ull;   // no step has this number
+  if (tid < 3 * 128) reinterpret_cast<volatile unsigned long long*>(smem + S::kTag)[tid] = ~0ull;   // (kLfin too) no step and no item has this number
   if (warp == kWarpQK) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sbase + S::kMisc), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -589,7 +589,7 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     const int r = tid & 127;
     const uint32_t lane_addr = static_cast<uint32_t>((warp & 3) * 32) << 16;
     volatile unsigned long long* tag = reinterpret_cast<volatile unsigned long long*>(smem + S::kTag) + r;
-    volatile float* lfin = reinterpret_cast<volatile float*>(smem + S::kLfin) + r;
+    volatile unsigned long long* lfin = reinterpret_cast<volatile unsigned long long*>(smem + S::kLfin) + r;
     const uint32_t o_addr = tmem + lane_addr + kColO;
     const uint32_t p_to = map_to_rank(B.p_full(0), 0), o_free_to = map_to_rank(B.o_free(), 0);
     const int tok_r = r / p.G, head_r = r - tok_r * p.G;   // token and head within the tile
@@ -735,9 +735,10 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
             l_sum += (a + b) + (c + d);
           }
           if (s == steps - 2) {
-            // This group's last step of the item, but not the item's: hand the row sum to the group that writes the output.  (That
-            // group reads it before it publishes a tag of the next item, and this place is written again two items on.)
-            lfin[(items & 1u) * 128] = l_sum;
+            // This group's last step of the item, but not the item's: hand the row sum to the group that writes the output, with the
+            // item's number (in the second CTA the barriers on the way between the two lie in the first one and order nothing here).
+            // (That group reads it before it publishes a tag of the next item, and this place is written again two items on.)
+            lfin[(items & 1u) * 128] = tagged(items, l_sum);
           }
           wait_st();
           fence_before();
@@ -754,12 +755,13 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
 
         if (s == steps - 1) {
           // ---- this group took the item's last step: it writes the item's output
-          ok = mbar_wait_warp(B.o_done(sb), sph, s_abort);      // PVs complete in order
+          unsigned long long other = tagged(items, 0.f);
+          if (!warp_rests && steps > 1) other = tag_wait(lfin + (items & 1u) * 128, items, s_abort);
+          ok = mbar_wait_warp(B.o_done(sb), sph, s_abort) && __all_sync(0xffffffffu, has_tag(other, items));      // PVs complete in order
           if (!ok) break;
           if (!warp_rests) {
             fence_after();
-            float l_row = l_sum;
-            if (steps > 1) l_row = fmaf(lfin[(items & 1u) * 128], m_in == m_ref ? 1.f : fast_exp2(m_in - m_ref), l_row);   // the other's sum is relative to the reference it last saw
+            const float l_row = fmaf(value_of(other), m_in == m_ref ? 1.f : fast_exp2(m_in - m_ref), l_sum);   // the other's sum is relative to the reference it last saw
             const float inv = l_row > 0.f ? 1.f / l_row : (l_row == 0.f ? 0.f : l_row);                 // a NaN sum stays one
             const int slot = it.slot < 0 ? -1 : it.slot + static_cast<int>(rank);
             // The accumulator is given back as soon as it is in registers: the next item's first PV waits for that.
