@@ -297,11 +297,13 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
 }
 // 2^x of a pair on the FMA and integer pipes (x <= ~8): x = n + f with n whole and f in [-1/2, 1/2] (adding and taking off
 // 1.5 * 2^23 rounds to a whole number), a cubic for 2^f fitted over that interval (relative error 1e-4, well below the bf16
-// rounding of what it is used for), n added to the exponent field.  A NaN comes out as 2^-126: the caller looks for those.
+// rounding of what it is used for), n added to the exponent field.  At -127 and below, -inf among them, the sum is exactly 0 (f = 0,
+// 2^f = 1, and n takes its whole exponent away); between -127 and -126 it is some number from 0 to 2^-126.  A NaN comes out as 0:
+// the caller looks for those.
 __device__ __forceinline__ void poly_exp2_pair(uint64_t x2, float& p0, float& p1) {
   float a, b;
   unpack2(x2, a, b);
-  const uint64_t xc = pack2(fmaxf(a, -126.f), fmaxf(b, -126.f));
+  const uint64_t xc = pack2(fmaxf(a, -127.f), fmaxf(b, -127.f));
   const uint64_t t2 = add2(xc, pack2(12582912.f, 12582912.f));
   const uint64_t u2 = add2(t2, pack2(-12582912.f, -12582912.f));
   const uint64_t f2 = fma2(u2, pack2(-1.f, -1.f), xc);

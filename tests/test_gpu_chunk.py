@@ -583,3 +583,19 @@ def test_row_sums_change_hands_between_items_of_a_few_steps(E):
     torch.cuda.synchronize()
     assert all(torch.equal(outs[0].view(torch.int16), o.view(torch.int16)) for o in outs[1:])
     assert float((outs[0].float() - 1).abs().max()) <= 2.0 ** -8 + 2.0 ** -8 + 5e-4
+
+
+@pytest.mark.parametrize("prefix", [20, 6000])
+@pytest.mark.parametrize("single", [False, True])
+def test_the_largest_values_in_slots_that_a_row_does_not_see(E, single, prefix):
+    """The weight of a slot that a row does not see is 0, whatever finite value stands there."""
+    c = Case([6] + [0] * 7 if single else [140], [prefix] + [5] * 7 if single else [prefix], 4, 2, 128, seed=63, spare=0 if single else 3)
+    first, end = prefix + (2 if single else 110), prefix + c.n[0]
+    c.v[0, :, first:end] = 3e38
+    c.v[0, :, first:end:3] = -3e38
+    out, status = c.run(E)
+    want, spread = c.want()
+    assert status == 0
+    n = first - prefix
+    err, tol = np.abs(out.double().numpy() - want)[:n], (2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 5e-4) * spread)[:n]
+    assert (err <= tol).all(), (err.max(), (err / tol).max())
