@@ -47,14 +47,23 @@ __device__ __forceinline__ uint4 narrow(const float* f) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// Eight e4m3 codes of f * inv (round to nearest even, magnitudes above 448 become 448, NaN stays NaN).  `inv` is the reciprocal
-// of the scale within one fp32 step: a product can be two steps off the quotient, which matters only within 2^-22 of a tie.
-__device__ __forceinline__ uint2 codes(const float* f, float inv) {
+// Eight e4m3 codes of f / scale (round to nearest even, magnitudes above 448 become 448, NaN stays NaN).
+// With q = f * inv, up to two steps of fp32 off, what is missing is exactly (f - q scale) / scale, and f - q scale is a number of fp32:
+// adding it times `inv` leaves an error of 2^-44 before the sum is rounded to fp32.  So a value at the middle between two codes is
+// seen to be there.  Where q is large its magnitude is cut at 1024 first (the sum is large all the same): an infinite one would
+// make f - q scale infinite, too.
+__device__ __forceinline__ float2 quotients(float2 f, float scale, float inv) {
+  float2 q = make_float2(f.x * inv, f.y * inv);
+  asm("min.NaN.xorsign.abs.f32 %0, %0, %1;" : "+f"(q.x) : "f"(1024.f));      // (of the magnitudes; the sign stays)
+  asm("min.NaN.xorsign.abs.f32 %0, %0, %1;" : "+f"(q.y) : "f"(1024.f));
+  return make_float2(fmaf(fmaf(-q.x, scale, f.x), inv, q.x), fmaf(fmaf(-q.y, scale, f.y), inv, q.y));
+}
+__device__ __forceinline__ uint2 codes(const float* f, float scale, float inv) {
   uint32_t w[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const float2 lo = make_float2(f[4 * i] * inv, f[4 * i + 1] * inv);
-    const float2 hi = make_float2(f[4 * i + 2] * inv, f[4 * i + 3] * inv);
+    const float2 lo = quotients(make_float2(f[4 * i], f[4 * i + 1]), scale, inv);
+    const float2 hi = quotients(make_float2(f[4 * i + 2], f[4 * i + 3]), scale, inv);
     w[i] = __nv_cvt_float2_to_fp8x2(lo, __NV_SATFINITE, __NV_E4M3) | (static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(hi, __NV_SATFINITE, __NV_E4M3)) << 16);
   }
   return make_uint2(w[0], w[1]);
@@ -196,8 +205,8 @@ __global__ void __launch_bounds__(kRopeThreads, 4) rope_kernel(RopeParams p) {
       widen(in.a, x);
       widen(in.b, y);
       if (turn && !is_v) rotate(x, y);
-      *reinterpret_cast<uint2*>(dst + va) = codes(x, inv);
-      *reinterpret_cast<uint2*>(dst + vb) = codes(y, inv);
+      *reinterpret_cast<uint2*>(dst + va) = codes(x, in.scale, inv);
+      *reinterpret_cast<uint2*>(dst + vb) = codes(y, in.scale, inv);
       return;
     }
     uint4 out_a = in.a, out_b = in.b;

@@ -337,3 +337,37 @@ def test_caches_of_more_than_2_31_elements(E, page, fp8):
     assert torch.equal(bits(kv.k), bits(big_k[part])) and torch.equal(bits(kv.v), bits(big_v[part]))
     rest = (slice(0, far),) if page else (slice(None), slice(None), slice(c.kc.shape[2], None))
     assert not bool(big_k[rest].any()) and not bool(big_v[rest].any())
+
+
+def _nearest_codes(x):
+    """The e4m3 code nearest to each fp32 value (a tie goes to the even code), by search in the table of values."""
+    table = S.e4m3(np.arange(127))
+    x = np.asarray(x, dtype=np.float64)
+    lo = np.clip(np.searchsorted(table, np.abs(x), side="right") - 1, 0, 125)
+    d_lo, d_hi = np.abs(x) - table[lo], table[lo + 1] - np.abs(x)
+    code = np.where((d_hi < d_lo) | ((d_hi == d_lo) & (lo % 2 == 1)), lo + 1, lo)
+    return (code | np.where(np.signbit(x), 128, 0)).astype(np.uint8)
+
+
+def test_fp8_codes_are_the_nearest_to_the_fp32_quotient(E):
+    """Values at the middle between two codes, times scales that are no powers of two (products exact in bf16), and others; position 0 turns
+    by nothing, so keys are compared too."""
+    B = 24
+    c = Case([1] * B, [0] * B, 1, 4, 128, fp8=True, seed=33, rows=B)
+    c.qkv[:, 1:] *= 3
+    ties = np.array([(2 * m + 1) / 16 * 2.0 ** e for m in range(8, 16) for e in range(-6, 8)] + [(2 * m + 1) * 2.0 ** -10 for m in range(8)] + [-1.0625, -2.125] * 4)
+    assert len(ties) == 128
+    for b in range(12):
+        for h, odd in enumerate((3, 5, 7, 3 * 2.0 ** -40)):
+            scale = odd * 2.0 ** -(b + 2)
+            c.ks[b, h] = c.vs[b, h] = scale
+            for row in (1 + h, 5 + h):
+                c.qkv[b, row] = torch.tensor(ties * scale).bfloat16()
+                assert (c.qkv[b, row].double().numpy() == ties * scale).all()
+    _, kv, status, _ = _run_chunk(E, c)
+    assert status == 0
+    for rows, cache, scale in ((slice(1, 5), kv.k, c.ks), (slice(5, 9), kv.v, c.vs)):
+        x = c.qkv[:, rows].float().numpy() / scale.numpy()[:, :, None]
+        assert x.dtype == np.float32 and np.abs(x).max() > 448
+        want, got = _nearest_codes(x), cache.cpu().numpy()[:, :, 0]
+        assert (got == want).all(), (got != want).sum()
