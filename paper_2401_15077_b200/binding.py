@@ -652,8 +652,11 @@ class KVStore:
 ROPE_KINDS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "banded": 4}
 
 
-def eagle_rope_frequencies(rotary_dim, base=10000.0, kind="plain", factor=1.0, context=0.0, low=1.0, high=32.0, device=None):
-    """Rotary frequencies (fp64 [rotary_dim / 2], radians per position, on ``device`` or the host) and the amplitude."""
+def eagle_rope_frequencies(rotary_dim, base=10000.0, kind="plain", factor=1.0, context=0.0, low=None, high=None, device=None):
+    """Rotary frequencies (fp64 [rotary_dim / 2], radians per position, on ``device`` or the host) and the amplitude.  ``low`` and ``high``
+    are 1 and 32 where they are not given, 1 and 4 with ``kind="banded"``."""
+    low = 1.0 if low is None else low
+    high = (4.0 if kind == "banded" else 32.0) if high is None else high
     if kind not in ROPE_KINDS:
         raise EagleError(f"unknown kind of scaling {kind!r}")
     freqs, amplitude = torch.empty(max(int(rotary_dim), 0) // 2, dtype=torch.float64), ctypes.c_float(0.0)

@@ -234,3 +234,15 @@ def test_chunk_workspace_covers_calls_with_fewer_tokens(E):
             few = [s for n, s in zip(counts, sizes) if n <= batch]
             assert few == sorted(few) and all(s >= few[-1] for n, s in zip(counts, sizes) if n > batch)
             assert sizes == sorted(sizes)
+
+
+def test_the_usual_ends_of_a_band_are_those_of_its_kind():
+    from paper_2401_15077_b200 import binding, build
+    build.build()
+    for kind, low, high in (("banded", 1.0, 4.0), ("yarn", 1.0, 32.0)):
+        kw = dict(base=500000.0, kind=kind, factor=8.0, context=8192.0)
+        got, amplitude = binding.eagle_rope_frequencies(128, **kw)
+        want, amplitude_want = S.rope_frequencies(128, low=low, high=high, **kw)
+        assert np.allclose(got.numpy(), want, rtol=1e-12, atol=0) and abs(amplitude - amplitude_want) < 1e-6
+        given, _ = binding.eagle_rope_frequencies(128, low=2.0, high=16.0, **kw)
+        assert np.allclose(given.numpy(), S.rope_frequencies(128, low=2.0, high=16.0, **kw)[0], rtol=1e-12, atol=0)
