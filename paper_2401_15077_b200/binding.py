@@ -675,10 +675,10 @@ def _rope_rows(t, name, lead, dev):
         if lead[1] > 1:
             raise EagleError(f"{name} must have its rows a constant stride apart")
         row = stride[0]
-    if row <= 0:                       # one row may have any stride; 0 stands for dense rows in the descriptor
-        if math.prod(lead) > 1:
-            raise EagleError(f"{name} must have rows of its own (it is expanded)")
+    if math.prod(lead) <= 1:           # one row may have any stride; 0 stands for dense rows in the descriptor
         row = 0
+    elif row <= 0:
+        raise EagleError(f"{name} must have rows of its own (it is expanded)")
     return t.data_ptr(), row
 
 

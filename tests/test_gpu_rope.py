@@ -371,3 +371,29 @@ def test_fp8_codes_are_the_nearest_to_the_fp32_quotient(E):
         assert x.dtype == np.float32 and np.abs(x).max() > 448
         want, got = _nearest_codes(x), cache.cpu().numpy()[:, :, 0]
         assert (got == want).all(), (got != want).sum()
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_a_lone_row_may_have_any_stride(E, tree):
+    """Heads first, tokens second, as attention layers often keep them: with one token its heads are dense, and there is no second row."""
+    c = Case([1], [5], 4, 2, 64, seed=34, rows=1, tree=1 if tree else None)
+    lens, freqs = _ints(c.lens).to(DEV), c.freqs.to(DEV)
+    rest = (lens, _ints([[-1]]).to(DEV) if tree else c.start.to(DEV), freqs)
+    call = E.eagle_tree_rope_append if tree else E.eagle_rope_append
+    dense = [t.to(DEV).contiguous() for t in (c.q, c.k, c.v)]
+
+    def by_heads(t):
+        t = t.transpose(-3, -2)
+        return torch.empty(t.shape, dtype=t.dtype, device=DEV).copy_(t).transpose(-3, -2)
+
+    heads_first = [by_heads(t) for t in dense]
+    assert all(t.stride(-3) == 64 for t in heads_first)
+    a, b = c.store(E), c.store(E)
+    out_a, out_b = call(*dense, a, *rest), call(*heads_first, b, *rest)
+    assert torch.equal(out_a, out_b) and all(torch.equal(x.view(torch.int16), y.view(torch.int16)) for x, y in ((a.k, b.k), (a.v, b.v)))
+    # the queries turned in place, a lone row of a projection's output among them
+    for q in (heads_first[0], c.qkv.to(DEV)[..., :4, :]):
+        assert q.is_contiguous() and torch.equal(call(q, dense[1], dense[2], c.store(E), *rest, q_out=q), out_a)
+    if not tree:
+        none = [by_heads(t)[:0] for t in dense]
+        assert call(*none, c.store(E), lens, _ints([0, 0]).to(DEV), freqs).shape == (0, 4, 64)

@@ -246,3 +246,14 @@ def test_the_usual_ends_of_a_band_are_those_of_its_kind():
         assert np.allclose(got.numpy(), want, rtol=1e-12, atol=0) and abs(amplitude - amplitude_want) < 1e-6
         given, _ = binding.eagle_rope_frequencies(128, low=2.0, high=16.0, **kw)
         assert np.allclose(given.numpy(), S.rope_frequencies(128, low=2.0, high=16.0, **kw)[0], rtol=1e-12, atol=0)
+
+
+def test_row_strides_of_lone_and_missing_rows(E):
+    """What stands for the stride in the descriptor (0: dense) when there is no second row."""
+    one = torch.zeros(4, 1, 64, dtype=torch.bfloat16)
+    assert E._rope_rows(one.transpose(0, 1), "q", torch.Size((1,)), one.device) == (one.data_ptr(), 0)
+    assert E._rope_rows(one.transpose(0, 1)[None], "q", torch.Size((1, 1)), one.device) == (one.data_ptr(), 0)
+    assert E._rope_rows(one.transpose(0, 1)[:0], "q", torch.Size((0,)), one.device)[1] == 0
+    wide = torch.zeros(3, 10, 64, dtype=torch.bfloat16)
+    assert E._rope_rows(wide[:, 2:6], "q", torch.Size((3,)), wide.device) == (wide.data_ptr() + 2 * 64 * 2, 640)
+    assert E._rope_rows(wide[:, None, 2:6], "q", torch.Size((3, 1)), wide.device)[1] == 640
