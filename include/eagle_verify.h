@@ -242,7 +242,7 @@ const uint64_t* eagle_tree_verify_plan_masks(const eagle_attn_desc* desc);
 void eagle_set_wait_limit_ns(uint64_t ns);
 
 /*
- * Test hook (fault injection for the time-out path; not for production use): attention launches made after this call
+ * Test hook (fault injection for the time-out path; not for production use): attention launches (tree and chunk) made after this call
  * have their K/V producer stop issuing copies after `after_tiles` tiles per CTA, so the consumers' waits run out and
  * the kernel reports EAGLE_ERR_TIMEOUT.  Nothing is in flight when it returns.  A negative value switches it off.
  */
@@ -588,7 +588,8 @@ size_t eagle_chunk_attn_workspace(const eagle_chunk_desc* desc);
  * one that is not may reach rows of the same sequence that do not see it (its probability there is 0, and 0 * inf is NaN).
  * Rows outside every sequence are left as they were.  A sequence with L_b < 0 or L_b + n_b over its slots reports EAGLE_ERR_SEQ,
  * one with a block-table entry in use outside [0, num_pages) EAGLE_ERR_PAGE: its rows are zeros.  Starts that descend or
- * leave [0, N] report EAGLE_ERR_SEQ and no row is computed.  Three launches (planner, attention, merge), asynchronous on
+ * leave [0, N] report EAGLE_ERR_SEQ and no row is computed.  A wait inside the attention kernel that runs out reports EAGLE_ERR_TIMEOUT, and rows inside the
+ * sequences may then hold anything (eagle_set_wait_limit_ns).  Three launches (planner, attention, merge), asynchronous on
  * `stream`; calls that share a workspace must not overlap on the GPU.  Calls with N <= B run a kernel made for single tokens (it is
  * right for any lengths, but reads a sequence's cache once for every 16 / G of its tokens).
  */

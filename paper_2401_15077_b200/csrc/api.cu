@@ -78,6 +78,8 @@ int usable_device(int* sm_count) {
 
 unsigned long long wait_limit_ns() { return g_wait_limit_ns.load(std::memory_order_relaxed); }
 
+int32_t stall_after_tiles() { return g_stall_after_tiles.load(std::memory_order_relaxed); }
+
 }  // namespace eagle
 
 using namespace eagle;

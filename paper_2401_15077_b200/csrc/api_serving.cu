@@ -224,6 +224,7 @@ int eagle_chunk_attn(const eagle_chunk_desc* desc, const void* q, const eagle_kv
   p.scale_log2 = scale * 1.4426950408889634f;
   p.status = d.status;
   p.wait_limit_ns = wait_limit_ns();
+  p.stall_after_tiles = stall_after_tiles();
   return launch_chunk(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? EAGLE_OK : EAGLE_ERR_LAUNCH;
 }
 

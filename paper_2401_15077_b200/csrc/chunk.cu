@@ -326,7 +326,9 @@ __device__ __forceinline__ unsigned long long tag_wait(volatile unsigned long lo
   return tag_wait_slow(slot, want, abort_flag);
 }
 
-template <int D, bool PAGED>
+// (STALL: of the test hook that lets the waits run out, an instantiation of its own because the comparison would cost every other
+// call 2 to 3 %.)
+template <int D, bool PAGED, bool STALL>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                   const __grid_constant__ CUtensorMap map_q) {
@@ -445,8 +447,12 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     ck.wrong = cv.wrong = false;
     advance(ck, false);
     advance(cv, true);
+    [[maybe_unused]] int keys = 0, values = 0;                     // tiles issued
     auto next_key = [&]() {
       if (!ck.valid || !ok) return;
+      if constexpr (STALL) {
+        if (keys++ >= p.stall_after_tiles) return;
+      }
       if (ck.fresh) {
         // box of TPT tokens x G heads x 64 columns: rows land in (token, head) order; rows of the next sequence (or zeros past
         // the tensor) that come along are computed and never written
@@ -474,6 +480,9 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     };
     for (int i = 0; i < 3; ++i) next_key();
     while (cv.valid && ok) {
+      if constexpr (STALL) {
+        if (values++ >= p.stall_after_tiles) break;
+      }
       ok = mbar_wait_warp(B.v_empty(vr.slot), vr.par ^ 1u, s_abort);
       if (!ok) break;
       if (lane == 0) mbar_expect_tx(B.v_full(vr.slot), S::kVBytes);
@@ -918,7 +927,9 @@ cudaError_t launch_tiles(const ChunkParams& p, cudaStream_t stream) {
       !map_bf16_3d(&mq, p.q, D, p.Hq, p.N, 64, p.G, p.tpt))
     return cudaErrorInvalidValue;
   BehindLaunch at(2 * p.num_workers, kThreads, Smem<D>::kBytes, stream);
-  return cudaLaunchKernelEx(&at.config, paged ? chunk_attn_kernel<D, true> : chunk_attn_kernel<D, false>, p, mk, mv, mq);
+  auto kernel = p.stall_after_tiles >= 0 ? (paged ? chunk_attn_kernel<D, true, true> : chunk_attn_kernel<D, false, true>)
+                                         : (paged ? chunk_attn_kernel<D, true, false> : chunk_attn_kernel<D, false, false>);
+  return cudaLaunchKernelEx(&at.config, kernel, p, mk, mv, mq);
 }
 
 template <int D>
@@ -940,17 +951,18 @@ cudaError_t launch_all(const ChunkParams& p, cudaStream_t stream) {
   return cudaSuccess;
 }
 
+template <int D>
+cudaError_t prepare() {
+  for (auto kernel : {chunk_attn_kernel<D, false, false>, chunk_attn_kernel<D, true, false>, chunk_attn_kernel<D, false, true>, chunk_attn_kernel<D, true, true>}) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::kBytes);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
 }  // namespace
 
-cudaError_t chunk_prepare(int head_dim) {
-  cudaError_t e;
-  if (head_dim == 128) {
-    e = cudaFuncSetAttribute(chunk_attn_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<128>::kBytes);
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(chunk_attn_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<128>::kBytes);
-  }
-  e = cudaFuncSetAttribute(chunk_attn_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<64>::kBytes);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(chunk_attn_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<64>::kBytes);
-}
+cudaError_t chunk_prepare(int head_dim) { return head_dim == 128 ? prepare<128>() : prepare<64>(); }
 
 cudaError_t launch_chunk(const ChunkParams& p, cudaStream_t stream) { return p.D == 128 ? launch_all<128>(p, stream) : launch_all<64>(p, stream); }
 

@@ -71,6 +71,7 @@ struct ChunkParams {
   float scale_log2;
   int32_t* status;
   unsigned long long wait_limit_ns;
+  int32_t stall_after_tiles;     // test hook: the kernels' STALL instantiations issue copies of that many tiles and no more (negative: off)
   ChunkWork work;
 };
 

@@ -62,7 +62,7 @@ __device__ __forceinline__ float quad_sum(float x) {
   return x + __shfl_xor_sync(0xffffffffu, x, 2);
 }
 
-template <int D, bool PAGED>
+template <int D, bool PAGED, bool STALL>                     // (STALL: of the test hook, as in chunk.cu)
 __global__ void __launch_bounds__(kRowThreads, 1)
 chunk_rows_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
   using S = RowSmem<D>;
@@ -139,7 +139,11 @@ chunk_rows_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
     };
     advance();
     Ring<S::kStages> ring;
+    [[maybe_unused]] int tiles = 0;                        // issued
     while (more) {
+      if constexpr (STALL) {
+        if (tiles++ >= p.stall_after_tiles) break;
+      }
       if (!mbar_wait_warp(empty(ring.slot), ring.par ^ 1u, s_abort)) break;
       if (lane == 0) mbar_expect_tx(full(ring.slot), S::kStage);
       __syncwarp();
@@ -338,13 +342,18 @@ cudaError_t launch(const ChunkParams& p, cudaStream_t stream) {
   const long long n2 = paged ? static_cast<long long>(p.num_pages) * p.Hkv : static_cast<long long>(p.B) * p.Hkv;
   if (!map_bf16_3d(&mk, p.k, D, n1, n2, 64, box_rows, 1) || !map_bf16_3d(&mv, p.v, D, n1, n2, 64, box_rows, 1)) return cudaErrorInvalidValue;
   BehindLaunch at(p.num_workers, kRowThreads, RowSmem<D>::kBytes, stream);
-  return cudaLaunchKernelEx(&at.config, paged ? chunk_rows_kernel<D, true> : chunk_rows_kernel<D, false>, p, mk, mv);
+  auto kernel = p.stall_after_tiles >= 0 ? (paged ? chunk_rows_kernel<D, true, true> : chunk_rows_kernel<D, false, true>)
+                                         : (paged ? chunk_rows_kernel<D, true, false> : chunk_rows_kernel<D, false, false>);
+  return cudaLaunchKernelEx(&at.config, kernel, p, mk, mv);
 }
 
 template <int D>
 cudaError_t prepare() {
-  const cudaError_t e = cudaFuncSetAttribute(chunk_rows_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowSmem<D>::kBytes);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(chunk_rows_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, RowSmem<D>::kBytes);
+  for (auto kernel : {chunk_rows_kernel<D, false, false>, chunk_rows_kernel<D, true, false>, chunk_rows_kernel<D, false, true>, chunk_rows_kernel<D, true, true>}) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, RowSmem<D>::kBytes);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace

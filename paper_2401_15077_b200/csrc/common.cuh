@@ -241,5 +241,6 @@ void count_launch();
 // The current device's number of SMs; EAGLE_ERR_DEVICE when it is not an sm_100 device.
 int usable_device(int* sm_count);
 unsigned long long wait_limit_ns();
+int32_t stall_after_tiles();          // of eagle_test_stall_kv_producer
 
 }  // namespace eagle

@@ -599,3 +599,33 @@ def test_the_largest_values_in_slots_that_a_row_does_not_see(E, single, prefix):
     n = first - prefix
     err, tol = np.abs(out.double().numpy() - want)[:n], (2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 5e-4) * spread)[:n]
     assert (err <= tol).all(), (err.max(), (err / tol).max())
+
+
+@pytest.mark.parametrize("tiles", [0, 2, 9])
+@pytest.mark.parametrize("d,page", [(128, 0), (128, 16), (64, 0), (64, 64)])
+@pytest.mark.parametrize("single", [False, True])
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(E, single, d, page, tiles):
+    """The copies of every CTA fall silent after some tiles (test hook) and the limit is 2 ms: the call returns by itself with the status
+    of a time-out, rows outside the sequences are as they were, and an ordinary call right after gives the same bits as one before."""
+    c = Case(*(([1, 1], [60000, 31000]) if single else ([70, 0, 5], [40000, 3, 31000])), 8, 4, d, page=page, seed=81, spare=0 if single else 3)
+    q, kv = c.q.to(DEV), E.KVStore(c.k.to(DEV), c.v.to(DEV), block_table=None if c.table is None else c.table.to(DEV))
+    lens, start, used = _ints(c.lens).to(DEV), c.start.to(DEV), sum(c.n)
+
+    def call():
+        out, status = torch.full(c.q.shape, 7.0, dtype=torch.bfloat16, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        E.eagle_chunk_attn(q, kv, lens, start, out, status=status)
+        torch.cuda.synchronize()
+        return out, int(status.item())
+
+    want, status = call()
+    assert status == 0
+    E.set_wait_limit_ns(2_000_000)
+    E.test_stall_kv_producer(tiles)
+    try:
+        out, status = call()
+    finally:
+        E.test_stall_kv_producer(-1)
+        E.set_wait_limit_ns(0)
+    assert status == -8 and (out[used:] == 7.0).all()
+    out, status = call()
+    assert status == 0 and torch.equal(out.view(torch.int16), want.view(torch.int16))
