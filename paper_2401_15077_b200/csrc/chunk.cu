@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
         const long long np = q.parts;
         v.a = static_cast<int>(np) * Hkv;
         // sum over the parts of L + (p + 1) UT, but the last one ends at n
-        v.b = (np * (q.L + kChunkItemKeys) + ut * (np * (np + 1) / 2) - (np * ut - q.n)) * Hkv;
+        v.b = (np * (static_cast<long long>(q.L) + kChunkItemKeys) + ut * (np * (np + 1) / 2) - (np * ut - q.n)) * Hkv;
       }
     }
     Sum2 tot;
@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
     const long long keys = q.L + (pr + 1ll) * ut - (r == 0 ? over : 0);
     un.tiles = static_cast<int>((keys + kChunkTile - 1) / kChunkTile);
     if (x) {
-      const long long before = static_cast<long long>(r) * (q.L + kChunkItemKeys) +
+      const long long before = r * (static_cast<long long>(q.L) + kChunkItemKeys) +
                                ut * ((static_cast<long long>(q.parts) * (q.parts + 1) - static_cast<long long>(pr + 1) * (pr + 2)) / 2) - (r > 0 ? over : 0);
       *x = cost_of[b] + before * Hkv + un.g * (keys + kChunkItemKeys);
     }

@@ -629,3 +629,20 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(E, single, 
     assert status == -8 and (out[used:] == 7.0).all()
     out, status = call()
     assert status == 0 and torch.equal(out.view(torch.int16), want.view(torch.int16))
+
+
+@pytest.mark.parametrize("n", [1, 2])
+def test_as_many_slots_as_a_length_can_name(E, n):
+    """2^31 - 1 slots, the same page of 2^20 over and over: all scores are 0 and all values 1, so every partial sum is a whole number and
+    the output is 1."""
+    k, v = (torch.full((1, 1, 1 << 20, 64), x, dtype=torch.bfloat16, device=DEV) for x in (0.0, 1.0))
+    kv, status = E.KVStore(k, v, block_table=torch.zeros(1, 1 << 11, dtype=torch.int32, device=DEV)), torch.zeros(1, dtype=torch.int32, device=DEV)
+    q = torch.ones(n, 1, 64, dtype=torch.bfloat16, device=DEV)
+    for slots, want in ((2 ** 31 - 1, 0), (2 ** 31 - 1 - 300, 0)):
+        status.zero_()
+        out = E.eagle_chunk_attn(q, kv, _ints([slots - n]).to(DEV), _ints([0, n]).to(DEV), status=status)
+        torch.cuda.synchronize()
+        assert int(status.item()) == want and (out == 1).all()
+    E.eagle_chunk_attn(q, kv, _ints([2 ** 31 - n]).to(DEV), _ints([0, n]).to(DEV), out, status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == -6 and (out == 0).all()
