@@ -540,7 +540,7 @@ typedef struct eagle_rope_desc {
  * Token i of sequence b turns by position L_b + i (or positions[row]) and goes to slot L_b + i.  Pair (x, y) of frequency f at
  * position p becomes amplitude * (x cos pf - y sin pf, y cos pf + x sin pf); the angle is reduced in fp64, the rotation is
  * fp32, rounded once.  Keys of an fp8 cache are stored as the nearest e4m3 code of key / k_scale[b, h] in fp32 (ties go
- * to the even code, magnitudes above 448 become 448), values likewise.  Nothing else in the cache changes.  Rows outside every sequence (behind the last one) are
+ * to the even code, magnitudes above 448 become 448; scales are normal numbers of fp32), values likewise.  Nothing else in the cache changes.  Rows outside every sequence (behind the last one) are
  * not written.  A sequence with L_b < 0 or more tokens than its slots reports EAGLE_ERR_SEQ: its rows of q_out
  * are zeros and nothing of it is stored; starts that descend or leave [0, N] report it too, and rows that they do not place
  * are left alone.  A token whose page is outside the pool reports EAGLE_ERR_PAGE and is not stored.

@@ -56,7 +56,7 @@ __device__ __forceinline__ float2 quotients(float2 f, float scale, float inv) {
   float2 q = make_float2(f.x * inv, f.y * inv);
   asm("min.NaN.xorsign.abs.f32 %0, %0, %1;" : "+f"(q.x) : "f"(1024.f));      // (of the magnitudes; the sign stays)
   asm("min.NaN.xorsign.abs.f32 %0, %0, %1;" : "+f"(q.y) : "f"(1024.f));
-  return make_float2(fmaf(fmaf(-q.x, scale, f.x), inv, q.x), fmaf(fmaf(-q.y, scale, f.y), inv, q.y));
+  return make_float2(fmaf(-fmaf(q.x, scale, -f.x), inv, q.x), fmaf(-fmaf(q.y, scale, -f.y), inv, q.y));      // (these signs keep that of a zero)
 }
 __device__ __forceinline__ uint2 codes(const float* f, float scale, float inv) {
   uint32_t w[2];

@@ -397,3 +397,18 @@ def test_a_lone_row_may_have_any_stride(E, tree):
     if not tree:
         none = [by_heads(t)[:0] for t in dense]
         assert call(*none, c.store(E), lens, _ints([0, 0]).to(DEV), freqs).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -126, 2.0 ** -100, 1.0, 3.0, 2.0 ** 100])
+def test_fp8_codes_of_zeros_infinities_and_extreme_scales(E, scale):
+    """The sign of a zero, values whose quotient leaves fp32's range, scales at the edge of the normal numbers."""
+    c = Case([1] * 3, [0] * 3, 1, 2, 128, fp8=True, seed=35, rows=3)
+    c.ks.fill_(scale), c.vs.fill_(scale)
+    c.qkv[:, 1:] = (c.qkv[:, 1:].double() * 100 * scale).bfloat16()
+    c.qkv[:, 3, :6] = torch.tensor([float("inf"), -float("inf"), 0.0, -0.0, 3e38, -3e38]).bfloat16()
+    _, kv, status, _ = _run_chunk(E, c)
+    assert status == 0
+    for rows, cache in ((slice(1, 3), kv.k), (slice(3, 5), kv.v)):
+        with np.errstate(over="ignore"):
+            x = c.qkv[:, rows].float().numpy() / np.float32(scale)
+        assert (_nearest_codes(x) == cache.cpu().numpy()[:, :, 0]).all()
