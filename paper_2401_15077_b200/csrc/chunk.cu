@@ -11,9 +11,10 @@
 // loaded once for both, and each SM reads half of the operand from its shared memory.
 //
 // What bounds it is the way of one score buffer around the loop (score MMA, softmax, PV MMA, and a wait between each two): about 4700
-// cycles, with three buffers on it 1550 per 128 keys, of which the tensor cores need 1036.  A prompt of 4096 tokens, 32 heads, D = 128
-// (137 GFLOP, causal): 154 us, 890 TFLOP/s; two chunks of 2048 tokens behind 16384 (1.17 TFLOP in 0.97 to 1.10 ms, by the clock that
-// the power limit leaves): 1.06 to 1.2 PFLOP/s of the 1.65 (1.40 sustained) that a large matrix product reaches.
+// cycles, with three buffers on it 1550 per 128 keys, of which the tensor cores need 1036.  Replayed from a graph, a prompt of 4096
+// tokens, 32 heads, D = 128 (137 GFLOP, causal) takes 154 us, 890 TFLOP/s (180 us as a single call on cold inputs: 765); two chunks of
+// 2048 tokens behind 16384 (1.17 TFLOP) 1.05 to 1.13 ms, by the clock that the power limit leaves (a call: 1.17 ms, 1.0 PFLOP/s), where a
+// large matrix product reaches 1.65 PFLOP/s, 1.40 sustained.
 #include "chunk.cuh"
 #include "tc.cuh"
 

@@ -14,8 +14,19 @@ constexpr int kChunkSnap = 2;
 // 128 rows on the tensor cores of both; the row kernel's are single CTAs, with one query tile of 16 rows.  A query tile is
 // TPT tokens times the G heads of a group.  Calls with no more rows than sequences (single tokens) take the row kernel: there
 // the keys and values are streamed once for a few rows, and what counts is how steadily they come.  64 single tokens over 512 to
-// 8192 slots, 32 heads over 8: 208 us, the tile kernel 249 us; one token over 65536, 64 heads over 8: 61 us against
-// 77 us.  The row kernel is right for more tokens too, but reads the cache again for every 16 / G of them.
+// 8192 slots, 32 heads over 8: 203 us, the tile kernel 249 us; one token over 65536, 64 heads over 8: 59.5 us against
+// 77 us.  The host sees numbers and no lengths, so the rule takes N <= B for single tokens.  The row kernel is right for more tokens of
+// a sequence too, but reads its cache again for every 16 / G of them.  Rows against tiles in us (cold caches, D = 128, 8 KV heads):
+//   a token each, 64 sequences of 512 to 4112 slots    32 heads 127 : 152   64 heads 127 : 152   no groups 395 : 524
+//   two tokens in every other of them                  32 heads  80 :  94   64 heads  82 :  94   no groups 225 : 281
+//   four in every fourth                               32 heads  51 :  59   64 heads  64 :  59   no groups 129 : 152
+//   one chunk behind 8192 slots, all others empty
+//     of 8 tokens                                      32 heads  29 :  31   64 heads  37 :  33   no groups  28 :  29
+//     of 64 tokens                                     32 heads  88 :  35   64 heads 154 :  41   no groups  37 :  35
+//     of 200 tokens                                    32 heads 231 :  55   64 heads 444 :  80   no groups  76 :  35
+// So it is wrong for a chunk of many tokens among as many empty sequences; a caller that has one gets the tile kernel by leaving
+// empty sequences out, or with a row behind the last sequence (N > B).  A decode batch with such a spare row takes the tile kernel, 1.2 to 1.3
+// times as long.
 constexpr int kTileRows = 128, kFewRows = 16;
 inline bool chunk_takes_rows(const eagle_chunk_desc& d) { return d.num_tokens <= d.batch; }
 

@@ -8,9 +8,9 @@
 // instructions: scores leave one as the operand of the next).  The four are joined when the item ends, which the copies of the next
 // item do not wait for.
 //
-// 64 single tokens over 512 to 8192 slots (1.21 GB of keys and values, 32 heads over 8, D = 128): 208 us with planner and merge,
-// 5.8 TB/s of the 6.6 TB/s that a plain copy reaches; one token over 65536 slots (268 MB, 64 heads over 8): 61 us, 4.4 TB/s (planner,
-// merge and two launches are about 12 us of it).
+// 64 single tokens over 512 to 8192 slots (1.21 GB of keys and values, 32 heads over 8, D = 128): 203 us with planner and merge (from a
+// graph; a call 212 us), 6.0 TB/s of the 6.6 TB/s that a plain copy reaches; one token over 65536 slots (268 MB, 64 heads over 8): 59.5 us,
+// 4.5 TB/s (planner, merge and two launches are about 12 us of it).
 #include "chunk.cuh"
 #include "tc.cuh"
 

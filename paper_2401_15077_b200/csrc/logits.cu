@@ -15,9 +15,9 @@
 // Counts are integers and a token's biases are added up by one thread in list order, so a call gives the same bits every time.
 //
 // Bound by HBM for a batch of trees, and there by what a CTA does before its first row: all its loads set out together as soon as
-// the sequence's lengths are known.  64 trees of 16 to 64 nodes x 32000 tokens, 4096 tokens of history, biases and masks (699 MB): 135 us,
-// 5.2 of the 6.6 TB/s that a plain copy reaches (147 us with the loads where they are used).  16 bf16 rows of 129537 tokens: 8.3 us,
-// of which 1.9 us would be the bytes: two rounds of CTAs, a launch and three trips to memory.
+// the sequence's lengths are known.  Replayed from a graph, 64 trees of 16 to 64 nodes x 32000 tokens, 4096 tokens of history, biases and
+// masks (699 MB): 135 us, 5.2 of the 6.6 TB/s that a plain copy reaches (147 us with the loads where they are used).  16 bf16 rows of 129537
+// tokens: 8.3 to 9.3 us, of which 1.9 us would be the bytes: two rounds of CTAs, a launch and three trips to memory.
 #include "logits.cuh"
 
 namespace eagle {
@@ -150,7 +150,8 @@ __global__ void __launch_bounds__(kLogThreads, 4) logits_kernel(LogitsParams p) 
   }
   __syncthreads();
 
-  // z' = (z > 0 ? z / rho : z * rho) + add for a token that is there already, z + add for any other
+  // z' = (z > 0 ? z / rho : z * rho) + add for a token that is there already, z + add for any other (the product with 1 / rho is one
+  // rounding more than a quotient, and one instruction where a division for every logit would be ten)
   const float inv_rho = 1.f / rho;
   float add[kPerThread];
   uint32_t seen = 0;

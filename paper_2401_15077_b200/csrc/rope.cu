@@ -15,9 +15,9 @@
 // pairs in halves needs; units of the heads to come are on their way while one is turned.  (With tokens spread over a CTA and the
 // sines read from shared memory for each unit, those reads, four-way bank conflicts among them, cost as much as the loads.)
 // The kernel moves (2 Hq + 2 Hkv + 2 Hkv) * D elements a token and is bound by HBM for long chunks, by launch and memory
-// latency for short ones.  8192 tokens, 64 heads over 8, D = 128 (336 MB): 58 us, 5.8 TB/s of the 6.6 TB/s that a plain copy reaches;
+// latency for short ones.  From a graph, 8192 tokens, 64 heads over 8, D = 128 (336 MB): 58 us, 5.8 TB/s of the 6.6 TB/s that a plain copy reaches;
 // 64 trees of 16 to 64 nodes, 32 heads over 8 (64 MB, one round of CTAs): 17 us, 3.7 TB/s; 6900 tokens into e4m3 codes (164 MB): 38 us,
-// 4.3 TB/s, where the conversions' registers leave no room for more loads; one token: 3.3 us.  Measured and no better: three units
+// 4.3 TB/s, where the conversions' registers leave no room for more loads (some spill already); one token: 3.3 to 4.2 us.  Measured and no better: three units
 // in flight (spills: 64 us for the 8192 tokens), 32 or 64 warps per SM asked for below (18.6 and 19.5 us for the trees).
 #include <cuda_fp8.h>
 
