@@ -225,9 +225,10 @@ __device__ __forceinline__ void poly_exp2_pair(uint64_t x2, float& p0, float& p1
   p1 = __uint_as_float(__float_as_uint(tb) * 0x800000u + __float_as_uint(rb));
 }
 
+// (NaN when one of the three is)
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
 
@@ -680,7 +681,9 @@ attn_kernel(AttnParams p, const __grid_constant__ CUtensorMap map_k, const __gri
             mx[3] = max3(mx[3], __uint_as_float(rb[e]), __uint_as_float(rb[e + 1]));
           }
         }
-        const float tmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale_log2;   // scale > 0
+        const float tmax = max3(max3(mx[0], mx[1], mx[2]), mx[3], -INFINITY) * scale_log2;   // scale > 0
+        // a visible score that is NaN or +inf makes the row NaN (through its sum: the polynomial below passes neither on)
+        if (!(tmax < INFINITY)) l_sum = __uint_as_float(0x7fffffffu);
 
         if (key0 + kTileN > kv_end) {
           // rows of the V tile past prefix + tree may hold anything: zero them so that 0 * garbage cannot reach O
@@ -808,7 +811,7 @@ attn_kernel(AttnParams p, const __grid_constant__ CUtensorMap map_k, const __gri
             const float w = m_in == m_ref ? 1.f : fast_exp2(m_in - m_ref);
             l_row = fmaf(*lfin, w, l_row);
           }
-          const float inv = l_row > 0.f ? v_scale / l_row : 0.f;   // (v_scale is 1 unless the cache is fp8)
+          const float inv = l_row > 0.f ? v_scale / l_row : (l_row == 0.f ? 0.f : l_row);   // a NaN sum stays one (v_scale is 1 unless the cache is fp8)
           // The accumulator is read 32 columns at a time, the next chunk's load in flight while this one is scaled and
           // stored.  These stores sit on the seam between two items (the group cannot take its next step, and the next
           // item's first PV cannot start, before they are issued), and with a row per thread every lane of a store
@@ -848,7 +851,8 @@ attn_kernel(AttnParams p, const __grid_constant__ CUtensorMap map_k, const __gri
             if (c + 2 < D / 32) tmem_ld32(o_addr + (c + 2) * 32, oa);
             store_chunk(ob, c + 1);
           }
-          if (row_valid && it.slot >= 0) p.part_ml[static_cast<size_t>(it.slot) * kBlockM + r] = make_float2(m_ref, l_row);
+          // (the reference of a NaN sum may be infinite: 0 stands for it, so that the combine takes the piece)
+          if (row_valid && it.slot >= 0) p.part_ml[static_cast<size_t>(it.slot) * kBlockM + r] = make_float2(l_row == l_row ? m_ref : 0.f, l_row);
           tc_fence_before();
           mbar_arrive(B.o_free());            // the next item's first PV may overwrite the accumulator
         }

@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(kCombineThreads) combine_kernel(AttnParams p) 
     float m_new = m_star;
 #pragma unroll
     for (int u = 0; u < kPiecesAtOnce; ++u) {
-      use[u] = s0 + u < ct.count && t1[u] > t0[u] && ml[u].y > 0.f && ml[u].x > -INFINITY;
+      use[u] = s0 + u < ct.count && t1[u] > t0[u] && !(ml[u].y <= 0.f) && ml[u].x > -INFINITY;     // (a NaN sum counts: it makes the row NaN)
       if (use[u]) m_new = fmaxf(m_new, ml[u].x);
     }
     if (m_new == -INFINITY) continue;
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kCombineThreads) combine_kernel(AttnParams p) 
       acc[3] += v[u].w * w;
     }
   }
-  const float inv = l_star > 0.f ? 1.f / l_star : 0.f;
+  const float inv = l_star > 0.f ? 1.f / l_star : (l_star == 0.f ? 0.f : l_star);     // a NaN sum stays one
   __nv_bfloat16* dst = p.out + ((static_cast<size_t>(ct.b) * p.T_max + i) * p.Hq + h) * D + c4 * 4;
   __nv_bfloat162 lo = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv);
   __nv_bfloat162 hi = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv);

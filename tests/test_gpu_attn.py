@@ -368,3 +368,27 @@ def test_full_size_sampled_rows(E, oracle, name):
                                       inp.seq_lens[b:b + 1], inp.tree_parent[b:b + 1], inp.tree_sizes[b:b + 1])
         err = np.abs(got[b, :n, g * G:(g + 1) * G] - ref[0, :n])
         assert err.max() <= MAX_ABS and err.mean() <= MEAN_ABS, (b, g, err.max(), err.mean())
+
+
+@pytest.mark.parametrize("num_splits", [0, 1, 3])
+def test_a_visible_key_that_is_not_a_number_makes_its_rows_nan_wherever_it_is(E, num_splits):
+    """At every place of a tile's first 32 columns and some later ones, in whole units and in cut ones: the rows that see the key are
+    NaN, and all others keep their bits (a key of the tree is seen by its node and the nodes below)."""
+    cfg = W.scaled(W.CONFIGS["tiny"], batch=2, num_q_heads=4, num_kv_heads=2, head_dim=128, prefix=(700, 900), tree=(9, 12), max_depth=5)
+    inp = W.make_attn_inputs(cfg, salt=21)
+    want, status = _run(E, inp, num_splits=num_splits)
+    assert status == 0
+    L, n, parent = int(inp.seq_lens[0]), int(inp.tree_sizes[0]), inp.tree_parent[0].tolist()
+    good = inp.k_cache.clone()
+    for at in list(range(33)) + [63, 64, 97, 127, 128, 513, L - 1, L, L + 3, L + n - 1]:
+        inp.k_cache = good.clone()
+        inp.k_cache[0, :, at] = float("nan")
+        out, status = _run(E, inp, num_splits=num_splits)
+        hit = torch.zeros(out.shape[:2], dtype=torch.bool)
+        for i in range(n):
+            m = i
+            while m >= 0 and m != at - L:
+                m = parent[m]
+            hit[0, i] = at < L or m >= 0
+        assert status == 0 and out[hit].isnan().all(), at
+        assert torch.equal(out[~hit].view(torch.int16), want[~hit].view(torch.int16)), at

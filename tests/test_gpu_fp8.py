@@ -277,3 +277,25 @@ def test_paged_fp8_plan_once_attend_many_and_bad_page(E, oracle):
     sizes[b] = 0                         # the oracle within the bounds, not with the first call bit for bit)
     ref[b] = 0.0
     _check(got, ref, sizes)
+
+
+@pytest.mark.parametrize("num_splits", [0, 1, 3])
+def test_the_nan_code_in_a_visible_key_makes_its_rows_nan_wherever_it_is(E, num_splits):
+    """As for the bf16 cache: at every place of a tile's first 32 columns and some later ones, in whole units and in cut ones, for keys and
+    for values."""
+    cfg = W.scaled(W.CONFIGS["7b_mha"], batch=2, num_q_heads=4, num_kv_heads=2, prefix=(700, 900), tree=(9, 12), max_depth=5)
+    inp = W.make_attn_inputs(cfg, salt=21)
+    f8 = W.make_fp8_cache(inp)
+    want, status = _run(E, inp, f8, num_splits=num_splits)
+    assert status == 0
+    n = int(inp.tree_sizes[0])
+    keys, values = f8.k_codes, f8.v_codes
+    for at in list(range(33)) + [63, 64, 97, 127, 128, 513, int(inp.seq_lens[0]) - 1]:
+        for name, good, code in (("k_codes", keys, 0x7f), ("v_codes", values, 0xff)):
+            bad = good.clone()
+            bad[0, :, at] = code
+            f8.k_codes, f8.v_codes = keys, values
+            setattr(f8, name, bad)
+            out, status = _run(E, inp, f8, num_splits=num_splits)
+            assert status == 0 and out[0, :n].isnan().all(), (name, at)
+            assert torch.equal(out[1].view(torch.int16), want[1].view(torch.int16)) and (out[0, n:] == 0).all()
