@@ -206,12 +206,13 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 }
 // 2^x for a packed pair on the FMA / ALU pipes (x <= ~8): split x into an integer n and a fraction f in [-0.5, 0.5]
 // with the add-a-large-constant trick, evaluate a cubic for 2^f (relative error 1e-4, far below the bf16 rounding of
-// P) and put n into the exponent field.  Used for a fraction of the exponentials so that the special-function
+// P) and put n into the exponent field.  At -127 and below, -inf among them, the sum is exactly 0 (f = 0, 2^f = 1, and n takes its
+// whole exponent away), so an invisible key has no weight.  Used for a fraction of the exponentials so that the special-function
 // unit, which takes 8 cycles per warp instruction, is not the only thing the softmax waits for.
 __device__ __forceinline__ void poly_exp2_pair(uint64_t x2, float& p0, float& p1) {
   float a, b;
   unpack2(x2, a, b);
-  const uint64_t xc2 = pack2(fmaxf(a, -126.f), fmaxf(b, -126.f));
+  const uint64_t xc2 = pack2(fmaxf(a, -127.f), fmaxf(b, -127.f));
   const uint64_t t2 = add2(xc2, pack2(12582912.f, 12582912.f));
   const uint64_t u2 = add2(t2, pack2(-12582912.f, -12582912.f));
   const uint64_t f2 = fma2(u2, pack2(-1.f, -1.f), xc2);

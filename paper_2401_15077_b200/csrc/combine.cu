@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kCombineThreads) combine_kernel(AttnParams p) 
       v[u] = *reinterpret_cast<const float4*>(p.part_o + (slot * (D / 4) + c4) * (kBlockM * 4) + r * 4);
     }
     // a piece counts when its item is not empty (an empty item never wrote its slot) and the row saw a key in it
-    // (a row all of whose keys in the piece were masked keeps the reference -inf; its sum may hold rounding dust)
+    // (a row all of whose keys in the piece were masked keeps the reference -inf and the sum 0)
     bool use[kPiecesAtOnce];
     float m_new = m_star;
 #pragma unroll

@@ -392,3 +392,25 @@ def test_a_visible_key_that_is_not_a_number_makes_its_rows_nan_wherever_it_is(E,
             hit[0, i] = at < L or m >= 0
         assert status == 0 and out[hit].isnan().all(), at
         assert torch.equal(out[~hit].view(torch.int16), want[~hit].view(torch.int16)), at
+
+
+def test_the_largest_values_in_tree_slots_that_a_row_does_not_see(E, oracle):
+    """The weight of a sibling is 0, whatever finite value stands there."""
+    cfg = W.scaled(W.CONFIGS["tiny"], batch=2, num_q_heads=4, num_kv_heads=2, head_dim=128, prefix=(0, 300), tree=(64, 64), max_depth=2)
+    inp = W.make_attn_inputs(cfg, salt=22)
+    seen = torch.zeros(2, 64, 64, dtype=torch.bool)      # [sequence, node, its ancestors and itself]
+    for b in range(2):
+        for i in range(64):
+            m = i
+            while m >= 0:
+                seen[b, i, m] = True
+                m = int(inp.tree_parent[b, m])
+    big = torch.arange(64) >= 40                          # these nodes' values are the largest: rows that see none of them keep theirs
+    for b in range(2):
+        inp.v_cache[b, :, int(inp.seq_lens[b]) + torch.nonzero(big).flatten()] = 3e38
+    rows = ~(seen & big).any(-1)
+    assert int(rows.sum()) > 40
+    ref = oracle.tree_verify_attn(inp.q, inp.k_cache, inp.v_cache, inp.seq_lens, inp.tree_parent, inp.tree_sizes)
+    out, status = _run(E, inp)
+    err = np.abs(out.double().numpy() - ref)[rows.numpy()]
+    assert status == 0 and err.max() <= MAX_ABS and err.mean() <= MEAN_ABS, err.max()
