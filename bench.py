@@ -51,10 +51,9 @@ SM_COUNT, EX2_PER_SM_PER_CLK = 148, 16      # special-function rate behind the e
 # profiles/attn_kernel_serving_mix_b16.md, keyed by (workload, batch), with the SHA-256 of the attention kernel's source
 # the captures were taken on: when the source has changed since, the figure is stale and `traffic` is reported as null.
 NCU_TRAFFIC = {
-    "attn_cu_sha256": "45abb4aec25ea42f4cba9b9c12940521db7b31208c3f05b689e433d667c06e1e",
-    # full size: one-pass metric list, two launches averaged (1176.3 MB read + 22.8 MB written); batch 16: --set full
-    # (taken before the epilogue's stores changed; the reads it measures did not)
-    "bytes": {("serving_mix", 64): 1_176_343_168 + 22_765_312, ("serving_mix", 16): 313_046_528 + 9_554_304},
+    "attn_cu_sha256": "cded3ed9770290e99a8df23dbe84729e972d62750621df8be034c7dc2d269e0c",
+    # one-pass metric list, two launches averaged: full size 1176.2 MB read + 23.1 MB written, batch 16 313.1 + 6.8 MB
+    "bytes": {("serving_mix", 64): 1_176_164_000 + 23_070_592, ("serving_mix", 16): 313_080_832 + 6_835_968},
 }
 
 

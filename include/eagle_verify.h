@@ -94,7 +94,9 @@ size_t eagle_tree_verify_attn_workspace(const eagle_attn_desc* desc);
  *                                                 over j < L_b and j = L_b + m, m an ancestor of i or i itself;
  *                                                 rows of nodes i >= tree size are written as zeros
  *
- * Arithmetic: bf16 inputs, fp32 scores / softmax / accumulation, bf16 output (round to nearest even).
+ * Arithmetic: bf16 inputs, fp32 scores / softmax / accumulation, bf16 output (round to nearest even).  |scale * q.k| has to stay
+ * below 2^20, 2^17 with an fp8 cache: the row maximum that the exponentials are relative to has 16 significant bits.  A score of a
+ * visible key that is NaN or +infinite makes the rows that see it NaN.
  * q, k_cache and v_cache must be 16-byte aligned, out 32-byte aligned (else EAGLE_ERR_SHAPE).  Launches, in order on `stream`: the planner (tree masks +
  * work list), the split-KV attention kernel, the combine kernel.  The workspace must not be shared by
  * calls that can overlap on the GPU.
