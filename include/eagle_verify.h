@@ -49,7 +49,8 @@ enum {
   EAGLE_ERR_TIMEOUT = -8,    /* device-detected: a bounded wait inside a kernel ran out */
   EAGLE_ERR_DEVICE = -9,     /* the GPU is not an sm_100 device, or it lacks a required limit */
   EAGLE_ERR_PATH = -10,      /* device-detected: an accepted path that is not an increasing list of tree nodes whose slots exist */
-  EAGLE_ERR_PAGE = -11       /* device-detected: a block-table entry of a page in use outside [0, num_pages) */
+  EAGLE_ERR_PAGE = -11,        /* device-detected: a block-table entry of a page in use outside [0, num_pages) */
+  EAGLE_ERR_ROW = -12          /* device-detected: a row of logits whose values are all -infinity or NaN: nothing can be drawn from it */
 };
 
 #define EAGLE_MAX_TREE 64
@@ -642,6 +643,152 @@ typedef struct eagle_logits_desc {
  */
 int eagle_tree_logits_adjust(const eagle_logits_desc* desc, const void* logits, const int32_t* draft_tokens, const int32_t* tree_parent,
                              float* out, eagle_stream_t stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------------------------------
+ * A cache in 8 bits with a scale for each block of slots and head; attention with a sliding window and a few first slots that stay
+ * visible; sampling with temperature, top-k, top-p and min-p.
+ */
+
+/*
+ * The block-scaled cache.  The calls below take an eagle_kv_store whose k and v hold e4m3 codes (as for eagle_tree_verify_attn_fp8,
+ * head_dim 128) together with a block size in their descriptor: BS = 16, 32, 64 or 128 slots of one KV head share one fp32 scale,
+ *     key = value(code) * k_scale[block],  value = value(code) * v_scale[block].
+ *   contiguous: codes [B, Hkv, kv_capacity, 128], scales [B, Hkv, kv_capacity / BS], kv_capacity a multiple of BS
+ *   paged:      codes [num_pages, Hkv, page_size, 128], scales [num_pages, Hkv, page_size / BS], page_size a multiple of BS
+ * The range of a sequence's keys need not be known when it starts, as it has to be with one scale per (sequence, KV head): a block's
+ * scale follows what is stored in it.  The append calls write the scales although the struct declares them const.
+ */
+typedef struct eagle_block_desc {
+  int32_t batch;                /* B, 0 .. 65535 */
+  int32_t num_tokens;           /* N >= 0: rows of q, k, v and q_out (chunk form) */
+  int32_t max_tree;             /* T_max <= 64 (tree form; q, k, v and q_out have B * T_max rows) */
+  int32_t num_q_heads;          /* Hq >= 0 (0: only the cache is written) */
+  int32_t num_kv_heads;         /* Hkv >= 1 */
+  int32_t rotary_dim;           /* R: a multiple of 16, <= 128, as for eagle_rope_append */
+  int32_t interleaved;          /* 0: element m turns with m + R/2; nonzero: element 2m with 2m + 1 */
+  int32_t block_size;           /* BS */
+  float amplitude;              /* factor on sines and cosines; 0 means 1 */
+  int64_t q_stride, k_stride, v_stride;   /* as for eagle_rope_append (head_dim is 128) */
+  const double* freqs;          /* device double [R / 2], radians per position */
+  const int32_t* positions;     /* chunk form: device int32 [N], or NULL: a token's position is its slot */
+  const int32_t* tree_sizes;    /* tree form: device int32 [B] ([1] when shared_tree is set), or NULL */
+  int32_t shared_tree;          /* tree form, nonzero: tree_parent is int32 [T_max], one tree for every sequence */
+  int32_t* status;              /* device int32 or NULL */
+} eagle_block_desc;
+
+/*
+ * Rotary positions of new tokens, and their keys and values into a block-scaled cache, in one launch.  Rows, positions, slots, strides,
+ * q_out and what is reported are those of eagle_rope_append; what differs is how keys and values are stored.  Per KV head, for keys
+ * and values alike, the new tokens of a block (rotated in fp32, not rounded before) with the largest finite magnitude a need the scale
+ *     s(a) = 2^e, e the least whole number from -40 to 120 with a <= 448 * 2^e       (e = -40 where nothing is finite, or all is 0).
+ * A block that begins at or behind slot L_b takes it.  The block that slot L_b lies inside of holds older slots: it keeps its scale if that is
+ * at least s(a), and takes s(a) otherwise, its older codes then stored again as the nearest code of value(code) * old / new.  New codes are the
+ * nearest e4m3 code of x / scale in fp32 (ties to the even code, magnitudes above 448 become 448, NaN stays NaN).
+ * A power of two loses nothing against a finer scale, since codes are floating-point numbers, and storing older codes again costs them
+ * at most the bits that leave the bottom of the range.  An old scale has to be a normal number above 0; blocks that hold no slot of a sequence
+ * in use may have any.  No block may be shared by two sequences that append.
+ */
+int eagle_block_append(const eagle_block_desc* desc, const void* q, const void* k, const void* v, void* q_out, const eagle_kv_store* kv,
+                       const int32_t* seq_lens, const int32_t* token_start, eagle_stream_t stream);
+
+/*
+ * The same for the nodes of draft trees, in the layout of eagle_tree_rope_append.  All blocks that a tree's slots L_b .. L_b + n_b - 1 lie in
+ * take one scale per KV head: s(a) of the whole tree, or that of the block that holds older slots where it is larger.  So the accepted
+ * path is committed by eagle_tree_commit / eagle_tree_commit_paged on the codes (head_dim 64 there), as for any cache of codes: rows move as bytes
+ * between blocks of one scale.
+ */
+int eagle_tree_block_append(const eagle_block_desc* desc, const void* q, const void* k, const void* v, void* q_out, const eagle_kv_store* kv,
+                            const int32_t* seq_lens, const int32_t* tree_parent, eagle_stream_t stream);
+
+typedef struct eagle_window_desc {
+  int32_t batch;                /* B, 0 .. 65535 */
+  int32_t num_tokens;           /* N >= 0: rows of q and out (chunk form) */
+  int32_t max_tree;             /* T_max, 0 .. 64 (tree form; q and out have B * T_max rows); ignored by the chunk form */
+  int32_t num_q_heads;          /* Hq; Hq % Hkv == 0, group size G = Hq / Hkv <= 16 */
+  int32_t num_kv_heads;         /* Hkv */
+  int32_t head_dim;             /* D: 64 or 128; 128 with a block-scaled cache */
+  int32_t block_size;           /* 0: a bf16 cache; else the block-scaled cache's BS */
+  int32_t window;               /* W: 0 for no limit; tree form: 0 or at least EAGLE_MAX_TREE, so that a node's own path is always inside */
+  int32_t sinks;                /* S >= 0: the first S slots stay visible (no effect with W = 0) */
+  float sm_scale;               /* softmax scale, > 0; 0 means 1/sqrt(D) */
+  const int32_t* tree_sizes;    /* tree form: device int32 [B] ([1] when shared_tree is set), or NULL */
+  int32_t shared_tree;          /* tree form, nonzero: tree_parent is int32 [T_max], one tree for every sequence */
+  void* workspace;              /* device, 256-byte aligned, >= eagle_window_attn_workspace() bytes */
+  size_t workspace_bytes;
+  int32_t* status;              /* device int32 or NULL */
+} eagle_window_desc;
+
+/* Bytes of scratch one call with this descriptor, or with fewer tokens, needs: of the chunk form with max_tree = 0, else of the tree form
+ * (host function, no CUDA work); 0 if the shape is unsupported. */
+size_t eagle_window_attn_workspace(const eagle_window_desc* desc);
+
+/*
+ * Attention of one layer for chunks of new tokens, as eagle_chunk_attn, with a sliding window and over a cache in either form.
+ * The token at position p (its slot, L_b + i) sees the key of slot j iff
+ *     j <= p  and  (W = 0  or  j > p - W  or  j < S).
+ * kv holds bf16 (block_size 0, no scales) or block-scaled codes.  Keys and values of slots that no token of the call sees are not used,
+ * pages that hold only such slots are not read and their block-table entries may be anything: pages that a window has left behind may go back
+ * to the pool.  Work is proportional to what is visible.
+ *
+ * Arithmetic: as for eagle_chunk_attn over bf16.  Over codes the products are fp16 (every e4m3 number is one exactly): a query row is
+ * scaled by a power of two so that its largest magnitude is in [1, 2), then rounded to fp16 (half a step is 2^-12 of an element, and 2^-25 of the
+ * row's largest for those below 2^-14 of it); scores take their block's scale in fp32; a probability times its block's value scale is
+ * rounded to fp16; sums are fp32.  Scales of values have to be from 2^-60 to 2^60, those of keys normal numbers above 0.
+ * A visible score that is NaN or +infinite makes its row NaN.  Slots past the chunk may hold anything; what holds for slots in use and for the size of scores is
+ * as for eagle_chunk_attn (values of slots in use have to be finite), with NaN codes in the place of values that are not.
+ * Device-detected errors, rows outside every sequence, time-outs, launches and the rule N <= B are those of eagle_chunk_attn, too.
+ */
+int eagle_window_attn(const eagle_window_desc* desc, const void* q, const eagle_kv_store* kv, const int32_t* seq_lens,
+                      const int32_t* token_start, void* out, eagle_stream_t stream);
+
+/*
+ * The same for the nodes of draft trees, in the layout of eagle_tree_verify_attn: q and out are device bf16 [B, T_max, Hq, D], node i of
+ * sequence b lies in slot L_b + i, at position p = L_b + depth(i) - 1, and sees the prefix's slots j < L_b with (W = 0 or j > p - W or j < S), its
+ * ancestors and itself.  Rows of nodes >= tree size are written as zeros.  An invalid tree reports EAGLE_ERR_TREE, a tree that does not fit
+ * EAGLE_ERR_SEQ: the sequence's rows are zeros.
+ */
+int eagle_tree_window_attn(const eagle_window_desc* desc, const void* q, const eagle_kv_store* kv, const int32_t* seq_lens,
+                           const int32_t* tree_parent, void* out, eagle_stream_t stream);
+
+#define EAGLE_MAX_SAMPLE_VOCAB (1 << 20)
+
+typedef struct eagle_sample_desc {
+  int32_t batch;                /* B, 0 .. 65535 */
+  int32_t rows;                 /* R >= 0: rows per sequence (1: plain decoding; T_max + 1: the target's rows of a draft tree) */
+  int32_t vocab;                /* V, 1 .. EAGLE_MAX_SAMPLE_VOCAB */
+  int32_t bf16;                 /* 0: logits are fp32; nonzero: bf16 */
+  const int32_t* num_rows;      /* device int32 [B], or NULL: R rows each (clamped to [0, R]); later rows are neither read nor written */
+  const float* temperature;     /* device fp32 [B] or NULL (1); a temperature that is not above 0 is greedy */
+  const int32_t* top_k;         /* device int32 [B] or NULL (off); k <= 0 or >= V is off */
+  const float* top_p;           /* device fp32 [B] or NULL (off); 1 or more, and NaN, is off */
+  const float* min_p;           /* device fp32 [B] or NULL (off); 0 or less, and NaN, is off */
+  int32_t* status;              /* device int32 or NULL */
+} eagle_sample_desc;
+
+/*
+ * Sampling with temperature, top-k, top-p and min-p: a token per row, and / or the distribution that it is drawn from.  The rows are those that
+ * eagle_tree_logits_adjust leaves (or bf16 rows of the output layer); the distributions are what eagle_tree_accept takes as target_probs
+ * and draft_probs and eagle_tree_expand as draft_probs, so that acceptance stays exact under these filters (Algorithm 1 returns exactly the
+ * distribution that it is given).
+ *
+ *   logits   device fp32 or bf16 [B, R, V]
+ *   uniforms device fp32 [B, R] in [0, 1), or NULL with tokens NULL
+ *   tokens   device int32 [B, R] or NULL
+ *   probs    device fp32 [B, R, V] or NULL; may not be `logits`
+ *
+ * With w(v) = exp((z(v) - max z) / temperature) and the tokens in descending order of z, equal ones in ascending order of their id:
+ *   top-k   the first k tokens stay
+ *   top-p   of these, a token stays if the w of those before it sum to less than p times the sum of all of these (the first always does)
+ *   min-p   of these, those with w >= min(min_p, 1) stay
+ * probs are w over the sum of what stays, 0 elsewhere; the token is the smallest v with sum_{x <= v} w(x) > u times that sum, over what
+ * stays, in ascending order of the id.  A greedy row keeps the first token alone.  NaN logits count as -infinity; where some are +infinity these
+ * share the mass.  A row without any value above -infinity reports EAGLE_ERR_ROW: token -1, probs 0.
+ *
+ * Orders are exact; w is taken in fp64 (error below 2^-45) and summed in integers, so results do not depend on how the work is split, and a decision can
+ * differ from the definition only within about 1e-12 of its boundary.  One launch; no workspace.
+ */
+int eagle_sample(const eagle_sample_desc* desc, const void* logits, const float* uniforms, int32_t* tokens, float* probs, eagle_stream_t stream);
 
 /* Human-readable name of a return / status code (host function; never NULL). */
 const char* eagle_status_string(int code);

@@ -26,7 +26,8 @@ EXPORTS = ["eagle_tree_verify_attn_workspace", "eagle_tree_verify_attn", "eagle_
            "eagle_tree_verify_attn_fp8", "eagle_tree_verify_attn_planned_fp8", "eagle_tree_verify_attn_paged_fp8",
            "eagle_tree_verify_attn_planned_paged_fp8", "eagle_tree_accept_cluster_width_greedy", "eagle_rope_frequencies",
            "eagle_rope_append", "eagle_tree_rope_append", "eagle_chunk_attn_workspace", "eagle_chunk_attn",
-           "eagle_tree_logits_adjust"]
+           "eagle_tree_logits_adjust", "eagle_block_append", "eagle_tree_block_append", "eagle_window_attn_workspace", "eagle_window_attn",
+           "eagle_tree_window_attn", "eagle_sample"]
 _lib = None
 
 
@@ -102,6 +103,26 @@ class LogitsDesc(ctypes.Structure):
                 ("bias_len", ctypes.c_void_p), ("allowed", ctypes.c_void_p), ("status", ctypes.c_void_p)]
 
 
+class BlockDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("batch", "num_tokens", "max_tree", "num_q_heads", "num_kv_heads", "rotary_dim", "interleaved",
+                                               "block_size")] + [("amplitude", ctypes.c_float)] +
+                [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")] +
+                [("freqs", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("tree_sizes", ctypes.c_void_p), ("shared_tree", ctypes.c_int32),
+                 ("status", ctypes.c_void_p)])
+
+
+class WindowDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("batch", "num_tokens", "max_tree", "num_q_heads", "num_kv_heads", "head_dim", "block_size", "window",
+                                               "sinks")] +
+                [("sm_scale", ctypes.c_float), ("tree_sizes", ctypes.c_void_p), ("shared_tree", ctypes.c_int32), ("workspace", ctypes.c_void_p),
+                 ("workspace_bytes", ctypes.c_size_t), ("status", ctypes.c_void_p)])
+
+
+class SampleDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("batch", "rows", "vocab", "bf16")] +
+                [(n, ctypes.c_void_p) for n in ("num_rows", "temperature", "top_k", "top_p", "min_p", "status")])
+
+
 def load():
     """Loads the shared library (once).  Raises if it has not been built."""
     global _lib
@@ -174,6 +195,16 @@ def load():
         lib.eagle_chunk_attn.restype = ctypes.c_int
         lib.eagle_tree_logits_adjust.argtypes = [ctypes.POINTER(LogitsDesc), vp, vp, vp, vp, vp]
         lib.eagle_tree_logits_adjust.restype = ctypes.c_int
+        for fn in (lib.eagle_block_append, lib.eagle_tree_block_append):
+            fn.argtypes = [ctypes.POINTER(BlockDesc), vp, vp, vp, vp, ctypes.POINTER(KVStoreDesc), vp, vp, vp]
+            fn.restype = ctypes.c_int
+        lib.eagle_window_attn_workspace.argtypes = [ctypes.POINTER(WindowDesc)]
+        lib.eagle_window_attn_workspace.restype = ctypes.c_size_t
+        for fn in (lib.eagle_window_attn, lib.eagle_tree_window_attn):
+            fn.argtypes = [ctypes.POINTER(WindowDesc), vp, ctypes.POINTER(KVStoreDesc), vp, vp, vp, vp]
+            fn.restype = ctypes.c_int
+        lib.eagle_sample.argtypes = [ctypes.POINTER(SampleDesc), vp, vp, vp, vp, vp]
+        lib.eagle_sample.restype = ctypes.c_int
         lib.eagle_status_string.argtypes = [ctypes.c_int]
         lib.eagle_status_string.restype = ctypes.c_char_p
         lib.eagle_launch_count.restype = ctypes.c_uint64
@@ -632,16 +663,22 @@ def _stream_of(dev):
 
 class KVStore:
     """A cache as the calls around verification take it: k / v [B,Hkv,S,D], or [num_pages,Hkv,page_size,D] with ``block_table``
-    [B,max_pages_per_seq] int32; bf16, or uint8 e4m3 codes with ``k_scale`` / ``v_scale`` fp32 [B,Hkv].  Holds the tensors."""
+    [B,max_pages_per_seq] int32; bf16, or uint8 e4m3 codes with ``k_scale`` / ``v_scale`` fp32 [B,Hkv], or with ``block_size`` (slots that
+    share a scale) fp32 [B or num_pages,Hkv,slots / block_size].  Holds the tensors."""
 
-    def __init__(self, k, v, *, block_table=None, k_scale=None, v_scale=None):
+    def __init__(self, k, v, *, block_table=None, k_scale=None, v_scale=None, block_size=0):
         if k.dim() != 4 or k.shape != v.shape or (k_scale is None) != (v_scale is None) or (block_table is not None and block_table.dim() != 2):
             raise EagleError("bad cache: k and v of one 4-d shape, both scales or neither, a 2-d block table")
+        self.block_size = int(block_size)
+        if self.block_size and (k_scale is None or self.block_size < 0 or k.shape[2] % self.block_size):
+            raise EagleError("bad cache: blocks need scales, and slots (of a page) that are a multiple of the block size")
         self.k, self.v, self.block_table, self.k_scale, self.v_scale = k, v, block_table, k_scale, v_scale
         self.num_kv_heads, self.head_dim, self.fp8 = k.shape[1], k.shape[3], k_scale is not None
         self.batch = k.shape[0] if block_table is None else block_table.shape[0]
         dtype, dev = torch.uint8 if self.fp8 else torch.bfloat16, k.device
         scales = torch.Size((self.batch, self.num_kv_heads)) if self.fp8 else None
+        if self.block_size:
+            scales = torch.Size((k.shape[0], k.shape[1], k.shape[2] // self.block_size))
         paged = block_table is not None
         self.desc = KVStoreDesc(_here(k, dtype, "k", dev), _here(v, dtype, "v", dev), _here(k_scale, torch.float32, "k_scale", dev, scales),
                                 _here(v_scale, torch.float32, "v_scale", dev, scales), 0 if paged else k.shape[2],
@@ -682,7 +719,7 @@ def _rope_rows(t, name, lead, dev):
     return t.data_ptr(), row
 
 
-def _rope_append(name, tree, q, k, v, kv, seq_lens, order, freqs, q_out, interleaved, amplitude, positions, tree_sizes, shared_tree, status):
+def _rope_append(name, tree, blocks, q, k, v, kv, seq_lens, order, freqs, q_out, interleaved, amplitude, positions, tree_sizes, shared_tree, status):
     dev, lead = _current(q, "q"), q.shape[:-2]
     if q.dim() != (4 if tree else 3) or k.dim() != q.dim() or v.dim() != q.dim():
         raise EagleError("q, k, v must be " + ("[B, T, heads, D]" if tree else "[N, heads, D]"))
@@ -690,6 +727,8 @@ def _rope_append(name, tree, q, k, v, kv, seq_lens, order, freqs, q_out, interle
     if k.shape[-1] != D or v.shape[-2:] != k.shape[-2:] or kv.head_dim != D or kv.num_kv_heads != Hkv or kv.batch != B or kv.k.device != dev or \
             freqs.dim() != 1 or (tree and lead[0] != B):
         raise EagleError("inconsistent shapes")
+    if bool(kv.block_size) != blocks:
+        raise EagleError("the cache must be block-scaled" if blocks else "a block-scaled cache takes eagle_block_append")
     T = lead[1] if tree else 0
     if tree:
         _check_tree(order, tree_sizes, B, T, shared_tree)
@@ -700,7 +739,11 @@ def _rope_append(name, tree, q, k, v, kv, seq_lens, order, freqs, q_out, interle
     qp, qs = _rope_rows(q, "q", lead, dev)
     kp, ks = _rope_rows(k, "k", lead, dev)
     vp, vs = _rope_rows(v, "v", lead, dev)
-    d = RopeDesc(B, 0 if tree else lead[0], T, Hq, Hkv, D, 2 * freqs.shape[0], 1 if interleaved else 0, float(amplitude), qs, ks, vs,
+    if blocks and D != 128:
+        raise EagleError("a block-scaled cache has heads of 128")
+    shape = (B, 0 if tree else lead[0], T, Hq, Hkv) + (() if blocks else (D,)) + (2 * freqs.shape[0], 1 if interleaved else 0) + \
+        ((kv.block_size,) if blocks else ())
+    d = (BlockDesc if blocks else RopeDesc)(*shape, float(amplitude), qs, ks, vs,
                  _here(freqs, torch.float64, "freqs", dev), _here(positions, torch.int32, "positions", dev, lead),
                  _here(tree_sizes, torch.int32, "tree_sizes", dev), 1 if shared_tree else 0, _here(status, torch.int32, "status", dev))
     rc = getattr(load(), name)(ctypes.byref(d), qp, kp, vp, _here(q_out, torch.bfloat16, "q_out", dev, q.shape), ctypes.byref(kv.desc),
@@ -714,7 +757,7 @@ def eagle_rope_append(q, k, v, kv, seq_lens, token_start, freqs, q_out=None, *, 
     """Rotary positions of packed new tokens, keys and values into the cache ``kv`` (a ``KVStore``) IN PLACE.  q [N,Hq,D], k / v
     [N,Hkv,D] bf16 (slices of one projection's rows are taken as they are); token_start [B+1] int32; freqs fp64 [R/2].
     Returns q_out [N,Hq,D]; rows outside every sequence are left as they are."""
-    return _rope_append("eagle_rope_append", False, q, k, v, kv, seq_lens, token_start, freqs, q_out, interleaved, amplitude, positions, None, False,
+    return _rope_append("eagle_rope_append", False, False, q, k, v, kv, seq_lens, token_start, freqs, q_out, interleaved, amplitude, positions, None, False,
                         status)
 
 
@@ -722,8 +765,22 @@ def eagle_tree_rope_append(q, k, v, kv, seq_lens, tree_parent, freqs, q_out=None
                            status=None, shared_tree=False):
     """The same for the nodes of draft trees: q [B,T,Hq,D], k / v [B,T,Hkv,D]; a node's position is its sequence's length plus
     its depth - 1, its slot the length plus its index."""
-    return _rope_append("eagle_tree_rope_append", True, q, k, v, kv, seq_lens, tree_parent, freqs, q_out, interleaved, amplitude, None, tree_sizes,
+    return _rope_append("eagle_tree_rope_append", True, False, q, k, v, kv, seq_lens, tree_parent, freqs, q_out, interleaved, amplitude, None, tree_sizes,
                         shared_tree, status)
+
+
+def eagle_block_append(q, k, v, kv, seq_lens, token_start, freqs, q_out=None, *, interleaved=False, amplitude=1.0, positions=None, status=None):
+    """``eagle_rope_append`` into a block-scaled cache (a ``KVStore`` with ``block_size``): codes and the blocks' scales are written IN PLACE."""
+    return _rope_append("eagle_block_append", False, True, q, k, v, kv, seq_lens, token_start, freqs, q_out, interleaved, amplitude, positions, None,
+                        False, status)
+
+
+def eagle_tree_block_append(q, k, v, kv, seq_lens, tree_parent, freqs, q_out=None, *, tree_sizes=None, interleaved=False, amplitude=1.0,
+                            status=None, shared_tree=False):
+    """``eagle_tree_rope_append`` into a block-scaled cache; the blocks of a tree's slots take one scale per KV head, so that the accepted path is
+    committed by ``eagle_tree_commit`` / ``eagle_tree_commit_paged`` on the codes."""
+    return _rope_append("eagle_tree_block_append", True, True, q, k, v, kv, seq_lens, tree_parent, freqs, q_out, interleaved, amplitude, None,
+                        tree_sizes, shared_tree, status)
 
 
 def eagle_chunk_attn_workspace(batch, num_tokens, num_q_heads, num_kv_heads, head_dim) -> int:
@@ -787,6 +844,80 @@ def eagle_tree_logits_adjust(logits, draft_tokens=None, tree_parent=None, out=No
                                          _here(tree_parent, i32, "tree_parent", dev) if T else None, _here(out, f32, "out", dev, logits.shape), _stream_of(dev))
     _check(rc, "eagle_tree_logits_adjust")
     return out
+
+
+def eagle_window_attn_workspace(batch, num_tokens, num_q_heads, num_kv_heads, head_dim, *, max_tree=0) -> int:
+    """Bytes for a call over ``num_tokens`` packed rows or fewer, or with ``max_tree`` over trees (``num_tokens`` is not used then)."""
+    d = WindowDesc(batch, num_tokens, max_tree, num_q_heads, num_kv_heads, head_dim)
+    n = load().eagle_window_attn_workspace(ctypes.byref(d))
+    if n == 0:
+        raise EagleError("unsupported attention shape")
+    return int(n)
+
+
+def _window_attn(name, tree, q, kv, seq_lens, order, out, tree_sizes, shared_tree, window, sinks, sm_scale, workspace, status):
+    dev = _current(q, "q")
+    if q.dim() != (4 if tree else 3) or kv.head_dim != q.shape[-1] or kv.batch != seq_lens.numel() or kv.k.device != dev or (tree and q.shape[0] != kv.batch):
+        raise EagleError("inconsistent shapes (q " + ("[B, T, Hq, D]" if tree else "[N, Hq, D]") + ", a cache of as many sequences as seq_lens)")
+    if kv.fp8 and not kv.block_size:
+        raise EagleError("the cache must be bf16 or block-scaled")
+    B, Hq, D, T = kv.batch, q.shape[-2], q.shape[-1], q.shape[1] if tree else 0
+    if tree:
+        _check_tree(order, tree_sizes, B, T, shared_tree)
+    elif order.shape != (B + 1,):
+        raise EagleError("token_start must be [B + 1]")
+    N = 0 if tree else q.shape[0]
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None and (T if tree else N) > 0:
+        workspace = torch.empty(eagle_window_attn_workspace(B, N, Hq, kv.num_kv_heads, D, max_tree=T), dtype=torch.uint8, device=dev)
+    d = WindowDesc(B, N, T, Hq, kv.num_kv_heads, D, kv.block_size, int(window), int(sinks), float(sm_scale),
+                   _here(tree_sizes, torch.int32, "tree_sizes", dev), 1 if shared_tree else 0, _here(workspace, torch.uint8, "workspace", dev),
+                   0 if workspace is None else workspace.numel(), _here(status, torch.int32, "status", dev))
+    rc = getattr(load(), name)(ctypes.byref(d), _here(q, torch.bfloat16, "q", dev), ctypes.byref(kv.desc), _here(seq_lens, torch.int32, "seq_lens", dev),
+                               _here(order, torch.int32, "tree_parent" if tree else "token_start", dev), _here(out, torch.bfloat16, "out", dev, q.shape),
+                               _stream_of(dev))
+    _check(rc, name)
+    return out
+
+
+def eagle_window_attn(q, kv, seq_lens, token_start, out=None, *, window=0, sinks=0, sm_scale=0.0, workspace=None, status=None):
+    """``eagle_chunk_attn`` with a sliding window (the token at position p sees slots j <= p with j > p - window, or j < sinks; 0: no limit) over a
+    bf16 or block-scaled ``KVStore``.  q [N,Hq,D] bf16.  Returns out [N,Hq,D]; rows outside every sequence are left as they are."""
+    return _window_attn("eagle_window_attn", False, q, kv, seq_lens, token_start, out, None, False, window, sinks, sm_scale, workspace, status)
+
+
+def eagle_tree_window_attn(q, kv, seq_lens, tree_parent, out=None, *, tree_sizes=None, shared_tree=False, window=0, sinks=0, sm_scale=0.0,
+                           workspace=None, status=None):
+    """The same for draft trees: q [B,T,Hq,D] bf16; a node sees the prefix within the window of its position (or among the sinks), its
+    ancestors and itself.  Returns out [B,T,Hq,D]; rows of nodes past a tree's size are zeros."""
+    return _window_attn("eagle_tree_window_attn", True, q, kv, seq_lens, tree_parent, out, tree_sizes, shared_tree, window, sinks, sm_scale, workspace,
+                        status)
+
+
+def eagle_sample(logits, uniforms=None, tokens=None, probs=None, *, temperature=None, top_k=None, top_p=None, min_p=None, num_rows=None,
+                 with_probs=False, status=None):
+    """Sampling from rows of logits [B,R,V] (fp32 or bf16) with per-sequence temperature / top_p / min_p (fp32 [B]) and top_k (int32 [B]):
+    tokens int32 [B,R] where ``uniforms`` fp32 [B,R] are given, and the filtered distributions fp32 [B,R,V] where ``probs`` or ``with_probs``
+    asks for them.  ``num_rows`` int32 [B]: rows in use, the others stay as they are.  Returns (tokens, probs)."""
+    dev = _current(logits, "logits")
+    if logits.dim() != 3 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise EagleError("logits must be fp32 or bf16 [B, R, V]")
+    B, R, V = logits.shape
+    per_seq, per_row, f32, i32 = torch.Size((B,)), torch.Size((B, R)), torch.float32, torch.int32
+    if uniforms is None and tokens is not None:
+        raise EagleError("tokens need uniforms")
+    if uniforms is not None and tokens is None:
+        tokens = torch.empty(per_row, dtype=i32, device=dev)
+    if probs is None and with_probs:
+        probs = torch.empty(logits.shape, dtype=f32, device=dev)
+    d = SampleDesc(B, R, V, 1 if logits.dtype == torch.bfloat16 else 0, _here(num_rows, i32, "num_rows", dev, per_seq),
+                   _here(temperature, f32, "temperature", dev, per_seq), _here(top_k, i32, "top_k", dev, per_seq), _here(top_p, f32, "top_p", dev, per_seq),
+                   _here(min_p, f32, "min_p", dev, per_seq), _here(status, i32, "status", dev))
+    rc = load().eagle_sample(ctypes.byref(d), _here(logits, logits.dtype, "logits", dev), _here(uniforms, f32, "uniforms", dev, per_row),
+                             _here(tokens, i32, "tokens", dev, per_row), _here(probs, f32, "probs", dev, logits.shape), _stream_of(dev))
+    _check(rc, "eagle_sample")
+    return tokens, probs
 
 
 class HostStepRunner:

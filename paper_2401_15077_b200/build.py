@@ -13,7 +13,7 @@ SOURCES = sorted((PKG / "csrc").glob("*.cu"))
 HEADERS = sorted((PKG / "csrc").glob("*.cuh")) + [ROOT / "include" / "eagle_verify.h"]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
 
 
 def needs_build() -> bool:

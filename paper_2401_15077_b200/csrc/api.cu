@@ -754,6 +754,7 @@ const char* eagle_status_string(int code) {
     case EAGLE_ERR_DEVICE: return "no usable sm_100 device is current";
     case EAGLE_ERR_PATH: return "invalid accepted path (not increasing, outside the tree, or past the cache)";
     case EAGLE_ERR_PAGE: return "block-table entry of a page in use outside the page pool";
+    case EAGLE_ERR_ROW: return "a row of logits that nothing can be drawn from";
     default: return "unknown status";
   }
 }

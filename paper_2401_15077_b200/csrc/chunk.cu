@@ -85,6 +85,9 @@ __device__ __forceinline__ int cut_tile(long long pos, long long x, int tiles) {
 // stays within its equal share W / P: they then start neighbouring units at the same time, walk the same keys at the same
 // pace and share them through L2.  The units that are left are cut in contiguous shares that fill each worker up to W / P exactly,
 // so the split needs at most P - 1 cuts whatever the lengths are.
+// SPAN (calls with a window or a tree): sequences may come as trees, which are checked here, and with a window a unit costs at most the
+// window, the sinks and its own tokens, rounded up by two tiles (its true number of tiles depends on where the window begins).
+template <bool SPAN>
 __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p) {
   __shared__ Sum2 s_warp[kPlanThreads / 32];
   __shared__ long long s_pos[kMaxPlanCtas + 1], s_cost[kNearSeqs], s_x[kNearUnits + 1];
@@ -99,13 +102,58 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
   launch_dependents();
   // the packed layout has to be an ascending list of starts inside the tensor: everything below relies on it
   int bad = 0;
+  const bool tree = SPAN && p.tree > 0;
+  if (tree) {
+    // a tree that is not one is noted where the pages that do not exist will be, and refused with its sequence
+    for (int b = tid; b < B; b += kPlanThreads) {
+      const int n = p.tree_sizes ? p.tree_sizes[p.shared_tree ? 0 : b] : p.tree;
+      w.bad_page[b] = n < 0 || n > p.tree;
+    }
+    __syncthreads();
+    const long long nodes = static_cast<long long>(p.shared_tree ? 1 : B) * p.tree;
+    for (long long at = tid; at < nodes; at += kPlanThreads) {
+      const int b = static_cast<int>(at / p.tree), i = static_cast<int>(at - static_cast<long long>(b) * p.tree);
+      const int n = p.tree_sizes ? p.tree_sizes[b] : p.tree, up = p.tree_parent[at];
+      if (i < n && (up < -1 || up >= i)) w.bad_page[b] = 1;
+    }
+    __syncthreads();
+    if (p.shared_tree) {
+      const int wrong = w.bad_page[0];
+      __syncthreads();
+      for (int b = tid; b < B; b += kPlanThreads) w.bad_page[b] = wrong;
+      __syncthreads();
+    }
+  }
   for (int b = tid; b < B; b += kPlanThreads) {
-    const int s = p.token_start[b], e = p.token_start[b + 1];
-    if (s < 0 || e < s || e > p.N) bad = 1;
+    int s, e;
+    if (tree) {
+      const int n = p.tree_sizes ? p.tree_sizes[p.shared_tree ? 0 : b] : p.tree;
+      s = b * p.tree;
+      e = s + n;
+      if (w.bad_page[b]) {
+        e = s;
+        report_status(p.status, EAGLE_ERR_TREE);
+      }
+    } else {
+      s = p.token_start[b];
+      e = p.token_start[b + 1];
+      if (s < 0 || e < s || e > p.N) bad = 1;
+    }
     if (b < kNearSeqs) s_seq[b] = ChunkSeq{s, e - s, p.seq_lens[b], 0};
   }
   bad = __syncthreads_or(bad);
   if (bad && tid == 0) report_status(p.status, EAGLE_ERR_SEQ);
+
+  // With a window: the cost of a unit that ends `keys` slots into its sequence, and of the whole parts [lo, hi).
+  const bool windowed = SPAN && p.window > 0;
+  const long long cap = windowed ? static_cast<long long>(p.window) + ut + (p.sinks + kChunkTile - 1) / kChunkTile * kChunkTile + 2 * kChunkTile : 0;
+  auto capped = [&](const ChunkSeq&, long long keys) { return (keys < cap ? keys : cap) + kChunkItemKeys; };
+  auto between = [&](const ChunkSeq& q, int lo, int hi) {
+    const long long at = q.L < cap ? (cap - q.L) / ut : 0;                 // the first part that ends past the cap
+    const long long mid = at < lo ? lo : (at < hi ? at : hi);
+    const long long n = mid - lo;
+    return n * (q.L + static_cast<long long>(kChunkItemKeys)) + ut * ((mid * (mid + 1) - lo * (lo + 1ll)) / 2) + (hi - mid) * (cap + kChunkItemKeys);
+  };
 
   // ---- sequences: validity, units and cost, and where both start
   Sum2 carry = {0, 0};
@@ -118,6 +166,10 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
       if (B <= kNearSeqs) {
         q = s_seq[b];
         n = q.n;
+      } else if (tree) {
+        q.start = b * p.tree;
+        q.L = p.seq_lens[b];
+        n = w.bad_page[b] ? 0 : (p.tree_sizes ? p.tree_sizes[p.shared_tree ? 0 : b] : p.tree);
       } else {
         q.start = p.token_start[b];
         q.L = p.seq_lens[b];
@@ -132,6 +184,8 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
         q.parts = ceil_div(q.n, ut);
         const long long np = q.parts;
         v.a = static_cast<int>(np) * Hkv;
+        if (windowed) v.b = (capped(q, q.L + static_cast<long long>(q.n)) + between(q, 0, q.parts - 1)) * Hkv;
+        else
         // sum over the parts of L + (p + 1) UT, but the last one ends at n
         v.b = (np * (static_cast<long long>(q.L) + kChunkItemKeys) + ut * (np * (np + 1) / 2) - (np * ut - q.n)) * Hkv;
       }
@@ -171,7 +225,10 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
     const long long over = static_cast<long long>(q.parts) * ut - q.n;     // the last part is that much shorter
     const long long keys = q.L + (pr + 1ll) * ut - (r == 0 ? over : 0);
     un.tiles = static_cast<int>((keys + kChunkTile - 1) / kChunkTile);
-    if (x) {
+    if (windowed) {
+      un.tiles -= chunk_span(p, q.L, pr * ut).skip;
+      if (x) *x = cost_of[b] + (r == 0 ? 0 : capped(q, q.L + static_cast<long long>(q.n)) + between(q, pr + 1, q.parts - 1)) * Hkv + un.g * capped(q, keys);
+    } else if (x) {
       const long long before = r * (static_cast<long long>(q.L) + kChunkItemKeys) +
                                ut * ((static_cast<long long>(q.parts) * (q.parts + 1) - static_cast<long long>(pr + 1) * (pr + 2)) / 2) - (r > 0 ? over : 0);
       *x = cost_of[b] + before * Hkv + un.g * (keys + kChunkItemKeys);
@@ -299,33 +356,6 @@ struct Bars {
   __device__ __forceinline__ uint32_t o_done(uint32_t i) const { return at(kSAt + 2 * kSBufs + i); }     // its PV has finished (both CTAs)
   __device__ __forceinline__ uint32_t o_free() const { return at(kSAt + 3 * kSBufs); }                   // an item's accumulators have been read (first CTA only)
 };
-
-// A float with a number, written and read in one piece.
-__device__ __forceinline__ unsigned long long tagged(uint32_t number, float x) { return static_cast<unsigned long long>(number) << 32 | __float_as_uint(x); }
-__device__ __forceinline__ float value_of(unsigned long long t) { return __uint_as_float(static_cast<uint32_t>(t)); }
-__device__ __forceinline__ bool has_tag(unsigned long long t, uint32_t want) { return static_cast<uint32_t>(t >> 32) == want; }
-// Bounded wait for the word with number `want` in shared memory; one with another number when the CTA was aborted or the time
-// limit passed.
-__device__ __noinline__ unsigned long long tag_wait_slow(volatile unsigned long long* slot, uint32_t want, volatile int* abort_flag) {
-  const unsigned long long t0 = global_timer(), limit = *reinterpret_cast<volatile unsigned long long*>(abort_flag + 1);
-  for (uint32_t spins = 1;; ++spins) {
-    const unsigned long long t = *slot;
-    if (has_tag(t, want)) return t;
-    if ((spins & 63u) == 0) {
-      if (*abort_flag) return tagged(~want, 0.f);
-      if (global_timer() - t0 > limit) {
-        *abort_flag = 1;
-        return tagged(~want, 0.f);
-      }
-    }
-    __nanosleep(20);
-  }
-}
-__device__ __forceinline__ unsigned long long tag_wait(volatile unsigned long long* slot, uint32_t want, volatile int* abort_flag) {
-  const unsigned long long t = *slot;
-  if (has_tag(t, want)) return t;
-  return tag_wait_slow(slot, want, abort_flag);
-}
 
 // (STALL: of the test hook that lets the waits run out, an instantiation of its own because the comparison would cost every other
 // call 2 to 3 %.)
@@ -831,9 +861,10 @@ chunk_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, cons
 // each: rows of a sequence that does not fit its cache, or whose block table names a page outside the pool, become zeros.  Nothing
 // orders the two kinds of blocks, so those of a cut unit leave the rows of such a sequence alone; every page in use has been copied
 // from by some worker, so the attention kernel has looked at all of them.
+// SPAN: a tree's rows past its size become zeros as well.
 constexpr int kMergeThreads = 256;
 
-template <int D>
+template <int D, bool SPAN>
 __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams p, int row_blocks) {
   wait_for_prerequisites();                              // partials and outputs of the attention kernel are there
   const ChunkWork& w = p.work;
@@ -841,11 +872,18 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams 
   if (static_cast<int>(blockIdx.x) >= records * halves * row_blocks) {
     const int b = blockIdx.x - records * halves * row_blocks;
     const ChunkSeq q = w.seq[b];
-    const int s = p.token_start[b], e = p.token_start[b + 1];
-    if (s < 0 || e <= s || e > p.N) return;
     const bool wrong = w.bad_page[b] != 0;
+    int s, e;
+    if (SPAN && p.tree > 0) {
+      s = b * p.tree + (wrong ? 0 : q.n);
+      e = (b + 1) * p.tree;
+    } else {
+      s = p.token_start[b];
+      e = p.token_start[b + 1];
+    }
+    if (s < 0 || e <= s || e > p.N) return;
     if (wrong && tid == 0) report_status(p.status, EAGLE_ERR_PAGE);
-    if (q.n > 0 && !wrong) return;                       // (n = 0: the planner refused it, and reported it)
+    if (q.n > 0 && !wrong && !(SPAN && p.tree > 0)) return;      // (n = 0: the planner refused it, and reported it)
     uint4* out = reinterpret_cast<uint4*>(p.out + static_cast<size_t>(s) * p.Hq * D);
     const size_t vecs = static_cast<size_t>(e - s) * p.Hq * (D / 8);
     for (size_t i = tid; i < vecs; i += kMergeThreads) out[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -933,23 +971,35 @@ cudaError_t launch_tiles(const ChunkParams& p, cudaStream_t stream) {
   return cudaLaunchKernelEx(&at.config, kernel, p, mk, mv, mq);
 }
 
+template <bool SPAN>
+cudaError_t launch_plan_kernel(const ChunkParams& p, cudaStream_t stream) {
+  chunk_plan_kernel<SPAN><<<1, kPlanThreads, 0, stream>>>(p);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  count_launch();
+  return cudaSuccess;
+}
+
+template <int D, bool SPAN>
+cudaError_t launch_merge_kernel(const ChunkParams& p, cudaStream_t stream) {
+  const int rows = p.max_rows < p.rows ? p.max_rows : p.rows, row_blocks = (rows + 7) / 8;
+  BehindLaunch at(p.num_workers * (p.few ? 1 : 2) * row_blocks + p.B, kMergeThreads, 0, stream);
+  const cudaError_t e = cudaLaunchKernelEx(&at.config, chunk_merge_kernel<D, SPAN>, p, row_blocks);
+  if (e != cudaSuccess) return e;
+  count_launch();
+  return cudaSuccess;
+}
+
 template <int D>
 cudaError_t launch_all(const ChunkParams& p, cudaStream_t stream) {
   // Both kernels after the planner are launched programmatically: their prologues (and the launches themselves) overlap the
   // kernel before, whose results they wait for.
-  chunk_plan_kernel<<<1, kPlanThreads, 0, stream>>>(p);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = launch_plan_kernel<false>(p, stream);
   if (e != cudaSuccess) return e;
-  count_launch();
   e = p.few ? launch_chunk_rows(p, stream) : launch_tiles<D>(p, stream);
   if (e != cudaSuccess) return e;
   count_launch();
-  const int rows = p.max_rows < p.rows ? p.max_rows : p.rows, row_blocks = (rows + 7) / 8;
-  BehindLaunch at(p.num_workers * (p.few ? 1 : 2) * row_blocks + p.B, kMergeThreads, 0, stream);
-  e = cudaLaunchKernelEx(&at.config, chunk_merge_kernel<D>, p, row_blocks);
-  if (e != cudaSuccess) return e;
-  count_launch();
-  return cudaSuccess;
+  return launch_merge_kernel<D, false>(p, stream);
 }
 
 template <int D>
@@ -964,6 +1014,12 @@ cudaError_t prepare() {
 }  // namespace
 
 cudaError_t chunk_prepare(int head_dim) { return head_dim == 128 ? prepare<128>() : prepare<64>(); }
+
+cudaError_t launch_chunk_plan(const ChunkParams& p, cudaStream_t stream) { return launch_plan_kernel<true>(p, stream); }
+
+cudaError_t launch_chunk_merge(const ChunkParams& p, cudaStream_t stream) {
+  return p.D == 128 ? launch_merge_kernel<128, true>(p, stream) : launch_merge_kernel<64, true>(p, stream);
+}
 
 cudaError_t launch_chunk(const ChunkParams& p, cudaStream_t stream) { return p.D == 128 ? launch_all<128>(p, stream) : launch_all<64>(p, stream); }
 

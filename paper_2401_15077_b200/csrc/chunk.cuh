@@ -1,4 +1,5 @@
-// Plan records, workspace and parameters of the chunk attention (chunk.cu, chunk_rows.cu).
+// Plan records, workspace and parameters of the chunk attention (chunk.cu, chunk_rows.cu) and of the attention with a window, over
+// bf16 or block-scaled caches, of chunks or trees (window.cu, window_rows.cu), which shares planner and merge.
 #pragma once
 #include "common.cuh"
 
@@ -84,7 +85,42 @@ struct ChunkParams {
   unsigned long long wait_limit_ns;
   int32_t stall_after_tiles;     // test hook: the kernels' STALL instantiations issue copies of that many tiles and no more (negative: off)
   ChunkWork work;
+  // Calls with a window, a tree or block scales (the planner's and the merge's SPAN instantiations); 0 and null elsewhere
+  int32_t window, sinks;         // W (0: no limit) and S, both at most the capacity
+  int32_t tree;                  // T_max of the tree form: sequence b has the rows from b * tree on; 0: chunk form
+  const int32_t* tree_parent;
+  const int32_t* tree_sizes;
+  int32_t shared_tree;
+  const float* k_scale;          // one per block and KV head, or null: bf16
+  const float* v_scale;
+  int32_t block_shift;
+  long long head_blocks;         // blocks from one KV head to the next
 };
+
+// What a unit whose first token is `first` sees of its sequence: slots below `sinks` and from `low` on.  K/V tiles that hold neither are
+// left out: the plan counts tiles without them, and tile t of the plan is tile(t) of the sequence.
+struct ChunkSpan {
+  int low, sinks;
+  int before, skip;              // tiles in front of the gap, tiles in it
+  __host__ __device__ int tile(int t) const { return t < before ? t : t + skip; }
+  // a page that holds no slot that is seen is not looked up: the first one behind the gap stands for it (its rows are masked)
+  __device__ int page(int pi, int shift) const { return pi < (low >> shift) && pi > ((sinks - 1) >> shift) ? low >> shift : pi; }
+  __device__ bool sees(int key) const { return key >= low || key < sinks; }
+  __device__ bool sees_all(int key, int n) const { return key >= low || key + n <= sinks || low <= sinks; }
+  __device__ bool sees_some(int key, int n) const { return key + n > low || key < sinks; }
+};
+__host__ __device__ inline ChunkSpan chunk_span(const ChunkParams& p, int L, int first) {
+  ChunkSpan s = {0, 0, 0, 0};
+  if (p.window > 0) {
+    const int low = L + (p.tree ? 0 : first) - p.window + 1;
+    s.low = low > 0 ? low : 0;
+    s.sinks = p.sinks < s.low ? p.sinks : s.low;
+    const int w0 = s.low / kChunkTile, before = (s.sinks + kChunkTile - 1) / kChunkTile;
+    s.before = before < w0 ? before : w0;
+    s.skip = w0 - s.before;
+  }
+  return s;
+}
 
 // Partial slots: a worker's share of the cut units begins and ends inside a unit at the most, with the query tiles of both.
 // `sms` bounds the workers.
@@ -121,5 +157,11 @@ cudaError_t chunk_prepare(int head_dim);
 cudaError_t chunk_rows_prepare(int head_dim);
 cudaError_t launch_chunk_rows(const ChunkParams& p, cudaStream_t stream);      // the row kernel alone, behind the planner
 cudaError_t launch_chunk(const ChunkParams& p, cudaStream_t stream);
+cudaError_t launch_chunk_plan(const ChunkParams& p, cudaStream_t stream);      // SPAN instantiations
+cudaError_t launch_chunk_merge(const ChunkParams& p, cudaStream_t stream);
+cudaError_t window_prepare(int head_dim);
+cudaError_t window_rows_prepare(int head_dim);
+cudaError_t launch_window_rows(const ChunkParams& p, cudaStream_t stream);
+cudaError_t launch_window(const ChunkParams& p, cudaStream_t stream);
 
 }  // namespace eagle

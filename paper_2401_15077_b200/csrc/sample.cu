@@ -1,0 +1,644 @@
+// Sampling with temperature, top-k, top-p and min-p: a token per row of logits, and / or the distribution that it is drawn from.
+//
+// With w(v) = exp((z(v) - max z) / temperature), what the filters leave is the first tokens of the order (z descending, id ascending): all
+// with a greater z than some z*, and the first few of those that equal it.  So nothing is sorted: each filter looks for its cut (z*, how many
+// of z*) by a histogram over z and a ranking of the few values in the bin that the cut falls into.
+//   top-k   counts; top-p: masses, after the mass of all that top-k left; min-p: w >= min_p, a comparison
+// A cluster of C CTAs takes a row, each a slice of the vocabulary, which stays in shared memory (in the logits' own type) for all passes
+// over it; histograms are merged and candidates exchanged through distributed shared memory.
+//
+// Weights are fp64 (argument, reduction, polynomial of degree 9) and are summed as integers of 2^-q, q = 42 .. 44 with the vocabulary's
+// size: sums then depend neither on the order of atomics nor on C, and cuts and draws are decided as if in 64 bits, which fp32 sums
+// over 10^5 tokens (relative 1e-6) would not.
+//
+// What top-p may cut off is bounded before its histogram is taken: n tokens of weights below (1 - p) Z / n sum to less than (1 - p) Z, so
+// the cut is not among them.  Of a vocabulary's long tail nothing reaches the atomics then.
+#include <cooperative_groups.h>
+
+#include <type_traits>
+#include <utility>
+
+#include "sample.cuh"
+
+namespace eagle {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kCountBins = 2048, kMassBins = 1024;
+constexpr int kCandidates = kThreads;        // values that are ranked against one another, a thread each
+constexpr size_t kSliceBytes = 160 * 1024;   // of a slice that stays in shared memory
+
+typedef unsigned long long u64;
+
+// Shared memory behind the slice.
+struct Shared {
+  union {
+    uint32_t count[kCountBins];                                      // top-k's histogram
+    struct { u64 mass[kMassBins]; uint32_t number[kMassBins]; } m;   // top-p's
+  } hist;
+  u64 slot[2][kMaxCluster][2];       // exchanges, by turns
+  u64 warp_sum[kWarps];
+  uint32_t list[kCandidates];        // this CTA's candidates
+  uint32_t all[kCandidates];         // the cluster's
+  u64 weight[kCandidates];
+  uint32_t n, lo, hi;                // candidates found here, their range
+  // a cut, found by one thread or by several with the same result
+  uint32_t cut_key, cut_take, cut_ties;
+  uint32_t bin, bin_number;
+  u64 base;
+};
+
+// Order-preserving number of a float (no NaN, no negative zero), and back.
+__device__ __forceinline__ uint32_t key_of(float z) {
+  const uint32_t u = __float_as_uint(z);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+
+// 2^x for -1000 < x <= 0: the nearest whole number goes to the exponent, what is left, f in [-1/2, 1/2], through the polynomial that
+// interpolates 2^f there at Chebyshev nodes (constant set to 1, so that whole numbers are exact; error 2e-14).
+__device__ __forceinline__ double exp2_double(double x) {
+  const double n = rint(x), f = x - n;
+  double r = 1.0205905413765595e-07;
+  r = fma(r, f, 1.325964524488711e-06);
+  r = fma(r, f, 1.5252672924850737e-05);
+  r = fma(r, f, 0.0001540343375125101);
+  r = fma(r, f, 0.0013333558200794592);
+  r = fma(r, f, 0.009618129193934313);
+  r = fma(r, f, 0.05550410866465167);
+  r = fma(r, f, 0.2402265069564034);
+  r = fma(r, f, 0.6931471805599462);
+  r = fma(r, f, 1.0);
+  return __hiloint2double(__double2hiint(r) + (static_cast<int>(n) << 20), __double2loint(r));
+}
+
+struct Weigher {
+  float top;             // the row's largest value
+  double top_d, rate;    // log2(e) / temperature
+  double unit;           // 2^q
+  __device__ __forceinline__ double real(float z) const {
+    if (z == top) return 1.0;                             // (infinite ones too)
+    const double x = (static_cast<double>(z) - top_d) * rate;
+    return x > -1000.0 ? exp2_double(x) : 0.0;            // -infinity, and NaN from infinities, are 0
+  }
+  // A weight of at most 1 as an integer: adding 2^52 leaves it in the low bits of the sum.
+  __device__ __forceinline__ u64 whole(double w) const { return __double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull; }
+};
+
+// One value of a row in its canonical form: NaN as -infinity, negative zero as zero.
+__device__ __forceinline__ float clean(float z) {
+  if (z != z) return -INFINITY;
+  return z + 0.f;
+}
+
+template <typename T>
+struct Vec {
+  static constexpr int kLen = 16 / sizeof(T);
+  uint4 raw;
+  __device__ __forceinline__ float at(int e) const {
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    else return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+  }
+  __device__ __forceinline__ void set(int e, float z) {
+    uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(z);
+    else w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | (__float_as_uint(z) & 0xffff0000u) : (w[e >> 1] & 0xffff0000u) | (__float_as_uint(z) >> 16);
+    raw = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+__device__ __forceinline__ u64 warp_sum64(u64 v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ u64 warp_scan64(u64 v, int lane) {      // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const u64 x = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
+
+// RESIDENT: the slice is in shared memory; else it is read again from the logits in each pass (vocabularies beyond 8 x 160 KB).
+template <typename T, bool RESIDENT>
+__global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int slice) {
+  constexpr int kVec = Vec<T>::kLen, kTile = kThreads * kVec;
+  extern __shared__ __align__(16) unsigned char dyn[];
+  T* const held = reinterpret_cast<T*>(dyn);
+  const int tiles = slice / kTile;
+  u64* const part = reinterpret_cast<u64*>(dyn + (RESIDENT ? static_cast<size_t>(slice) * sizeof(T) : 0));      // [tiles][warps]
+  uint32_t* const ties = reinterpret_cast<uint32_t*>(part + tiles * kWarps);                                      // [tiles][warps]
+  __shared__ Shared s;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long row = blockIdx.x / C;
+  const int b = static_cast<int>(row / p.R), r = static_cast<int>(row - static_cast<long long>(b) * p.R);
+  if (p.num_rows && r >= p.num_rows[b]) return;           // (all of the cluster)
+
+  // ---- the slice.  Positions count from the 16-byte boundary at or before the row's first element, so that vectors are aligned.
+  auto started = cluster.barrier_arrive();                // (shared memory of the others is there once all have started)
+  const T* const src = static_cast<const T*>(p.logits) + row * p.V;
+  const int off = static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
+  const int first = rank * slice - off;                   // id of the slice's position 0
+  auto load = [&](int pos) {                              // canonical values of a vector; what is outside of the row is -infinity
+    Vec<T> v;
+    const int id = first + pos;
+    if (id >= 0 && id + kVec <= p.V) {
+      v.raw = __ldg(reinterpret_cast<const uint4*>(src + id));
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) v.set(e, clean(v.at(e)));
+    } else {
+      v.raw = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        float z = -INFINITY;
+        if (id + e >= 0 && id + e < p.V) z = clean(static_cast<float>(src[id + e]));
+        v.set(e, z);
+      }
+    }
+    return v;
+  };
+  auto fetch = [&](int pos) {
+    if constexpr (RESIDENT) {
+      Vec<T> v;
+      v.raw = *reinterpret_cast<const uint4*>(held + pos);
+      return v;
+    } else {
+      return load(pos);
+    }
+  };
+
+  // Two numbers of each CTA to all of them; every thread gets them by rank from the returned slots.
+  int turn = 0;
+  auto exchange = [&](u64 a, u64 c) {                     // (a, c: of thread 0)
+    if (warp == 0) {
+      a = __shfl_sync(0xffffffffu, a, 0);
+      c = __shfl_sync(0xffffffffu, c, 0);
+      if (lane < C) {
+        u64* to = cluster.map_shared_rank(&s.slot[turn][rank][0], lane);
+        to[0] = a;
+        to[1] = c;
+      }
+    }
+    cluster.sync();
+    const u64(*got)[2] = s.slot[turn];
+    turn ^= 1;
+    return got;
+  };
+  auto block_sum = [&](u64 v) {                           // of all threads, for all threads
+    v = warp_sum64(v);
+    __syncthreads();
+    if (lane == 0) s.warp_sum[warp] = v;
+    __syncthreads();
+    u64 t = lane < kWarps ? s.warp_sum[lane] : 0;
+    return warp_sum64(t);
+  };
+  auto cluster_sum = [&](u64 v) {
+    const u64 mine = block_sum(v);
+    const u64(*got)[2] = exchange(mine, 0);
+    u64 t = 0;
+    for (int c = 0; c < C; ++c) t += got[c][0];
+    return t;
+  };
+
+  // ---- the largest value
+  uint32_t top_key = 0;
+  for (int i = 0; i < tiles; ++i) {
+    const int pos = (i * kThreads + tid) * kVec;
+    const Vec<T> v = load(pos);
+    if constexpr (RESIDENT) *reinterpret_cast<uint4*>(held + pos) = v.raw;
+    float m = v.at(0);
+#pragma unroll
+    for (int e = 1; e < kVec; ++e) m = fmaxf(m, v.at(e));
+    top_key = max(top_key, key_of(m));
+  }
+  top_key = __reduce_max_sync(0xffffffffu, top_key);
+  if (lane == 0) s.warp_sum[warp] = top_key;
+  __syncthreads();
+  top_key = __reduce_max_sync(0xffffffffu, lane < kWarps ? static_cast<uint32_t>(s.warp_sum[lane]) : 0u);
+  cluster.barrier_wait(std::move(started));
+  {
+    const u64(*got)[2] = exchange(top_key, 0);
+    for (int c = 0; c < C; ++c) top_key = max(top_key, static_cast<uint32_t>(got[c][0]));
+  }
+  Weigher w;
+  w.top = value_of_key(top_key);
+  const bool nothing = w.top == -INFINITY;
+  if (nothing && rank == 0 && tid == 0) {
+    report_status(p.status, EAGLE_ERR_ROW);
+    if (p.tokens) p.tokens[row] = -1;
+  }
+  const float temperature = p.temperature ? p.temperature[b] : 1.f;
+  const int k = p.top_k ? p.top_k[b] : 0;
+  const float top_p = p.top_p ? p.top_p[b] : 1.f;
+  const double least = p.min_p ? static_cast<double>(fminf(fmaxf(p.min_p[b], 0.f), 1.f)) : 0.0;      // (NaN: 0)
+  const bool greedy = !(temperature > 0.f);
+  w.top_d = w.top;
+  w.rate = 1.4426950408889634 / (greedy ? 1.0 : static_cast<double>(temperature));
+  const int q = min(44, 62 - (32 - __clz(p.V - 1)));
+  w.unit = __hiloint2double((1023 + q) << 20, 0);
+
+  // ---- the cut: tokens with a greater key stay, and the first `take` of those that equal it (`some`: these are not all of them)
+  uint32_t cut = 0, take = 0;
+  bool some = false;
+
+  // Merged histogram -> the bin in which the prefix reaches the target, with what lies before it.  `reached(before, after)` is true in that
+  // bin only.  Every CTA of the cluster does all of it.
+  auto find_bin = [&](auto* bins, const uint32_t* number, int n_bins, auto reached) {
+    cluster.sync();                                       // all histograms are complete
+    const int per = n_bins / kThreads;
+    u64 v[kCountBins / kThreads], sum = 0;
+    for (int i = 0; i < per; ++i) {
+      v[i] = 0;
+      for (int c = 0; c < C; ++c) v[i] += cluster.map_shared_rank(bins, c)[tid * per + i];
+      sum += v[i];
+    }
+    u64 inc = warp_scan64(sum, lane);
+    __syncthreads();
+    if (lane == 31) s.warp_sum[warp] = inc;
+    __syncthreads();
+    u64 before = inc - sum;
+    for (int x = 0; x < warp; ++x) before += s.warp_sum[x];
+    for (int i = 0; i < per; ++i) {
+      if (reached(before, before + v[i])) {
+        s.bin = tid * per + i;
+        s.base = before;
+        uint32_t n = 0;
+        if (number) for (int c = 0; c < C; ++c) n += cluster.map_shared_rank(number, c)[tid * per + i];
+        s.bin_number = number ? n : static_cast<uint32_t>(v[i]);
+      }
+      before += v[i];
+    }
+    cluster.sync();                                       // (nobody reads these histograms any more)
+  };
+  auto clear = [&](uint32_t* words, int n) {
+    for (int i = tid; i < n; i += kThreads) words[i] = 0;
+    __syncthreads();
+  };
+  // Values of a bin are ranked against one another; a bin with too many of them is cut finer first, by their keys.  `member(z)`: lies in the bin;
+  // MASS: before and target are masses, else counts.
+  auto rank_in_bin = [&](auto member, auto is_mass, u64 base, double target) {
+    constexpr bool MASS = decltype(is_mass)::value;
+    uint32_t lo = 0, hi = 0xffffffffu;
+    for (;;) {
+      if (tid == 0) { s.n = 0; s.lo = 0xffffffffu; s.hi = 0; }
+      __syncthreads();
+      uint32_t least = 0xffffffffu, most = 0;
+      for (int i = 0; i < tiles; ++i) {
+        const Vec<T> v = fetch((i * kThreads + tid) * kVec);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          const float z = v.at(e);
+          const uint32_t key = key_of(z);
+          if (member(z) && key >= lo && key <= hi) {
+            least = min(least, key);
+            most = max(most, key);
+            const uint32_t at = atomicAdd(&s.n, 1u);
+            if (at < kCandidates) s.list[at] = key;
+          }
+        }
+      }
+      least = __reduce_min_sync(0xffffffffu, least);
+      most = __reduce_max_sync(0xffffffffu, most);
+      if (lane == 0) { atomicMin(&s.lo, least); atomicMax(&s.hi, most); }
+      __syncthreads();
+      const u64(*got)[2] = exchange(s.n, static_cast<u64>(s.lo) << 32 | s.hi);
+      uint32_t n = 0, mine_at = 0;
+      lo = 0xffffffffu;
+      hi = 0;
+      for (int c = 0; c < C; ++c) {
+        n += static_cast<uint32_t>(got[c][0]);
+        lo = min(lo, static_cast<uint32_t>(got[c][1] >> 32));
+        hi = max(hi, static_cast<uint32_t>(got[c][1]));
+      }
+      if (lo == hi) {                                     // they are all equal
+        if (tid == 0) {
+          u64 need = n;
+          const u64 one = MASS ? w.whole(w.real(value_of_key(lo))) : 1;
+          const double x = ceil((target - static_cast<double>(base)) / static_cast<double>(one));
+          if (x < static_cast<double>(n)) need = x > 1.0 ? static_cast<u64>(x) : 1;
+          s.cut_key = lo;
+          s.cut_take = static_cast<uint32_t>(need);
+          s.cut_ties = n;
+        }
+        break;
+      }
+      if (n <= kCandidates) {
+        for (int c = 0; c < C; ++c) {
+          const int m = static_cast<int>(got[c][0]);
+          if (tid < m) s.all[mine_at + tid] = cluster.map_shared_rank(s.list, c)[tid];
+          mine_at += m;
+        }
+        __syncthreads();
+        if constexpr (MASS) {
+          if (tid < n) s.weight[tid] = w.whole(w.real(value_of_key(s.all[tid])));
+          __syncthreads();
+        }
+        if (tid < n) {
+          const uint32_t key = s.all[tid];
+          u64 before = base, one = 1;
+          uint32_t equal = 0;
+          for (uint32_t j = 0; j < n; ++j) {
+            const uint32_t other = s.all[j];
+            if (other > key) before += MASS ? s.weight[j] : 1;
+            equal += other == key;
+          }
+          if constexpr (MASS) one = s.weight[tid];
+          if (static_cast<double>(before) < target && !(static_cast<double>(before + equal * one) < target)) {
+            const double x = ceil((target - static_cast<double>(before)) / static_cast<double>(one));
+            s.cut_key = key;                              // (threads with this key all write the same)
+            s.cut_take = x < static_cast<double>(equal) ? (x > 1.0 ? static_cast<uint32_t>(x) : 1u) : equal;
+            s.cut_ties = equal;
+          }
+        }
+        break;
+      }
+      // finer bins over [lo, hi], from the top
+      const uint32_t top = hi, span = hi - lo;
+      const int shift = max(0, 32 - __clz(span) - 10);    // span >> shift is below kMassBins
+      clear(reinterpret_cast<uint32_t*>(&s.hist), sizeof(s.hist) / 4);
+      for (int i = 0; i < tiles; ++i) {
+        const Vec<T> v = fetch((i * kThreads + tid) * kVec);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          const float z = v.at(e);
+          const uint32_t key = key_of(z);
+          if (member(z) && key >= lo && key <= hi) {
+            const uint32_t at = (top - key) >> shift;
+            atomicAdd(&s.hist.m.mass[at], MASS ? w.whole(w.real(z)) : 1ull);
+          }
+        }
+      }
+      const u64 base_now = base;
+      find_bin(s.hist.m.mass, nullptr, kMassBins, [&](u64 before, u64 after) {
+        return static_cast<double>(base_now + before) < target && !(static_cast<double>(base_now + after) < target);
+      });
+      base += s.base;
+      hi = top - (s.bin << shift);
+      lo = max(lo, hi - ((1u << shift) - 1u));
+    }
+    __syncthreads();
+    cut = s.cut_key;
+    take = s.cut_take;
+    some = take < s.cut_ties;
+    cluster.sync();                                       // (the lists have been read)
+  };
+
+  const bool by_k = !nothing && !greedy && k > 1 && k < p.V;
+  if (nothing) {
+    cut = 0xffffffffu;                                    // nothing stays
+  } else if (greedy || k == 1 || top_p <= 0.f) {
+    cut = top_key;
+    take = 1;
+    some = true;
+  }
+  if (by_k && cut == 0) {
+    auto bin_of = [&](float z) { return z == w.top ? 0 : static_cast<int>(fminf((w.top - z) * 64.f, kCountBins - 1.f)); };
+    clear(s.hist.count, kCountBins);
+    for (int i = 0; i < tiles; ++i) {
+      const int pos = (i * kThreads + tid) * kVec;
+      const Vec<T> v = fetch(pos);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const int id = first + pos + e;
+        if (id >= 0 && id < p.V) atomicAdd(&s.hist.count[bin_of(v.at(e))], 1u);
+      }
+    }
+    const u64 want = static_cast<u64>(k);
+    find_bin(s.hist.count, static_cast<const uint32_t*>(nullptr), kCountBins, [&](u64 before, u64 after) { return before < want && after >= want; });
+    const int bin = static_cast<int>(s.bin);
+    // (positions outside of the row hold -infinity too: they stand behind every token, and have no mass)
+    rank_in_bin([&](float z) { return bin_of(z) == bin; }, std::false_type{}, s.base, static_cast<double>(k));
+  }
+  if (!nothing && top_p < 1.f && !(cut == top_key && take == 1)) {
+    u64 sum = 0;
+    for (int i = 0; i < tiles; ++i) {
+      const Vec<T> v = fetch((i * kThreads + tid) * kVec);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        if (key_of(v.at(e)) > cut) sum += w.whole(w.real(v.at(e)));
+    }
+    const u64 above = cluster_sum(sum);
+    const u64 one = take ? w.whole(w.real(value_of_key(cut))) : 0;
+    const u64 all = above + take * one;
+    const double target = static_cast<double>(top_p) * static_cast<double>(all);
+    if (static_cast<double>(above) < target) {            // among the last ones that top-k left
+      const double x = ceil((target - static_cast<double>(above)) / static_cast<double>(one));
+      if (x < static_cast<double>(take)) {
+        take = x > 1.0 ? static_cast<uint32_t>(x) : 1u;
+        some = true;
+      }
+    } else {
+      const double n = by_k ? k : p.V;
+      const double tail = (1.0 - static_cast<double>(top_p)) * static_cast<double>(all) / w.unit / n;     // see above
+      const float depth = static_cast<float>((fmax(-log2(tail), 0.0) + 1e-3) / w.rate);
+      const float scale = (kMassBins - 1.f) / depth;
+      const uint32_t floor_key = cut;
+      auto bin_of = [&](float z) { return z == w.top ? 0.f : (w.top - z) * scale; };
+      auto member = [&](float z) { return key_of(z) > floor_key && bin_of(z) < kMassBins; };
+      clear(reinterpret_cast<uint32_t*>(&s.hist), sizeof(s.hist) / 4);
+      for (int i = 0; i < tiles; ++i) {
+        const Vec<T> v = fetch((i * kThreads + tid) * kVec);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          const float z = v.at(e);
+          if (member(z)) atomicAdd(&s.hist.m.mass[static_cast<int>(bin_of(z))], w.whole(w.real(z)));
+        }
+      }
+      find_bin(s.hist.m.mass, nullptr, kMassBins, [&](u64 before, u64 after) {
+        return static_cast<double>(before) < target && !(static_cast<double>(after) < target);
+      });
+      const int bin = static_cast<int>(s.bin);
+      rank_in_bin([&](float z) { return member(z) && static_cast<int>(bin_of(z)) == bin; }, std::true_type{}, s.base, target);
+    }
+  }
+
+  // ---- where only the first of equal values stay: how many there are before each warp's part of each tile
+  u64 ties_before = 0;
+  if (some) {
+    uint32_t mine = 0;
+    for (int i = 0; i < tiles; ++i) {
+      const Vec<T> v = fetch((i * kThreads + tid) * kVec);
+      uint32_t n = 0;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) n += key_of(v.at(e)) == cut;
+      n = __reduce_add_sync(0xffffffffu, n);
+      if (lane == 0) ties[i * kWarps + warp] = n;
+      mine += n;
+    }
+    const u64 here = block_sum(lane == 0 ? mine : 0);
+    const u64(*got)[2] = exchange(here, 0);
+    for (int c = 0; c < rank; ++c) ties_before += got[c][0];
+    if (warp == 0) {                                      // exclusive prefix sums in place
+      u64 carry = ties_before;
+      for (int at = 0; at < tiles * kWarps; at += 32) {
+        const u64 n = at + lane < tiles * kWarps ? ties[at + lane] : 0;
+        const u64 inc = warp_scan64(n, lane);
+        if (at + lane < tiles * kWarps) ties[at + lane] = static_cast<uint32_t>(carry + inc - n);
+        carry += __shfl_sync(0xffffffffu, inc, 31);
+      }
+    }
+    __syncthreads();
+  }
+  // Weights of what stays in this thread's vector of tile i (all lanes together).
+  auto weigh = [&](const Vec<T>& v, int group, double* e_out) {
+    uint32_t rank_of = 0;
+    if (some) {
+      uint32_t n = 0;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) n += key_of(v.at(e)) == cut;
+      uint32_t inc = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += x;
+      }
+      rank_of = ties[group] + inc - n;
+    }
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      const uint32_t key = key_of(v.at(e));
+      bool stays = key > cut;
+      if (key == cut) stays = !some ? take > 0 : rank_of++ < take;
+      double x = 0.0;
+      if (stays) x = w.real(v.at(e));
+      e_out[e] = x < least ? 0.0 : x;
+    }
+  };
+
+  // ---- the mass of what stays
+  u64 sum = 0;
+  for (int i = 0; i < tiles; ++i) {
+    double e[kVec];
+    weigh(fetch((i * kThreads + tid) * kVec), i * kWarps + warp, e);
+    u64 t = 0;
+#pragma unroll
+    for (int x = 0; x < kVec; ++x) t += w.whole(e[x]);
+    t = warp_sum64(t);
+    if (lane == 0) part[i * kWarps + warp] = t;
+    sum += t;
+  }
+  const u64 here = block_sum(lane == 0 ? sum : 0);
+  u64 before = 0, all = 0;
+  {
+    const u64(*got)[2] = exchange(here, 0);
+    for (int c = 0; c < C; ++c) {
+      if (c < rank) before += got[c][0];
+      all += got[c][0];
+    }
+  }
+
+  // ---- the draw: the CTA, the warp's part of a tile, the lane and the element in which the prefix passes u times the sum
+  if (p.tokens && !nothing && warp == 0) {
+    const double total = static_cast<double>(all);
+    double t = static_cast<double>(p.uniforms[row]) * total;
+    t = t < total ? fmax(t, 0.0) : total * 0.9999999999999999;      // (u outside of [0, 1))
+    if (here > 0 && !(static_cast<double>(before) > t) && static_cast<double>(before + here) > t) {
+      u64 carry = before;
+      int group = -1;
+      for (int at = 0; at < tiles * kWarps; at += 32) {
+        const u64 n = at + lane < tiles * kWarps ? part[at + lane] : 0;
+        const u64 inc = warp_scan64(n, lane);
+        const unsigned hit = __ballot_sync(0xffffffffu, static_cast<double>(carry + inc) > t);
+        if (hit) {
+          const int l = __ffs(hit) - 1;
+          group = at + l;
+          carry += __shfl_sync(0xffffffffu, inc - n, l);
+          break;
+        }
+        carry += __shfl_sync(0xffffffffu, inc, 31);
+      }
+      // (group >= 0: the CTA's sum passes t)
+      const int pos = ((group / kWarps) * kThreads + (group % kWarps) * 32 + lane) * kVec;
+      double e[kVec];
+      weigh(fetch(pos), group, e);
+      u64 mine = 0;
+#pragma unroll
+      for (int x = 0; x < kVec; ++x) mine += w.whole(e[x]);
+      const u64 inc = warp_scan64(mine, lane);
+      const unsigned hit = __ballot_sync(0xffffffffu, static_cast<double>(carry + inc) > t);
+      if (lane == __ffs(hit) - 1) {
+        u64 run = carry + inc - mine;
+        int found = kVec - 1;
+#pragma unroll
+        for (int x = kVec - 1; x >= 0; --x) {
+          u64 upto = run;
+#pragma unroll
+          for (int y = 0; y <= x; ++y) upto += w.whole(e[y]);
+          if (static_cast<double>(upto) > t) found = x;
+        }
+        p.tokens[row] = first + pos + found;
+      }
+    }
+  }
+
+  // ---- the distribution
+  if (p.probs) {
+    float* const dst = p.probs + row * p.V;
+    const double inv = nothing ? 0.0 : w.unit / static_cast<double>(all);
+    const bool wide = ((reinterpret_cast<uintptr_t>(dst) - 4 * static_cast<uintptr_t>(off)) & 15) == 0;
+    for (int i = 0; i < tiles; ++i) {
+      const int pos = (i * kThreads + tid) * kVec, id = first + pos;
+      double e[kVec];
+      weigh(fetch(pos), i * kWarps + warp, e);
+      if (wide && id >= 0 && id + kVec <= p.V) {
+#pragma unroll
+        for (int x = 0; x < kVec; x += 4)
+          *reinterpret_cast<float4*>(dst + id + x) = make_float4(static_cast<float>(e[x] * inv), static_cast<float>(e[x + 1] * inv),
+                                                                 static_cast<float>(e[x + 2] * inv), static_cast<float>(e[x + 3] * inv));
+      } else {
+#pragma unroll
+        for (int x = 0; x < kVec; ++x)
+          if (id + x >= 0 && id + x < p.V) dst[id + x] = static_cast<float>(e[x] * inv);
+      }
+    }
+  }
+  cluster.sync();                                         // nobody leaves while another may still read or write here
+}
+
+template <typename T>
+cudaError_t launch(const SampleParams& p, int sm_count, cudaStream_t stream) {
+  constexpr int kTile = kThreads * Vec<T>::kLen;
+  const long long rows = static_cast<long long>(p.B) * p.R, positions = static_cast<long long>(p.V) + Vec<T>::kLen;
+  // As many CTAs to a row as fill the machine, while each has at least a tile of the vocabulary, and enough to hold the row in shared memory.
+  int C = 1;
+  auto slice_of = [&](int c) { return static_cast<int>(((positions + c - 1) / c + kTile - 1) / kTile * kTile); };
+  while (C < kMaxCluster && (slice_of(C) * sizeof(T) > kSliceBytes || (rows * C < sm_count && slice_of(C) > kTile))) C *= 2;
+  const int slice = slice_of(C);
+  const bool resident = slice * sizeof(T) <= kSliceBytes;
+  const size_t bytes = (resident ? slice * sizeof(T) : 0) + static_cast<size_t>(slice / kTile) * kWarps * 12;
+  auto kernel = resident ? sample_kernel<T, true> : sample_kernel<T, false>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSliceBytes + 16384));
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t config = {};
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = C;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  config.gridDim = dim3(static_cast<unsigned>(rows * C));
+  config.blockDim = dim3(kThreads);
+  config.dynamicSmemBytes = bytes;
+  config.stream = stream;
+  config.attrs = &attr;
+  config.numAttrs = 1;
+  e = cudaLaunchKernelEx(&config, kernel, p, slice);
+  if (e != cudaSuccess) return e;
+  count_launch();
+  return cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t launch_sample(const SampleParams& p, int sm_count, cudaStream_t stream) {
+  return p.bf16 ? launch<__nv_bfloat16>(p, sm_count, stream) : launch<float>(p, sm_count, stream);
+}
+
+}  // namespace eagle

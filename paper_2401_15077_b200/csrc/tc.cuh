@@ -10,6 +10,12 @@ namespace tc {
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 
+// Waits that do not succeed at once go on in a function of their own, so that they take no room in the loops; a kernel that moves registers
+// between its warps (setmaxnreg) cannot call functions and defines this to have them inline.
+#ifndef EAGLE_SLOW_WAIT
+#define EAGLE_SLOW_WAIT __noinline__
+#endif
+
 // ------------------------------------------------------------------------------------------------ mbarriers, bounded waits
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -57,7 +63,7 @@ __device__ __forceinline__ unsigned long long global_timer() {
 }
 // Every wait gives up after the limit that the host set (it sits in shared memory right behind the abort flag), raises
 // the flag and returns false; so does every other wait of the CTA from then on.
-static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+static __device__ EAGLE_SLOW_WAIT bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   const unsigned long long t0 = global_timer(), limit = *reinterpret_cast<volatile unsigned long long*>(abort_flag + 1);
   for (uint32_t spins = 1;; ++spins) {
     if (mbar_try_wait(bar, parity)) return true;
@@ -76,13 +82,47 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 }
 // After an abort: copies and MMAs that the CTA has issued may still be at work on its shared and tensor memory.  They take
 // microseconds; this waits a hundred before it may leave.
-static __device__ __noinline__ void let_work_land() {
+static __device__ EAGLE_SLOW_WAIT void let_work_land() {
   const unsigned long long t0 = global_timer();
   while (global_timer() - t0 < 100000ull) __nanosleep(1000);
+}
+// A wait for arrivals with release at cluster scope, whose senders' stores to their own shared memory are to be seen by what follows.
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (!mbar_wait(bar, parity, abort_flag)) return false;
+  asm volatile("fence.acq_rel.cluster;" ::: "memory");
+  return true;
 }
 // mbar_wait with a verdict that is uniform over the warp (the callers go on to warp-collective instructions).
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
+
+// ------------------------------------------------------------------------------------------------ words with numbers
+// A float with a number, written and read in one piece.
+__device__ __forceinline__ unsigned long long tagged(uint32_t number, float x) { return static_cast<unsigned long long>(number) << 32 | __float_as_uint(x); }
+__device__ __forceinline__ float value_of(unsigned long long t) { return __uint_as_float(static_cast<uint32_t>(t)); }
+__device__ __forceinline__ bool has_tag(unsigned long long t, uint32_t want) { return static_cast<uint32_t>(t >> 32) == want; }
+// Bounded wait for the word with number `want` in shared memory; one with another number when the CTA was aborted or the time
+// limit passed.
+static __device__ EAGLE_SLOW_WAIT unsigned long long tag_wait_slow(volatile unsigned long long* slot, uint32_t want, volatile int* abort_flag) {
+  const unsigned long long t0 = global_timer(), limit = *reinterpret_cast<volatile unsigned long long*>(abort_flag + 1);
+  for (uint32_t spins = 1;; ++spins) {
+    const unsigned long long t = *slot;
+    if (has_tag(t, want)) return t;
+    if ((spins & 63u) == 0) {
+      if (*abort_flag) return tagged(~want, 0.f);
+      if (global_timer() - t0 > limit) {
+        *abort_flag = 1;
+        return tagged(~want, 0.f);
+      }
+    }
+    __nanosleep(20);
+  }
+}
+__device__ __forceinline__ unsigned long long tag_wait(volatile unsigned long long* slot, uint32_t want, volatile int* abort_flag) {
+  const unsigned long long t = *slot;
+  if (has_tag(t, want)) return t;
+  return tag_wait_slow(slot, want, abort_flag);
 }
 
 // Counts steps through a ring of N slots: the slot of the next step, and the parity of its use.
@@ -164,6 +204,10 @@ __device__ __forceinline__ void st16(uint32_t addr, const uint32_t* r) {
 __host__ __device__ constexpr uint32_t instr_desc(int M, int N, bool b_mn_major) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn_major ? (1u << 16) : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
          (static_cast<uint32_t>(M >> 4) << 24);
+}
+// The same for fp16 x fp16 -> fp32.
+__host__ __device__ constexpr uint32_t instr_desc_half(int M, int N, bool b_mn_major) {
+  return (1u << 4) | (b_mn_major ? (1u << 16) : 0u) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 // Shared-memory descriptor of a swizzled tile.  Low word: start address and leading-dimension offset, so stepping along the
 // contraction is a 32-bit add; high word: stride of 8-row groups, version, swizzle (128-byte rows, or 64-byte rows).
