@@ -87,10 +87,16 @@ static __device__ EAGLE_SLOW_WAIT void let_work_land() {
   while (global_timer() - t0 < 100000ull) __nanosleep(1000);
 }
 // A wait for arrivals with release at cluster scope, whose senders' stores to their own shared memory are to be seen by what follows.
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  if (!mbar_wait(bar, parity, abort_flag)) return false;
-  asm volatile("fence.acq_rel.cluster;" ::: "memory");
-  return true;
+  if (mbar_try_wait_cluster(bar, parity)) return true;
+  return mbar_wait_slow(bar, parity, abort_flag) && mbar_try_wait_cluster(bar, parity);      // (the phase is over: the second try succeeds at once)
 }
 // mbar_wait with a verdict that is uniform over the warp (the callers go on to warp-collective instructions).
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -180,6 +186,19 @@ __device__ __forceinline__ void ld32(uint32_t addr, uint32_t* r) {
         "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
         "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ld16(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void st8(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+      ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+      : "memory");
 }
 __device__ __forceinline__ void st32(uint32_t addr, const uint32_t* r) {
   asm volatile(

@@ -15,7 +15,6 @@
 // take ks * scale as their factor, and the maximum is taken over z + log2 vs, so that 2^(z + log2 vs - m) is the weight of
 // the codes themselves and fits fp16 whatever the scales are; the row sum divides by vs again.  Query rows are multiplied by a power of two, so that they fit
 // fp16 as well, and the scores by its inverse.  A warp brings the scales of each step's 128 keys.
-#define EAGLE_SLOW_WAIT __forceinline__
 #include "window.cuh"
 
 namespace eagle {
@@ -28,7 +27,7 @@ constexpr int kSBufs = 3;                // score buffers in tensor memory; step
 constexpr uint32_t kTmemCols = 512;      // S0 S1 S2 | O; P (packed, 64 columns) overwrites the front of its S
 constexpr uint32_t kColO = 384;
 constexpr float kRescaleThreshold = 8.0f;   // log2 units: the accumulator is rescaled when the row maximum outgrows its reference by more
-constexpr int kPolyStride = 2;           // one pair of exponentials in so many is a polynomial on the FMA pipe (measured in chunk.cu)
+constexpr int kPolyStride = 2;           // bf16: one pair of exponentials in so many is a polynomial on the FMA pipe (measured in chunk.cu)
 constexpr int kGroups = kChunkTile / 16; // groups of 16 keys in a tile, the smallest block
 
 template <int D, bool CODES>
@@ -59,20 +58,20 @@ struct Smem {
   static constexpr int kFactor = kLfin + 2 * 128 * 8;        // uint64 [kFactors][128 rows]: item number | the row's factor
   static constexpr int kScale = kFactor + (CODES ? kFactors * 128 * 8 : 0);  // float4 [kSBufs][kGroups]: ks * scale, log2 vs, 1 / vs
   static constexpr int kBar = kScale + (CODES ? kSBufs * kGroups * 16 : 0);
-  static constexpr int kNumBars = CODES ? 2 * (kKStages + kVStages) + 3 * (kKSlots + kVSlots) + 8 + 4 * kSBufs + 1 : 2 * (kKSlots + 2) + 3 * kVSlots + 3 * kSBufs + 1;
+  static constexpr int kNumBars = CODES ? 2 * (kKStages + kVStages) + 3 * (kKSlots + kVSlots) + 8 + 3 * kSBufs + 1 : 2 * (kKSlots + 2) + 3 * kVSlots + 3 * kSBufs + 1;
   static constexpr int kMisc = (kBar + 8 * kNumBars + 15) / 16 * 16;         // tensor-memory base, abort flag, wait limit (8 bytes)
   static constexpr int kBytes = kMisc + 16;
   static_assert(kBytes <= 227 * 1024, "shared memory of an SM");
 };
 
-// The same places in both CTAs.  ready (first CTA only): a tile can be read by the MMAs in both CTAs, or over codes in the second one; done (codes): this
-// CTA's half has been widened; empty: the MMAs have finished with the slot (both CTAs).
+// The same places in both CTAs.  ready (first CTA only): a tile can be read by the MMAs, in both CTAs; full, done (codes): the second CTA's half has been widened,
+// which one of its idle warps passes on; empty: the MMAs have finished with the slot (both CTAs).
 template <int D, bool CODES>
 struct Bars {
   using S = Smem<D, CODES>;
   uint32_t base;
   static constexpr uint32_t kVAt = 2 * S::kKSlots, kQAt = kVAt + 3 * S::kVSlots, kSAt = kQAt + 4, kCAt = kSAt + 3 * kSBufs + 1;
-  static constexpr uint32_t kKStageAt = kCAt + S::kKSlots + 4 + kSBufs, kVStageAt = kKStageAt + 2 * S::kKStages;
+  static constexpr uint32_t kKStageAt = kCAt + S::kKSlots + 4, kVStageAt = kKStageAt + 2 * S::kKStages;
   __device__ __forceinline__ uint32_t at(uint32_t i) const { return base + 8u * i; }
   __device__ __forceinline__ uint32_t k_ready(uint32_t i) const { return at(i); }
   __device__ __forceinline__ uint32_t k_empty(uint32_t i) const { return at(S::kKSlots + i); }
@@ -89,17 +88,12 @@ struct Bars {
   __device__ __forceinline__ uint32_t k_done(uint32_t i) const { return at(kCAt + i); }
   __device__ __forceinline__ uint32_t q_full(uint32_t i) const { return at(kCAt + S::kKSlots + i); }     // a query tile has landed
   __device__ __forceinline__ uint32_t q_done(uint32_t i) const { return at(kCAt + S::kKSlots + 2 + i); }
-  __device__ __forceinline__ uint32_t scales(uint32_t i) const { return at(kCAt + S::kKSlots + 4 + i); } // of a step
   __device__ __forceinline__ uint32_t kc_full(uint32_t i) const { return at(kKStageAt + i); }
   __device__ __forceinline__ uint32_t kc_empty(uint32_t i) const { return at(kKStageAt + S::kKStages + i); }
   __device__ __forceinline__ uint32_t vc_full(uint32_t i) const { return at(kVStageAt + i); }
   __device__ __forceinline__ uint32_t vc_empty(uint32_t i) const { return at(kVStageAt + S::kVStages + i); }
 };
 
-template <int N>
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ uint4 load_shared(uint32_t addr) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
@@ -110,8 +104,10 @@ __device__ __forceinline__ void store_shared(uint32_t addr, const uint4& v) {
 }
 // Sixteen codes as two vectors of eight fp16 numbers.
 __device__ __forceinline__ void widen_codes(const uint4& c, uint4& lo, uint4& hi) {
-  lo = make_uint4(half_of_codes(c.x), half_of_codes(c.x >> 16), half_of_codes(c.y), half_of_codes(c.y >> 16));
-  hi = make_uint4(half_of_codes(c.z), half_of_codes(c.z >> 16), half_of_codes(c.w), half_of_codes(c.w >> 16));
+  half_of_codes(c.x, lo.x, lo.y);
+  half_of_codes(c.y, lo.z, lo.w);
+  half_of_codes(c.z, hi.x, hi.y);
+  half_of_codes(c.w, hi.z, hi.w);
 }
 
 template <int D, bool PAGED, bool CODES, bool STALL>       // (STALL: of the test hook, as in chunk.cu)
@@ -138,21 +134,20 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
     prefetch_map(&map_k);
     prefetch_map(&map_v);
     prefetch_map(&map_q);
-    for (int i = 0; i < kKSlots; ++i) { mbar_init(B.k_ready(i), 1); mbar_init(B.k_empty(i), 1); }
-    for (int i = 0; i < kVSlots; ++i) { mbar_init(B.v_full(i), CODES ? 4 : 1); mbar_init(B.v_ready(i), CODES ? 1 : 2); mbar_init(B.v_empty(i), 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(B.q_ready(i), 1); mbar_init(B.q_empty(i), 1); }
+    for (int i = 0; i < kKSlots; ++i) { mbar_init(B.k_ready(i), CODES ? 2 : 1); mbar_init(B.k_empty(i), 1); }
+    for (int i = 0; i < kVSlots; ++i) { mbar_init(B.v_full(i), 1); mbar_init(B.v_ready(i), 2); mbar_init(B.v_empty(i), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(B.q_ready(i), CODES ? 3 : 1); mbar_init(B.q_empty(i), 1); }
     for (int i = 0; i < kSBufs; ++i) {
-      mbar_init(B.s_full(i), 1);
+      mbar_init(B.s_full(i), CODES ? 2 : 1);       // (codes: the step's scales as well)
       mbar_init(B.p_full(i), 8);           // a group's four warps, in both CTAs
       mbar_init(B.o_done(i), 1);
     }
     mbar_init(B.o_free(), 8);
     if constexpr (CODES) {
-      for (int i = 0; i < kKSlots; ++i) mbar_init(B.k_done(i), 4);
-      for (int i = 0; i < 2; ++i) { mbar_init(B.q_full(i), 1); mbar_init(B.q_done(i), 4); }
-      for (int i = 0; i < kSBufs; ++i) mbar_init(B.scales(i), 1);
-      for (int i = 0; i < S::kKStages; ++i) { mbar_init(B.kc_full(i), 1); mbar_init(B.kc_empty(i), 4); }
-      for (int i = 0; i < S::kVStages; ++i) { mbar_init(B.vc_full(i), 1); mbar_init(B.vc_empty(i), 4); }
+      for (int i = 0; i < kKSlots; ++i) mbar_init(B.k_done(i), 1);
+      for (int i = 0; i < 2; ++i) { mbar_init(B.q_full(i), 1); mbar_init(B.q_done(i), 2); }
+      for (int i = 0; i < S::kKStages; ++i) { mbar_init(B.kc_full(i), 1); mbar_init(B.kc_empty(i), 1); }
+      for (int i = 0; i < S::kVStages; ++i) { mbar_init(B.vc_full(i), 1); mbar_init(B.vc_empty(i), 1); }
     }
     *s_abort = 0;
     *reinterpret_cast<volatile unsigned long long*>(smem + S::kMisc + 8) = p.wait_limit_ns;
@@ -185,7 +180,6 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
   auto span_of = [&](const Item& it) { return chunk_span(p, it.L, it.part * p.ut); };
 
   if (warp >= R::kConv) {
-    if constexpr (CODES) fewer_registers<88>();
     if (warp == R::kProducer) {
       // =========================================================================== copies
       // Order: K(0), K(1), K(2), then V(g), K(g + 3), g counting this pair's steps over all items (the score MMA runs up to three
@@ -247,136 +241,151 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
       ck.tile = ck.end = cv.tile = cv.end = 0;
       ck.valid = cv.valid = true;
       ck.wrong = cv.wrong = false;
-      advance(ck, false);
-      advance(cv, true);
+      // One loop, so that the code of a step stands here once: n = -4 looks up the first tiles, from -3 on a K tile is asked for, from 0 on V(n) before it.
       [[maybe_unused]] int keys = 0, values = 0;                     // tiles issued
-      auto next_key = [&]() {
-        if (!ck.valid || !ok) return;
-        if constexpr (STALL) {
-          if (keys++ >= p.stall_after_tiles) return;
-        }
-        if (ck.fresh) {
-          // box of TPT tokens x G heads x 64 columns: rows land in (token, head) order; rows of the next sequence (or zeros past
-          // the tensor) that come along are computed and never written
-          const uint32_t qb = q_items & 1u;
-          ok = mbar_wait_warp(B.q_empty(qb), ((q_items >> 1) & 1u) ^ 1u, s_abort);
-          if (!ok) return;
-          if (lane == 0) {
-            if constexpr (CODES) mbar_expect_tx(B.q_full(qb), S::kSlabs * p.tpt * p.G * 128);
-            else if (rank == 0) mbar_expect_tx(B.q_ready(qb), 2 * S::kSlabs * p.tpt * p.G * 128);
-#pragma unroll
-            for (int sl = 0; sl < S::kSlabs; ++sl) {
-              const uint32_t dst = sbase + S::kQ + qb * S::kQBytes + sl * S::kQSlab;
-              const int token = ck.it.start + (2 * ck.it.part + half) * p.tpt;
-              if constexpr (CODES) tma_load_3d(dst, &map_q, sl * 64, ck.it.g * p.G, token, B.q_full(qb));
-              else tma_load_3d_pair(dst, &map_q, sl * 64, ck.it.g * p.G, token, B.q_ready(qb) + to_first);
-            }
+#pragma unroll 1
+      for (int n = -4; ok; ++n) {
+        if (n >= 0) {
+          if (!cv.valid) break;
+          if constexpr (STALL) {
+            if (values++ >= p.stall_after_tiles) break;
           }
-          ++q_items;
-        }
-        if constexpr (CODES) {
-          ok = mbar_wait_warp(B.kc_empty(kr.slot), kr.par ^ 1u, s_abort);
-          if (!ok) return;
-          if (lane == 0) mbar_expect_tx(B.kc_full(kr.slot), S::kKCodes);
+          const uint32_t full = CODES ? B.vc_full(vr.slot) : B.v_full(vr.slot);
+          ok = mbar_wait_warp(CODES ? B.vc_empty(vr.slot) : B.v_empty(vr.slot), vr.par ^ 1u, s_abort);
+          if (!ok) break;
+          if (lane == 0) mbar_expect_tx(full, CODES ? S::kVCodes : S::kVBytes);
           __syncwarp();
-          if (k_r0 < 64) tma_load_3d(sbase + S::kKC + kr.slot * S::kKCodes + k_r0 * 128, &map_k, 0, ck.y, place(ck), B.kc_full(kr.slot));
-        } else {
-          ok = mbar_wait_warp(B.k_empty(kr.slot), kr.par ^ 1u, s_abort);
-          if (!ok) return;
-          if (lane == 0 && rank == 0) mbar_expect_tx(B.k_ready(kr.slot), 2 * S::kKBytes);
-          const int sl = lane % S::kSlabs;
-          if (k_r0 < 64)
-            tma_load_3d_pair(sbase + S::kK + kr.slot * S::kKBytes + sl * S::kKSlab + k_r0 * 128, &map_k, sl * 64, ck.y, place(ck),
-                             B.k_ready(kr.slot) + to_first);
+          if (v_r0 < kChunkTile) {
+            if constexpr (CODES) tma_load_3d(sbase + S::kVC + vr.slot * S::kVCodes + v_r0 * 64, &map_v, half * 64, cv.y, place(cv), full);
+            else tma_load_3d(sbase + S::kV + vr.slot * S::kVBytes + v_r0 * D, &map_v, half * (D / 2), cv.y, place(cv), full);
+          }
+          vr.step();
         }
-        kr.step();
+        if (n == -4 || n >= 0) advance(cv, true);
+        if (!ck.valid) continue;
+        if (n >= -3) {
+          if constexpr (STALL) {
+            if (keys++ >= p.stall_after_tiles) continue;
+          }
+          if (ck.fresh) {
+            // box of TPT tokens x G heads x 64 columns: rows land in (token, head) order; rows of the next sequence (or zeros past
+            // the tensor) that come along are computed and never written
+            const uint32_t qb = q_items & 1u;
+            ok = mbar_wait_warp(B.q_empty(qb), ((q_items >> 1) & 1u) ^ 1u, s_abort);
+            if (!ok) break;
+            if (lane == 0) {
+              if constexpr (CODES) mbar_expect_tx(B.q_full(qb), S::kSlabs * p.tpt * p.G * 128);
+              else if (rank == 0) mbar_expect_tx(B.q_ready(qb), 2 * S::kSlabs * p.tpt * p.G * 128);
+#pragma unroll
+              for (int sl = 0; sl < S::kSlabs; ++sl) {
+                const uint32_t dst = sbase + S::kQ + qb * S::kQBytes + sl * S::kQSlab;
+                const int token = ck.it.start + (2 * ck.it.part + half) * p.tpt;
+                if constexpr (CODES) tma_load_3d(dst, &map_q, sl * 64, ck.it.g * p.G, token, B.q_full(qb));
+                else tma_load_3d_pair(dst, &map_q, sl * 64, ck.it.g * p.G, token, B.q_ready(qb) + to_first);
+              }
+            }
+            ++q_items;
+          }
+          if constexpr (CODES) {
+            ok = mbar_wait_warp(B.kc_empty(kr.slot), kr.par ^ 1u, s_abort);
+            if (!ok) break;
+            if (lane == 0) mbar_expect_tx(B.kc_full(kr.slot), S::kKCodes);
+            __syncwarp();
+            if (k_r0 < 64) tma_load_3d(sbase + S::kKC + kr.slot * S::kKCodes + k_r0 * 128, &map_k, 0, ck.y, place(ck), B.kc_full(kr.slot));
+          } else {
+            ok = mbar_wait_warp(B.k_empty(kr.slot), kr.par ^ 1u, s_abort);
+            if (!ok) break;
+            if (lane == 0 && rank == 0) mbar_expect_tx(B.k_ready(kr.slot), 2 * S::kKBytes);
+            const int sl = lane % S::kSlabs;
+            if (k_r0 < 64)
+              tma_load_3d_pair(sbase + S::kK + kr.slot * S::kKBytes + sl * S::kKSlab + k_r0 * 128, &map_k, sl * 64, ck.y, place(ck),
+                               B.k_ready(kr.slot) + to_first);
+          }
+          kr.step();
+        }
         advance(ck, false);
-      };
-      for (int i = 0; i < 3; ++i) next_key();
-      while (cv.valid && ok) {
-        if constexpr (STALL) {
-          if (values++ >= p.stall_after_tiles) break;
-        }
-        const uint32_t full = CODES ? B.vc_full(vr.slot) : B.v_full(vr.slot);
-        ok = mbar_wait_warp(CODES ? B.vc_empty(vr.slot) : B.v_empty(vr.slot), vr.par ^ 1u, s_abort);
-        if (!ok) break;
-        if (lane == 0) mbar_expect_tx(full, CODES ? S::kVCodes : S::kVBytes);
-        __syncwarp();
-        if (v_r0 < kChunkTile) {
-          if constexpr (CODES) tma_load_3d(sbase + S::kVC + vr.slot * S::kVCodes + v_r0 * 64, &map_v, half * 64, cv.y, place(cv), full);
-          else tma_load_3d(sbase + S::kV + vr.slot * S::kVBytes + v_r0 * D, &map_v, half * (D / 2), cv.y, place(cv), full);
-        }
-        vr.step();
-        advance(cv, true);
-        next_key();
       }
     } else if (warp == R::kRelay) {
       bool ok = true;
       uint32_t steps = 0, items = 0;
       if constexpr (CODES) {
         // =========================================================================== scales
-        // Four steps at a time, a lane per step and group of 16 keys: so the two dependent reads (page, scales) are on their way for four steps at
-        // once.  A step's entries are free when the PV of the step three before has finished, as its score buffer is.  Groups that the unit
-        // sees nothing of take 1, whatever their blocks hold.
-        struct Place {
-          Item it;
-          ChunkSpan span;
-          int i, tile;
-        } at;
-        at.i = -1;
-        at.tile = 0;
-        at.it.t1 = 0;
+        // Four steps at a time, a lane per step and group of 16 keys, and one round of four ahead: pages are looked up two rounds before their
+        // scales are handed on, scales are read one round before.  A step's entries are free when the PV of the step three before has
+        // finished, as its score buffer is.  Groups that the unit sees nothing of take 1, whatever their blocks hold.
         const int sub = lane >> 3, group = lane & 7;
-        bool more = true;
-        while (more && ok) {
-          // this lane's step of the four (lanes of a step walk alike; a list that ends earlier leaves later lanes without one)
-          int key = -1;
-          Item it = at.it;
-          ChunkSpan span = at.span;
-          int found = 0;
+        Item at;
+        ChunkSpan span = {};
+        int at_i = -1, tile = 0;
+        at.t1 = 0;
+        struct Round {
+          int found;                                       // steps in it
+          int g, row, page;                                // of this lane's step: KV head, slot in its page, page; row < 0: nothing to read
+        };
+        auto look_up = [&]() {
+          Round r = {0, 0, -1, 0};
+#pragma unroll 1
           for (int j = 0; j < 4; ++j) {
-            if (++at.tile >= at.it.t1) {
-              for (++at.i; at.i < n_items; ++at.i) {
-                at.it = item(at.i);
-                if (at.it.t1 > at.it.t0) break;
+            if (++tile >= at.t1) {
+              for (++at_i; at_i < n_items; ++at_i) {
+                at = item(at_i);
+                if (at.t1 > at.t0) break;
               }
-              if (at.i >= n_items) {
-                more = false;
+              if (at_i >= n_items) {
+                at.t1 = 0;
                 break;
               }
-              at.span = span_of(at.it);
-              at.tile = at.it.t0;
+              span = span_of(at);
+              tile = at.t0;
               ++items;
             }
-            ++found;
+            ++r.found;
             if (j == sub) {
-              it = at.it;
-              span = at.span;
-              key = span.tile(at.tile) * kChunkTile + group * 16;
+              const int key = span.tile(tile) * kChunkTile + group * 16;
+              if (key < at.L + at.n && span.sees_some(key, 16)) {
+                r.g = at.g;
+                r.row = key;
+                r.page = at.b;
+                if (PAGED) {
+                  r.page = __ldg(p.block_table + static_cast<size_t>(at.b) * p.max_pages + (key >> p.page_shift));
+                  r.row = key & (p.page_size - 1);
+                }
+              }
             }
           }
-          float ks = 1.f, vs = 1.f;
-          if (key >= 0 && key < it.L + it.n && span.sees_some(key, 16)) {
-            int page = it.b, row = key;
-            if (PAGED) {
-              page = __ldg(p.block_table + static_cast<size_t>(it.b) * p.max_pages + (key >> p.page_shift));
-              row = key & (p.page_size - 1);
-              if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(p.num_pages)) page = 0;
-            }
-            const long long place = (static_cast<long long>(page) * p.Hkv + it.g) * p.head_blocks + (row >> p.block_shift);
-            ks = p.k_scale[place];
-            vs = p.v_scale[place];
+          return r;
+        };
+        auto read = [&](const Round& r, float& ks, float& vs) {
+          ks = vs = 1.f;
+          if (r.row >= 0) {
+            const int page = PAGED && static_cast<uint32_t>(r.page) >= static_cast<uint32_t>(p.num_pages) ? 0 : r.page;
+            const long long place = (static_cast<long long>(page) * p.Hkv + r.g) * p.head_blocks + (r.row >> p.block_shift);
+            ks = __ldg(p.k_scale + place);
+            vs = __ldg(p.v_scale + place);
           }
+        };
+        Round now = {0, 0, -1, 0}, next = now;
+        float ks = 1.f, vs = 1.f;
+#pragma unroll 1
+        do {
+          const Round later = look_up();
+          float ks_next, vs_next;
+          read(next, ks_next, vs_next);
           const uint4 entry = make_uint4(__float_as_uint(ks * p.scale_log2), __float_as_uint(fast_log2(vs)), __float_as_uint(fast_rcp(vs)), 0u);
-          for (int j = 0; j < found && ok; ++j, ++steps) {
+#pragma unroll 1
+          for (int j = 0; j < now.found && ok; ++j, ++steps) {
             const uint32_t sb = steps % kSBufs;
             if (steps >= kSBufs) ok = mbar_wait_warp(B.o_done(sb), ((steps / kSBufs) & 1u) ^ 1u, s_abort);
             if (!ok) break;
             if (j == sub) store_shared(sbase + S::kScale + (sb * kGroups + group) * 16, entry);
             __syncwarp();
-            if (lane == 0) mbar_arrive(B.scales(sb));
+            if (lane == 0) mbar_arrive(B.s_full(sb));
           }
-        }
+          now = next;
+          next = later;
+          ks = ks_next;
+          vs = vs_next;
+        } while (now.found + next.found > 0 && ok);
       } else {
         // =========================================================================== V tiles that have landed
         // Values of slots that the unit does not see may be anything, and 0 * garbage must not reach O: they are zeroed here before the first
@@ -430,24 +439,24 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
           if (it.t1 <= it.t0) continue;
           const uint32_t qb = items & 1u;
           if constexpr (CODES) {
-            ok = mbar_wait(B.q_done(qb), (items >> 1) & 1u, s_abort);
             if (rank != 0) {
+              ok = mbar_wait(B.q_done(qb), (items >> 1) & 1u, s_abort);
               if (ok) mbar_arrive_release_pair(B.q_ready(qb) + to_first);
             } else {
-              ok = ok && mbar_wait_cluster(B.q_ready(qb), (items >> 1) & 1u, s_abort);
+              ok = mbar_wait_cluster(B.q_ready(qb), (items >> 1) & 1u, s_abort);
             }
           } else {
             ok = mbar_wait(B.q_ready(qb), (items >> 1) & 1u, s_abort);
           }
           for (int t = it.t0; t < it.t1 && ok; ++t, ++steps) {
             if constexpr (CODES) {
-              ok = mbar_wait(B.k_done(kr.slot), kr.par, s_abort);
               if (rank != 0) {
+                ok = mbar_wait(B.k_done(kr.slot), kr.par, s_abort);
                 if (ok) mbar_arrive_release_pair(B.k_ready(kr.slot) + to_first);
                 kr.step();
                 continue;
               }
-              ok = ok && mbar_wait_cluster(B.k_ready(kr.slot), kr.par, s_abort);
+              ok = mbar_wait_cluster(B.k_ready(kr.slot), kr.par, s_abort);
             } else {
               ok = mbar_wait(B.k_ready(kr.slot), kr.par, s_abort);
             }
@@ -479,13 +488,13 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
           if (it.t1 <= it.t0) continue;
           for (int t = it.t0; t < it.t1 && ok; ++t) {
             if constexpr (CODES) {
-              ok = mbar_wait(B.v_full(vr.slot), vr.par, s_abort);
               if (rank != 0) {
+                ok = mbar_wait(B.v_full(vr.slot), vr.par, s_abort);
                 if (ok) mbar_arrive_release_pair(B.v_ready(vr.slot) + to_first);
                 vr.step();
                 continue;
               }
-              ok = ok && mbar_wait_cluster(B.v_ready(vr.slot), vr.par, s_abort);
+              ok = mbar_wait_cluster(B.v_ready(vr.slot), vr.par, s_abort);
             } else {
               ok = mbar_wait(B.v_ready(vr.slot), vr.par, s_abort);
             }
@@ -504,107 +513,98 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
       }
     } else {
       // =========================================================================== widening (codes)
-      // The four warps share every tile: K(0), K(1), K(2), then V(g), K(g + 3), an item's query tile before its first K tile.  The eight
-      // lanes of a 16-byte access meet no bank twice: K's lanes of the upper columns store their odd piece first.
+      // Two warps take the K tiles in turn, two the V tiles: what a tile costs is mostly waiting (for the codes, for the slot, for shared memory), so
+      // four tiles are under way at a time.  The K warps turn an item's queries, too, half the rows each.  The eight lanes of a 16-byte access
+      // meet no bank twice: K's lanes of the upper columns store their odd piece first.
       if constexpr (CODES) {
-        const int w = warp - R::kConv, thread = w * 32 + lane;
-        Ring<S::kKStages> kc;
-        Ring<S::kVStages> vc;
-        Ring<kKSlots> kr;
-        Ring<kVSlots> vr;
+        const uint32_t w = static_cast<uint32_t>(warp - R::kConv) & 1u;
+        const bool is_v = warp >= R::kConv + 2;
         bool ok = true;
-        uint32_t items = 0;
-        int ki = -1, kt = 0, kend = 0;                     // the K tiles' place in the work list
-        bool k_more = true;
-        auto next_key = [&]() {
-          if (!k_more || !ok) return;
-          if (++kt >= kend) {
-            for (++ki; ki < n_items; ++ki) {
-              const Item it = item(ki);
-              kt = it.t0;
-              kend = it.t1;
-              if (kend > kt) break;
-            }
-            if (ki >= n_items) {
-              k_more = false;
-              return;
-            }
+        uint32_t g = 0, items = 0;
+        for (int i = 0; i < n_items && ok; ++i) {
+          const Item it = item(i);
+          if (it.t1 <= it.t0) continue;
+          const ChunkSpan span = span_of(it);
+          if (!is_v) {
             // ---- the item's queries, in place: a lane per row
             const uint32_t qb = items & 1u;
             ok = mbar_wait_warp(B.q_full(qb), (items >> 1) & 1u, s_abort);
-            if (!ok) return;
-            const uint32_t at = sbase + S::kQ + qb * S::kQBytes + thread * 128, swz = thread & 7;
-            uint32_t top = 0;
-#pragma unroll 4
-            for (int e = 0; e < 16; ++e) {
-              const uint4 v = load_shared(at + (e >> 3) * S::kQSlab + (((e & 7) ^ swz) << 4));
-              top = max(max(top, max(magnitude_bits(v.x), magnitude_bits(v.y))), max(magnitude_bits(v.z), magnitude_bits(v.w)));
-            }
-            const RowFactor f = row_factor(top);
-#pragma unroll 4
-            for (int e = 0; e < 16; ++e) {
-              const uint32_t to = at + (e >> 3) * S::kQSlab + (((e & 7) ^ swz) << 4);
-              const uint4 v = load_shared(to);
-              store_shared(to, make_uint4(half_of_bf16(v.x, f.down), half_of_bf16(v.y, f.down), half_of_bf16(v.z, f.down), half_of_bf16(v.w, f.down)));
-            }
-            reinterpret_cast<volatile unsigned long long*>(smem + S::kFactor)[(items % S::kFactors) * 128 + thread] = tagged(items, f.up);
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(B.q_done(qb));
-            ++items;
-          }
-          ok = mbar_wait_warp(B.kc_full(kc.slot), kc.par, s_abort) && mbar_wait_warp(B.k_empty(kr.slot), kr.par ^ 1u, s_abort);
-          if (!ok) return;
-          const uint32_t from = sbase + S::kKC + kc.slot * S::kKCodes, to = sbase + S::kK + kr.slot * S::kKBytes;
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int j = u * 128 + thread, row = j >> 3, piece = j & 7;
-            uint4 lo, hi;
-            widen_codes(load_shared(from + j * 16), lo, hi);
-            const uint32_t at = to + (piece >> 2) * S::kKSlab + row * 128, first = 2 * (piece & 3), flip = piece >> 2;
-            store_shared(at + (((first + flip) ^ (row & 7)) << 4), flip ? hi : lo);
-            store_shared(at + (((first + 1 - flip) ^ (row & 7)) << 4), flip ? lo : hi);
-          }
-          fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(B.k_done(kr.slot));
-            mbar_arrive(B.kc_empty(kc.slot));
-          }
-          kc.step();
-          kr.step();
-        };
-        for (int i = 0; i < 3; ++i) next_key();
-        for (int i = 0; i < n_items && ok; ++i) {
-          const Item it = item(i);
-          const ChunkSpan span = span_of(it);
-          for (int t = it.t0; t < it.t1 && ok; ++t) {
-            ok = mbar_wait_warp(B.vc_full(vc.slot), vc.par, s_abort) && mbar_wait_warp(B.v_empty(vr.slot), vr.par ^ 1u, s_abort);
             if (!ok) break;
-            const uint32_t from = sbase + S::kVC + vc.slot * S::kVCodes, to = sbase + S::kV + vr.slot * S::kVBytes;
-            // values of slots that the unit does not see may be anything, and 0 * garbage must not reach O
-            const int key0 = span.tile(t) * kChunkTile, in_use = it.L + it.n;
-            const bool clean = key0 + kChunkTile <= in_use && span.sees_all(key0, kChunkTile);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const int j = u * 128 + thread, row = j >> 2, piece = j & 3;
-              uint4 c = load_shared(from + j * 16), lo, hi;
-              if (!clean && (key0 + row >= in_use || !span.sees(key0 + row))) c = make_uint4(0u, 0u, 0u, 0u);
-              widen_codes(c, lo, hi);
-              const uint32_t at = to + row * 128;
-              store_shared(at + (((2 * piece) ^ (row & 7)) << 4), lo);
-              store_shared(at + (((2 * piece + 1) ^ (row & 7)) << 4), hi);
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+              const int row = static_cast<int>(w) * 64 + half * 32 + lane;
+              const uint32_t at = sbase + S::kQ + qb * S::kQBytes + row * 128, swz = row & 7;
+              uint32_t top = 0;
+#pragma unroll 8
+              for (int e = 0; e < 16; ++e) {
+                const uint4 v = load_shared(at + (e >> 3) * S::kQSlab + (((e & 7) ^ swz) << 4));
+                top = max(max(top, max(magnitude_bits(v.x), magnitude_bits(v.y))), max(magnitude_bits(v.z), magnitude_bits(v.w)));
+              }
+              const RowFactor f = row_factor(top);
+#pragma unroll 4
+              for (int e = 0; e < 16; ++e) {
+                const uint32_t to = at + (e >> 3) * S::kQSlab + (((e & 7) ^ swz) << 4);
+                const uint4 v = load_shared(to);
+                store_shared(to, make_uint4(half_of_bf16(v.x, f.down), half_of_bf16(v.y, f.down), half_of_bf16(v.z, f.down), half_of_bf16(v.w, f.down)));
+              }
+              reinterpret_cast<volatile unsigned long long*>(smem + S::kFactor)[(items % S::kFactors) * 128 + row] = tagged(items, f.up);
             }
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) {
-              mbar_arrive(B.v_full(vr.slot));
-              mbar_arrive(B.vc_empty(vc.slot));
-            }
-            vc.step();
-            vr.step();
-            next_key();
+            if (lane == 0) mbar_arrive(rank == 0 ? B.q_ready(qb) : B.q_done(qb));
           }
+          ++items;
+          for (int t = it.t0 + static_cast<int>((g ^ w) & 1u); t < it.t1 && ok; t += 2) {
+            const uint32_t gs = g + (t - it.t0);
+            if (!is_v) {
+              const uint32_t st = gs % S::kKStages, sl = gs % kKSlots;
+              ok = mbar_wait_warp(B.kc_full(st), (gs / S::kKStages) & 1u, s_abort) && mbar_wait_warp(B.k_empty(sl), ((gs / kKSlots) & 1u) ^ 1u, s_abort);
+              if (!ok) break;
+              const uint32_t piece = lane & 7, flip = piece >> 2, row0 = lane >> 3;
+              const uint32_t from = sbase + S::kKC + st * S::kKCodes + lane * 16, to = sbase + S::kK + sl * S::kKBytes + flip * S::kKSlab;
+              const uint32_t one = 2 * (piece & 3) + flip, two = 2 * (piece & 3) + 1 - flip;
+#pragma unroll 4
+              for (uint32_t u = 0; u < 16; ++u) {
+                const uint32_t row = u * 4 + row0;
+                uint4 lo, hi;
+                widen_codes(load_shared(from + u * 512), lo, hi);
+                store_shared(to + row * 128 + ((one ^ (row & 7)) << 4), flip ? hi : lo);
+                store_shared(to + row * 128 + ((two ^ (row & 7)) << 4), flip ? lo : hi);
+              }
+              fence_proxy_async();
+              __syncwarp();
+              if (lane == 0) {
+                mbar_arrive(rank == 0 ? B.k_ready(sl) : B.k_done(sl));
+                mbar_arrive(B.kc_empty(st));
+              }
+            } else {
+              const uint32_t st = gs % S::kVStages, sl = gs % kVSlots;
+              ok = mbar_wait_warp(B.vc_full(st), (gs / S::kVStages) & 1u, s_abort) && mbar_wait_warp(B.v_empty(sl), ((gs / kVSlots) & 1u) ^ 1u, s_abort);
+              if (!ok) break;
+              // values of slots that the unit does not see may be anything, and 0 * garbage must not reach O
+              const int key0 = span.tile(t) * kChunkTile, in_use = it.L + it.n;
+              const bool clean = key0 + kChunkTile <= in_use && span.sees_all(key0, kChunkTile);
+              const uint32_t piece = lane & 3, row0 = lane >> 2;
+              const uint32_t from = sbase + S::kVC + st * S::kVCodes + lane * 16, to = sbase + S::kV + sl * S::kVBytes + row0 * 128;
+              const uint32_t one = ((2 * piece) ^ row0) << 4, two = ((2 * piece + 1) ^ row0) << 4;
+#pragma unroll 4
+              for (uint32_t u = 0; u < 16; ++u) {
+                const int key = key0 + static_cast<int>(u * 8 + row0);
+                uint4 c = load_shared(from + u * 512), lo, hi;
+                if (!clean && (key >= in_use || !span.sees(key))) c = make_uint4(0u, 0u, 0u, 0u);
+                widen_codes(c, lo, hi);
+                store_shared(to + u * 1024 + one, lo);
+                store_shared(to + u * 1024 + two, hi);
+              }
+              fence_proxy_async();
+              __syncwarp();
+              if (lane == 0) {
+                mbar_arrive(rank == 0 ? B.v_ready(sl) : B.v_full(sl));
+                mbar_arrive(B.vc_empty(st));
+              }
+            }
+          }
+          g += static_cast<uint32_t>(it.t1 - it.t0);
         }
       }
     }
@@ -615,7 +615,6 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
     // takes its exponentials, and the other picks it up at step g + 1; each keeps its own part of the row sum.  fp32 throughout, in the log2
     // domain; the probabilities are rounded to bf16 (relative 2^-8 each) or, over codes and times vs, to fp16 (2^-11) for the tensor cores, the sum that divides
     // them is kept from the unrounded ones.
-    if constexpr (CODES) more_registers<168>();
     const uint32_t grp = static_cast<uint32_t>(warp >> 2);
     const int r = tid & 127;
     const uint32_t lane_addr = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -670,7 +669,6 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
         const uint32_t gs = sg + s, sb = gs % kSBufs, sph = (gs / kSBufs) & 1u;
         const uint32_t s_addr = tmem + lane_addr + sb * 128;
         ok = mbar_wait_warp(B.s_full(sb), sph, s_abort);
-        if constexpr (CODES) ok = ok && mbar_wait_warp(B.scales(sb), sph, s_abort);
         if (!ok) break;
         if (!warp_rests) {
           fence_after();
@@ -703,51 +701,56 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
             }
             wait_st();
           }
-          // ---- row maximum.  Chunks 0 and 1 stay in registers, chunks 2 and 3 are fetched again for the exponentials.
+          // ---- row maximum.  bf16: chunks 0 and 1 stay in registers, chunks 2 and 3 are fetched again for the exponentials.  Codes: all are fetched
+          // twice, in short loops.  The code that a step runs through in all sixteen warps is more than the instruction caches hold, so that straight
+          // lines cost more than what they do: with the loops unrolled and a third of the exponentials on the FMA pipe a step took half as
+          // long again.
           const uint32_t scale_at = sbase + S::kScale + sb * kGroups * 16;
           uint32_t ra[32], rb[32];
           float tmax = -INFINITY;
           bool odd = false;                                // a visible score that is NaN or +inf
-          {
+          if constexpr (CODES) {
+            auto top_of = [&](const uint32_t* raw, int group) {      // of 16 scores, with their scales
+              float x = -INFINITY, y = -INFINITY;
+#pragma unroll
+              for (int e = 0; e < 16; e += 4) {
+                x = max3_nan(x, __uint_as_float(raw[e]), __uint_as_float(raw[e + 1]));
+                y = max3_nan(y, __uint_as_float(raw[e + 2]), __uint_as_float(raw[e + 3]));
+              }
+              const uint4 c = load_shared(scale_at + group * 16);
+              tmax = max3_nan(tmax, fmaf(max3_nan(x, y, -INFINITY), __uint_as_float(c.x) * up, __uint_as_float(c.y)), -INFINITY);
+            };
+            ld32(s_addr, ra);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+              wait_ld();
+              ld32(s_addr + h * 64 + 32, rb);
+              top_of(ra, 4 * h);
+              top_of(ra + 16, 4 * h + 1);
+              wait_ld();
+              if (h == 0) ld32(s_addr + 64, ra);
+              top_of(rb, 4 * h + 2);
+              top_of(rb + 16, 4 * h + 3);
+            }
+            ld16(s_addr, ra);                              // (the first scores again)
+            odd = !(tmax < INFINITY);
+          } else {
             uint32_t rc[32], rd[32];
             ld32(s_addr + 64, rc);
             ld32(s_addr + 96, rd);
             ld32(s_addr, ra);
             ld32(s_addr + 32, rb);
             wait_ld();
-            if constexpr (CODES) {
-              auto top_of = [&](const uint32_t* raw, int group) {      // of 16 scores, with their scales
-                float x = -INFINITY, y = -INFINITY;
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                  x = max3_nan(x, __uint_as_float(raw[e]), __uint_as_float(raw[e + 1]));
-                  y = max3_nan(y, __uint_as_float(raw[e + 2]), __uint_as_float(raw[e + 3]));
-                }
-                const uint4 c = load_shared(scale_at + group * 16);
-                const float z = fmaf(max3_nan(x, y, -INFINITY), __uint_as_float(c.x) * up, __uint_as_float(c.y));
-                odd |= !(z < INFINITY);
-                tmax = fmaxf(tmax, z);
-              };
-              top_of(rc, 4);
-              top_of(rc + 16, 5);
-              top_of(rd, 6);
-              top_of(rd + 16, 7);
-              top_of(ra, 0);
-              top_of(ra + 16, 1);
-              top_of(rb, 2);
-              top_of(rb + 16, 3);
-            } else {
-              float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-              for (int e = 0; e < 32; e += 2) {
-                mx[0] = max3_nan(mx[0], __uint_as_float(rc[e]), __uint_as_float(rc[e + 1]));
-                mx[1] = max3_nan(mx[1], __uint_as_float(rd[e]), __uint_as_float(rd[e + 1]));
-                mx[2] = max3_nan(mx[2], __uint_as_float(ra[e]), __uint_as_float(ra[e + 1]));
-                mx[3] = max3_nan(mx[3], __uint_as_float(rb[e]), __uint_as_float(rb[e + 1]));
-              }
-              tmax = max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], -INFINITY) * scale_log2;   // scale > 0
-              odd = !(tmax < INFINITY);
+            for (int e = 0; e < 32; e += 2) {
+              mx[0] = max3_nan(mx[0], __uint_as_float(rc[e]), __uint_as_float(rc[e + 1]));
+              mx[1] = max3_nan(mx[1], __uint_as_float(rd[e]), __uint_as_float(rd[e + 1]));
+              mx[2] = max3_nan(mx[2], __uint_as_float(ra[e]), __uint_as_float(ra[e + 1]));
+              mx[3] = max3_nan(mx[3], __uint_as_float(rb[e]), __uint_as_float(rb[e + 1]));
             }
+            tmax = max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], -INFINITY) * scale_log2;   // scale > 0
+            odd = !(tmax < INFINITY);
           }
           // such a score makes the row NaN (through its sum: not every exponential below passes one on)
           if (odd) l_sum = __uint_as_float(0x7fffffffu);
@@ -792,58 +795,70 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
           }
           // ---- exponentials and packed P over score columns that have been read
           const float neg_base = m_ref == -INFINITY ? 0.f : -m_ref;
-          uint64_t ls2[2] = {0ull, 0ull};
-          uint32_t pk[16];
-          auto exp_pair = [&](const uint32_t* raw, int e, uint64_t scale2, uint64_t base2, float& p0, float& p1) {
-            const uint64_t x2 = fma2(pack2(__uint_as_float(raw[2 * e]), __uint_as_float(raw[2 * e + 1])), scale2, base2);
-            if (e % kPolyStride == kPolyStride - 1) {
-              poly_exp2_pair(x2, p0, p1);
-            } else {
-              float a, b;
-              unpack2(x2, a, b);
-              p0 = fast_exp2(a);
-              p1 = fast_exp2(b);
-            }
-          };
-          auto exp_chunk = [&](const uint32_t* raw, int c) {
-            if constexpr (CODES) {
+          if constexpr (CODES) {
+            auto exp_group = [&](const uint32_t* raw, int group) {   // 16 scores with their scales
+              const uint4 c = load_shared(scale_at + group * 16);
+              const float a = __uint_as_float(c.x) * up, base = __uint_as_float(c.y) + neg_base + kHalfShift;
+              const uint64_t scale2 = pack2(a, a), base2 = pack2(base, base);
+              uint64_t ls2[2] = {0ull, 0ull};
+              uint32_t pk[8];
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {                // 16 scores with their scales
-                const uint4 sc = load_shared(scale_at + (2 * c + h) * 16);
-                const float a = __uint_as_float(sc.x) * up, base = __uint_as_float(sc.y) + neg_base + kHalfShift;
-                const uint64_t scale2 = pack2(a, a), base2 = pack2(base, base);
-                ls2[0] = ls2[1] = 0ull;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                  float p0, p1;
-                  exp_pair(raw + 16 * h, e, scale2, base2, p0, p1);
-                  ls2[e & 1] = add2(ls2[e & 1], pack2(p0, p1));
-                  pk[8 * h + e] = pack_half(p0, p1);
-                }
+              for (int e = 0; e < 8; ++e) {
                 float x, y;
-                unpack2(add2(ls2[0], ls2[1]), x, y);
-                l_sum = fmaf(x + y, __uint_as_float(sc.z), l_sum);
+                unpack2(fma2(pack2(__uint_as_float(raw[2 * e]), __uint_as_float(raw[2 * e + 1])), scale2, base2), x, y);
+                float p0, p1;
+                if (e == 7) {                              // (one pair in eight on the FMA pipe: 3 % faster than none, one in four 1 %)
+                  poly_exp2_pair(pack2(x, y), p0, p1);
+                } else {
+                  p0 = fast_exp2(x);
+                  p1 = fast_exp2(y);
+                }
+                ls2[e & 1] = add2(ls2[e & 1], pack2(p0, p1));
+                pk[e] = pack_half(p0, p1);
               }
-            } else {
-              const uint64_t scale2 = pack2(scale_log2, scale_log2), base2 = pack2(neg_base, neg_base);
+              st8(s_addr + group * 8, pk);
+              float x, y;
+              unpack2(add2(ls2[0], ls2[1]), x, y);
+              l_sum = fmaf(x + y, __uint_as_float(c.z), l_sum);
+            };
+#pragma unroll 1
+            for (int h = 0; h < 4; ++h) {
+              wait_ld();
+              ld16(s_addr + h * 32 + 16, rb);
+              exp_group(ra, 2 * h);
+              wait_ld();
+              if (h < 3) ld16(s_addr + h * 32 + 32, ra);
+              exp_group(rb, 2 * h + 1);
+            }
+          } else {
+            uint64_t ls2[2] = {0ull, 0ull};
+            const uint64_t scale2 = pack2(scale_log2, scale_log2), base2 = pack2(neg_base, neg_base);
+            uint32_t pk[16];
+            auto exp_chunk = [&](const uint32_t* raw, int c) {
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
+                const uint64_t x2 = fma2(pack2(__uint_as_float(raw[2 * e]), __uint_as_float(raw[2 * e + 1])), scale2, base2);
                 float p0, p1;
-                exp_pair(raw, e, scale2, base2, p0, p1);
+                if (e % kPolyStride == kPolyStride - 1) {
+                  poly_exp2_pair(x2, p0, p1);
+                } else {
+                  float a, b;
+                  unpack2(x2, a, b);
+                  p0 = fast_exp2(a);
+                  p1 = fast_exp2(b);
+                }
                 ls2[e & 1] = add2(ls2[e & 1], pack2(p0, p1));
                 pk[e] = pack_bf16(p0, p1);
               }
-            }
-            st16(s_addr + c * 16, pk);
-          };
-          exp_chunk(ra, 0);
-          ld32(s_addr + 64, ra);
-          exp_chunk(rb, 1);
-          ld32(s_addr + 96, rb);
-          wait_ld();
-          exp_chunk(ra, 2);
-          exp_chunk(rb, 3);
-          if constexpr (!CODES) {
+              st16(s_addr + c * 16, pk);
+            };
+            exp_chunk(ra, 0);
+            ld32(s_addr + 64, ra);
+            exp_chunk(rb, 1);
+            ld32(s_addr + 96, rb);
+            wait_ld();
+            exp_chunk(ra, 2);
+            exp_chunk(rb, 3);
             float a, b, c, d;
             unpack2(ls2[0], a, b);
             unpack2(ls2[1], c, d);
@@ -879,29 +894,48 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
             const float l_row = fmaf(value_of(other), m_in == m_ref ? 1.f : fast_exp2(m_in - m_ref), l_sum);   // the other's sum is relative to the reference it last saw
             const float inv = l_row > 0.f ? 1.f / l_row : (l_row == 0.f ? 0.f : l_row);                 // a NaN sum stays one
             const int slot = it.slot < 0 ? -1 : it.slot + static_cast<int>(rank);
-            // The accumulator is given back as soon as it is in registers: the next item's first PV waits for that.
-            uint32_t o[D];
+            __nv_bfloat16* out_row = p.out + (static_cast<size_t>(it.start + token) * p.Hq + it.g * p.G + head_r) * D;
+            // an fp32 partial is laid out [4 columns][row], so that the lanes of a store write consecutive 16-byte pieces
+            float* part = p.work.part_o + static_cast<size_t>(slot < 0 ? 0 : slot) * (D / 4) * (128 * 4) + r * 4;
+            auto write = [&](const uint32_t* o, int c) {     // 32 columns of the accumulator
+              if (row_valid && slot < 0) {
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) ld32(o_addr + c * 32, o + c * 32);
-            wait_ld();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_pair(o_free_to);
-            if (row_valid && slot < 0) {
-              __nv_bfloat16* out_row = p.out + (static_cast<size_t>(it.start + token) * p.Hq + it.g * p.G + head_r) * D;
+                for (int e = 0; e < 32; e += 16) {
+                  uint32_t v[8];
 #pragma unroll
-              for (int e = 0; e < D; e += 16) {
-                uint32_t v[8];
+                  for (int k = 0; k < 8; ++k) v[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
+                  st_global_v8(out_row + c * 32 + e, v);
+                }
+              } else if (row_valid) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
-                st_global_v8(out_row + e, v);
+                for (int e = 0; e < 32; e += 4)
+                  *reinterpret_cast<uint4*>(part + (c * 8 + e / 4) * (128 * 4)) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
               }
-            } else if (row_valid) {
-              // an fp32 partial is laid out [4 columns][row], so that the lanes of a store write consecutive 16-byte pieces
-              float* part = p.work.part_o + static_cast<size_t>(slot) * (D / 4) * (128 * 4) + r * 4;
+            };
+            if constexpr (CODES) {
+              uint32_t o[32];
+#pragma unroll 1
+              for (int c = 0; c < D / 32; ++c) {
+                ld32(o_addr + c * 32, o);
+                wait_ld();
+                if (c == D / 32 - 1) {
+                  fence_before();
+                  __syncwarp();
+                  if (lane == 0) mbar_arrive_pair(o_free_to);
+                }
+                write(o, c);
+              }
+            } else {
+              // The accumulator is given back as soon as it is in registers: the next item's first PV waits for that.
+              uint32_t o[D];
 #pragma unroll
-              for (int e = 0; e < D; e += 4)
-                *reinterpret_cast<uint4*>(part + (e / 4) * (128 * 4)) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+              for (int c = 0; c < D / 32; ++c) ld32(o_addr + c * 32, o + c * 32);
+              wait_ld();
+              fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive_pair(o_free_to);
+#pragma unroll
+              for (int c = 0; c < D / 32; ++c) write(o + c * 32, c);
             }
             if (row_valid && slot >= 0) p.work.part_ml[static_cast<size_t>(slot) * 128 + r] = make_float2(m_ref, l_row);
           } else if (lane == 0) {

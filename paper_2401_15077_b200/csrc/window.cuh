@@ -1,7 +1,5 @@
 // What the two attention kernels with a window share (window.cu, window_rows.cu): fp16 operands, e4m3 codes, scales of blocks.
 #pragma once
-#include <cuda_fp8.h>
-
 #include "chunk.cuh"
 #include "tc.cuh"
 
@@ -17,10 +15,9 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-// Two e4m3 codes as two fp16 numbers (exact).
-__device__ __forceinline__ uint32_t half_of_codes(uint32_t two) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two & 0xffffu), __NV_E4M3);
-  return static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16;
+// Four e4m3 codes as four fp16 numbers (exact).
+__device__ __forceinline__ void half_of_codes(uint32_t four, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(four));
 }
 __device__ __forceinline__ float fast_log2(float x) {
   float y;

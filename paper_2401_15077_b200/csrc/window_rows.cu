@@ -296,7 +296,11 @@ window_rows_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
               const uint4 c = load_shared(k_at + (j * 8 + spread) * 128 + (((h * 4 + quad) ^ spread) << 4));
               const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
-              for (int k = 0; k < 4; ++k) mma_16x8x16<true>(sc[j], qa[h * 4 + k], half_of_codes(w[k]), half_of_codes(w[k] >> 16));
+              for (int k = 0; k < 4; ++k) {
+                uint32_t b0, b1;
+                half_of_codes(w[k], b0, b1);
+                mma_16x8x16<true>(sc[j], qa[h * 4 + k], b0, b1);
+              }
             }
           } else {
 #pragma unroll
@@ -409,8 +413,11 @@ window_rows_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
                 const uint32_t even = __byte_perm(vb[2 * h], vb[2 * h + 1], 0x6420), odd = __byte_perm(vb[2 * h], vb[2 * h + 1], 0x7531);
-                mma_16x8x16<true>(o[(2 * d + h) * 2], pa[k], half_of_codes(even), half_of_codes(even >> 16));
-                mma_16x8x16<true>(o[(2 * d + h) * 2 + 1], pa[k], half_of_codes(odd), half_of_codes(odd >> 16));
+                uint32_t b0, b1;
+                half_of_codes(even, b0, b1);
+                mma_16x8x16<true>(o[(2 * d + h) * 2], pa[k], b0, b1);
+                half_of_codes(odd, b0, b1);
+                mma_16x8x16<true>(o[(2 * d + h) * 2 + 1], pa[k], b0, b1);
               }
             }
           }
