@@ -1,5 +1,6 @@
 // C ABI of the calls around verification (rotary appends, attention of chunks, logit adjustment, sampling): argument checks and launches.
 // As in api.cu nothing here allocates or synchronises.
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 
@@ -163,7 +164,7 @@ bool prepared(int head_dim, bool window = false) {
   std::lock_guard<std::mutex> lock(g_prepared_mutex);
   bool& done = g_prepared[dev][head_dim == 128][window];
   if (!done)
-    done = window ? window_prepare(head_dim) == cudaSuccess && window_rows_prepare(head_dim) == cudaSuccess
+    done = window ? window_prepare(head_dim) == cudaSuccess && window_rows_prepare(head_dim) == cudaSuccess && window_codes_prepare() == cudaSuccess
                   : chunk_prepare(head_dim) == cudaSuccess && chunk_rows_prepare(head_dim) == cudaSuccess;
   return done;
 }
@@ -180,22 +181,25 @@ eagle_chunk_desc rows_of(const eagle_window_desc& d, bool tree) {
   return as;
 }
 
-size_t chunk_workspace(const eagle_chunk_desc& desc) {
+size_t chunk_workspace(const eagle_chunk_desc& desc, int few_rows = kFewRows) {
   ChunkWork w;
   int workers = 0;
-  if (!carve_chunk_work(desc, nullptr, kMaxPlanCtas, &w, &workers)) return 0;
+  if (!carve_chunk_work(desc, nullptr, kMaxPlanCtas, &w, &workers, few_rows)) return 0;
   size_t bytes = w.bytes;
   if (!chunk_takes_rows(desc)) {           // enough for fewer tokens too, single ones among them
     eagle_chunk_desc d = desc;
     d.num_tokens = d.batch;
-    if (carve_chunk_work(d, nullptr, kMaxPlanCtas, &w, &workers) && w.bytes > bytes) bytes = w.bytes;
+    if (carve_chunk_work(d, nullptr, kMaxPlanCtas, &w, &workers, few_rows) && w.bytes > bytes) bytes = w.bytes;
   }
   return bytes;
 }
 
+// Query rows of the row kernel over codes.
+int code_rows(const eagle_chunk_desc& d) { return d.num_kv_heads > 0 && d.num_q_heads / d.num_kv_heads <= 8 ? 8 : kFewRows; }
+
 // Everything of an attention call but what tells the forms apart.
 void fill_attention(ChunkParams* params, const eagle_chunk_desc& d, float sm_scale, const void* q, const eagle_kv_store& kv, const int32_t* seq_lens,
-                    const int32_t* token_start, void* out, int32_t* status) {
+                    const int32_t* token_start, void* out, int32_t* status, int few_rows = kFewRows) {
   ChunkParams& p = *params;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.k = static_cast<const __nv_bfloat16*>(kv.k);
@@ -211,7 +215,7 @@ void fill_attention(ChunkParams* params, const eagle_chunk_desc& d, float sm_sca
   p.G = d.num_q_heads / d.num_kv_heads;
   p.D = d.head_dim;
   p.few = chunk_takes_rows(d);
-  p.rows = p.few ? kFewRows : kTileRows;
+  p.rows = p.few ? few_rows : kTileRows;
   p.tpt = p.rows / p.G;
   p.ut = p.few ? p.tpt : 2 * p.tpt;
   p.max_rows = static_cast<int>(std::fmin(1.0e9, static_cast<double>(d.num_tokens) * p.G));
@@ -234,7 +238,8 @@ int window_call(const eagle_window_desc* desc, bool tree, const void* q, const e
   const eagle_chunk_desc as = rows_of(d, tree);
   ChunkParams p = {};
   ChunkWork need;
-  if (!(d.sm_scale >= 0.f) || !(d.sm_scale < 3.0e38f) || !carve_chunk_work(as, nullptr, kMaxPlanCtas, &need, &p.num_workers)) return EAGLE_ERR_SHAPE;
+  const int few_rows = d.block_size ? code_rows(as) : kFewRows;
+  if (!(d.sm_scale >= 0.f) || !(d.sm_scale < 3.0e38f) || !carve_chunk_work(as, nullptr, kMaxPlanCtas, &need, &p.num_workers, few_rows)) return EAGLE_ERR_SHAPE;
   if (d.window < 0 || d.sinks < 0 || (tree && d.window > 0 && d.window < kMaxTree)) return EAGLE_ERR_SHAPE;
   if (d.block_size == 0 && (kv->k_scale || kv->v_scale)) return EAGLE_ERR_SHAPE;
   int rc = check_store(*kv, d.head_dim, d.num_kv_heads, &p.capacity);
@@ -248,8 +253,8 @@ int window_call(const eagle_window_desc* desc, bool tree, const void* q, const e
   const int dev = usable_device(&sms);
   if (dev != EAGLE_OK) return dev;
   if (!prepared(d.head_dim, true)) return EAGLE_ERR_DEVICE;
-  carve_chunk_work(as, d.workspace, sms, &p.work, &p.num_workers);
-  fill_attention(&p, as, d.sm_scale, q, *kv, seq_lens, tree ? nullptr : order, out, d.status);
+  carve_chunk_work(as, d.workspace, sms, &p.work, &p.num_workers, few_rows);
+  fill_attention(&p, as, d.sm_scale, q, *kv, seq_lens, tree ? nullptr : order, out, d.status, few_rows);
   // (a window that reaches past the capacity is no limit)
   p.window = d.window > p.capacity ? 0 : d.window;
   p.sinks = d.sinks > p.capacity ? static_cast<int>(p.capacity) : d.sinks;
@@ -327,7 +332,10 @@ size_t eagle_chunk_attn_workspace(const eagle_chunk_desc* desc) { return desc ? 
 
 size_t eagle_window_attn_workspace(const eagle_window_desc* desc) {
   if (!desc || desc->max_tree < 0 || desc->max_tree > kMaxTree) return 0;
-  return chunk_workspace(rows_of(*desc, desc->max_tree > 0));
+  const eagle_chunk_desc as = rows_of(*desc, desc->max_tree > 0);
+  size_t bytes = chunk_workspace(as);      // for a cache in either form
+  if (bytes > 0 && code_rows(as) != kFewRows) bytes = std::max(bytes, chunk_workspace(as, code_rows(as)));
+  return bytes;
 }
 
 int eagle_chunk_attn(const eagle_chunk_desc* desc, const void* q, const eagle_kv_store* kv, const int32_t* seq_lens,

@@ -1,5 +1,5 @@
 // Plan records, workspace and parameters of the chunk attention (chunk.cu, chunk_rows.cu) and of the attention with a window, over
-// bf16 or block-scaled caches, of chunks or trees (window.cu, window_rows.cu), which shares planner and merge.
+// bf16 or block-scaled caches, of chunks or trees (window.cu, window_rows.cu, window_codes.cu), which shares planner and merge.
 #pragma once
 #include "common.cuh"
 
@@ -123,13 +123,13 @@ __host__ __device__ inline ChunkSpan chunk_span(const ChunkParams& p, int L, int
 }
 
 // Partial slots: a worker's share of the cut units begins and ends inside a unit at the most, with the query tiles of both.
-// `sms` bounds the workers.
-inline bool carve_chunk_work(const eagle_chunk_desc& d, void* base, int sms, ChunkWork* w, int* num_workers) {
+// `sms` bounds the workers; few_rows: rows of the row kernel's query tiles (those of codes has 8 where a group has no more heads).
+inline bool carve_chunk_work(const eagle_chunk_desc& d, void* base, int sms, ChunkWork* w, int* num_workers, int few_rows = kFewRows) {
   if (d.batch < 0 || d.num_tokens < 0 || d.num_kv_heads <= 0 || d.num_q_heads <= 0 || d.num_q_heads % d.num_kv_heads) return false;
   const int G = d.num_q_heads / d.num_kv_heads;
   if (G > kMaxGroup || (d.head_dim != 64 && d.head_dim != 128) || d.batch > 65535) return false;
   const bool few = chunk_takes_rows(d);
-  const int rows = few ? kFewRows : kTileRows, tiles = few ? 1 : 2, workers = (sms < kMaxPlanCtas ? sms : kMaxPlanCtas) / tiles;
+  const int rows = few ? few_rows : kTileRows, tiles = few ? 1 : 2, workers = (sms < kMaxPlanCtas ? sms : kMaxPlanCtas) / tiles;
   const size_t B = static_cast<size_t>(d.batch), ut = tiles * (rows / G);
   const size_t units = static_cast<size_t>(d.num_kv_heads) * (d.num_tokens / ut + B);
   if (units > (1u << 28)) return false;
@@ -161,7 +161,9 @@ cudaError_t launch_chunk_plan(const ChunkParams& p, cudaStream_t stream);      /
 cudaError_t launch_chunk_merge(const ChunkParams& p, cudaStream_t stream);
 cudaError_t window_prepare(int head_dim);
 cudaError_t window_rows_prepare(int head_dim);
-cudaError_t launch_window_rows(const ChunkParams& p, cudaStream_t stream);
+cudaError_t launch_window_rows(const ChunkParams& p, cudaStream_t stream);      // bf16
+cudaError_t window_codes_prepare();
+cudaError_t launch_window_codes(const ChunkParams& p, cudaStream_t stream);     // codes
 cudaError_t launch_window(const ChunkParams& p, cudaStream_t stream);
 
 }  // namespace eagle

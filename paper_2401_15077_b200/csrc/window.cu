@@ -1004,7 +1004,7 @@ cudaError_t window_prepare(int head_dim) {
 cudaError_t launch_window(const ChunkParams& p, cudaStream_t stream) {
   cudaError_t e = launch_chunk_plan(p, stream);
   if (e != cudaSuccess) return e;
-  if (p.few) e = launch_window_rows(p, stream);
+  if (p.few) e = p.k_scale ? launch_window_codes(p, stream) : launch_window_rows(p, stream);
   else if (p.k_scale) e = launch_tiles<128, true>(p, stream);
   else e = p.D == 128 ? launch_tiles<128, false>(p, stream) : launch_tiles<64, false>(p, stream);
   if (e != cudaSuccess) return e;
