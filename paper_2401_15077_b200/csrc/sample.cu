@@ -29,26 +29,31 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kCountBins = 2048, kMassBins = 1024;
-constexpr int kCandidates = kThreads;        // values that are ranked against one another, a thread each
-constexpr size_t kSliceBytes = 160 * 1024;   // of a slice that stays in shared memory
+constexpr int kFew = 448;                    // (at least a tile's 32 x 8 and a carry of 31)
+constexpr int kCandidates = 128;             // values that are ranked against one another, a thread each (more are cut finer first, which takes less)
+constexpr size_t kSliceBytes = 160 * 1024;   // of a slice that stays in shared memory, at the most
+constexpr size_t kPairBytes = 66 * 1024;     // and where two CTAs are to fit an SM
 
 typedef unsigned long long u64;
 
 // Shared memory behind the slice.
 struct Shared {
   union {
-    uint32_t count[kCountBins];                                      // top-k's histogram
-    struct { u64 mass[kMassBins]; uint32_t number[kMassBins]; } m;   // top-p's
+    uint32_t count[kCountBins];      // top-k's histogram
+    uint32_t mass[2][kMassBins];     // top-p's: low and high words
   } hist;
   u64 slot[2][kMaxCluster][2];       // exchanges, by turns
   u64 warp_sum[kWarps];
+  double roots[16];                  // (sixteen 8-byte words: no two share a bank)
+  float few[kWarps][kFew];           // a warp's values that are left of its part of the slice, or of a tile, side by side
   uint32_t list[kCandidates];        // this CTA's candidates
   uint32_t all[kCandidates];         // the cluster's
   u64 weight[kCandidates];
   uint32_t n, lo, hi;                // candidates found here, their range
   // a cut, found by one thread or by several with the same result
   uint32_t cut_key, cut_take, cut_ties;
-  uint32_t bin, bin_number;
+  u64 cut_base;
+  uint32_t bin;
   u64 base;
 };
 
@@ -59,40 +64,56 @@ __device__ __forceinline__ uint32_t key_of(float z) {
 }
 __device__ __forceinline__ float value_of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// 2^x for -1000 < x <= 0: the nearest whole number goes to the exponent, what is left, f in [-1/2, 1/2], through the polynomial that
-// interpolates 2^f there at Chebyshev nodes (constant set to 1, so that whole numbers are exact; error 2e-14).
-__device__ __forceinline__ double exp2_double(double x) {
-  const double n = rint(x), f = x - n;
-  double r = 1.0205905413765595e-07;
-  r = fma(r, f, 1.325964524488711e-06);
-  r = fma(r, f, 1.5252672924850737e-05);
-  r = fma(r, f, 0.0001540343375125101);
-  r = fma(r, f, 0.0013333558200794592);
-  r = fma(r, f, 0.009618129193934313);
-  r = fma(r, f, 0.05550410866465167);
-  r = fma(r, f, 0.2402265069564034);
-  r = fma(r, f, 0.6931471805599462);
-  r = fma(r, f, 1.0);
-  return __hiloint2double(__double2hiint(r) + (static_cast<int>(n) << 20), __double2loint(r));
+// 2^(j / 16)
+__constant__ double kRoots[16] = {1.0, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916, 1.189207115002721, 1.241857812073484, 1.2968395546510096, 1.3542555469368927, 1.4142135623730951, 1.4768261459394993, 1.5422108254079407, 1.6104903319492543, 1.681792830507429, 1.7562521603732995, 1.8340080864093424, 1.9152065613971474};
+// 2^(x / 16) for -16000 < x <= 0: the nearest whole number is taken off by adding and subtracting 1.5 * 2^52, its low four bits go through the table, the others
+// to the exponent, and what is left, f in [-1/2, 1/2], through 1 + f times the polynomial that interpolates (2^(f / 16) - 1) / f at Chebyshev
+// nodes (relative error 9e-15).
+__device__ __forceinline__ double exp2_sixteenths(double x, const double* roots) {
+  const double big = x + 6755399441055744.0, f = x - (big - 6755399441055744.0);
+  const int n = __double2loint(big);
+  double r = 1.2716049516906705e-09;
+  r = fma(r, f, 1.4676387238435006e-07);
+  r = fma(r, f, 1.3550807778387664e-05);
+  r = fma(r, f, 0.0009383847926296646);
+  r = fma(r, f, 0.04332169878499658);
+  r = fma(r, f, 1.0) * roots[n & 15];
+  return __hiloint2double(__double2hiint(r) + ((n >> 4) << 20), __double2loint(r));
 }
 
 struct Weigher {
   float top;             // the row's largest value
-  double top_d, rate;    // log2(e) / temperature
+  double top_d, rate;    // 16 log2(e) / temperature
   double unit;           // 2^q
+  const double* roots;
   __device__ __forceinline__ double real(float z) const {
-    if (z == top) return 1.0;                             // (infinite ones too)
     const double x = (static_cast<double>(z) - top_d) * rate;
-    return x > -1000.0 ? exp2_double(x) : 0.0;            // -infinity, and NaN from infinities, are 0
+    const double e = x > -16000.0 ? exp2_sixteenths(x, roots) : 0.0;      // -infinity, and NaN from infinities, are 0
+    return z == top ? 1.0 : e;                            // (infinite ones too)
   }
   // A weight of at most 1 as an integer: adding 2^52 leaves it in the low bits of the sum.
   __device__ __forceinline__ u64 whole(double w) const { return __double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull; }
 };
 
-// One value of a row in its canonical form: NaN as -infinity, negative zero as zero.
-__device__ __forceinline__ float clean(float z) {
-  if (z != z) return -INFINITY;
-  return z + 0.f;
+// Values of a row in their canonical form: NaN as -infinity, negative zero as zero.  (A maximum passes over NaN; one word: one value or two.)
+__device__ __forceinline__ float clean(float z) { return fmaxf(z, -INFINITY) + 0.f; }
+template <typename T>
+__device__ __forceinline__ uint32_t clean_word(uint32_t w) {
+  if constexpr (sizeof(T) == 4) return __float_as_uint(clean(__uint_as_float(w)));
+  else {
+    const __nv_bfloat162 lowest = __floats2bfloat162_rn(-INFINITY, -INFINITY), zero = __floats2bfloat162_rn(0.f, 0.f);
+    const __nv_bfloat162 z = __hadd2_rn(__hmax2(*reinterpret_cast<const __nv_bfloat162*>(&w), lowest), zero);
+    return *reinterpret_cast<const uint32_t*>(&z);
+  }
+}
+// The larger one, of each half.
+template <typename T>
+__device__ __forceinline__ uint32_t max_word(uint32_t a, uint32_t b) {
+  if constexpr (sizeof(T) == 4) return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  else {
+    const __nv_bfloat162 z = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&z);
+  }
 }
 
 template <typename T>
@@ -135,6 +156,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
   const int tiles = slice / kTile;
   u64* const part = reinterpret_cast<u64*>(dyn + (RESIDENT ? static_cast<size_t>(slice) * sizeof(T) : 0));      // [tiles][warps]
   uint32_t* const ties = reinterpret_cast<uint32_t*>(part + tiles * kWarps);                                      // [tiles][warps]
+  uint16_t* const segment = reinterpret_cast<uint16_t*>(ties + tiles * kWarps);                                   // [tiles][warps]: where a tile's part of a list begins
   __shared__ Shared s;
   cg::cluster_group cluster = cg::this_cluster();
   const int C = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
@@ -144,6 +166,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
   if (p.num_rows && r >= p.num_rows[b]) return;           // (all of the cluster)
 
   // ---- the slice.  Positions count from the 16-byte boundary at or before the row's first element, so that vectors are aligned.
+  if (tid < 16) s.roots[tid] = kRoots[tid];
   auto started = cluster.barrier_arrive();                // (shared memory of the others is there once all have started)
   const T* const src = static_cast<const T*>(p.logits) + row * p.V;
   const int off = static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
@@ -153,8 +176,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
     const int id = first + pos;
     if (id >= 0 && id + kVec <= p.V) {
       v.raw = __ldg(reinterpret_cast<const uint4*>(src + id));
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) v.set(e, clean(v.at(e)));
+      v.raw = make_uint4(clean_word<T>(v.raw.x), clean_word<T>(v.raw.y), clean_word<T>(v.raw.z), clean_word<T>(v.raw.w));
     } else {
       v.raw = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
@@ -209,17 +231,89 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
     return t;
   };
 
+  // The values of a warp's part of a tile that `stays(z)` picks, side by side in shared memory behind the `from` first, so that what is expensive (an
+  // exponential in fp64) is done for 32 of them at a time however few there are in a vector.  at[e]: where element e is, -1: left out.
+  // Returns their number.
+  float* const few = s.few[warp];
+  auto pick = [&](const Vec<T>& v, int from, auto stays, int* at) {
+    int n = from;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      const bool in = stays(v.at(e));
+      const unsigned mask = __ballot_sync(0xffffffffu, in);
+      at[e] = in ? n + __popc(mask & ((1u << lane) - 1u)) : -1;
+      if (in) few[at[e]] = v.at(e);
+      n += __popc(mask);
+    }
+    __syncwarp();
+    return n;
+  };
+  // Once a bound is known below which nothing stays, each warp keeps the rest of its part of the slice in that way, if there is room for it in
+  // all warps of the CTA: `listed`.  The passes from then on go over these lists.
+  bool listed = false;
+  int n_listed = 0;
+  auto make_list = [&](auto stays) {
+    __syncthreads();
+    bool fits = true;
+    int n = 0;
+    for (int i = 0; i < tiles && fits; ++i) {
+      int at[kVec];
+      if (lane == 0) segment[i * kWarps + warp] = static_cast<uint16_t>(n);
+      n = pick(fetch((i * kThreads + tid) * kVec), n, stays, at);
+      fits = i + 1 >= tiles || n <= kFew - 32 * kVec;      // (room for another tile)
+    }
+    listed = !__syncthreads_or(!fits);
+    n_listed = n;
+  };
+  auto in_segment = [&](int i, int* to) {                 // [returned, *to) of the list: tile i
+    *to = i + 1 < tiles ? segment[(i + 1) * kWarps + warp] : n_listed;
+    return static_cast<int>(segment[i * kWarps + warp]);
+  };
+  // `done(z)` for every value that may stay (those outside of the row too, unless there is a list).
+  auto for_all = [&](auto done) {
+    if (listed) {
+      for (int j = lane; j < n_listed; j += 32) done(few[j]);
+      return;
+    }
+    for (int i = 0; i < tiles; ++i) {
+      const Vec<T> v = fetch((i * kThreads + tid) * kVec);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) done(v.at(e));
+    }
+  };
+  // The same for those that `stays`, where `done` is expensive; without a list values are carried over from tile to tile until there are 32.
+  auto for_few = [&](auto stays, auto done) {
+    if (listed) {
+      for (int j = lane; j < n_listed; j += 32)
+        if (stays(few[j])) done(few[j]);
+      return;
+    }
+    int n = 0;
+    for (int i = 0; i < tiles; ++i) {
+      int at[kVec];
+      n = pick(fetch((i * kThreads + tid) * kVec), n, stays, at);
+      int base = 0;
+      for (; base + 32 <= n; base += 32) done(few[base + lane]);
+      const float rest = base + lane < n ? few[base + lane] : 0.f;
+      n -= base;
+      __syncwarp();
+      if (lane < n) few[lane] = rest;
+      __syncwarp();
+    }
+    if (lane < n) done(few[lane]);
+    __syncwarp();
+  };
+
   // ---- the largest value
-  uint32_t top_key = 0;
+  uint32_t most = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;     // -infinity
+#pragma unroll 4
   for (int i = 0; i < tiles; ++i) {
     const int pos = (i * kThreads + tid) * kVec;
     const Vec<T> v = load(pos);
     if constexpr (RESIDENT) *reinterpret_cast<uint4*>(held + pos) = v.raw;
-    float m = v.at(0);
-#pragma unroll
-    for (int e = 1; e < kVec; ++e) m = fmaxf(m, v.at(e));
-    top_key = max(top_key, key_of(m));
+    most = max_word<T>(most, max_word<T>(max_word<T>(v.raw.x, v.raw.y), max_word<T>(v.raw.z, v.raw.w)));
   }
+  uint32_t top_key = sizeof(T) == 4 ? key_of(__uint_as_float(most)) : max(key_of(__uint_as_float(most << 16)), key_of(__uint_as_float(most & 0xffff0000u)));
   top_key = __reduce_max_sync(0xffffffffu, top_key);
   if (lane == 0) s.warp_sum[warp] = top_key;
   __syncthreads();
@@ -241,43 +335,62 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
   const float top_p = p.top_p ? p.top_p[b] : 1.f;
   const double least = p.min_p ? static_cast<double>(fminf(fmaxf(p.min_p[b], 0.f), 1.f)) : 0.0;      // (NaN: 0)
   const bool greedy = !(temperature > 0.f);
+  w.rate = 16.0 * 1.4426950408889634 / (greedy ? 1.0 : static_cast<double>(temperature));
   w.top_d = w.top;
-  w.rate = 1.4426950408889634 / (greedy ? 1.0 : static_cast<double>(temperature));
+  w.roots = s.roots;
   const int q = min(44, 62 - (32 - __clz(p.V - 1)));
   w.unit = __hiloint2double((1023 + q) << 20, 0);
 
-  // ---- the cut: tokens with a greater key stay, and the first `take` of those that equal it (`some`: these are not all of them)
-  uint32_t cut = 0, take = 0;
-  bool some = false;
+  // ---- the cut: tokens with a greater value stay, and the first `take` of those that equal it (`some`: these are not all of them).  `mass`: of
+  // all that stay, where a search for the cut has found it.
+  float cut = -INFINITY;
+  uint32_t take = 0xffffffffu;
+  bool some = false, known = false;
+  u64 mass = 0;
 
   // Merged histogram -> the bin in which the prefix reaches the target, with what lies before it.  `reached(before, after)` is true in that
   // bin only.  Every CTA of the cluster does all of it.
-  auto find_bin = [&](auto* bins, const uint32_t* number, int n_bins, auto reached) {
+  // (A histogram is cleared again only behind a further exchange, so that nobody reads it any more.)
+  auto find_bin = [&](auto is_mass, auto reached) {
+    constexpr bool MASS = decltype(is_mass)::value;
+    constexpr int kPer = (MASS ? kMassBins : kCountBins) / kThreads;
     cluster.sync();                                       // all histograms are complete
-    const int per = n_bins / kThreads;
-    u64 v[kCountBins / kThreads], sum = 0;
-    for (int i = 0; i < per; ++i) {
-      v[i] = 0;
-      for (int c = 0; c < C; ++c) v[i] += cluster.map_shared_rank(bins, c)[tid * per + i];
-      sum += v[i];
+    u64 v[kPer], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = 0;
+    for (int c = 0; c < C; ++c) {
+      const auto& hist = *cluster.map_shared_rank(&s.hist, c);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if constexpr (MASS) v[i] += hist.mass[0][tid * kPer + i] + (static_cast<u64>(hist.mass[1][tid * kPer + i]) << 32);
+        else v[i] += hist.count[tid * kPer + i];
+      }
     }
-    u64 inc = warp_scan64(sum, lane);
-    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) sum += v[i];
+    const u64 inc = warp_scan64(sum, lane);
     if (lane == 31) s.warp_sum[warp] = inc;
     __syncthreads();
     u64 before = inc - sum;
-    for (int x = 0; x < warp; ++x) before += s.warp_sum[x];
-    for (int i = 0; i < per; ++i) {
+    {
+      u64 t = lane < kWarps && lane < warp ? s.warp_sum[lane] : 0;
+      before += warp_sum64(t);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
       if (reached(before, before + v[i])) {
-        s.bin = tid * per + i;
+        s.bin = tid * kPer + i;
         s.base = before;
-        uint32_t n = 0;
-        if (number) for (int c = 0; c < C; ++c) n += cluster.map_shared_rank(number, c)[tid * per + i];
-        s.bin_number = number ? n : static_cast<uint32_t>(v[i]);
       }
       before += v[i];
     }
-    cluster.sync();                                       // (nobody reads these histograms any more)
+    __syncthreads();
+  };
+  // Exact 64-bit sums by 32-bit atomics: the carry goes along with the high word.
+  auto add_mass = [&](int bin, u64 x) {
+    const uint32_t lo = static_cast<uint32_t>(x), old = atomicAdd(&s.hist.mass[0][bin], lo);
+    const uint32_t hi = static_cast<uint32_t>(x >> 32) + (old + lo < old ? 1u : 0u);
+    if (hi) atomicAdd(&s.hist.mass[1][bin], hi);
   };
   auto clear = [&](uint32_t* words, int n) {
     for (int i = tid; i < n; i += kThreads) words[i] = 0;
@@ -292,20 +405,15 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
       if (tid == 0) { s.n = 0; s.lo = 0xffffffffu; s.hi = 0; }
       __syncthreads();
       uint32_t least = 0xffffffffu, most = 0;
-      for (int i = 0; i < tiles; ++i) {
-        const Vec<T> v = fetch((i * kThreads + tid) * kVec);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const float z = v.at(e);
-          const uint32_t key = key_of(z);
-          if (member(z) && key >= lo && key <= hi) {
-            least = min(least, key);
-            most = max(most, key);
-            const uint32_t at = atomicAdd(&s.n, 1u);
-            if (at < kCandidates) s.list[at] = key;
-          }
+      for_all([&](float z) {
+        const uint32_t key = key_of(z);
+        if (member(z) && key >= lo && key <= hi) {
+          least = min(least, key);
+          most = max(most, key);
+          const uint32_t at = atomicAdd(&s.n, 1u);
+          if (at < kCandidates) s.list[at] = key;
         }
-      }
+      });
       least = __reduce_min_sync(0xffffffffu, least);
       most = __reduce_max_sync(0xffffffffu, most);
       if (lane == 0) { atomicMin(&s.lo, least); atomicMax(&s.hi, most); }
@@ -327,6 +435,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
           if (x < static_cast<double>(n)) need = x > 1.0 ? static_cast<u64>(x) : 1;
           s.cut_key = lo;
           s.cut_take = static_cast<uint32_t>(need);
+          s.cut_base = base;
           s.cut_ties = n;
         }
         break;
@@ -357,6 +466,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
             s.cut_key = key;                              // (threads with this key all write the same)
             s.cut_take = x < static_cast<double>(equal) ? (x > 1.0 ? static_cast<uint32_t>(x) : 1u) : equal;
             s.cut_ties = equal;
+            s.cut_base = before;
           }
         }
         break;
@@ -365,20 +475,12 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
       const uint32_t top = hi, span = hi - lo;
       const int shift = max(0, 32 - __clz(span) - 10);    // span >> shift is below kMassBins
       clear(reinterpret_cast<uint32_t*>(&s.hist), sizeof(s.hist) / 4);
-      for (int i = 0; i < tiles; ++i) {
-        const Vec<T> v = fetch((i * kThreads + tid) * kVec);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const float z = v.at(e);
-          const uint32_t key = key_of(z);
-          if (member(z) && key >= lo && key <= hi) {
-            const uint32_t at = (top - key) >> shift;
-            atomicAdd(&s.hist.m.mass[at], MASS ? w.whole(w.real(z)) : 1ull);
-          }
-        }
-      }
+      for_all([&](float z) {
+        const uint32_t key = key_of(z);
+        if (member(z) && key >= lo && key <= hi) add_mass((top - key) >> shift, MASS ? w.whole(w.real(z)) : 1ull);
+      });
       const u64 base_now = base;
-      find_bin(s.hist.m.mass, nullptr, kMassBins, [&](u64 before, u64 after) {
+      find_bin(std::true_type{}, [&](u64 before, u64 after) {
         return static_cast<double>(base_now + before) < target && !(static_cast<double>(base_now + after) < target);
       });
       base += s.base;
@@ -386,21 +488,24 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
       lo = max(lo, hi - ((1u << shift) - 1u));
     }
     __syncthreads();
-    cut = s.cut_key;
+    cut = value_of_key(s.cut_key);
     take = s.cut_take;
     some = take < s.cut_ties;
-    cluster.sync();                                       // (the lists have been read)
+    mass = s.cut_base + take * (MASS ? w.whole(w.real(cut)) : 1);
+    // (the others have read the candidates before the next exchange, and those are written again only behind one)
   };
 
   const bool by_k = !nothing && !greedy && k > 1 && k < p.V;
   if (nothing) {
-    cut = 0xffffffffu;                                    // nothing stays
+    cut = INFINITY;                                       // nothing stays
+    take = 0;
   } else if (greedy || k == 1 || top_p <= 0.f) {
-    cut = top_key;
+    cut = w.top;
     take = 1;
-    some = true;
+    some = known = true;
+    mass = w.whole(1.0);
   }
-  if (by_k && cut == 0) {
+  if (by_k && !some) {
     auto bin_of = [&](float z) { return z == w.top ? 0 : static_cast<int>(fminf((w.top - z) * 64.f, kCountBins - 1.f)); };
     clear(s.hist.count, kCountBins);
     for (int i = 0; i < tiles; ++i) {
@@ -413,51 +518,57 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
       }
     }
     const u64 want = static_cast<u64>(k);
-    find_bin(s.hist.count, static_cast<const uint32_t*>(nullptr), kCountBins, [&](u64 before, u64 after) { return before < want && after >= want; });
+    find_bin(std::false_type{}, [&](u64 before, u64 after) { return before < want && after >= want; });
     const int bin = static_cast<int>(s.bin);
+    make_list([&](float z) { return bin_of(z) <= bin; });
     // (positions outside of the row hold -infinity too: they stand behind every token, and have no mass)
     rank_in_bin([&](float z) { return bin_of(z) == bin; }, std::false_type{}, s.base, static_cast<double>(k));
   }
-  if (!nothing && top_p < 1.f && !(cut == top_key && take == 1)) {
+  if (!nothing && top_p < 1.f && !(cut == w.top && take == 1)) {
     u64 sum = 0;
-    for (int i = 0; i < tiles; ++i) {
-      const Vec<T> v = fetch((i * kThreads + tid) * kVec);
+    const bool whole_row = cut == -INFINITY && take == 0xffffffffu;
+    if (whole_row) {
+#pragma unroll 2
+      for (int i = 0; i < tiles; ++i) {
+        const Vec<T> v = fetch((i * kThreads + tid) * kVec);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e)
-        if (key_of(v.at(e)) > cut) sum += w.whole(w.real(v.at(e)));
+        for (int e = 0; e < kVec; ++e) sum += w.whole(w.real(v.at(e)));
+      }
+    } else {
+      for_few([&](float z) { return z > cut; }, [&](float z) { sum += w.whole(w.real(z)); });
     }
     const u64 above = cluster_sum(sum);
-    const u64 one = take ? w.whole(w.real(value_of_key(cut))) : 0;
-    const u64 all = above + take * one;
+    const u64 one = whole_row ? 0 : w.whole(w.real(cut));
+    const u64 all = whole_row ? above : above + take * one;
     const double target = static_cast<double>(top_p) * static_cast<double>(all);
-    if (static_cast<double>(above) < target) {            // among the last ones that top-k left
+    if (!whole_row && static_cast<double>(above) < target) {      // among the last ones that top-k left
       const double x = ceil((target - static_cast<double>(above)) / static_cast<double>(one));
       if (x < static_cast<double>(take)) {
         take = x > 1.0 ? static_cast<uint32_t>(x) : 1u;
         some = true;
       }
+      mass = above + take * one;
+      known = true;
     } else {
       const double n = by_k ? k : p.V;
       const double tail = (1.0 - static_cast<double>(top_p)) * static_cast<double>(all) / w.unit / n;     // see above
-      const float depth = static_cast<float>((fmax(-log2(tail), 0.0) + 1e-3) / w.rate);
+      const float depth = static_cast<float>((fmax(-log2(tail), 0.0) + 1e-3) * 16.0 / w.rate);
       const float scale = (kMassBins - 1.f) / depth;
-      const uint32_t floor_key = cut;
+      const float floor = cut;                            // (values of -infinity have no mass: nothing is lost where it is that)
       auto bin_of = [&](float z) { return z == w.top ? 0.f : (w.top - z) * scale; };
-      auto member = [&](float z) { return key_of(z) > floor_key && bin_of(z) < kMassBins; };
+      auto member = [&](float z) { return z > floor && bin_of(z) < kMassBins; };
+      if (!listed) make_list(member);
       clear(reinterpret_cast<uint32_t*>(&s.hist), sizeof(s.hist) / 4);
-      for (int i = 0; i < tiles; ++i) {
-        const Vec<T> v = fetch((i * kThreads + tid) * kVec);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const float z = v.at(e);
-          if (member(z)) atomicAdd(&s.hist.m.mass[static_cast<int>(bin_of(z))], w.whole(w.real(z)));
-        }
-      }
-      find_bin(s.hist.m.mass, nullptr, kMassBins, [&](u64 before, u64 after) {
+      for_few(member, [&](float z) { add_mass(static_cast<int>(bin_of(z)), w.whole(w.real(z))); });
+      find_bin(std::true_type{}, [&](u64 before, u64 after) {
         return static_cast<double>(before) < target && !(static_cast<double>(after) < target);
       });
-      const int bin = static_cast<int>(s.bin);
-      rank_in_bin([&](float z) { return member(z) && static_cast<int>(bin_of(z)) == bin; }, std::true_type{}, s.base, target);
+      const float bin = static_cast<float>(s.bin);
+      rank_in_bin([&](float z) {
+        const float x = bin_of(z);
+        return x >= bin && x < bin + 1.f && z > floor;
+      }, std::true_type{}, s.base, target);
+      known = true;
     }
   }
 
@@ -466,10 +577,15 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
   if (some) {
     uint32_t mine = 0;
     for (int i = 0; i < tiles; ++i) {
-      const Vec<T> v = fetch((i * kThreads + tid) * kVec);
       uint32_t n = 0;
+      if (listed) {
+        int to;
+        for (int j = in_segment(i, &to) + lane; j < to; j += 32) n += few[j] == cut;
+      } else {
+        const Vec<T> v = fetch((i * kThreads + tid) * kVec);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) n += key_of(v.at(e)) == cut;
+        for (int e = 0; e < kVec; ++e) n += v.at(e) == cut;
+      }
       n = __reduce_add_sync(0xffffffffu, n);
       if (lane == 0) ties[i * kWarps + warp] = n;
       mine += n;
@@ -488,13 +604,13 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
     }
     __syncthreads();
   }
-  // Weights of what stays in this thread's vector of tile i (all lanes together).
-  auto weigh = [&](const Vec<T>& v, int group, double* e_out) {
+  // Of this warp's part of a tile: what stays, picked (see above); min-p takes out more when the weights are known.
+  auto pick_left = [&](const Vec<T>& v, int group, int* at) {
     uint32_t rank_of = 0;
     if (some) {
       uint32_t n = 0;
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) n += key_of(v.at(e)) == cut;
+      for (int e = 0; e < kVec; ++e) n += v.at(e) == cut;
       uint32_t inc = n;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -503,38 +619,58 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
       }
       rank_of = ties[group] + inc - n;
     }
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-      const uint32_t key = key_of(v.at(e));
-      bool stays = key > cut;
-      if (key == cut) stays = !some ? take > 0 : rank_of++ < take;
-      double x = 0.0;
-      if (stays) x = w.real(v.at(e));
-      e_out[e] = x < least ? 0.0 : x;
-    }
+    return pick(v, 0, [&](float z) { return z > cut || (z == cut && (some ? rank_of++ < take : take > 0)); }, at);
+  };
+  auto left = [&](float z) {
+    const double x = w.real(z);
+    return x < least ? 0.0 : x;
   };
 
-  // ---- the mass of what stays
-  u64 sum = 0;
-  for (int i = 0; i < tiles; ++i) {
-    double e[kVec];
-    weigh(fetch((i * kThreads + tid) * kVec), i * kWarps + warp, e);
-    u64 t = 0;
-#pragma unroll
-    for (int x = 0; x < kVec; ++x) t += w.whole(e[x]);
-    t = warp_sum64(t);
-    if (lane == 0) part[i * kWarps + warp] = t;
-    sum += t;
-  }
-  const u64 here = block_sum(lane == 0 ? sum : 0);
-  u64 before = 0, all = 0;
-  {
+  // ---- the mass of what stays; where a token is drawn, of each warp's part of each tile as well
+  u64 before = 0, all = mass;
+  u64 here = 0;
+  if (p.tokens || !known || least > 0.0) {
+    all = 0;
+    u64 sum = 0;
+    for (int i = 0; i < tiles; ++i) {
+      u64 t = 0;
+      if (listed) {
+        int to;
+        uint32_t seen = some ? ties[i * kWarps + warp] : 0;
+        for (int j = in_segment(i, &to); j < to; j += 32) {
+          const float z = j + lane < to ? few[j + lane] : -INFINITY;
+          bool stays = j + lane < to && z >= cut;
+          if (some) {
+            const unsigned equal = __ballot_sync(0xffffffffu, stays && z == cut);
+            if (z == cut) stays = stays && seen + __popc(equal & ((1u << lane) - 1u)) < take;
+            seen += __popc(equal);
+          } else if (z == cut) {
+            stays = stays && take > 0;
+          }
+          if (stays) t += w.whole(left(z));
+        }
+      } else {
+        int at[kVec];
+        const int n = pick_left(fetch((i * kThreads + tid) * kVec), i * kWarps + warp, at);
+        for (int x = lane; x < n; x += 32) t += w.whole(left(few[x]));
+        __syncwarp();
+      }
+      if (p.tokens) {
+        t = warp_sum64(t);
+        if (lane == 0) part[i * kWarps + warp] = t;
+        t = lane == 0 ? t : 0;
+      }
+      sum += t;
+    }
+    here = block_sum(sum);
     const u64(*got)[2] = exchange(here, 0);
     for (int c = 0; c < C; ++c) {
       if (c < rank) before += got[c][0];
       all += got[c][0];
     }
   }
+
+  __syncthreads();                                        // (the lists are not needed any more: what follows picks from tiles again)
 
   // ---- the draw: the CTA, the warp's part of a tile, the lane and the element in which the prefix passes u times the sum
   if (p.tokens && !nothing && warp == 0) {
@@ -558,11 +694,15 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
       }
       // (group >= 0: the CTA's sum passes t)
       const int pos = ((group / kWarps) * kThreads + (group % kWarps) * 32 + lane) * kVec;
-      double e[kVec];
-      weigh(fetch(pos), group, e);
-      u64 mine = 0;
+      const Vec<T> v = fetch(pos);
+      int at[kVec];
+      pick_left(v, group, at);
+      u64 e[kVec], mine = 0;
 #pragma unroll
-      for (int x = 0; x < kVec; ++x) mine += w.whole(e[x]);
+      for (int x = 0; x < kVec; ++x) {
+        e[x] = at[x] >= 0 ? w.whole(left(v.at(x))) : 0;
+        mine += e[x];
+      }
       const u64 inc = warp_scan64(mine, lane);
       const unsigned hit = __ballot_sync(0xffffffffu, static_cast<double>(carry + inc) > t);
       if (lane == __ffs(hit) - 1) {
@@ -572,7 +712,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
         for (int x = kVec - 1; x >= 0; --x) {
           u64 upto = run;
 #pragma unroll
-          for (int y = 0; y <= x; ++y) upto += w.whole(e[y]);
+          for (int y = 0; y <= x; ++y) upto += e[y];
           if (static_cast<double>(upto) > t) found = x;
         }
         p.tokens[row] = first + pos + found;
@@ -587,17 +727,21 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
     const bool wide = ((reinterpret_cast<uintptr_t>(dst) - 4 * static_cast<uintptr_t>(off)) & 15) == 0;
     for (int i = 0; i < tiles; ++i) {
       const int pos = (i * kThreads + tid) * kVec, id = first + pos;
-      double e[kVec];
-      weigh(fetch(pos), i * kWarps + warp, e);
+      int at[kVec];
+      const int n = pick_left(fetch(pos), i * kWarps + warp, at);
+      for (int x = lane; x < n; x += 32) few[x] = static_cast<float>(left(few[x]) * inv);
+      __syncwarp();
+      float out[kVec];
+#pragma unroll
+      for (int x = 0; x < kVec; ++x) out[x] = at[x] >= 0 ? few[at[x]] : 0.f;
+      __syncwarp();
       if (wide && id >= 0 && id + kVec <= p.V) {
 #pragma unroll
-        for (int x = 0; x < kVec; x += 4)
-          *reinterpret_cast<float4*>(dst + id + x) = make_float4(static_cast<float>(e[x] * inv), static_cast<float>(e[x + 1] * inv),
-                                                                 static_cast<float>(e[x + 2] * inv), static_cast<float>(e[x + 3] * inv));
+        for (int x = 0; x < kVec; x += 4) *reinterpret_cast<float4*>(dst + id + x) = make_float4(out[x], out[x + 1], out[x + 2], out[x + 3]);
       } else {
 #pragma unroll
         for (int x = 0; x < kVec; ++x)
-          if (id + x >= 0 && id + x < p.V) dst[id + x] = static_cast<float>(e[x] * inv);
+          if (id + x >= 0 && id + x < p.V) dst[id + x] = out[x];
       }
     }
   }
@@ -608,13 +752,14 @@ template <typename T>
 cudaError_t launch(const SampleParams& p, int sm_count, cudaStream_t stream) {
   constexpr int kTile = kThreads * Vec<T>::kLen;
   const long long rows = static_cast<long long>(p.B) * p.R, positions = static_cast<long long>(p.V) + Vec<T>::kLen;
-  // As many CTAs to a row as fill the machine, while each has at least a tile of the vocabulary, and enough to hold the row in shared memory.
+  // Enough CTAs to a row to hold it in the shared memory of CTAs that are two to an SM, and more while all of them find a place at once and each has
+  // more than a tile of the vocabulary.
   int C = 1;
   auto slice_of = [&](int c) { return static_cast<int>(((positions + c - 1) / c + kTile - 1) / kTile * kTile); };
-  while (C < kMaxCluster && (slice_of(C) * sizeof(T) > kSliceBytes || (rows * C < sm_count && slice_of(C) > kTile))) C *= 2;
+  while (C < kMaxCluster && (slice_of(C) * sizeof(T) > kPairBytes || (rows * C <= sm_count && slice_of(C) > kTile))) C *= 2;
   const int slice = slice_of(C);
   const bool resident = slice * sizeof(T) <= kSliceBytes;
-  const size_t bytes = (resident ? slice * sizeof(T) : 0) + static_cast<size_t>(slice / kTile) * kWarps * 12;
+  const size_t bytes = (resident ? slice * sizeof(T) : 0) + static_cast<size_t>(slice / kTile) * kWarps * 14;
   auto kernel = resident ? sample_kernel<T, true> : sample_kernel<T, false>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSliceBytes + 16384));
   if (e != cudaSuccess) return e;
