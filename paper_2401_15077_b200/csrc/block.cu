@@ -120,10 +120,14 @@ struct Rows {
 
 template <bool TREE, bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
-  extern __shared__ __align__(16) float2 s_cs[];           // [rows][R / 2]; for queries [warps][R / 2]
+  // sines and cosines of [rows or depths], the eight pairs of a lane in four 16-byte pieces [4][kLanes] (eight lanes of a read are then neighbours);
+  // for queries [warps][R / 2]
+  extern __shared__ __align__(16) float2 s_cs[];
   __shared__ long long s_row[kMaxBlock];                   // cache row (KV head 0) of each new row, -1: not stored
   __shared__ long long s_scale[kMaxTouched];               // each block's place among the scales (KV head 0), -1: none
-  __shared__ int s_pos[kMaxBlock];
+  __shared__ int s_pos[kMaxBlock];                         // position of a row; in the tree form, of a depth
+  __shared__ int s_turn[kMaxBlock];                        // place of a row in the table
+  __shared__ float s_top[kWarps];
   const RopeParams& r = p.r;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, half = r.R / 2;
   const int u = lane & (kLanes - 1), sub = lane / kLanes;
@@ -206,11 +210,14 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
   }
 
   // ================================================================================================ keys and values
-  const int job = blockIdx.x / p.store_groups, h_lo = (blockIdx.x - job * p.store_groups) * p.store_heads, h_hi = min(2 * r.Hkv, h_lo + p.store_heads);
-  const bool any_keys = h_lo < r.Hkv;
+  const int job = blockIdx.x / p.store_groups, h_lo = (blockIdx.x - job * p.store_groups) * p.store_heads;
+  const int warps = kWarps / p.store_heads, part = warp % warps, head_of = h_lo + warp / warps;      // warps per head, this one's part and head
+  const bool any_keys = h_lo < r.Hkv, some_head = head_of < 2 * r.Hkv;
+  const int row0 = part * kRowsAtOnce + sub, step = warps * kRowsAtOnce;
 
-  // One head's rows: the maximum, the scale, the codes.
-  auto store_head = [&](const Rows& rows, int head) {
+  // One head's rows: the maximum, the scale, the codes.  (All warps of the CTA.)
+  auto store_head = [&](const Rows& rows) {
+    const int head = some_head ? head_of : 0;
     const bool is_v = head >= r.Hkv;
     const int g = is_v ? head - r.Hkv : head;
     const long long stride = is_v ? r.v_stride : r.k_stride;
@@ -221,20 +228,38 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
       const uint4 a = *reinterpret_cast<const uint4*>(src + i * stride + va), b = *reinterpret_cast<const uint4*>(src + i * stride + vb);
       widen(a, x);
       widen(b, y);
-      if (turn && !is_v) rotate<INTERLEAVED>(x, y, s_cs + i * half + 8 * u);
+      if (turn && !is_v) {
+        float2 cs[8];
+        const float4* at = reinterpret_cast<const float4*>(s_cs) + s_turn[i] * (4 * kLanes) + u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 c = at[e * kLanes];
+          cs[2 * e] = make_float2(c.x, c.y);
+          cs[2 * e + 1] = make_float2(c.z, c.w);
+        }
+        rotate<INTERLEAVED>(x, y, cs);
+      }
     };
     const long long first_scale = s_scale[0];
     float held = 0.f;
     if (rows.old > 0 && first_scale >= 0) held = scales[first_scale + g * p.head_blocks];
     float top = 0.f;
+    if (some_head) {
 #pragma unroll 4
-    for (int i = sub; i < rows.n; i += kRowsAtOnce) {
-      float x[8], y[8];
-      fetch(i, x, y);
+      for (int i = row0; i < rows.n; i += step) {
+        float x[8], y[8];
+        fetch(i, x, y);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(finite_magnitude(x[e]), finite_magnitude(y[e])));
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(finite_magnitude(x[e]), finite_magnitude(y[e])));
+      }
     }
     top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));      // (magnitudes order as their bits do)
+    if (warps > 1) {
+      if (lane == 0) s_top[warp] = top;
+      __syncthreads();                                     // (the older scale has been read by all, too)
+      for (int w = 0; w < warps; ++w) top = fmaxf(top, s_top[warp - part + w]);
+    }
+    if (!some_head) return;
     const float need = scale_for(top);
     const bool grown = held > 0.f && need > held;
     const float scale = held > 0.f && !grown ? held : need;
@@ -242,7 +267,7 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
       // older codes again, by the new scale
       const float ratio = held * __uint_as_float(0x7f000000u - __float_as_uint(scale));      // 1 / 2^e
       uint8_t* old = cache + (s_row[0] - rows.old) * D;
-      for (int i = sub; i < rows.old; i += kRowsAtOnce) {
+      for (int i = row0; i < rows.old; i += step) {
         float f[16];
         decode(*reinterpret_cast<const uint4*>(old + i * D + 16 * u), f);
 #pragma unroll
@@ -254,7 +279,7 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
     float inv;
     asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(scale));
 #pragma unroll 2
-    for (int i = sub; i < rows.n; i += kRowsAtOnce) {
+    for (int i = row0; i < rows.n; i += step) {
       const long long to = s_row[i];
       if (to < 0) continue;
       float x[8], y[8];
@@ -262,7 +287,7 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
       *reinterpret_cast<uint2*>(cache + to * D + va) = codes(x, scale, inv);
       *reinterpret_cast<uint2*>(cache + to * D + vb) = codes(y, scale, inv);
     }
-    if (lane < rows.blocks && s_scale[lane] >= 0) scales[s_scale[lane] + g * p.head_blocks] = scale;
+    if (part == 0 && lane < rows.blocks && s_scale[lane] >= 0) scales[s_scale[lane] + g * p.head_blocks] = scale;
   };
   // Cache row and scale of a slot (KV head 0).
   auto scale_at = [&](int b, int slot) -> long long {
@@ -271,15 +296,15 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
     if (page < 0 || page >= r.num_pages) return -1;
     return static_cast<long long>(page) * r.Hkv * p.head_blocks + ((slot & (r.page_size - 1)) >> p.block_shift);
   };
-  auto store = [&](const Rows& rows) {
+  auto store = [&](const Rows& rows, int angles) {         // angles: positions in s_pos
     if (any_keys) {
-      for (int i = threadIdx.x; i < rows.n * half; i += kThreads) {
-        const int at = i / half;
-        s_cs[i] = turn_by(r, s_pos[at], i - at * half);
+      for (int i = threadIdx.x; i < angles * half; i += kThreads) {
+        const int at = i / half, m = i - at * half;
+        s_cs[((at * 4 + ((m >> 1) & 3)) * kLanes + (m >> 3)) * 2 + (m & 1)] = turn_by(r, s_pos[at], m);
       }
-      __syncthreads();
     }
-    for (int h = h_lo + warp; h < h_hi; h += kWarps) store_head(rows, h);
+    __syncthreads();
+    store_head(rows);
   };
 
   if constexpr (TREE) {
@@ -296,13 +321,15 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
       for (int i = 0; i < 2; ++i)
         if (lane + 32 * i < tree.n) {
           s_row[lane + 32 * i] = rope_row(r, b, tree.L + lane + 32 * i);
-          s_pos[lane + 32 * i] = tree.L + tree.depth[i] - 1;
+          s_turn[lane + 32 * i] = tree.depth[i] - 1;
+          s_pos[lane + 32 * i] = tree.L + lane + 32 * i;
         }
     } else if (warp == 1 && lane < blocks) {
       s_scale[lane] = scale_at(b, ((tree.L >> p.block_shift) + lane) << p.block_shift);
     }
+    const int deepest = __reduce_max_sync(0xffffffffu, max(lane < tree.n ? tree.depth[0] : 0, lane + 32 < tree.n ? tree.depth[1] : 0));
     __syncthreads();
-    store(Rows{b * r.T, tree.n, tree.L & (p.block_size - 1), blocks});
+    store(Rows{b * r.T, tree.n, tree.L & (p.block_size - 1), blocks}, deepest);
   } else {
     const int end = min(r.N, (job + 1) * p.span);
     int t = job * p.span;
@@ -332,11 +359,12 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
       const long long row = rope_row(r, seq, slot);
       for (int i = threadIdx.x; i < rest; i += kThreads) {
         s_row[i] = row < 0 ? -1 : row + i;
+        s_turn[i] = i;
         s_pos[i] = r.positions ? r.positions[t + i] : slot + i;
       }
       if (threadIdx.x == 0) s_scale[0] = scale_at(seq, slot);
       __syncthreads();
-      if (row >= 0) store(Rows{t, rest, in_block, 1});     // (uniform: a block lies in one page)
+      if (row >= 0) store(Rows{t, rest, in_block, 1}, rest);      // (uniform: a block lies in one page)
       t += rest;
     }
   }
@@ -359,9 +387,10 @@ cudaError_t launch_block(const BlockParams& p_in, bool tree, int sm_count, cudaS
   BlockParams p = p_in;
   RopeParams& r = p.r;
   const long long tokens = tree ? static_cast<long long>(r.B) * r.T : r.N;
-  const int half = r.R / 2;
-  // keys and values: a warp per head, eight to a CTA; the rows of a CTA are a block's, or fewer while two CTAs per SM are not there
-  p.store_heads = kWarps;
+  // keys and values: sixteen rows and more to a warp, up to four warps per head, eight warps to a CTA (64 trees of 16 to 64 nodes: 43 us with
+  // a warp per head); the rows of a CTA are a block's, or fewer while two CTAs per SM are not there
+  const long long each = tree ? r.T : (r.N + static_cast<long long>(r.B) - 1) / r.B, held = each < p.block_size || tree ? each : p.block_size;
+  p.store_heads = held >= 64 ? 2 : (held >= 32 ? 4 : kWarps);
   p.store_groups = (2 * r.Hkv + p.store_heads - 1) / p.store_heads;
   p.span = p.block_size;
   while (!tree && p.span > 1 && (r.N + p.span - 1) / p.span * static_cast<long long>(p.store_groups) < 2 * sm_count) p.span /= 2;
@@ -375,7 +404,7 @@ cudaError_t launch_block(const BlockParams& p_in, bool tree, int sm_count, cudaS
   if (stores + turns > 0x7fffffffll) return cudaErrorInvalidValue;
   p.store_ctas = static_cast<int>(stores);
   const long long most = tree ? r.T : (p.block_size < r.N ? p.block_size : r.N);
-  const size_t smem = sizeof(float2) * half * static_cast<size_t>(most > kWarps ? most : kWarps);
+  const size_t smem = sizeof(float2) * (D / 2) * static_cast<size_t>(most > kWarps ? most : kWarps);
   const unsigned blocks = static_cast<unsigned>(stores + turns);
   const cudaError_t e = tree ? launch<true>(p, blocks, smem, stream) : launch<false>(p, blocks, smem, stream);
   if (e != cudaSuccess) return e;
