@@ -535,13 +535,13 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
               const int row = static_cast<int>(w) * 64 + half * 32 + lane;
               const uint32_t at = sbase + S::kQ + qb * S::kQBytes + row * 128, swz = row & 7;
               uint32_t top = 0;
-#pragma unroll 8
+#pragma unroll 1
               for (int e = 0; e < 16; ++e) {
                 const uint4 v = load_shared(at + (e >> 3) * S::kQSlab + (((e & 7) ^ swz) << 4));
                 top = max(max(top, max(magnitude_bits(v.x), magnitude_bits(v.y))), max(magnitude_bits(v.z), magnitude_bits(v.w)));
               }
               const RowFactor f = row_factor(top);
-#pragma unroll 4
+#pragma unroll 1
               for (int e = 0; e < 16; ++e) {
                 const uint32_t to = at + (e >> 3) * S::kQSlab + (((e & 7) ^ swz) << 4);
                 const uint4 v = load_shared(to);
@@ -563,7 +563,7 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
               const uint32_t piece = lane & 7, flip = piece >> 2, row0 = lane >> 3;
               const uint32_t from = sbase + S::kKC + st * S::kKCodes + lane * 16, to = sbase + S::kK + sl * S::kKBytes + flip * S::kKSlab;
               const uint32_t one = 2 * (piece & 3) + flip, two = 2 * (piece & 3) + 1 - flip;
-#pragma unroll 4
+#pragma unroll 1
               for (uint32_t u = 0; u < 16; ++u) {
                 const uint32_t row = u * 4 + row0;
                 uint4 lo, hi;
@@ -587,7 +587,7 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
               const uint32_t piece = lane & 3, row0 = lane >> 2;
               const uint32_t from = sbase + S::kVC + st * S::kVCodes + lane * 16, to = sbase + S::kV + sl * S::kVBytes + row0 * 128;
               const uint32_t one = ((2 * piece) ^ row0) << 4, two = ((2 * piece + 1) ^ row0) << 4;
-#pragma unroll 4
+#pragma unroll 1
               for (uint32_t u = 0; u < 16; ++u) {
                 const int key = key0 + static_cast<int>(u * 8 + row0);
                 uint4 c = load_shared(from + u * 512), lo, hi;
@@ -710,27 +710,28 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
           float tmax = -INFINITY;
           bool odd = false;                                // a visible score that is NaN or +inf
           if constexpr (CODES) {
-            auto top_of = [&](const uint32_t* raw, int group) {      // of 16 scores, with their scales
+            auto top_of = [&](const uint32_t* raw, const uint4& c) {      // of 16 scores, with their scales
               float x = -INFINITY, y = -INFINITY;
 #pragma unroll
               for (int e = 0; e < 16; e += 4) {
                 x = max3_nan(x, __uint_as_float(raw[e]), __uint_as_float(raw[e + 1]));
                 y = max3_nan(y, __uint_as_float(raw[e + 2]), __uint_as_float(raw[e + 3]));
               }
-              const uint4 c = load_shared(scale_at + group * 16);
               tmax = max3_nan(tmax, fmaf(max3_nan(x, y, -INFINITY), __uint_as_float(c.x) * up, __uint_as_float(c.y)), -INFINITY);
             };
             ld32(s_addr, ra);
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
+              const uint4 c0 = load_shared(scale_at + h * 64), c1 = load_shared(scale_at + h * 64 + 16);
+              const uint4 c2 = load_shared(scale_at + h * 64 + 32), c3 = load_shared(scale_at + h * 64 + 48);
               wait_ld();
               ld32(s_addr + h * 64 + 32, rb);
-              top_of(ra, 4 * h);
-              top_of(ra + 16, 4 * h + 1);
+              top_of(ra, c0);
+              top_of(ra + 16, c1);
               wait_ld();
               if (h == 0) ld32(s_addr + 64, ra);
-              top_of(rb, 4 * h + 2);
-              top_of(rb + 16, 4 * h + 3);
+              top_of(rb, c2);
+              top_of(rb + 16, c3);
             }
             ld16(s_addr, ra);                              // (the first scores again)
             odd = !(tmax < INFINITY);
@@ -796,8 +797,7 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
           // ---- exponentials and packed P over score columns that have been read
           const float neg_base = m_ref == -INFINITY ? 0.f : -m_ref;
           if constexpr (CODES) {
-            auto exp_group = [&](const uint32_t* raw, int group) {   // 16 scores with their scales
-              const uint4 c = load_shared(scale_at + group * 16);
+            auto exp_group = [&](const uint32_t* raw, int group, const uint4& c) {   // 16 scores with their scales
               const float a = __uint_as_float(c.x) * up, base = __uint_as_float(c.y) + neg_base + kHalfShift;
               const uint64_t scale2 = pack2(a, a), base2 = pack2(base, base);
               uint64_t ls2[2] = {0ull, 0ull};
@@ -823,12 +823,13 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
             };
 #pragma unroll 1
             for (int h = 0; h < 4; ++h) {
+              const uint4 c0 = load_shared(scale_at + h * 32), c1 = load_shared(scale_at + h * 32 + 16);
               wait_ld();
               ld16(s_addr + h * 32 + 16, rb);
-              exp_group(ra, 2 * h);
+              exp_group(ra, 2 * h, c0);
               wait_ld();
               if (h < 3) ld16(s_addr + h * 32 + 32, ra);
-              exp_group(rb, 2 * h + 1);
+              exp_group(rb, 2 * h + 1, c1);
             }
           } else {
             uint64_t ls2[2] = {0ull, 0ull};
