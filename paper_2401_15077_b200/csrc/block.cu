@@ -118,8 +118,11 @@ struct Rows {
   int blocks;                    // blocks they lie in
 };
 
-template <bool TREE, bool INTERLEAVED>
+enum Form { kChunks, kTrees, kSingles };
+
+template <Form FORM, bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
+  constexpr bool TREE = FORM == kTrees;
   // sines and cosines of [rows or depths], the eight pairs of a lane in four 16-byte pieces [4][kLanes] (eight lanes of a read are then neighbours);
   // for queries [warps][R / 2]
   extern __shared__ __align__(16) float2 s_cs[];
@@ -209,6 +212,92 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
     return;
   }
 
+  // Cache row and scale of a slot (KV head 0).
+  auto scale_at = [&](int b, int slot) -> long long {
+    if (!r.block_table) return static_cast<long long>(b) * r.Hkv * p.head_blocks + (slot >> p.block_shift);
+    const int page = r.block_table[static_cast<size_t>(b) * r.max_pages + (slot >> r.page_shift)];
+    if (page < 0 || page >= r.num_pages) return -1;
+    return static_cast<long long>(page) * r.Hkv * p.head_blocks + ((slot & (r.page_size - 1)) >> p.block_shift);
+  };
+  // Codes of an older slot again, by a scale that has grown (16 of a lane).
+  auto store_again = [&](uint8_t* at, float held, float scale) {
+    const float ratio = held * __uint_as_float(0x7f000000u - __float_as_uint(scale));      // 1 / 2^e
+    float f[16];
+    decode(*reinterpret_cast<const uint4*>(at), f);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) f[e] *= ratio;
+    const uint2 lo = codes(f, 1.f, 1.f), hi = codes(f + 8, 1.f, 1.f);
+    *reinterpret_cast<uint4*>(at) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+  };
+
+  if constexpr (FORM == kSingles) {
+    // ============================================================================== keys and values of single tokens: a warp per row and some heads
+    const long long job = static_cast<long long>(blockIdx.x) * kWarps + warp, token_of = job / p.store_groups;
+    const int h_lo = static_cast<int>(job - token_of * p.store_groups) * p.store_heads, h_hi = min(2 * r.Hkv, h_lo + p.store_heads);
+    if (token_of >= r.N) return;
+    const int t = static_cast<int>(token_of), seq = owner_of(r.token_start, r.B, t, lane);
+    const int s = r.token_start[seq], e = r.token_start[seq + 1], L = r.seq_lens[seq];
+    if (s < 0 || s > t || t >= e || e > r.N) return;
+    if (L < 0 || static_cast<long long>(L) + (e - s) > r.capacity) {
+      if (lane == 0) report_status(r.status, EAGLE_ERR_SEQ);
+      return;
+    }
+    const int slot = L + (t - s), in_block = slot & (p.block_size - 1), n = min(e - t, p.block_size - in_block);
+    if (t != s && in_block != 0) return;                   // its block begins with an earlier row
+    const long long row = rope_row(r, seq, slot), at = scale_at(seq, slot);
+    if (row < 0) return;
+    float2* mine = s_cs + warp * half;
+    float2 cs[8];
+    auto angles = [&](int i) {
+      __syncwarp();
+      for (int m = lane; m < half; m += 32) mine[m] = turn_by(r, r.positions ? r.positions[t + i] : slot + i, m);
+      __syncwarp();
+#pragma unroll
+      for (int x = 0; x < 8; ++x) cs[x] = turn ? mine[8 * u + x] : make_float2(1.f, 0.f);
+    };
+    angles(0);
+    for (int h0 = h_lo; h0 < h_hi; h0 += kRowsAtOnce) {
+      const int head = h0 + sub;
+      const bool live = head < h_hi, is_v = head >= r.Hkv;
+      const int g = !live ? 0 : (is_v ? head - r.Hkv : head);
+      const long long stride = is_v ? r.v_stride : r.k_stride;
+      const __nv_bfloat16* src = (is_v ? r.v : r.k) + t * stride + g * D;
+      uint8_t* cache = static_cast<uint8_t*>(is_v ? r.v_cache : r.k_cache) + (row + g * r.head_rows) * D;
+      float* scale_to = (is_v ? p.v_scale : p.k_scale) + at + g * p.head_blocks;
+      const float held = in_block > 0 && live ? *scale_to : 0.f;
+      float x[8], y[8];
+      auto fetch = [&](int i) {
+        if (n > 1) angles(i);
+        widen(*reinterpret_cast<const uint4*>(src + i * stride + va), x);
+        widen(*reinterpret_cast<const uint4*>(src + i * stride + vb), y);
+        if (turn && !is_v) rotate<INTERLEAVED>(x, y, cs);
+      };
+      float top = 0.f;
+      for (int i = 0; i < n; ++i) {
+        fetch(i);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = fmaxf(top, fmaxf(finite_magnitude(x[k]), finite_magnitude(y[k])));
+      }
+#pragma unroll
+      for (int o = 1; o < kLanes; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float need = scale_for(top);
+      const bool grown = held > 0.f && need > held;
+      const float scale = held > 0.f && !grown ? held : need;
+      if (grown)
+        for (int i = 1; i <= in_block; ++i) store_again(cache - i * D + 16 * u, held, scale);
+      float inv;
+      asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(scale));
+      for (int i = 0; i < n; ++i) {
+        if (n > 1) fetch(i);
+        if (!live) continue;
+        *reinterpret_cast<uint2*>(cache + i * D + va) = codes(x, scale, inv);
+        *reinterpret_cast<uint2*>(cache + i * D + vb) = codes(y, scale, inv);
+      }
+      if (live && u == 0) *scale_to = scale;
+    }
+    return;
+  }
+
   // ================================================================================================ keys and values
   const int job = blockIdx.x / p.store_groups, h_lo = (blockIdx.x - job * p.store_groups) * p.store_heads;
   const int warps = kWarps / p.store_heads, part = warp % warps, head_of = h_lo + warp / warps;      // warps per head, this one's part and head
@@ -264,17 +353,8 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
     const bool grown = held > 0.f && need > held;
     const float scale = held > 0.f && !grown ? held : need;
     if (grown) {
-      // older codes again, by the new scale
-      const float ratio = held * __uint_as_float(0x7f000000u - __float_as_uint(scale));      // 1 / 2^e
       uint8_t* old = cache + (s_row[0] - rows.old) * D;
-      for (int i = row0; i < rows.old; i += step) {
-        float f[16];
-        decode(*reinterpret_cast<const uint4*>(old + i * D + 16 * u), f);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) f[e] *= ratio;
-        const uint2 lo = codes(f, 1.f, 1.f), hi = codes(f + 8, 1.f, 1.f);
-        *reinterpret_cast<uint4*>(old + i * D + 16 * u) = make_uint4(lo.x, lo.y, hi.x, hi.y);
-      }
+      for (int i = row0; i < rows.old; i += step) store_again(old + i * D + 16 * u, held, scale);
     }
     float inv;
     asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(scale));
@@ -288,13 +368,6 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
       *reinterpret_cast<uint2*>(cache + to * D + vb) = codes(y, scale, inv);
     }
     if (part == 0 && lane < rows.blocks && s_scale[lane] >= 0) scales[s_scale[lane] + g * p.head_blocks] = scale;
-  };
-  // Cache row and scale of a slot (KV head 0).
-  auto scale_at = [&](int b, int slot) -> long long {
-    if (!r.block_table) return static_cast<long long>(b) * r.Hkv * p.head_blocks + (slot >> p.block_shift);
-    const int page = r.block_table[static_cast<size_t>(b) * r.max_pages + (slot >> r.page_shift)];
-    if (page < 0 || page >= r.num_pages) return -1;
-    return static_cast<long long>(page) * r.Hkv * p.head_blocks + ((slot & (r.page_size - 1)) >> p.block_shift);
   };
   auto store = [&](const Rows& rows, int angles) {         // angles: positions in s_pos
     if (any_keys) {
@@ -370,9 +443,9 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
   }
 }
 
-template <bool TREE>
+template <Form FORM>
 cudaError_t launch(const BlockParams& p, unsigned blocks, size_t smem, cudaStream_t stream) {
-  auto kernel = p.r.interleaved ? block_kernel<TREE, true> : block_kernel<TREE, false>;
+  auto kernel = p.r.interleaved ? block_kernel<FORM, true> : block_kernel<FORM, false>;
   if (smem > 48 * 1024) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
@@ -394,7 +467,16 @@ cudaError_t launch_block(const BlockParams& p_in, bool tree, int sm_count, cudaS
   p.store_groups = (2 * r.Hkv + p.store_heads - 1) / p.store_heads;
   p.span = p.block_size;
   while (!tree && p.span > 1 && (r.N + p.span - 1) / p.span * static_cast<long long>(p.store_groups) < 2 * sm_count) p.span /= 2;
-  const long long stores = (tree ? r.B : (r.N + static_cast<long long>(p.span) - 1) / p.span) * p.store_groups;
+  long long stores = (tree ? r.B : (r.N + static_cast<long long>(p.span) - 1) / p.span) * p.store_groups;
+  const bool single = !tree && r.N <= r.B;
+  if (single) {
+    // as for the queries below: a row's heads go to several warps until there are sixteen warps per SM, or a warp has one step of heads
+    int parts = 1;
+    while (tokens * parts < 16ll * sm_count && 2 * r.Hkv > parts * kRowsAtOnce) parts *= 2;
+    p.store_heads = ((2 * r.Hkv + parts - 1) / parts + kRowsAtOnce - 1) / kRowsAtOnce * kRowsAtOnce;
+    p.store_groups = (2 * r.Hkv + p.store_heads - 1) / p.store_heads;
+    stores = (tokens * p.store_groups + kWarps - 1) / kWarps;
+  }
   // queries: a token's heads are split over several warps until there are sixteen warps per SM, or a warp has one step of heads
   int chunks = 1;
   while (tokens * chunks < 16ll * sm_count && r.Hq > chunks * kRowsAtOnce) chunks *= 2;
@@ -403,10 +485,11 @@ cudaError_t launch_block(const BlockParams& p_in, bool tree, int sm_count, cudaS
   const long long turns = (tokens * r.head_chunks + kWarps - 1) / kWarps;
   if (stores + turns > 0x7fffffffll) return cudaErrorInvalidValue;
   p.store_ctas = static_cast<int>(stores);
-  const long long most = tree ? r.T : (p.block_size < r.N ? p.block_size : r.N);
+  const long long most = tree ? r.T : (single ? 0 : (p.block_size < r.N ? p.block_size : r.N));
   const size_t smem = sizeof(float2) * (D / 2) * static_cast<size_t>(most > kWarps ? most : kWarps);
   const unsigned blocks = static_cast<unsigned>(stores + turns);
-  const cudaError_t e = tree ? launch<true>(p, blocks, smem, stream) : launch<false>(p, blocks, smem, stream);
+  const cudaError_t e = tree ? launch<kTrees>(p, blocks, smem, stream)
+                        : (single ? launch<kSingles>(p, blocks, smem, stream) : launch<kChunks>(p, blocks, smem, stream));
   if (e != cudaSuccess) return e;
   count_launch();
   return cudaSuccess;

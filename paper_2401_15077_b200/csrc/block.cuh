@@ -11,8 +11,8 @@ struct BlockParams {
   int32_t block_size, block_shift;
   long long head_blocks;         // blocks from one KV head to the next
   int32_t span;                  // chunk form: rows whose blocks a CTA takes
-  int32_t store_heads;           // keys' and values' heads that a CTA takes
-  int32_t store_groups, store_ctas;      // CTAs per span or tree, and in all; the queries' CTAs come behind them
+  int32_t store_heads;           // keys' and values' heads that a CTA takes (single tokens: a warp)
+  int32_t store_groups, store_ctas;      // CTAs (single tokens: warps) per span or tree, and CTAs in all; the queries' CTAs come behind them
 };
 
 cudaError_t launch_block(const BlockParams& p, bool tree, int sm_count, cudaStream_t stream);

@@ -146,8 +146,8 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
 
   // With a window: the cost of a unit that ends `keys` slots into its sequence, and of the whole parts [lo, hi).
   const bool windowed = SPAN && p.window > 0;
-  const long long cap = windowed ? static_cast<long long>(p.window) + ut + (p.sinks + kChunkTile - 1) / kChunkTile * kChunkTile + 2 * kChunkTile : 0;
-  auto capped = [&](const ChunkSeq&, long long keys) { return (keys < cap ? keys : cap) + kChunkItemKeys; };
+  const long long cap = windowed ? static_cast<long long>(p.window) + ut + (static_cast<long long>(p.sinks) + kChunkTile - 1) / kChunkTile * kChunkTile + 2 * kChunkTile : 0;
+  auto capped = [&](long long keys) { return (keys < cap ? keys : cap) + kChunkItemKeys; };
   auto between = [&](const ChunkSeq& q, int lo, int hi) {
     const long long at = q.L < cap ? (cap - q.L) / ut : 0;                 // the first part that ends past the cap
     const long long mid = at < lo ? lo : (at < hi ? at : hi);
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
         q.parts = ceil_div(q.n, ut);
         const long long np = q.parts;
         v.a = static_cast<int>(np) * Hkv;
-        if (windowed) v.b = (capped(q, q.L + static_cast<long long>(q.n)) + between(q, 0, q.parts - 1)) * Hkv;
+        if (windowed) v.b = (capped(q.L + static_cast<long long>(q.n)) + between(q, 0, q.parts - 1)) * Hkv;
         else
         // sum over the parts of L + (p + 1) UT, but the last one ends at n
         v.b = (np * (static_cast<long long>(q.L) + kChunkItemKeys) + ut * (np * (np + 1) / 2) - (np * ut - q.n)) * Hkv;
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
     un.tiles = static_cast<int>((keys + kChunkTile - 1) / kChunkTile);
     if (windowed) {
       un.tiles -= chunk_span(p, q.L, pr * ut).skip;
-      if (x) *x = cost_of[b] + (r == 0 ? 0 : capped(q, q.L + static_cast<long long>(q.n)) + between(q, pr + 1, q.parts - 1)) * Hkv + un.g * capped(q, keys);
+      if (x) *x = cost_of[b] + (r == 0 ? 0 : capped(q.L + static_cast<long long>(q.n)) + between(q, pr + 1, q.parts - 1)) * Hkv + un.g * capped(keys);
     } else if (x) {
       const long long before = r * (static_cast<long long>(q.L) + kChunkItemKeys) +
                                ut * ((static_cast<long long>(q.parts) * (q.parts + 1) - static_cast<long long>(pr + 1) * (pr + 2)) / 2) - (r > 0 ? over : 0);

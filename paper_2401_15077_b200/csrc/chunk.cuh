@@ -115,7 +115,7 @@ __host__ __device__ inline ChunkSpan chunk_span(const ChunkParams& p, int L, int
     const int low = L + (p.tree ? 0 : first) - p.window + 1;
     s.low = low > 0 ? low : 0;
     s.sinks = p.sinks < s.low ? p.sinks : s.low;
-    const int w0 = s.low / kChunkTile, before = (s.sinks + kChunkTile - 1) / kChunkTile;
+    const int w0 = s.low / kChunkTile, before = s.sinks / kChunkTile + (s.sinks % kChunkTile != 0);
     s.before = before < w0 ? before : w0;
     s.skip = w0 - s.before;
   }

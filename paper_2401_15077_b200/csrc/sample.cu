@@ -506,22 +506,24 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
     mass = w.whole(1.0);
   }
   if (by_k && !some) {
-    auto bin_of = [&](float z) { return z == w.top ? 0 : static_cast<int>(fminf((w.top - z) * 64.f, kCountBins - 1.f)); };
+    // Bins of 1/64 from the top down, the last for all below, by a rounding that never turns an order around (which is all that is asked of it):
+    // 64 (top - z) is rounded to a whole number in the low bits of its sum with 2^23.  Positions outside of the row are counted as -infinity: they
+    // stand behind every token, and have no mass.
+    constexpr float kWhole = 8388608.f;
+    const float shift = fminf(w.top * 64.f + kWhole, 3.0e38f);
+    auto place_of = [&](float z) { return fmaf(z, -64.f, shift); };
+    auto bin_of = [&](float z) { return static_cast<int>(__float_as_uint(fminf(fmaxf(place_of(z), kWhole), kWhole + (kCountBins - 1.f))) & 0x7fffffu); };
     clear(s.hist.count, kCountBins);
     for (int i = 0; i < tiles; ++i) {
-      const int pos = (i * kThreads + tid) * kVec;
-      const Vec<T> v = fetch(pos);
+      const Vec<T> v = fetch((i * kThreads + tid) * kVec);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const int id = first + pos + e;
-        if (id >= 0 && id < p.V) atomicAdd(&s.hist.count[bin_of(v.at(e))], 1u);
-      }
+      for (int e = 0; e < kVec; ++e) atomicAdd(&s.hist.count[bin_of(v.at(e))], 1u);
     }
     const u64 want = static_cast<u64>(k);
     find_bin(std::false_type{}, [&](u64 before, u64 after) { return before < want && after >= want; });
     const int bin = static_cast<int>(s.bin);
-    make_list([&](float z) { return bin_of(z) <= bin; });
-    // (positions outside of the row hold -infinity too: they stand behind every token, and have no mass)
+    const float last = bin == kCountBins - 1 ? INFINITY : kWhole + bin;
+    make_list([&](float z) { return place_of(z) <= last; });
     rank_in_bin([&](float z) { return bin_of(z) == bin; }, std::false_type{}, s.base, static_cast<double>(k));
   }
   if (!nothing && top_p < 1.f && !(cut == w.top && take == 1)) {

@@ -105,15 +105,18 @@ class Case:
 
 
 CHUNKS = {
-    "one_token": dict(n=[1], lens=[70], hq=4, hkv=4, block=64),
-    "one_token_first": dict(n=[1], lens=[0], hq=1, hkv=1, block=16),
+    "one_token": dict(n=[1], lens=[70], hq=4, hkv=4, block=64, spare=0),
+    "one_token_first": dict(n=[1], lens=[0], hq=1, hkv=1, block=16, spare=0),
     "block_edges": dict(n=[1, 1, 1, 2, 3, 16, 17], lens=[15, 16, 17, 15, 31, 16, 15], hq=8, hkv=2, block=16),
     "odd": dict(n=[0, 5, 1, 0, 77, 33], lens=[9, 3, 64, 0, 131, 0], hq=6, hkv=3, block=32, page=64, strided=True),
     "long": dict(n=[700, 301], lens=[45, 0], hq=8, hkv=8, block=128, page=128, interleaved=True, amplitude=1.2),
     "part_turned": dict(n=[130, 7], lens=[3, 60], hq=4, hkv=1, block=64, page=256, rotary=48, strided=True),
     "part_turned_neighbours": dict(n=[40, 7], lens=[3, 60], hq=2, hkv=2, block=16, page=16, rotary=16, interleaved=True),
     "positions": dict(n=[20, 40], lens=[8, 0], hq=4, hkv=2, block=32, positions=True),
-    "many_singles": dict(n=[1] * 300, lens=[(i * 37) % 200 for i in range(300)], hq=2, hkv=1, block=32, page=32),
+    "many_singles": dict(n=[1] * 300, lens=[(i * 37) % 200 for i in range(300)], hq=2, hkv=1, block=32, page=32, spare=0),
+    "many_singles_and_spare_rows": dict(n=[1] * 300, lens=[(i * 37) % 200 for i in range(300)], hq=2, hkv=1, block=32, page=32),
+    "chunks_among_empty_sequences": dict(n=[37, 0, 3, 1, 20] + [0] * 60, lens=[5, 9, 30, 0, 64] + [7] * 60, hq=4, hkv=3, block=16, page=32, spare=0, strided=True),
+    "singles_with_positions": dict(n=[1, 1, 1, 2], lens=[15, 16, 200, 63], hq=2, hkv=5, block=64, positions=True, interleaved=True, rotary=64, spare=0),
     "many_heads": dict(n=[9, 80], lens=[5, 64], hq=64, hkv=32, block=64),
     "no_queries": dict(n=[9, 80], lens=[5, 64], hq=0, hkv=2, block=64),
     "ragged": dict(n=[(i * 29) % 90 for i in range(40)], lens=[(i * 53) % 150 for i in range(40)], hq=4, hkv=2, block=64, page=64, strided=True),
@@ -229,6 +232,15 @@ def test_refused_sequences_and_pages(E):
     c.lens = [10, 1000, 2]
     q, status = c.run(E)
     assert status == -6 and (q[1, :5] == 0).all()
+    c = Case([1, 1, 1], [10, 32, 2], 4, 2, 16, page=16, seed=7, spare=0)
+    bad = int(c.table[1, 2])
+    c.table[1, 2] = -3
+    before = [t.clone() for t in (c.k, c.ks)]
+    q, status = c.run(E)
+    assert status == -11 and torch.equal(c.got[0][bad].cpu(), before[0][bad]) and torch.equal(c.got[2][bad].cpu(), before[1][bad])
+    c.lens = [10, -1, 2]
+    q, status = c.run(E)
+    assert status == -6 and (q[1] == 0).all() and not (q[0] == 0).all()
     c = Case([4, 5, 6], [10, 30, 2], 4, 2, 16, seed=7)
     c.order = _ints([0, 9, 4, 15])                           # starts that descend
     q, status = c.run(E)
