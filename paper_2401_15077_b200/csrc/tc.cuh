@@ -1,5 +1,5 @@
 // Tensor-core, tensor-memory, TMA and mbarrier instructions of sm_100a as inline functions, for kernels whose CTAs work in
-// pairs (chunk.cu), and the host functions that encode their tensor maps.
+// pairs (chunk.cu, window.cu), and the host functions that encode their tensor maps.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -9,12 +9,6 @@ namespace eagle {
 namespace tc {
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-
-// Waits that do not succeed at once go on in a function of their own, so that they take no room in the loops; a kernel that moves registers
-// between its warps (setmaxnreg) cannot call functions and defines this to have them inline.
-#ifndef EAGLE_SLOW_WAIT
-#define EAGLE_SLOW_WAIT __noinline__
-#endif
 
 // ------------------------------------------------------------------------------------------------ mbarriers, bounded waits
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
@@ -63,7 +57,7 @@ __device__ __forceinline__ unsigned long long global_timer() {
 }
 // Every wait gives up after the limit that the host set (it sits in shared memory right behind the abort flag), raises
 // the flag and returns false; so does every other wait of the CTA from then on.
-static __device__ EAGLE_SLOW_WAIT bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   const unsigned long long t0 = global_timer(), limit = *reinterpret_cast<volatile unsigned long long*>(abort_flag + 1);
   for (uint32_t spins = 1;; ++spins) {
     if (mbar_try_wait(bar, parity)) return true;
@@ -82,7 +76,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 }
 // After an abort: copies and MMAs that the CTA has issued may still be at work on its shared and tensor memory.  They take
 // microseconds; this waits a hundred before it may leave.
-static __device__ EAGLE_SLOW_WAIT void let_work_land() {
+static __device__ __noinline__ void let_work_land() {
   const unsigned long long t0 = global_timer();
   while (global_timer() - t0 < 100000ull) __nanosleep(1000);
 }
@@ -110,7 +104,7 @@ __device__ __forceinline__ float value_of(unsigned long long t) { return __uint_
 __device__ __forceinline__ bool has_tag(unsigned long long t, uint32_t want) { return static_cast<uint32_t>(t >> 32) == want; }
 // Bounded wait for the word with number `want` in shared memory; one with another number when the CTA was aborted or the time
 // limit passed.
-static __device__ EAGLE_SLOW_WAIT unsigned long long tag_wait_slow(volatile unsigned long long* slot, uint32_t want, volatile int* abort_flag) {
+static __device__ __noinline__ unsigned long long tag_wait_slow(volatile unsigned long long* slot, uint32_t want, volatile int* abort_flag) {
   const unsigned long long t0 = global_timer(), limit = *reinterpret_cast<volatile unsigned long long*>(abort_flag + 1);
   for (uint32_t spins = 1;; ++spins) {
     const unsigned long long t = *slot;
