@@ -785,8 +785,9 @@ typedef struct eagle_sample_desc {
  * stays, in ascending order of the id.  A greedy row keeps the first token alone.  NaN logits count as -infinity; where some are +infinity these
  * share the mass.  A row without any value above -infinity reports EAGLE_ERR_ROW: token -1, probs 0.
  *
- * Orders are exact; w is taken in fp64 (error below 2^-45) and summed in integers, so results do not depend on how the work is split, and a decision can
- * differ from the definition only within about 1e-12 of its boundary.  One launch; no workspace.
+ * Orders are exact; w is taken in fp64 (relative error below 2^-45) and summed as integers of at most 2^-46 of the largest w (V <= 2^17; 2^-43 at
+ * V = 2^20), so results do not depend on how the work is split, and a decision can differ from the definition only where a boundary is nearer than
+ * 1e-9 (1e-7 at V = 2^20) of the largest w at the worst, 1e-10 as a rule.  One launch; no workspace.
  */
 int eagle_sample(const eagle_sample_desc* desc, const void* logits, const float* uniforms, int32_t* tokens, float* probs, eagle_stream_t stream);
 

@@ -7,9 +7,9 @@
 // A cluster of C CTAs takes a row, each a slice of the vocabulary, which stays in shared memory (in the logits' own type) for all passes
 // over it; histograms are merged and candidates exchanged through distributed shared memory.
 //
-// Weights are fp64 (argument, reduction by a table of sixteenths, polynomial) and are summed as integers of 2^-q, q = 42 .. 44 with the vocabulary's
-// size: sums then depend neither on the order of atomics nor on C, and cuts and draws are decided as if in 64 bits, which fp32 sums
-// over 10^5 tokens (relative 1e-6) would not.
+// Weights are fp64 (argument, reduction by a table of sixteenths, polynomial) and are summed as integers of 2^-q, q = 43 .. 46 (the largest with which V
+// of them fit 63 bits): sums then depend neither on the order of atomics nor on C.  A sum over V tokens is off by V * 2^-(q+1) at the most (10^5 tokens:
+// 7e-10) and by 1e-13 * sqrt(V) or so of the largest weight as a rule; fp32 sums (relative 1e-6) would decide visibly otherwise.
 //
 // What top-p may cut off is bounded before its histogram is taken: n tokens of weights below (1 - p) Z / n sum to less than (1 - p) Z, so
 // the cut is not among them.  Of a vocabulary's long tail nothing reaches the atomics then.
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
   w.rate = 16.0 * 1.4426950408889634 / (greedy ? 1.0 : static_cast<double>(temperature));
   w.top_d = w.top;
   w.roots = s.roots;
-  const int q = min(44, 62 - (32 - __clz(p.V - 1)));
+  const int q = min(46, 63 - (32 - __clz(p.V - 1)));
   w.unit = __hiloint2double((1023 + q) << 20, 0);
 
   // ---- the cut: tokens with a greater value stay, and the first `take` of those that equal it (`some`: these are not all of them).  `mass`: of
@@ -559,7 +559,9 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
       known = true;
     } else {
       const double n = by_k ? k : p.V;
-      const double tail = (1.0 - static_cast<double>(top_p)) * static_cast<double>(all) / w.unit / n;     // see above
+      // see above; the sums are of rounded weights, which are up to half a unit larger, and below half a unit 0
+      const double half_unit = 0.5 / w.unit;
+      const double tail = fmax((1.0 - static_cast<double>(top_p)) * static_cast<double>(all) / w.unit / n - half_unit, half_unit);
       const float depth = static_cast<float>((fmax(-log2(tail), 0.0) + 1e-3) * 16.0 / w.rate);
       const float scale = (kMassBins - 1.f) / depth;
       const float floor = cut;                            // (values of -infinity have no mass: nothing is lost where it is that)

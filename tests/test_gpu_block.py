@@ -282,3 +282,28 @@ def test_replayed_from_a_graph(E):
         graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip((ks, vs), want[2:])) and torch.equal(k, want[0]) and torch.equal(v, want[1])
+
+
+@pytest.mark.parametrize("tree", [None, "random"])
+def test_pages_at_the_far_end_of_a_large_pool(E, tree):
+    """Offsets that pass 32 bits: the same sequences in the last pages of a large pool give the same codes and scales."""
+    case = Case([20, 1, 50], [70, 5, 130], 4, 4, 16, page=128, tree=tree)
+    q, status = case.run(E)
+    assert status == 0
+    near = [t.cpu() for t in case.got]
+    pages = 70000                                            # of 64 KB: more than 2^32 bytes
+    far = pages - case.k.shape[0]
+    assert far * case.k[0].numel() > 2 ** 32
+    big = []
+    for t in (case.k, case.v, case.ks, case.vs):
+        big.append(torch.empty(pages, *t.shape[1:], dtype=t.dtype, device=DEV))
+        big[-1][far:] = t.to(DEV)
+    store = E.KVStore(big[0], big[1], block_table=torch.where(case.table >= 0, case.table + far, case.table).to(DEV), k_scale=big[2], v_scale=big[3], block_size=16)
+    state = torch.zeros(1, dtype=torch.int32, device=DEV)
+    a, b, c = (t.contiguous().to(DEV) for t in case.qkv.split(case.split, dim=-2))
+    fn = E.eagle_tree_block_append if tree else E.eagle_block_append
+    got = fn(a, b, c, store, _ints(case.lens).to(DEV), case.order.to(DEV), case.freqs.to(DEV), torch.full(a.shape, 7.0, dtype=torch.bfloat16, device=DEV), status=state,
+             **{n: t.to(DEV) for n, t in case.extra.items()})
+    assert int(state.item()) == 0 and torch.equal(got.cpu(), q)
+    for t, want in zip(big, near):
+        assert torch.equal(t[far:].cpu(), want)

@@ -1,6 +1,6 @@
 """Sampling against the 64-bit definition.
 
-Which tokens stay and which one is drawn have to be equal: weights are fp64 (2^-45) and sums are integers of 2^-42 of the largest weight, so
+Which tokens stay and which one is drawn have to be equal: weights are fp64 (2^-45) and sums are integers of 2^-43 or less of the largest weight, so
 over 10^5 tokens a border is good to 1e-10 of the sum, and a draw closer to one than 1e-9 (none is, with these seeds) would not be compared.
 Probabilities are fp32 roundings (2^-24 relative) of numbers good to 1e-10 relative."""
 import numpy as np
@@ -241,3 +241,37 @@ def _accept(E, target, small, draft, parent, u):
     path, bonus = E.eagle_tree_accept(target, small, draft.to(DEV), parent.to(DEV), u.to(DEV), accept_len=n)[:2]
     torch.cuda.synchronize()
     return path.cpu(), bonus.cpu(), n.cpu()
+
+
+def test_top_p_next_to_one_over_the_largest_vocabulary(E):
+    """The tail's weights are below a unit of the sums and are rounded up, so that what they sum to is more than 1 - p, the definition's less: either
+    answer keeps the first two tokens, a prefix of the tail at the most, and their probabilities (the tail's sum is 1e-7)."""
+    V = 1 << 20
+    z = torch.full((1, 1, V), float(np.log(0.7 * 2.0 ** -43)))
+    z[0, 0, 700000], z[0, 0, 3] = 0.0, float(np.log(0.5))
+    for top_p in (1 - 2.0 ** -24, 1 - 2.0 ** -20):
+        tokens, probs, status = _run(E, z, torch.full((1, 1), 0.9), top_p=torch.full((1,), top_p))
+        assert status == 0 and int(tokens[0, 0]) == 700000
+        got = probs[0, 0].double().numpy()
+        assert abs(got[700000] - 2 / 3) < 4e-7 and abs(got[3] - 1 / 3) < 4e-7
+        got[[3, 700000]] = 0
+        kept = np.flatnonzero(got)
+        assert got.max() < 1e-13 and (len(kept) == 0 or kept[-1] - kept[0] + 1 - len(kept) <= 2)
+        assert top_p == 1 - 2.0 ** -24 or len(kept) == 0
+
+
+def test_more_elements_than_32_bits_count(E):
+    """The last rows of 33000 x 65537 logits (2^31 elements and more)."""
+    R, V, last = 33000, 65537, 3
+    z = torch.zeros(1, R, V, dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator().manual_seed(12)
+    tail = (torch.randn(1, last, V, generator=g) * 3).bfloat16()
+    z[:, R - last:] = tail.to(DEV)
+    u = torch.rand(1, R, generator=g)
+    kw = {"top_k": torch.full((1,), 50).int(), "top_p": torch.full((1,), 0.9)}
+    probs = torch.full((1, R, V), 7.0, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    tokens, _ = E.eagle_sample(z, u.to(DEV), None, probs, status=status, **{n: t.to(DEV) for n, t in kw.items()})
+    assert int(status.item()) == 0
+    _check(tail, u[:, R - last:], tokens[:, R - last:].cpu(), probs[:, R - last:].cpu(), **kw)
+    assert (tokens[:, :R - last] < 45).all() and (probs[:, R - last - 1].cpu() == torch.tensor([1 / 45] * 45 + [0.0] * (V - 45))).all()

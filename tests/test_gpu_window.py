@@ -395,3 +395,51 @@ def test_random_shapes(E):
         window = int(g.integers(64 if form == "tree" else 1, 600)) if g.random() < 0.7 else 0
         Case(n=n, lens=g.integers(0, 900, B).tolist(), hq=hq, hkv=hkv, d=d, page=page, block=block, window=window, sinks=int(g.integers(0, 200)) if g.random() < 0.5 else 0,
              tree=form == "tree", seed=seed, spare=int(g.integers(0, 2)) if form == "chunk" else 0).check(E)
+
+
+@pytest.mark.parametrize("block", [0, 16])
+@pytest.mark.parametrize("form", ["chunk", "singles", "tree"])
+def test_pages_at_the_far_end_of_a_large_pool(E, form, block):
+    """Offsets that pass 32 bits (elements and bytes): the same sequences in the last pages of a large pool give the same bits."""
+    n = {"chunk": [60, 0, 200], "singles": [1, 1, 1], "tree": [33, 1, 64]}[form]
+    case = Case(n, [700, 30, 90], 8, 4, page=128, block=block, window=300, sinks=5, tree=form == "tree", spare=0)
+    want = case.check(E)
+    pages = 36000 if block else 70000                        # of 64 KB of codes or 128 KB of bf16: more than 2^31 elements
+    far = pages - case.k.shape[0]
+    assert far * case.k[0].numel() > 2 ** 31 and (block or far * case.k[0].numel() * 2 > 2 ** 32)
+    k, v = (torch.empty(pages, *t.shape[1:], dtype=t.dtype, device=DEV) for t in (case.k, case.v))
+    k[far:], v[far:] = case.k.to(DEV), case.v.to(DEV)
+    scales = {}
+    if block:
+        ks, vs = (torch.empty(pages, *t.shape[1:], device=DEV) for t in (case.ks, case.vs))
+        ks[far:], vs[far:] = case.ks.to(DEV), case.vs.to(DEV)
+        scales = {"k_scale": ks, "v_scale": vs}
+    table = torch.where(case.table >= 0, case.table + far, case.table).to(DEV)
+    got, status = case.run(E, E.KVStore(k, v, block_table=table, block_size=block, **scales))
+    assert status == 0 and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("block", [0, 32])
+@pytest.mark.parametrize("form", ["chunk", "singles", "tree"])
+def test_a_window_far_into_a_long_sequence(E, form, block):
+    """What a window sees does not depend on how much lies in front of it: a sequence moved back by 2^24 slots."""
+    n = {"chunk": [150], "singles": [1], "tree": [40]}[form]
+    case = Case(n, [1000], 8, 2, block=block, window=500, tree=form == "tree", spare=0)
+    want = case.check(E)
+    move = 1 << 24
+    lens = _ints([1000 + move]).to(DEV)
+    k, v = (torch.empty(1, 2, move + t.shape[2], 128, dtype=t.dtype, device=DEV) for t in (case.k, case.v))
+    k[:, :, move:], v[:, :, move:] = case.k.to(DEV), case.v.to(DEV)
+    scales = {}
+    if block:
+        ks, vs = (torch.empty(1, 2, k.shape[2] // block, device=DEV) for _ in range(2))
+        ks[:, :, move // block:], vs[:, :, move // block:] = case.ks.to(DEV), case.vs.to(DEV)
+        scales = {"k_scale": ks, "v_scale": vs}
+    store = E.KVStore(k, v, block_size=block, **scales)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    if form == "tree":
+        got = E.eagle_tree_window_attn(case.q.to(DEV), store, lens, case.order.to(DEV), tree_sizes=_ints(n).to(DEV), status=status, **case.kw)
+    else:
+        got = E.eagle_window_attn(case.q.to(DEV), store, lens, case.order.to(DEV), status=status, **case.kw)
+    # (2^24 is a multiple of a K/V tile, so the steps are the same; how the work is cut is a matter of its cost, which is the same, too)
+    assert int(status.item()) == 0 and torch.equal(got.cpu(), want)
