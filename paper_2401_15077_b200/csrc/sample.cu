@@ -7,18 +7,23 @@
 // A cluster of C CTAs takes a row, each a slice of the vocabulary, which stays in shared memory (in the logits' own type) for all passes
 // over it; histograms are merged and candidates exchanged through distributed shared memory.
 //
+// A small top-k (k <= 256) takes another way: the k-th largest of the threads' own largest values bounds the k-th value from below, what is above it is
+// a few more than k tokens, these go to every CTA with their ids, and each CTA decides by itself, by ranks and prefix sums in that order.
+//
 // Weights are fp64 (argument, reduction by a table of sixteenths, polynomial) and are summed as integers of 2^-q, q = 43 .. 46 (the largest with which V
 // of them fit 63 bits): sums then depend neither on the order of atomics nor on C.  A sum over V tokens is off by V * 2^-(q+1) at the most (10^5 tokens:
 // 7e-10) and by 1e-13 * sqrt(V) or so of the largest weight as a rule; fp32 sums (relative 1e-6) would decide visibly otherwise.
 //
 // What top-p may cut off is bounded before its histogram is taken: n tokens of weights below (1 - p) Z / n sum to less than (1 - p) Z, so
-// the cut is not among them.  Of a vocabulary's long tail nothing reaches the atomics then.
+// the cut is not among them.  For Z a lower bound will do, which is what the threads' largest values weigh.  Of a vocabulary's long tail nothing reaches
+// the atomics then.
 //
-// What bounds it: instructions and their latencies (some 170 a token with top-p over a flat distribution, of which fp64 takes a third of the
-// time that the SMs issue) and nine cluster barriers of about a microsecond, not the bytes.  From a graph, 64 rows of 129537 bf16 logits with
-// all filters, tokens: 46 us (16.6 MB: 2.5 us); 656 rows of 32000 fp32 logits with top-p, distributions: 160 us (168 MB: 26 us; 45 of the 160 are the pass that
-// writes).  Measured on the way: exponentials and histogram updates element by element, without picking what is left: 86 and 332 us; one CTA per SM: 216 us for the
-// 656 rows; 512 candidates ranked at once: 53 us for the 64; positions of picked values by a scan over the lanes instead of a ballot per element: the same.
+// What bounds it: the latency of its five to eight phases, each a pass over shared memory and a cluster barrier of 1 to 2 us, not the bytes (without any exponential
+// and histogram update the 656 rows below take 110 us).  From a graph, 64 rows of 129537 bf16 logits, k log-uniform up to 12000, top-p, min-p, tokens: 46 us
+// (16.6 MB: 2.5 us), with k = 50: 15 us (by the way of a large k: 37 us), k = 256: 25 us (38); 656 rows of 32000 fp32 logits with top-p, distributions: 132 us (168 MB: 26 us).
+// Measured on the way: a pass for Z before the one for the histogram, lists of what can stay, 160 us for the 656 rows; every bin read from every CTA, 5 us more per
+// search; a CTA to a row that reads its logits again from L2 in each pass, 148 us; four CTAs to a row, 225 us; four CTAs of 256 threads per SM, 141 us;
+// candidates ranked in loops over all, 24 us for k = 50.
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -35,8 +40,9 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kCountBins = 2048, kMassBins = 1024;
-constexpr int kFew = 448;                    // (at least a tile's 32 x 8 and a carry of 31)
-constexpr int kCandidates = 128;             // values that are ranked against one another, a thread each (more are cut finer first, which takes less)
+constexpr int kCandidates = 512;             // a small top-k's, a thread each
+constexpr int kRanked = 256;                 // values of a bin that are ranked against one another (more are cut finer first)
+constexpr int kKept = 4096;                  // of a large top-k's values, those that a CTA lists
 constexpr size_t kSliceBytes = 160 * 1024;   // of a slice that stays in shared memory, at the most
 constexpr size_t kPairBytes = 66 * 1024;     // and where two CTAs are to fit an SM
 
@@ -50,18 +56,24 @@ struct Shared {
   } hist;
   u64 slot[2][kMaxCluster][2];       // exchanges, by turns
   u64 warp_sum[kWarps];
+  u64 coarse[kMaxCluster][kCountBins / 32];      // each CTA's histogram, 32 bins together
   double roots[16];                  // (sixteen 8-byte words: no two share a bank)
-  float few[kWarps][kFew];           // a warp's values that are left of its part of the slice, or of a tile, side by side
   uint32_t list[kCandidates];        // this CTA's candidates
-  uint32_t all[kCandidates];         // the cluster's
+  int list_id[kCandidates];
+  uint32_t all[kRanked];             // the cluster's
   u64 weight[kCandidates];
+  float kept[kKept];
   uint32_t n, lo, hi;                // candidates found here, their range
+  uint32_t n_kept;
   // a cut, found by one thread or by several with the same result
   uint32_t cut_key, cut_take, cut_ties;
   u64 cut_base;
   uint32_t bin;
-  u64 base;
+  u64 base, total;
+  float warp_low[kWarps];
 };
+
+static_assert(kCandidates <= kThreads && kRanked <= kThreads && 2 * kCandidates * sizeof(u64) <= sizeof(Shared::hist), "a thread each; two tables of them in the histogram's room");
 
 // Order-preserving number of a float (no NaN, no negative zero), and back.
 __device__ __forceinline__ uint32_t key_of(float z) {
@@ -72,33 +84,46 @@ __device__ __forceinline__ float value_of_key(uint32_t k) { return __uint_as_flo
 
 // 2^(j / 16)
 __constant__ double kRoots[16] = {1.0, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916, 1.189207115002721, 1.241857812073484, 1.2968395546510096, 1.3542555469368927, 1.4142135623730951, 1.4768261459394993, 1.5422108254079407, 1.6104903319492543, 1.681792830507429, 1.7562521603732995, 1.8340080864093424, 1.9152065613971474};
-// 2^(x / 16) for -16000 < x <= 0: the nearest whole number is taken off by adding and subtracting 1.5 * 2^52, its low four bits go through the table, the others
-// to the exponent, and what is left, f in [-1/2, 1/2], through 1 + f times the polynomial that interpolates (2^(f / 16) - 1) / f at Chebyshev
-// nodes (relative error 9e-15).
-__device__ __forceinline__ double exp2_sixteenths(double x, const double* roots) {
-  const double big = x + 6755399441055744.0, f = x - (big - 6755399441055744.0);
-  const int n = __double2loint(big);
-  double r = 1.2716049516906705e-09;
-  r = fma(r, f, 1.4676387238435006e-07);
-  r = fma(r, f, 1.3550807778387664e-05);
-  r = fma(r, f, 0.0009383847926296646);
-  r = fma(r, f, 0.04332169878499658);
-  r = fma(r, f, 1.0) * roots[n & 15];
-  return __hiloint2double(__double2hiint(r) + ((n >> 4) << 20), __double2loint(r));
-}
-
+// exp((z - top) / temperature) in parts: x = 16 log2(e) (z - top) / temperature goes to the nearest whole number n by adding and subtracting 1.5 * 2^52, whose
+// low four bits go through the table, the others to the exponent, and what is left, f in [-1/2, 1/2], through 1 + f times the polynomial
+// that interpolates (2^(f / 16) - 1) / f at Chebyshev nodes (relative error 9e-15).
 struct Weigher {
   float top;             // the row's largest value
+  float floor;           // values below it weigh less than 2^-980, or are -infinity, or beside +infinity: 0
   double top_d, rate;    // 16 log2(e) / temperature
-  double unit;           // 2^q
+  int q;                 // whole weights count 2^-q
   const double* roots;
+  __device__ __forceinline__ bool any(float z) const { return z >= floor; }
+  // (any(z) holds, or the result is not used; infinities, which are at the top, count as the largest number)
+  __device__ __forceinline__ void parts(float z, int more, double* near, double* root) const {
+    constexpr double kBig = 6755399441055744.0;
+    const double d = static_cast<double>(fminf(z, 3.4028234663852886e38f)) - top_d;
+    const double big = fma(d, rate, kBig), f = fma(d, rate, -(big - kBig));
+    const int n = __double2loint(big);
+    double r = 1.2716049516906705e-09;
+    r = fma(r, f, 1.4676387238435006e-07);
+    r = fma(r, f, 1.3550807778387664e-05);
+    r = fma(r, f, 0.0009383847926296646);
+    r = fma(r, f, 0.04332169878499658);
+    *near = fma(r, f, 1.0);
+    const double t = roots[n & 15];
+    *root = __hiloint2double(__double2hiint(t) + static_cast<int>(static_cast<uint32_t>((n >> 4) + more) << 20), __double2loint(t));
+  }
   __device__ __forceinline__ double real(float z) const {
-    const double x = (static_cast<double>(z) - top_d) * rate;
-    const double e = x > -16000.0 ? exp2_sixteenths(x, roots) : 0.0;      // -infinity, and NaN from infinities, are 0
-    return z == top ? 1.0 : e;                            // (infinite ones too)
+    double a, b;
+    parts(z, 0, &a, &b);
+    return any(z) ? a * b : 0.0;
   }
   // A weight of at most 1 as an integer: adding 2^52 leaves it in the low bits of the sum.
-  __device__ __forceinline__ u64 whole(double w) const { return __double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull; }
+  __device__ __forceinline__ u64 whole_if_any(float z) const {
+    double a, b;
+    parts(z, q, &a, &b);
+    return __double_as_longlong(fma(a, b, 4503599627370496.0)) & 0xfffffffffffffull;
+  }
+  __device__ __forceinline__ u64 whole(float z) const {
+    const u64 x = whole_if_any(z);
+    return any(z) ? x : 0ull;
+  }
 };
 
 // Values of a row in their canonical form: NaN as -infinity, negative zero as zero.  (A maximum passes over NaN; one word: one value or two.)
@@ -139,6 +164,13 @@ struct Vec {
   }
 };
 
+template <typename T>
+__device__ __forceinline__ float largest(const Vec<T>& v) {
+  const uint32_t m = max_word<T>(max_word<T>(v.raw.x, v.raw.y), max_word<T>(v.raw.z, v.raw.w));
+  if constexpr (sizeof(T) == 4) return __uint_as_float(m);
+  else return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+}
+
 __device__ __forceinline__ u64 warp_sum64(u64 v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -155,14 +187,13 @@ __device__ __forceinline__ u64 warp_scan64(u64 v, int lane) {      // inclusive
 
 // RESIDENT: the slice is in shared memory; else it is read again from the logits in each pass (vocabularies beyond 8 x 160 KB).
 template <typename T, bool RESIDENT>
-__global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int slice) {
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(SampleParams p, int slice) {
   constexpr int kVec = Vec<T>::kLen, kTile = kThreads * kVec;
   extern __shared__ __align__(16) unsigned char dyn[];
   T* const held = reinterpret_cast<T*>(dyn);
   const int tiles = slice / kTile;
   u64* const part = reinterpret_cast<u64*>(dyn + (RESIDENT ? static_cast<size_t>(slice) * sizeof(T) : 0));      // [tiles][warps]
   uint32_t* const ties = reinterpret_cast<uint32_t*>(part + tiles * kWarps);                                      // [tiles][warps]
-  uint16_t* const segment = reinterpret_cast<uint16_t*>(ties + tiles * kWarps);                                   // [tiles][warps]: where a tile's part of a list begins
   __shared__ Shared s;
   cg::cluster_group cluster = cg::this_cluster();
   const int C = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
@@ -174,6 +205,8 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
   // ---- the slice.  Positions count from the 16-byte boundary at or before the row's first element, so that vectors are aligned.
   if (tid < 16) s.roots[tid] = kRoots[tid];
   auto started = cluster.barrier_arrive();                // (shared memory of the others is there once all have started)
+  const float temperature = p.temperature ? p.temperature[b] : 1.f, top_p = p.top_p ? p.top_p[b] : 1.f, min_p = p.min_p ? p.min_p[b] : 0.f;
+  const int k = p.top_k ? p.top_k[b] : 0;
   const T* const src = static_cast<const T*>(p.logits) + row * p.V;
   const int off = static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
   const int first = rank * slice - off;                   // id of the slice's position 0
@@ -229,105 +262,72 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
     u64 t = lane < kWarps ? s.warp_sum[lane] : 0;
     return warp_sum64(t);
   };
-  auto cluster_sum = [&](u64 v) {
-    const u64 mine = block_sum(v);
-    const u64(*got)[2] = exchange(mine, 0);
-    u64 t = 0;
-    for (int c = 0; c < C; ++c) t += got[c][0];
-    return t;
-  };
-
-  // The values of a warp's part of a tile that `stays(z)` picks, side by side in shared memory behind the `from` first, so that what is expensive (an
-  // exponential in fp64) is done for 32 of them at a time however few there are in a vector.  at[e]: where element e is, -1: left out.
-  // Returns their number.
-  float* const few = s.few[warp];
-  auto pick = [&](const Vec<T>& v, int from, auto stays, int* at) {
-    int n = from;
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-      const bool in = stays(v.at(e));
-      const unsigned mask = __ballot_sync(0xffffffffu, in);
-      at[e] = in ? n + __popc(mask & ((1u << lane) - 1u)) : -1;
-      if (in) few[at[e]] = v.at(e);
-      n += __popc(mask);
-    }
-    __syncwarp();
-    return n;
-  };
-  // Once a bound is known below which nothing stays, each warp keeps the rest of its part of the slice in that way, if there is room for it in
-  // all warps of the CTA: `listed`.  The passes from then on go over these lists.
-  bool listed = false;
-  int n_listed = 0;
-  auto make_list = [&](auto stays) {
-    __syncthreads();
-    bool fits = true;
-    int n = 0;
-    for (int i = 0; i < tiles && fits; ++i) {
-      int at[kVec];
-      if (lane == 0) segment[i * kWarps + warp] = static_cast<uint16_t>(n);
-      n = pick(fetch((i * kThreads + tid) * kVec), n, stays, at);
-      fits = i + 1 >= tiles || n <= kFew - 32 * kVec;      // (room for another tile)
-    }
-    listed = !__syncthreads_or(!fits);
-    n_listed = n;
-  };
-  auto in_segment = [&](int i, int* to) {                 // [returned, *to) of the list: tile i
-    *to = i + 1 < tiles ? segment[(i + 1) * kWarps + warp] : n_listed;
-    return static_cast<int>(segment[i * kWarps + warp]);
-  };
-  // `done(z)` for every value that may stay (those outside of the row too, unless there is a list).
-  auto for_all = [&](auto done) {
-    if (listed) {
-      for (int j = lane; j < n_listed; j += 32) done(few[j]);
-      return;
-    }
+  // `body(i, vector)` for each tile in which some lane's `may(its largest value)`: what looks for large values passes over most tiles at a vote each.
+  auto for_tiles = [&](auto may, auto body) {
     for (int i = 0; i < tiles; ++i) {
       const Vec<T> v = fetch((i * kThreads + tid) * kVec);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) done(v.at(e));
+      if (__any_sync(0xffffffffu, may(largest<T>(v)))) body(i, v);
     }
   };
-  // The same for those that `stays`, where `done` is expensive; without a list values are carried over from tile to tile until there are 32.
-  auto for_few = [&](auto stays, auto done) {
-    if (listed) {
-      for (int j = lane; j < n_listed; j += 32)
-        if (stays(few[j])) done(few[j]);
-      return;
+
+  // `done(z, true)` for the elements of a vector in a mask, where it is expensive: one after the other of each lane where few are in it (`done(z, false)`: none).
+  auto for_mask = [&](const Vec<T>& v, int i, unsigned mask, auto done) {
+    const int steps = __reduce_max_sync(0xffffffffu, __popc(mask));
+    if (2 * steps > kVec) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) done(v.at(e), (mask >> e & 1u) != 0);
+    } else {
+      const int pos = (i * kThreads + tid) * kVec;
+      for (int j = 0; j < steps; ++j) {
+        float z = 0.f;
+        if (mask) {
+          const int at = pos + __ffs(mask) - 1;
+          if constexpr (RESIDENT) z = static_cast<float>(held[at]);
+          else z = clean(static_cast<float>(src[first + at]));
+        }
+        done(z, mask != 0);
+        mask &= mask - 1;
+      }
     }
-    int n = 0;
-    for (int i = 0; i < tiles; ++i) {
-      int at[kVec];
-      n = pick(fetch((i * kThreads + tid) * kVec), n, stays, at);
-      int base = 0;
-      for (; base + 32 <= n; base += 32) done(few[base + lane]);
-      const float rest = base + lane < n ? few[base + lane] : 0.f;
-      n -= base;
-      __syncwarp();
-      if (lane < n) few[lane] = rest;
-      __syncwarp();
-    }
-    if (lane < n) done(few[lane]);
-    __syncwarp();
   };
 
   // ---- the largest value
-  uint32_t most = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;     // -infinity
-#pragma unroll 4
+  float most = -INFINITY;                                 // this thread's
+#pragma unroll 8
   for (int i = 0; i < tiles; ++i) {
     const int pos = (i * kThreads + tid) * kVec;
     const Vec<T> v = load(pos);
     if constexpr (RESIDENT) *reinterpret_cast<uint4*>(held + pos) = v.raw;
-    most = max_word<T>(most, max_word<T>(max_word<T>(v.raw.x, v.raw.y), max_word<T>(v.raw.z, v.raw.w)));
+    most = fmaxf(most, largest<T>(v));
   }
-  uint32_t top_key = sizeof(T) == 4 ? key_of(__uint_as_float(most)) : max(key_of(__uint_as_float(most << 16)), key_of(__uint_as_float(most & 0xffff0000u)));
-  top_key = __reduce_max_sync(0xffffffffu, top_key);
+  // ... and a lower bound of the sum of the weights: what the threads' largest values weigh, in fp32 (each CTA's against its own largest value)
+  const bool greedy = !(temperature > 0.f);
+  const float rate32 = greedy ? 0.f : 1.4426950f / temperature;
+  float at_least = 0.f;
+  uint32_t top_key = __reduce_max_sync(0xffffffffu, key_of(most));
   if (lane == 0) s.warp_sum[warp] = top_key;
   __syncthreads();
   top_key = __reduce_max_sync(0xffffffffu, lane < kWarps ? static_cast<uint32_t>(s.warp_sum[lane]) : 0u);
+  {
+    float x = exp2f((most - value_of_key(top_key)) * rate32);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (lane == 0) s.warp_low[warp] = x;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    at_least = lane < kWarps ? s.warp_low[lane] : 0.f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) at_least += __shfl_xor_sync(0xffffffffu, at_least, o);
+  }
   cluster.barrier_wait(std::move(started));
   {
-    const u64(*got)[2] = exchange(top_key, 0);
+    const u64(*got)[2] = exchange(top_key, __float_as_uint(at_least));
     for (int c = 0; c < C; ++c) top_key = max(top_key, static_cast<uint32_t>(got[c][0]));
+    at_least = 0.f;
+    for (int c = 0; c < C; ++c)
+      at_least += __uint_as_float(static_cast<uint32_t>(got[c][1])) * exp2f((value_of_key(static_cast<uint32_t>(got[c][0])) - value_of_key(top_key)) * rate32);
+    at_least = at_least * 0.999f > 1.f && at_least < INFINITY ? at_least * 0.999f : 1.f;      // (1: the largest value's; NaN beside infinities)
   }
   Weigher w;
   w.top = value_of_key(top_key);
@@ -336,16 +336,22 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
     report_status(p.status, EAGLE_ERR_ROW);
     if (p.tokens) p.tokens[row] = -1;
   }
-  const float temperature = p.temperature ? p.temperature[b] : 1.f;
-  const int k = p.top_k ? p.top_k[b] : 0;
-  const float top_p = p.top_p ? p.top_p[b] : 1.f;
-  const double least = p.min_p ? static_cast<double>(fminf(fmaxf(p.min_p[b], 0.f), 1.f)) : 0.0;      // (NaN: 0)
-  const bool greedy = !(temperature > 0.f);
+  const double least = static_cast<double>(fminf(fmaxf(min_p, 0.f), 1.f));      // (NaN: 0)
   w.rate = 16.0 * 1.4426950408889634 / (greedy ? 1.0 : static_cast<double>(temperature));
-  w.top_d = w.top;
+  w.top_d = fminf(w.top, 3.4028234663852886e38f);
+  w.floor = w.top == INFINITY ? w.top : fmaxf(__double2float_ru(static_cast<double>(w.top) - 15680.0 / w.rate), -3.4028234663852886e38f);      // (2^-980)
   w.roots = s.roots;
-  const int q = min(46, 63 - (32 - __clz(p.V - 1)));
-  w.unit = __hiloint2double((1023 + q) << 20, 0);
+  w.q = min(46, 63 - (32 - __clz(p.V - 1)));
+  const double half_unit = __hiloint2double((1022 - w.q) << 20, 0);
+  // min-p: only next to the border a weight is needed to tell
+  float sure_in = -INFINITY, sure_out = -3.4028234663852886e38f;      // (-infinity has no weight)
+  if (least > 0.0) {
+    const double border = static_cast<double>(w.top) + log2(least) * 16.0 / w.rate, room = 1e-6 * (fabs(static_cast<double>(w.top)) + fabs(border));
+    const bool known_border = room < 1e300;               // (no infinity, no NaN)
+    sure_in = known_border ? static_cast<float>(border + room) : INFINITY;
+    if (known_border) sure_out = fmaxf(sure_out, static_cast<float>(border - room));
+  }
+  auto left = [&](float z) { return least == 0.0 || z > sure_in || (z >= sure_out && !(w.real(z) < least)); };
 
   // ---- the cut: tokens with a greater value stay, and the first `take` of those that equal it (`some`: these are not all of them).  `mass`: of
   // all that stay, where a search for the cut has found it.
@@ -354,43 +360,81 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
   bool some = false, known = false;
   u64 mass = 0;
 
-  // Merged histogram -> the bin in which the prefix reaches the target, with what lies before it.  `reached(before, after)` is true in that
-  // bin only.  Every CTA of the cluster does all of it.
-  // (A histogram is cleared again only behind a further exchange, so that nobody reads it any more.)
-  auto find_bin = [&](auto is_mass, auto reached) {
+  // A vector of the row's probabilities.
+  auto store = [&](float* dst, int pos, auto value) {
+    const int id = first + pos;
+    const bool wide = ((reinterpret_cast<uintptr_t>(dst) - 4 * static_cast<uintptr_t>(off)) & 15) == 0;
+    if (wide && id >= 0 && id + kVec <= p.V) {
+#pragma unroll
+      for (int x = 0; x < kVec; x += 4) *reinterpret_cast<float4*>(dst + id + x) = make_float4(value(x), value(x + 1), value(x + 2), value(x + 3));
+    } else {
+#pragma unroll
+      for (int x = 0; x < kVec; ++x)
+        if (id + x >= 0 && id + x < p.V) dst[id + x] = value(x);
+    }
+  };
+  // What a row's prefix has to pass.
+  auto drawn = [&](long long of_row, u64 of_all) {
+    const double total = static_cast<double>(of_all), t = static_cast<double>(p.uniforms[of_row]) * total;
+    return t < total ? fmax(t, 0.0) : total * 0.9999999999999999;      // (u outside of [0, 1))
+  };
+
+  // Merged histogram -> the bin in which the prefix, on top of `base`, reaches the target (that of the histogram's total), with what lies
+  // before it.  CTAs send one another the sums of 32 bins each; only the 32 bins that matter are then read from all of them (all bins, of four CTAs: 5 us).
+  // Every CTA finds the same.  Returns the total.
+  // (A histogram is cleared, and sums are sent again, only behind a further exchange, so that nobody reads them any more.)
+  auto find_bin = [&](auto is_mass, u64 base, auto target_of) {
     constexpr bool MASS = decltype(is_mass)::value;
-    constexpr int kPer = (MASS ? kMassBins : kCountBins) / kThreads;
-    cluster.sync();                                       // all histograms are complete
-    u64 v[kPer], sum = 0;
+    constexpr int kSegments = (MASS ? kMassBins : kCountBins) / 32;
+    auto bin_in = [&](const Shared& of, int bin) -> u64 {
+      if constexpr (MASS) return of.hist.mass[0][bin] + (static_cast<u64>(of.hist.mass[1][bin]) << 32);
+      else return of.hist.count[bin];
+    };
+    __syncthreads();                                      // this CTA's histogram is complete
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) v[i] = 0;
-    for (int c = 0; c < C; ++c) {
-      const auto& hist = *cluster.map_shared_rank(&s.hist, c);
+    for (int i = 0; i < kSegments / kWarps; ++i) {
+      const int segment = i * kWarps + warp;
+      const u64 sum = warp_sum64(bin_in(s, segment * 32 + lane));
+      if (lane < C) cluster.map_shared_rank(&s.coarse[rank][segment], lane)[0] = sum;
+    }
+    cluster.sync();
+    if (warp == 0) {
+      u64 v[kSegments / 32], sum = 0;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if constexpr (MASS) v[i] += hist.mass[0][tid * kPer + i] + (static_cast<u64>(hist.mass[1][tid * kPer + i]) << 32);
-        else v[i] += hist.count[tid * kPer + i];
+      for (int i = 0; i < kSegments / 32; ++i) {
+        v[i] = 0;
+        for (int c = 0; c < C; ++c) v[i] += s.coarse[c][lane * (kSegments / 32) + i];
+        sum += v[i];
       }
-    }
+      const u64 inc = warp_scan64(sum, lane), total = __shfl_sync(0xffffffffu, inc, 31);
+      const double target = target_of(total);
+      auto reached = [&](u64 before, u64 after) { return static_cast<double>(before) < target && !(static_cast<double>(after) < target); };
+      u64 before = base + inc - sum, at = 0;
+      int segment = -1;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) sum += v[i];
-    const u64 inc = warp_scan64(sum, lane);
-    if (lane == 31) s.warp_sum[warp] = inc;
-    __syncthreads();
-    u64 before = inc - sum;
-    {
-      u64 t = lane < kWarps && lane < warp ? s.warp_sum[lane] : 0;
-      before += warp_sum64(t);
-    }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      if (reached(before, before + v[i])) {
-        s.bin = tid * kPer + i;
-        s.base = before;
+      for (int i = 0; i < kSegments / 32; ++i) {
+        if (reached(before, before + v[i])) {
+          segment = lane * (kSegments / 32) + i;
+          at = before;
+        }
+        before += v[i];
       }
-      before += v[i];
+      const unsigned hit = __ballot_sync(0xffffffffu, segment >= 0);
+      if (hit) {
+        const int bin = __shfl_sync(0xffffffffu, segment, __ffs(hit) - 1) * 32 + lane;
+        at = __shfl_sync(0xffffffffu, at, __ffs(hit) - 1);
+        u64 x = 0;
+        for (int c = 0; c < C; ++c) x += bin_in(*cluster.map_shared_rank(&s, c), bin);
+        const u64 upto = at + warp_scan64(x, lane);
+        if (reached(upto - x, upto)) {
+          s.bin = bin;
+          s.base = upto - x;
+        }
+      }
+      if (lane == 0) s.total = total;
     }
     __syncthreads();
+    return s.total;
   };
   // Exact 64-bit sums by 32-bit atomics: the carry goes along with the high word.
   auto add_mass = [&](int bin, u64 x) {
@@ -402,23 +446,65 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
     for (int i = tid; i < n; i += kThreads) words[i] = 0;
     __syncthreads();
   };
-  // Values of a bin are ranked against one another; a bin with too many of them is cut finer first, by their keys.  `member(z)`: lies in the bin;
-  // MASS: before and target are masses, else counts.
-  auto rank_in_bin = [&](auto member, auto is_mass, u64 base, double target) {
+  // Values of a bin are ranked against one another; a bin with too many of them is cut finer first, by their keys.  `member(z)`: lies in the bin, which
+  // lies within [low, high] (about: with room at both ends); MASS: base (what lies above the bin) and target are masses, else counts.
+  // The one for top-k also lists what lies in its bin and above, for those that follow: they go over this list if there is room for it.
+  int kept = -1;                                          // values listed here (-1: none)
+  auto rank_in_bin = [&](float low, float high, auto member, auto is_mass, u64 base, double target) {
     constexpr bool MASS = decltype(is_mass)::value;
+    bool keep = !MASS;
     uint32_t lo = 0, hi = 0xffffffffu;
+    if (!(low <= high)) {                                 // (NaN)
+      low = -INFINITY;
+      high = INFINITY;
+    }
+    auto for_members = [&](auto done) {
+      auto one = [&](float z) {
+        if (z >= low && z <= high && member(z)) {
+          const uint32_t key = key_of(z);
+          if (key >= lo && key <= hi) done(z, key);
+        }
+      };
+      if (MASS && kept >= 0) {
+        for (int j = tid; j < kept; j += kThreads) one(s.kept[j]);
+        return;
+      }
+      for_tiles([&](float z) { return z >= low; }, [&](int, const Vec<T>& v) {
+        if (keep) {
+          unsigned mask = 0;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) mask |= (v.at(e) >= low ? 1u : 0u) << e;
+          const int n = __popc(mask);
+          int upto = n;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+          }
+          uint32_t at = 0;
+          if (lane == 31) at = atomicAdd(&s.n_kept, static_cast<uint32_t>(upto));
+          at = __shfl_sync(0xffffffffu, at, 31) + upto - n;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e)
+            if (mask >> e & 1u) {
+              if (at < kKept) s.kept[at] = v.at(e);
+              ++at;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) one(v.at(e));
+      });
+      keep = false;
+    };
     for (;;) {
       if (tid == 0) { s.n = 0; s.lo = 0xffffffffu; s.hi = 0; }
       __syncthreads();
       uint32_t least = 0xffffffffu, most = 0;
-      for_all([&](float z) {
-        const uint32_t key = key_of(z);
-        if (member(z) && key >= lo && key <= hi) {
-          least = min(least, key);
-          most = max(most, key);
-          const uint32_t at = atomicAdd(&s.n, 1u);
-          if (at < kCandidates) s.list[at] = key;
-        }
+      for_members([&](float, uint32_t key) {
+        least = min(least, key);
+        most = max(most, key);
+        const uint32_t at = atomicAdd(&s.n, 1u);
+        if (at < kRanked) s.list[at] = key;
       });
       least = __reduce_min_sync(0xffffffffu, least);
       most = __reduce_max_sync(0xffffffffu, most);
@@ -436,7 +522,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
       if (lo == hi) {                                     // they are all equal
         if (tid == 0) {
           u64 need = n;
-          const u64 one = MASS ? w.whole(w.real(value_of_key(lo))) : 1;
+          const u64 one = MASS ? w.whole(value_of_key(lo)) : 1;
           const double x = ceil((target - static_cast<double>(base)) / static_cast<double>(one));
           if (x < static_cast<double>(n)) need = x > 1.0 ? static_cast<u64>(x) : 1;
           s.cut_key = lo;
@@ -446,7 +532,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
         }
         break;
       }
-      if (n <= kCandidates) {
+      if (n <= kRanked) {
         for (int c = 0; c < C; ++c) {
           const int m = static_cast<int>(got[c][0]);
           if (tid < m) s.all[mine_at + tid] = cluster.map_shared_rank(s.list, c)[tid];
@@ -454,7 +540,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
         }
         __syncthreads();
         if constexpr (MASS) {
-          if (tid < n) s.weight[tid] = w.whole(w.real(value_of_key(s.all[tid])));
+          if (tid < n) s.weight[tid] = w.whole(value_of_key(s.all[tid]));
           __syncthreads();
         }
         if (tid < n) {
@@ -481,15 +567,9 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
       const uint32_t top = hi, span = hi - lo;
       const int shift = max(0, 32 - __clz(span) - 10);    // span >> shift is below kMassBins
       clear(reinterpret_cast<uint32_t*>(&s.hist), sizeof(s.hist) / 4);
-      for_all([&](float z) {
-        const uint32_t key = key_of(z);
-        if (member(z) && key >= lo && key <= hi) add_mass((top - key) >> shift, MASS ? w.whole(w.real(z)) : 1ull);
-      });
-      const u64 base_now = base;
-      find_bin(std::true_type{}, [&](u64 before, u64 after) {
-        return static_cast<double>(base_now + before) < target && !(static_cast<double>(base_now + after) < target);
-      });
-      base += s.base;
+      for_members([&](float z, uint32_t key) { add_mass((top - key) >> shift, MASS ? w.whole(z) : 1ull); });
+      find_bin(std::true_type{}, base, [&](u64) { return target; });
+      base = s.base;
       hi = top - (s.bin << shift);
       lo = max(lo, hi - ((1u << shift) - 1u));
     }
@@ -497,7 +577,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
     cut = value_of_key(s.cut_key);
     take = s.cut_take;
     some = take < s.cut_ties;
-    mass = s.cut_base + take * (MASS ? w.whole(w.real(cut)) : 1);
+    mass = s.cut_base + take * (MASS ? w.whole(cut) : 1);
     // (the others have read the candidates before the next exchange, and those are written again only behind one)
   };
 
@@ -509,267 +589,357 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleParams p, int sl
     cut = w.top;
     take = 1;
     some = known = true;
-    mass = w.whole(1.0);
+    mass = w.whole(w.top);
   }
-  if (by_k && !some) {
-    // Bins of 1/64 from the top down, the last for all below, by a rounding that never turns an order around (which is all that is asked of it):
-    // 64 (top - z) is rounded to a whole number in the low bits of its sum with 2^23.  Positions outside of the row are counted as -infinity: they
-    // stand behind every token, and have no mass.
-    constexpr float kWhole = 8388608.f;
-    const float shift = fminf(w.top * 64.f + kWhole, 3.0e38f);
-    auto place_of = [&](float z) { return fmaf(z, -64.f, shift); };
-    auto bin_of = [&](float z) { return static_cast<int>(__float_as_uint(fminf(fmaxf(place_of(z), kWhole), kWhole + (kCountBins - 1.f))) & 0x7fffffu); };
+  // Bins of 1/64 from the top down, the last for all below, by a rounding that never turns an order around (which is all that is asked of it):
+  // 64 (top - z) is rounded to a whole number in the low bits of its sum with 2^23.
+  constexpr float kWhole = 8388608.f;
+  const float shift_k = fmaxf(fminf(w.top * 64.f + kWhole, 3.0e38f), -3.0e38f);
+  auto place_of = [&](float z) { return fmaf(z, -64.f, shift_k); };
+  auto bin_of_k = [&](float z) { return static_cast<int>(__float_as_uint(fminf(fmaxf(place_of(z), kWhole), kWhole + (kCountBins - 1.f))) & 0x7fffffu); };
+  auto last_of = [&](int bin) { return bin == kCountBins - 1 ? INFINITY : kWhole + bin; };      // places up to it lie in the bin or above
+
+  // ---- top-k with a small k: the k-th largest of the threads' largest values is no larger than the row's, so what is above it holds the first k
+  // tokens, and (values being spread over the threads) few others.  These go to every CTA with their ids, which then decides by itself.
+  bool decided = false;
+  if (by_k && !some && k <= kCandidates / 2) {
+    clear(s.hist.count, kCountBins);
+    atomicAdd(&s.hist.count[bin_of_k(most)], 1u);
+    if (tid == 0) s.n = 0;
+    find_bin(std::false_type{}, 0, [&](u64) { return static_cast<double>(k); });
+    const float last = last_of(static_cast<int>(s.bin));
+    for_tiles([&](float z) { return place_of(z) <= last; }, [&](int i, const Vec<T>& v) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float z = v.at(e);
+        if (place_of(z) <= last && z > -INFINITY) {
+          const uint32_t at = atomicAdd(&s.n, 1u);
+          if (at < kCandidates) {
+            s.list[at] = key_of(z);
+            s.list_id[at] = first + (i * kThreads + tid) * kVec + e;
+          }
+        }
+      }
+    });
+    __syncthreads();
+    const u64(*got)[2] = exchange(s.n, 0);
+    int n = 0;
+    for (int c = 0; c < C; ++c) n += static_cast<int>(got[c][0]);
+    if (n <= kCandidates) {
+      decided = true;
+      // values with their ids in one number that descends as the order does; the histogram's room is free now
+      u64* const order = reinterpret_cast<u64*>(&s.hist), *const by_place = order + kCandidates, *const by_id = s.weight;
+      for (int c = 0, at = 0; c < C; ++c) {
+        const int m = static_cast<int>(got[c][0]);
+        if (tid < m) order[at + tid] = static_cast<u64>(cluster.map_shared_rank(s.list, c)[tid]) << 32 | ~static_cast<uint32_t>(cluster.map_shared_rank(s.list_id, c)[tid]);
+        at += m;
+      }
+      __syncthreads();
+      const u64 mine = tid < n ? order[tid] : 0;
+      const float z = value_of_key(static_cast<uint32_t>(mine >> 32));
+      const int id = static_cast<int>(~static_cast<uint32_t>(mine));
+      int place = 0, place_by_id = 0;
+      if (tid < n) {
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) {
+          const u64 other = order[j];
+          place += other > mine;
+          place_by_id += static_cast<uint32_t>(other) > static_cast<uint32_t>(mine);
+        }
+      }
+      // prefix sums (exclusive ones, in place) over the candidates; returns the total
+      auto prefix = [&](u64* of) {
+        __syncthreads();
+        const u64 x = tid < n ? of[tid] : 0, inc = warp_scan64(x, lane);
+        if (lane == 31) s.warp_sum[warp] = inc;
+        __syncthreads();
+        const u64 of_warp = lane < kWarps ? s.warp_sum[lane] : 0;
+        const u64 before = inc - x + warp_sum64(lane < warp ? of_warp : 0);
+        if (tid < n) of[tid] = before;
+        __syncthreads();
+        return warp_sum64(of_warp);
+      };
+      bool stays = tid < n && place < k;
+      const u64 weight = stays ? w.whole(z) : 0;
+      if (top_p < 1.f) {
+        if (tid < n) by_place[place] = weight;
+        const u64 sum = prefix(by_place);
+        stays = stays && static_cast<double>(by_place[place]) < static_cast<double>(top_p) * static_cast<double>(sum);
+      }
+      stays = stays && left(z);
+      if (tid < n) by_id[place_by_id] = stays ? weight : 0;
+      const u64 all = prefix(by_id);
+      if (stays && p.tokens && rank == 0) {
+        const double t = drawn(row, all);
+        const u64 before = by_id[place_by_id];
+        if (!(static_cast<double>(before) > t) && static_cast<double>(before + weight) > t) p.tokens[row] = id;
+      }
+      if (p.probs) {
+        float* const dst = p.probs + row * p.V;
+        for (int i = 0; i < tiles; ++i) store(dst, (i * kThreads + tid) * kVec, [](int) { return 0.f; });
+        __syncthreads();
+        const int at = id - first;
+        if (stays && at >= 0 && at < slice) dst[id] = static_cast<float>(w.real(z) * (1.0 / (static_cast<double>(all) * (2.0 * half_unit))));
+      }
+    }
+  }
+  if (by_k && !some && !decided) {
+    // positions outside of the row are counted as -infinity: they stand behind every token, and have no mass
+    __syncthreads();
+    if (tid == 0) s.n_kept = 0;
     clear(s.hist.count, kCountBins);
     for (int i = 0; i < tiles; ++i) {
       const Vec<T> v = fetch((i * kThreads + tid) * kVec);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) atomicAdd(&s.hist.count[bin_of(v.at(e))], 1u);
+      for (int e = 0; e < kVec; ++e) atomicAdd(&s.hist.count[bin_of_k(v.at(e))], 1u);
     }
-    const u64 want = static_cast<u64>(k);
-    find_bin(std::false_type{}, [&](u64 before, u64 after) { return before < want && after >= want; });
+    find_bin(std::false_type{}, 0, [&](u64) { return static_cast<double>(k); });
     const int bin = static_cast<int>(s.bin);
-    const float last = bin == kCountBins - 1 ? INFINITY : kWhole + bin;
-    make_list([&](float z) { return place_of(z) <= last; });
-    rank_in_bin([&](float z) { return bin_of(z) == bin; }, std::false_type{}, s.base, static_cast<double>(k));
+    const float room = fabsf(w.top) < 1e30f ? fabsf(w.top) * 1e-6f + 0.03125f : INFINITY;      // (a bin is 1/64, while the shift is exact enough)
+    rank_in_bin(bin == kCountBins - 1 ? -INFINITY : w.top - bin * 0.015625f - room, w.top - bin * 0.015625f + room, [&](float z) { return bin_of_k(z) == bin; },
+                std::false_type{}, s.base, static_cast<double>(k));
+    if (s.n_kept <= kKept) kept = static_cast<int>(s.n_kept);
   }
-  if (!nothing && top_p < 1.f && !(cut == w.top && take == 1)) {
-    u64 sum = 0;
-    const bool whole_row = cut == -INFINITY && take == 0xffffffffu;
-    if (whole_row) {
-#pragma unroll 2
+  if (!nothing && !decided && top_p < 1.f && !(cut == w.top && take == 1)) {
+    // masses of what is above the cut: bins from the top down to where nothing can be the cut any more (see above; the sums are of rounded weights,
+    // which are up to half a unit larger, and below half a unit 0).  What lies below counts with the last bin.
+    const double n = by_k ? k : p.V;
+    const double tail = fmax((1.0 - static_cast<double>(top_p)) * (by_k ? 1.0 : static_cast<double>(at_least)) / n - half_unit, half_unit);
+    const float depth = static_cast<float>((1e-3 - log2(tail)) * 16.0 / w.rate);
+    const float scale = (kMassBins - 1.f) / depth;
+    const float floor = cut;
+    const float half_top = 0.5f * static_cast<float>(w.top_d), twice = 2.f * scale;      // (differences of halves do not overflow)
+    auto bin_of = [&](float z) { return fmaf(fminf(z, 3.4028234663852886e38f), -0.5f, half_top) * twice; };
+    __syncthreads();
+    clear(reinterpret_cast<uint32_t*>(&s.hist), sizeof(s.hist) / 4);
+    u64 rest = 0;
+    auto count = [&](float z, bool in) {
+      const float x = bin_of(z);
+      const u64 weight = w.whole_if_any(z);
+      if (in && w.any(z)) {
+        if (x < kMassBins) add_mass(static_cast<int>(x), weight);
+        else rest += weight;
+      }
+    };
+    if (floor == -INFINITY) {
       for (int i = 0; i < tiles; ++i) {
         const Vec<T> v = fetch((i * kThreads + tid) * kVec);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) sum += w.whole(w.real(v.at(e)));
+        for (int e = 0; e < kVec; ++e) count(v.at(e), true);
       }
+    } else if (kept >= 0) {
+      for (int j = tid; j < kept; j += kThreads) count(s.kept[j], s.kept[j] > floor);
     } else {
-      for_few([&](float z) { return z > cut; }, [&](float z) { sum += w.whole(w.real(z)); });
+      for_tiles([&](float z) { return z > floor; }, [&](int i, const Vec<T>& v) {
+        unsigned mask = 0;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) mask |= (v.at(e) > floor ? 1u : 0u) << e;
+        for_mask(v, i, mask, count);
+      });
     }
-    const u64 above = cluster_sum(sum);
-    const u64 one = whole_row ? 0 : w.whole(w.real(cut));
-    const u64 all = whole_row ? above : above + take * one;
-    const double target = static_cast<double>(top_p) * static_cast<double>(all);
-    if (!whole_row && static_cast<double>(above) < target) {      // among the last ones that top-k left
+    rest = warp_sum64(rest);
+    if (lane == 0) add_mass(kMassBins - 1, rest);
+    const u64 one = floor == -INFINITY ? 0 : w.whole(cut);
+    auto target_of = [&](u64 above) { return static_cast<double>(top_p) * static_cast<double>(one == 0 ? above : above + take * one); };
+    const u64 above = find_bin(std::true_type{}, 0, target_of);
+    const double target = target_of(above);
+    if (one > 0 && static_cast<double>(above) < target) {      // among the last ones that top-k left
       const double x = ceil((target - static_cast<double>(above)) / static_cast<double>(one));
       if (x < static_cast<double>(take)) {
         take = x > 1.0 ? static_cast<uint32_t>(x) : 1u;
         some = true;
       }
       mass = above + take * one;
-      known = true;
     } else {
-      const double n = by_k ? k : p.V;
-      // see above; the sums are of rounded weights, which are up to half a unit larger, and below half a unit 0
-      const double half_unit = 0.5 / w.unit;
-      const double tail = fmax((1.0 - static_cast<double>(top_p)) * static_cast<double>(all) / w.unit / n - half_unit, half_unit);
-      const float depth = static_cast<float>((fmax(-log2(tail), 0.0) + 1e-3) * 16.0 / w.rate);
-      const float scale = (kMassBins - 1.f) / depth;
-      const float floor = cut;                            // (values of -infinity have no mass: nothing is lost where it is that)
-      auto bin_of = [&](float z) { return z == w.top ? 0.f : (w.top - z) * scale; };
-      auto member = [&](float z) { return z > floor && bin_of(z) < kMassBins; };
-      if (!listed) make_list(member);
-      clear(reinterpret_cast<uint32_t*>(&s.hist), sizeof(s.hist) / 4);
-      for_few(member, [&](float z) { add_mass(static_cast<int>(bin_of(z)), w.whole(w.real(z))); });
-      find_bin(std::true_type{}, [&](u64 before, u64 after) {
-        return static_cast<double>(before) < target && !(static_cast<double>(after) < target);
-      });
       const float bin = static_cast<float>(s.bin);
-      rank_in_bin([&](float z) {
+      const float room = fabsf(w.top) * 1e-6f + (1.f + 1e-3f * bin) / scale;
+      rank_in_bin(w.top - (bin + 1.f) / scale - room, w.top - bin / scale + room, [&](float z) {
         const float x = bin_of(z);
         return x >= bin && x < bin + 1.f && z > floor;
       }, std::true_type{}, s.base, target);
-      known = true;
     }
+    known = true;
   }
 
-  // ---- where only the first of equal values stay: how many there are before each warp's part of each tile
-  u64 ties_before = 0;
-  if (some) {
-    uint32_t mine = 0;
-    for (int i = 0; i < tiles; ++i) {
-      uint32_t n = 0;
-      if (listed) {
-        int to;
-        for (int j = in_segment(i, &to) + lane; j < to; j += 32) n += few[j] == cut;
-      } else {
-        const Vec<T> v = fetch((i * kThreads + tid) * kVec);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) n += v.at(e) == cut;
-      }
-      n = __reduce_add_sync(0xffffffffu, n);
-      if (lane == 0) ties[i * kWarps + warp] = n;
-      mine += n;
-    }
-    const u64 here = block_sum(lane == 0 ? mine : 0);
-    const u64(*got)[2] = exchange(here, 0);
-    for (int c = 0; c < rank; ++c) ties_before += got[c][0];
-    if (warp == 0) {                                      // exclusive prefix sums in place
-      u64 carry = ties_before;
-      for (int at = 0; at < tiles * kWarps; at += 32) {
-        const u64 n = at + lane < tiles * kWarps ? ties[at + lane] : 0;
-        const u64 inc = warp_scan64(n, lane);
-        if (at + lane < tiles * kWarps) ties[at + lane] = static_cast<uint32_t>(carry + inc - n);
-        carry += __shfl_sync(0xffffffffu, inc, 31);
-      }
-    }
-    __syncthreads();
-  }
-  // Of this warp's part of a tile: what stays, picked (see above); min-p takes out more when the weights are known.
-  auto pick_left = [&](const Vec<T>& v, int group, int* at) {
-    uint32_t rank_of = 0;
-    if (some) {
-      uint32_t n = 0;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) n += v.at(e) == cut;
-      uint32_t inc = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += x;
-      }
-      rank_of = ties[group] + inc - n;
-    }
-    return pick(v, 0, [&](float z) { return z > cut || (z == cut && (some ? rank_of++ < take : take > 0)); }, at);
-  };
-  auto left = [&](float z) {
-    const double x = w.real(z);
-    return x < least ? 0.0 : x;
-  };
-
-  // ---- the mass of what stays; where a token is drawn, of each warp's part of each tile as well
-  u64 before = 0, all = mass;
-  u64 here = 0;
-  if (p.tokens || !known || least > 0.0) {
-    all = 0;
-    u64 sum = 0;
-    for (int i = 0; i < tiles; ++i) {
+  // ---- the mass of what stays and, where only the first of equal values do, how many of these there are: in all, before this CTA, and (for the draw
+  // and the ranks) in each warp's part of each tile.  In order of the ids, `take` of the equal ones stay.
+  u64 before = 0, here = 0, all = mass;
+  uint32_t ties_before = 0;
+  const bool sums = p.tokens || !known || least > 0.0;
+  const u64 one = some && left(cut) ? w.whole(cut) : 0;
+  if (!decided && (sums || some)) {
+    u64 sum = 0, equal = 0;
+    if (lane == 0)
+      for (int i = 0; i < tiles; ++i) part[i * kWarps + warp] = ties[i * kWarps + warp] = 0;
+    __syncwarp();
+    for_tiles([&](float z) { return z >= cut; }, [&](int i, const Vec<T>& v) {
       u64 t = 0;
-      if (listed) {
-        int to;
-        uint32_t seen = some ? ties[i * kWarps + warp] : 0;
-        for (int j = in_segment(i, &to); j < to; j += 32) {
-          const float z = j + lane < to ? few[j + lane] : -INFINITY;
-          bool stays = j + lane < to && z >= cut;
-          if (some) {
-            const unsigned equal = __ballot_sync(0xffffffffu, stays && z == cut);
-            if (z == cut) stays = stays && seen + __popc(equal & ((1u << lane) - 1u)) < take;
-            seen += __popc(equal);
-          } else if (z == cut) {
-            stays = stays && take > 0;
-          }
-          if (stays) t += w.whole(left(z));
-        }
-      } else {
-        int at[kVec];
-        const int n = pick_left(fetch((i * kThreads + tid) * kVec), i * kWarps + warp, at);
-        for (int x = lane; x < n; x += 32) t += w.whole(left(few[x]));
-        __syncwarp();
+      uint32_t n = 0;
+      unsigned mask = 0;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float z = v.at(e);
+        n += some && z == cut;
+        mask |= (sums && (some ? z > cut : z >= cut) && z >= sure_out ? 1u : 0u) << e;
       }
+      for_mask(v, i, mask, [&](float z, bool in) {
+        const u64 weight = w.whole(z);
+        if (in && left(z)) t += weight;
+      });
+      n = __reduce_add_sync(0xffffffffu, n);
       if (p.tokens) {
         t = warp_sum64(t);
         if (lane == 0) part[i * kWarps + warp] = t;
         t = lane == 0 ? t : 0;
       }
+      if (lane == 0) ties[i * kWarps + warp] = n;
       sum += t;
-    }
-    here = block_sum(sum);
-    const u64(*got)[2] = exchange(here, 0);
+      equal += lane == 0 ? n : 0;
+    });
+    sum = block_sum(sum);
+    equal = some ? block_sum(equal) : 0;
+    const u64(*got)[2] = exchange(sum, equal);
+    if (sums) all = 0;
+    uint32_t seen = 0;
     for (int c = 0; c < C; ++c) {
-      if (c < rank) before += got[c][0];
-      all += got[c][0];
+      const uint32_t n = static_cast<uint32_t>(got[c][1]), in = seen < take ? min(n, take - seen) : 0u;
+      const u64 m = got[c][0] + in * one;
+      if (c == rank) {
+        before = all;
+        here = m;
+        ties_before = seen;
+      }
+      if (sums) all += m;
+      seen += n;
     }
   }
-
-  __syncthreads();                                        // (the lists are not needed any more: what follows picks from tiles again)
-
+  auto leaving = cluster.barrier_arrive();                // (of what is in the other CTAs nothing is read or written from here on)
   // ---- the draw: the CTA, the warp's part of a tile, the lane and the element in which the prefix passes u times the sum
-  if (p.tokens && !nothing && warp == 0) {
-    const double total = static_cast<double>(all);
-    double t = static_cast<double>(p.uniforms[row]) * total;
-    t = t < total ? fmax(t, 0.0) : total * 0.9999999999999999;      // (u outside of [0, 1))
-    if (here > 0 && !(static_cast<double>(before) > t) && static_cast<double>(before + here) > t) {
-      u64 carry = before;
-      int group = -1;
-      for (int at = 0; at < tiles * kWarps; at += 32) {
-        const u64 n = at + lane < tiles * kWarps ? part[at + lane] : 0;
-        const u64 inc = warp_scan64(n, lane);
-        const unsigned hit = __ballot_sync(0xffffffffu, static_cast<double>(carry + inc) > t);
-        if (hit) {
-          const int l = __ffs(hit) - 1;
-          group = at + l;
-          carry += __shfl_sync(0xffffffffu, inc - n, l);
-          break;
+  double t = 0.0;
+  bool draw = false;
+  if (p.tokens && !nothing && !decided) {
+    t = drawn(row, all);
+    draw = here > 0 && !(static_cast<double>(before) > t) && static_cast<double>(before + here) > t;
+  }
+  if (some && (p.probs || draw)) {
+    if (warp == 0) {                                      // exclusive prefix sums in place; parts with what stays of the equal ones
+      uint32_t carry = ties_before;
+      for (int at = lane; at - lane < tiles * kWarps; at += 32) {
+        const uint32_t n = at < tiles * kWarps ? ties[at] : 0;
+        uint32_t inc = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t x = __shfl_up_sync(0xffffffffu, inc, o);
+          if (lane >= o) inc += x;
+        }
+        const uint32_t seen = carry + inc - n;
+        if (at < tiles * kWarps) {
+          ties[at] = seen;
+          part[at] += (seen < take ? min(n, take - seen) : 0u) * one;
         }
         carry += __shfl_sync(0xffffffffu, inc, 31);
       }
-      // (group >= 0: the CTA's sum passes t)
-      const int pos = ((group / kWarps) * kThreads + (group % kWarps) * 32 + lane) * kVec;
-      const Vec<T> v = fetch(pos);
-      int at[kVec];
-      pick_left(v, group, at);
-      u64 e[kVec], mine = 0;
+    }
+    __syncthreads();
+  }
+  // Which elements of a vector of this warp's part of a tile stay (min-p aside).
+  auto which = [&](const Vec<T>& v, int group) {
+    unsigned stay = 0, equal = 0;
 #pragma unroll
-      for (int x = 0; x < kVec; ++x) {
-        e[x] = at[x] >= 0 ? w.whole(left(v.at(x))) : 0;
-        mine += e[x];
-      }
-      const u64 inc = warp_scan64(mine, lane);
+    for (int e = 0; e < kVec; ++e) {
+      stay |= (v.at(e) > cut ? 1u : 0u) << e;
+      equal |= (v.at(e) == cut ? 1u : 0u) << e;
+    }
+    if (!some) return take > 0 ? stay | equal : stay;
+    if (!__any_sync(0xffffffffu, equal != 0)) return stay;
+    uint32_t inc = __popc(equal);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += x;
+    }
+    uint32_t seen = ties[group] + inc - __popc(equal);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e)
+      if (equal >> e & 1u) stay |= (seen++ < take ? 1u : 0u) << e;
+    return stay;
+  };
+  if (draw && warp == 0) {
+    u64 carry = before;
+    int group = 0;
+    for (int at = 0; at < tiles * kWarps; at += 32) {
+      const u64 n = at + lane < tiles * kWarps ? part[at + lane] : 0;
+      const u64 inc = warp_scan64(n, lane);
       const unsigned hit = __ballot_sync(0xffffffffu, static_cast<double>(carry + inc) > t);
-      if (lane == __ffs(hit) - 1) {
-        u64 run = carry + inc - mine;
-        int found = kVec - 1;
-#pragma unroll
-        for (int x = kVec - 1; x >= 0; --x) {
-          u64 upto = run;
-#pragma unroll
-          for (int y = 0; y <= x; ++y) upto += e[y];
-          if (static_cast<double>(upto) > t) found = x;
-        }
-        p.tokens[row] = first + pos + found;
+      if (hit) {                                          // (it comes: the CTA's sum passes t)
+        const int l = __ffs(hit) - 1;
+        group = at + l;
+        carry += __shfl_sync(0xffffffffu, inc - n, l);
+        break;
       }
+      carry += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    const int pos = ((group / kWarps) * kThreads + (group % kWarps) * 32 + lane) * kVec;
+    const Vec<T> v = fetch(pos);
+    const unsigned stay = which(v, group);
+    u64 e[kVec], mine = 0;
+#pragma unroll
+    for (int x = 0; x < kVec; ++x) {
+      e[x] = (stay >> x & 1u) && left(v.at(x)) ? w.whole(v.at(x)) : 0;
+      mine += e[x];
+    }
+    const u64 inc = warp_scan64(mine, lane);
+    const unsigned hit = __ballot_sync(0xffffffffu, static_cast<double>(carry + inc) > t);
+    if (lane == __ffs(hit) - 1) {
+      u64 run = carry + inc - mine;
+      int found = kVec - 1;
+#pragma unroll
+      for (int x = kVec - 1; x >= 0; --x) {
+        u64 upto = run;
+#pragma unroll
+        for (int y = 0; y <= x; ++y) upto += e[y];
+        if (static_cast<double>(upto) > t) found = x;
+      }
+      p.tokens[row] = first + pos + found;
     }
   }
 
   // ---- the distribution
-  if (p.probs) {
+  if (p.probs && !decided) {
     float* const dst = p.probs + row * p.V;
-    const double inv = nothing ? 0.0 : w.unit / static_cast<double>(all);
-    const bool wide = ((reinterpret_cast<uintptr_t>(dst) - 4 * static_cast<uintptr_t>(off)) & 15) == 0;
+    const double inv = nothing ? 0.0 : 1.0 / (static_cast<double>(all) * (2.0 * half_unit));
     for (int i = 0; i < tiles; ++i) {
-      const int pos = (i * kThreads + tid) * kVec, id = first + pos;
-      int at[kVec];
-      const int n = pick_left(fetch(pos), i * kWarps + warp, at);
-      for (int x = lane; x < n; x += 32) few[x] = static_cast<float>(left(few[x]) * inv);
-      __syncwarp();
+      const int pos = (i * kThreads + tid) * kVec;
+      const Vec<T> v = fetch(pos);
       float out[kVec];
 #pragma unroll
-      for (int x = 0; x < kVec; ++x) out[x] = at[x] >= 0 ? few[at[x]] : 0.f;
-      __syncwarp();
-      if (wide && id >= 0 && id + kVec <= p.V) {
+      for (int x = 0; x < kVec; ++x) out[x] = 0.f;
+      if (__any_sync(0xffffffffu, largest<T>(v) >= cut)) {
+        const unsigned stay = which(v, i * kWarps + warp);
 #pragma unroll
-        for (int x = 0; x < kVec; x += 4) *reinterpret_cast<float4*>(dst + id + x) = make_float4(out[x], out[x + 1], out[x + 2], out[x + 3]);
-      } else {
-#pragma unroll
-        for (int x = 0; x < kVec; ++x)
-          if (id + x >= 0 && id + x < p.V) dst[id + x] = out[x];
+        for (int x = 0; x < kVec; ++x) {
+          const double weight = w.real(v.at(x));
+          out[x] = (stay >> x & 1u) && !(weight < least) ? static_cast<float>(weight * inv) : 0.f;
+        }
       }
+      store(dst, pos, [&](int x) { return out[x]; });
     }
   }
-  cluster.sync();                                         // nobody leaves while another may still read or write here
+  cluster.barrier_wait(std::move(leaving));               // nobody leaves while another may still read or write here
 }
 
 template <typename T>
 cudaError_t launch(const SampleParams& p, int sm_count, cudaStream_t stream) {
   constexpr int kTile = kThreads * Vec<T>::kLen;
   const long long rows = static_cast<long long>(p.B) * p.R, positions = static_cast<long long>(p.V) + Vec<T>::kLen;
-  // Enough CTAs to a row to hold it in the shared memory of CTAs that are two to an SM, and more while all of them find a place at once and each has
-  // more than a tile of the vocabulary.
+  // Enough CTAs to a row to hold it in the shared memory of CTAs that are two to an SM (figures for fewer and more: at the top), and more while all of them
+  // find a place at once and each has more than a tile of the vocabulary (top-p alone, a row of 129537 bf16 logits 30 us, else 43; eight of 32000 19 us, else 41).
   int C = 1;
   auto slice_of = [&](int c) { return static_cast<int>(((positions + c - 1) / c + kTile - 1) / kTile * kTile); };
   while (C < kMaxCluster && (slice_of(C) * sizeof(T) > kPairBytes || (rows * C <= sm_count && slice_of(C) > kTile))) C *= 2;
   const int slice = slice_of(C);
   const bool resident = slice * sizeof(T) <= kSliceBytes;
-  const size_t bytes = (resident ? slice * sizeof(T) : 0) + static_cast<size_t>(slice / kTile) * kWarps * 14;
+  const size_t bytes = (resident ? slice * sizeof(T) : 0) + static_cast<size_t>(slice / kTile) * kWarps * 12;
   auto kernel = resident ? sample_kernel<T, true> : sample_kernel<T, false>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSliceBytes + 16384));
   if (e != cudaSuccess) return e;

@@ -275,3 +275,47 @@ def test_more_elements_than_32_bits_count(E):
     assert int(status.item()) == 0
     _check(tail, u[:, R - last:], tokens[:, R - last:].cpu(), probs[:, R - last:].cpu(), **kw)
     assert (tokens[:, :R - last] < 45).all() and (probs[:, R - last - 1].cpu() == torch.tensor([1 / 45] * 45 + [0.0] * (V - 45))).all()
+
+
+def test_values_whose_differences_overflow(E):
+    """Logits of either sign next to the largest number, and filters that look at differences of them."""
+    g = torch.Generator().manual_seed(13)
+    B, V = 12, 5000
+    z = torch.randn(B, 1, V, generator=g)
+    z[:6] = -1e38 - z[:6].abs() * 5e37                       # all negative
+    z[6:9] = z[6:9] * 1e38
+    z[9] = 3e38
+    z[9, 0, ::2] = -3e38
+    z[10, 0] = 4.6e36 + z[10, 0] * 1e35                      # about where 64 of them overflow
+    z[11, 0] = -4.6e36 + z[11, 0] * 1e35
+    u = torch.rand(B, 1, generator=g)
+    t = torch.tensor([1.0, 1e37, float("inf"), 1e36, 3e38, 1.0, 1e38, float("inf"), 1e37, float("inf"), 1e35, 1e35])
+    k = torch.tensor([3, 50, 200, 128, 129, 5000, 7, 4000, 100, 0, 60, 3000]).int()
+    for kw in ({"temperature": t, "top_p": torch.full((B,), 0.6)}, {"temperature": t, "top_k": k}, {"temperature": t, "top_k": k, "top_p": torch.full((B,), 0.8)},
+               {"temperature": t, "min_p": torch.full((B,), 0.3)}):
+        tokens, probs, status = _run(E, z, u, **kw)
+        assert status == 0
+        _check(z, u, tokens, probs, **kw)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_small_top_k(E, bf16):
+    """Where the few tokens that can stay are looked for first: k up to and past the most that are taken that way, all the largest values side by side or
+    under one thread, many equal ones, fewer tokens than k."""
+    g = torch.Generator().manual_seed(14)
+    B, V = 40, 20011
+    z = torch.randn(B, 2, V, generator=g) * 2
+    z[8:16, :, 5000:5600] += 20                              # neighbours
+    z[16:24] = z[16:24].round()                              # thousands of equal values
+    z[24:28] = -float("inf")
+    for b in range(24, 28):
+        z[b, :, torch.randperm(V, generator=g)[:10 * (b - 23)]] = torch.randn(10 * (b - 23), generator=g)
+    z[28:32] = z[28:32].sort(-1).values
+    z = z.bfloat16() if bf16 else z
+    u = torch.rand(B, 2, generator=g)
+    k = torch.tensor([1, 2, 7, 50, 255, 256, 257, 300] * 5).int()
+    p, m = torch.tensor([0.3, 0.9, 0.99, 1.0, 0.05] * 8), torch.tensor([0.0, 0.1, 0.0, 0.02, 0.5, 0.0, 1.0] * 6)[:B]
+    for kw in ({"top_k": k}, {"top_k": k, "top_p": p}, {"top_k": k, "top_p": p, "min_p": m, "temperature": torch.linspace(0.2, 3, B)}):
+        tokens, probs, status = _run(E, z, u, **kw)
+        assert status == 0
+        _check(z, u, tokens, probs, **kw)
