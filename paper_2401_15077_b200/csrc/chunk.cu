@@ -26,6 +26,7 @@ using namespace tc;
 
 // ================================================================================================================ planner
 constexpr int kPlanThreads = 512;
+constexpr int kFewCut = 2 * kPlanThreads / 32;          // units, two to a warp
 constexpr int kNearSeqs = 256, kNearUnits = 4096;      // tables of calls this small stay in shared memory as well
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -93,6 +94,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
   __shared__ long long s_pos[kMaxPlanCtas + 1], s_cost[kNearSeqs], s_x[kNearUnits + 1];
   __shared__ int s_base[kNearSeqs], s_first[kMaxPlanCtas], s_last[kMaxPlanCtas];
   __shared__ ChunkSeq s_seq[kNearSeqs];
+  __shared__ int32_t s_bad[kNearSeqs];
   const int tid = threadIdx.x, P = p.num_workers, B = p.B, Hkv = p.Hkv, ut = p.ut;
   ChunkWork& w = p.work;
   ChunkSeq* seqs = B <= kNearSeqs ? s_seq : w.seq;
@@ -103,34 +105,33 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
   // the packed layout has to be an ascending list of starts inside the tensor: everything below relies on it
   int bad = 0;
   const bool tree = SPAN && p.tree > 0;
+  int32_t* bad_of = B <= kNearSeqs ? s_bad : w.bad_page;                    // trees that are none
+  const int own_n = tree && p.tree_sizes && tid < B ? p.tree_sizes[p.shared_tree ? 0 : tid] : p.tree, own_L = tid < B ? p.seq_lens[tid] : 0;      // (on their way)
   if (tree) {
-    // a tree that is not one is noted where the pages that do not exist will be, and refused with its sequence
-    for (int b = tid; b < B; b += kPlanThreads) {
-      const int n = p.tree_sizes ? p.tree_sizes[p.shared_tree ? 0 : b] : p.tree;
-      w.bad_page[b] = n < 0 || n > p.tree;
-    }
-    __syncthreads();
-    const long long nodes = static_cast<long long>(p.shared_tree ? 1 : B) * p.tree;
-    for (long long at = tid; at < nodes; at += kPlanThreads) {
-      const int b = static_cast<int>(at / p.tree), i = static_cast<int>(at - static_cast<long long>(b) * p.tree);
-      const int n = p.tree_sizes ? p.tree_sizes[b] : p.tree, up = p.tree_parent[at];
-      if (i < n && (up < -1 || up >= i)) w.bad_page[b] = 1;
-    }
-    __syncthreads();
+    const int lane = tid & 31, T = p.tree;
+    auto wrong = [&](int at) {                                               // (a warp)
+      const int n = p.tree_sizes ? p.tree_sizes[at] : T, up0 = lane < T ? p.tree_parent[at * T + lane] : -1, up1 = lane + 32 < T ? p.tree_parent[at * T + lane + 32] : -1;
+      return __any_sync(0xffffffffu, n < 0 || n > T || (lane < n && (up0 < -1 || up0 >= lane)) || (lane + 32 < n && (up1 < -1 || up1 >= lane + 32)));
+    };
     if (p.shared_tree) {
-      const int wrong = w.bad_page[0];
-      __syncthreads();
-      for (int b = tid; b < B; b += kPlanThreads) w.bad_page[b] = wrong;
-      __syncthreads();
+      const int no_tree = wrong(0);
+      for (int b = tid; b < B; b += kPlanThreads) bad_of[b] = no_tree;
+    } else {
+#pragma unroll 4
+      for (int b = tid >> 5; b < B; b += kPlanThreads / 32) {
+        const int no_tree = wrong(b);
+        if (lane == 0) bad_of[b] = no_tree;
+      }
     }
+    __syncthreads();
   }
   for (int b = tid; b < B; b += kPlanThreads) {
     int s, e;
     if (tree) {
-      const int n = p.tree_sizes ? p.tree_sizes[p.shared_tree ? 0 : b] : p.tree;
+      const int n = b == tid ? own_n : (p.tree_sizes ? p.tree_sizes[p.shared_tree ? 0 : b] : p.tree);
       s = b * p.tree;
       e = s + n;
-      if (w.bad_page[b]) {
+      if (bad_of[b]) {
         e = s;
         report_status(p.status, EAGLE_ERR_TREE);
       }
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
       e = p.token_start[b + 1];
       if (s < 0 || e < s || e > p.N) bad = 1;
     }
-    if (b < kNearSeqs) s_seq[b] = ChunkSeq{s, e - s, p.seq_lens[b], 0};
+    if (b < kNearSeqs) s_seq[b] = ChunkSeq{s, e - s, own_L, 0};              // (b = tid there)
   }
   bad = __syncthreads_or(bad);
   if (bad && tid == 0) report_status(p.status, EAGLE_ERR_SEQ);
@@ -239,10 +240,8 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
   long long own_x = 0;
   if (tid < U) own = unit_of(tid, &own_x);
   for (int u = tid; u < U; u += kPlanThreads) {
-    ChunkUnit un = own;
     long long x = own_x;
-    if (u != tid) un = unit_of(u, &x);
-    w.unit[u] = un;
+    if (u != tid) unit_of(u, &x);
     x_of[u] = x;
   }
   if (tid == 0) x_of[U] = W;
@@ -278,9 +277,15 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
     it[1] = make_int4(q.n, q.L, t0, t1);
     it[2] = make_int4(slot, 0, 0, 0);
   };
+  auto note = [&](const ChunkUnit& un, int u, int c_lo, int c_hi) {
+    const ChunkSeq q = seqs[un.b];
+    w.cut[c_lo] = ChunkCut{u, c_lo, c_hi, 0, un.b, un.g, un.part, q.start, q.n, {0, 0, 0}};
+  };
   // Whole units are items c * k + round.  Of the shares, piece (u, c) of unit u in worker c's share is item u + c; the units in
   // which a share begins and ends are noted for the worker.
-  for (int u = tid; u < U; u += kPlanThreads) {
+  // Few units that are cut are given to a warp each, a lane per piece (one thread after the 18 pieces of each of 8 units: 3 us), many to a thread each.
+  const bool by_warp = U - F <= kFewCut;
+  for (int u = tid; u < (by_warp ? F : U); u += kPlanThreads) {
     const ChunkUnit un = u == tid ? own : unit_of(u, nullptr);
     if (u < F) {
       emit((u % P) * k + u / P, un, 0, un.tiles, -1);
@@ -299,7 +304,22 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(ChunkParams p)
       s_first[c + 1] = u;
       t0 = t1;
     }
-    if (c > c_lo) w.cut[c_lo] = ChunkCut{u, c_lo, c, 0};
+    if (c > c_lo) note(un, u, c_lo, c);
+  }
+  if (by_warp) {
+    const int lane = tid & 31;
+    for (int u = F + (tid >> 5); u < U; u += kPlanThreads / 32) {
+      const ChunkUnit un = unit_of(u, nullptr);
+      const long long x0 = x_of[u], x1 = x_of[u + 1];
+      const int c_lo = last_le(s_pos, P, x0), c_hi = last_le(s_pos, P, x1 - 1);
+      for (int c = c_lo + lane; c <= c_hi; c += 32) {      // (a later cut is no earlier tile)
+        const int t0 = c == c_lo ? 0 : cut_tile(s_pos[c], x0, un.tiles), t1 = c == c_hi ? un.tiles : cut_tile(s_pos[c + 1], x0, un.tiles);
+        emit(u + c, un, t0, t1, t0 == 0 && t1 == un.tiles ? -1 : (2 * c + (t0 > 0 ? 0 : 1)) * tiles);
+        if (c > c_lo || s_pos[c] == x0) s_first[c] = u;
+        if (x1 >= s_pos[c + 1]) s_last[c] = u;
+      }
+      if (c_hi > c_lo && lane == 0) note(un, u, c_lo, c_hi);
+    }
   }
   __syncthreads();
   if (tid < P) {
@@ -894,11 +914,9 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams 
   const int rec = blockIdx.x / (halves * row_blocks), rest = blockIdx.x - rec * halves * row_blocks, half = rest / row_blocks, rb = rest - half * row_blocks;
   const ChunkCut cut = w.cut[rec];
   if (cut.unit < 0) return;
-  const ChunkUnit un = w.unit[cut.unit];
-  const ChunkSeq q = w.seq[un.b];
-  const int first = un.part * p.ut + half * p.tpt;
-  if (first + rb * 8 / p.G >= q.n || rb * 8 / p.G >= p.tpt) return;      // no row of this block belongs to the sequence
-  if (w.bad_page[un.b]) return;
+  const int first = cut.part * p.ut + half * p.tpt;
+  if (first + rb * 8 / p.G >= cut.n || rb * 8 / p.G >= p.tpt) return;    // no row of this block belongs to the sequence
+  const bool wrong = w.bad_page[cut.b] != 0;
   if (tid < 32) {
     int count = 0;
     for (int i = cut.c_lo; i <= cut.c_hi; i += 32) {
@@ -918,7 +936,7 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams 
   const int pieces = s_count;                            // 0: the cuts snapped to the unit's edges, its output is there already
   const int row = rb * 8 + ((tid >> 2) & 7), cols = (tid >> 5) * 4 + (tid & 3);      // row of the tile, group of 4 columns
   const int tok = row / p.G, head = row - tok * p.G, token = first + tok;
-  if (pieces == 0 || tok >= p.tpt || token >= q.n || cols >= D / 4) return;
+  if (wrong || pieces == 0 || tok >= p.tpt || token >= cut.n || cols >= D / 4) return;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i = 0; i < pieces; i += 4) {
@@ -952,7 +970,7 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_merge_kernel(ChunkParams 
   uint2 out;
   out.x = pack_bf16(o.x * inv, o.y * inv);
   out.y = pack_bf16(o.z * inv, o.w * inv);
-  *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(q.start + token) * p.Hq + un.g * p.G + head) * D + cols * 4) = out;
+  *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(cut.start + token) * p.Hq + cut.g * p.G + head) * D + cols * 4) = out;
 }
 
 template <int D>

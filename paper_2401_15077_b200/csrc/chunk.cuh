@@ -15,7 +15,7 @@ constexpr int kChunkSnap = 2;
 // 128 rows on the tensor cores of both; the row kernel's are single CTAs, with one query tile of 16 rows.  A query tile is
 // TPT tokens times the G heads of a group.  Calls with no more rows than sequences (single tokens) take the row kernel: there
 // the keys and values are streamed once for a few rows, and what counts is how steadily they come.  64 single tokens over 512 to
-// 8192 slots, 32 heads over 8: 203 us, the tile kernel 249 us; one token over 65536, 64 heads over 8: 59.5 us against
+// 8192 slots, 32 heads over 8: 203 us, the tile kernel 249 us; one token over 65536, 64 heads over 8: 58 us against
 // 77 us.  The host sees numbers and no lengths, so the rule takes N <= B for single tokens.  The row kernel is right for more tokens of
 // a sequence too, but reads its cache again for every 16 / G of them.  Rows against tiles in us (cold caches, D = 128, 8 KV heads):
 //   a token each, 64 sequences of 512 to 4112 slots    32 heads 127 : 152   64 heads 127 : 152   no groups 395 : 524
@@ -46,8 +46,10 @@ struct alignas(16) ChunkItem {
   int32_t pad[3];
 };
 // A unit whose output is merged from the pieces (unit, c), c_lo <= c <= c_hi; unit < 0: none.
-struct ChunkCut {
+struct alignas(16) ChunkCut {
   int32_t unit, c_lo, c_hi, pad;
+  int32_t b, g, part, start;     // of the unit, and of its sequence
+  int32_t n, pad2[3];
 };
 
 struct ChunkWork {
@@ -55,7 +57,6 @@ struct ChunkWork {
   int32_t* unit_base;      // [B]
   long long* cost_base;    // [B]
   long long* x;            // [units + 1]: where each unit starts on the work line
-  ChunkUnit* unit;         // [units]
   ChunkItem* items;        // [units + workers]
   int4* cta;               // [workers]: whole units (first, count), pieces (first, count)
   ChunkCut* cut;           // [workers]
@@ -142,7 +143,6 @@ inline bool carve_chunk_work(const eagle_chunk_desc& d, void* base, int sms, Chu
   w->unit_base = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * B));
   w->cost_base = reinterpret_cast<long long*>(take(sizeof(long long) * B));
   w->x = reinterpret_cast<long long*>(take(sizeof(long long) * (units + 1)));
-  w->unit = reinterpret_cast<ChunkUnit*>(take(sizeof(ChunkUnit) * units));
   w->items = reinterpret_cast<ChunkItem*>(take(sizeof(ChunkItem) * (units + workers)));
   w->cta = reinterpret_cast<int4*>(take(sizeof(int4) * workers));
   w->cut = reinterpret_cast<ChunkCut*>(take(sizeof(ChunkCut) * workers));

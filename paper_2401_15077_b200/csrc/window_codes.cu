@@ -18,7 +18,7 @@
 // single warp for both was what the kernel waited for).
 //
 // From a graph, with planner and merge: 64 single tokens over 512 to 8192 slots, 32 heads over 8 (608 MB): 125 us, 4.9 TB/s (278 us as 16 query rows by
-// 8 keys, four warps' worth of copies at a time and one warp for pages and scales); one token over 65536 slots, 64 heads over 8 (134 MB): 43 us (planner,
+// 8 keys, four warps' worth of copies at a time and one warp for pages and scales); one token over 65536 slots, 64 heads over 8 (134 MB): 42 us (planner,
 // merge and their launches are about 12 us of it).
 #include "window.cuh"
 
