@@ -42,6 +42,8 @@ template <int D, bool CODES>
 struct Smem {
   static constexpr int kKSlots = CODES ? 3 : 5, kVSlots = CODES ? 3 : 4;     // rings of half tiles that the MMAs read
   static constexpr int kKStages = 4, kVStages = 3;           // and of half tiles of codes
+  // (the two warps that widen K tiles take every other step each, those of V likewise)
+  static_assert(!CODES || (kKStages % 2 == 0 && kVStages == kVSlots), "a stage belongs to one warp, or its tile's turn tells its uses apart");
   static constexpr int kFactors = 5;                         // items whose rows' factors are kept: the MMAs are three steps ahead of the softmax, the widening two items ahead of them
   static constexpr int kSlabs = D / 64;                      // 64 16-bit numbers = one 128-byte swizzled row
   static constexpr int kQSlab = 128 * 128, kQBytes = kSlabs * kQSlab;
@@ -579,7 +581,9 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
               }
             } else {
               const uint32_t st = gs % S::kVStages, sl = gs % kVSlots;
-              ok = mbar_wait_warp(B.vc_full(st), (gs / S::kVStages) & 1u, s_abort) && mbar_wait_warp(B.v_empty(sl), ((gs / kVSlots) & 1u) ^ 1u, s_abort);
+              // The tile's turn first: V's stages change owners from use to use, and a wait by parity does not tell the use before last from this one.
+              // With as many tiles as stages, the tile being free says that the stage's last use is over.
+              ok = mbar_wait_warp(B.v_empty(sl), ((gs / kVSlots) & 1u) ^ 1u, s_abort) && mbar_wait_warp(B.vc_full(st), (gs / S::kVStages) & 1u, s_abort);
               if (!ok) break;
               // values of slots that the unit does not see may be anything, and 0 * garbage must not reach O
               const int key0 = span.tile(t) * kChunkTile, in_use = it.L + it.n;

@@ -443,3 +443,36 @@ def test_a_window_far_into_a_long_sequence(E, form, block):
         got = E.eagle_window_attn(case.q.to(DEV), store, lens, case.order.to(DEV), status=status, **case.kw)
     # (2^24 is a multiple of a K/V tile, so the steps are the same; how the work is cut is a matter of its cost, which is the same, too)
     assert int(status.item()) == 0 and torch.equal(got.cpu(), want)
+
+
+@pytest.mark.parametrize("form", ["chunk", "tree"])
+def test_tiles_over_codes_whose_copies_land_in_any_order(E, form):
+    """The same call many times, its pages spread over a large pool of which a part is in the L2 cache, another one busy reading beside it: the same bits."""
+    n = {"chunk": [300, 77], "tree": [64, 20] * 8}[form]
+    case = Case(n, [4000, 2500] * (len(n) // 2), 8, 4, page=16, block=16, tree=form == "tree", spare=0, seed=17)
+    want = case.check(E)
+    pages, g = 20000, torch.Generator().manual_seed(18)      # of 8 KB each for keys and values: more than the L2 cache holds
+    to = torch.randperm(pages, generator=g)[:case.k.shape[0]]
+    moved = []
+    for t in (case.k, case.v, case.ks, case.vs):
+        moved.append(torch.zeros(pages, *t.shape[1:], dtype=t.dtype, device=DEV))
+        moved[-1][to.to(DEV)] = t.to(DEV)
+    store = E.KVStore(moved[0], moved[1], k_scale=moved[2], v_scale=moved[3], block_size=16,
+                      block_table=torch.where(case.table >= 0, to.int()[case.table.clamp(min=0).long()], case.table).to(DEV))
+    q, lens, order, sizes = case.q.to(DEV), _ints(case.lens).to(DEV), case.order.to(DEV), _ints(n).to(DEV)
+    other, side, differ = torch.empty(1 << 26, device=DEV), torch.cuda.Stream(), torch.zeros((), dtype=torch.int64, device=DEV)
+    outs = [torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    want = want.to(DEV)
+    torch.cuda.synchronize()
+    for i in range(300):
+        with torch.cuda.stream(side):
+            if i % 3:
+                other.add_(1.0)
+        out = outs[i % 2]
+        if form == "tree":
+            E.eagle_tree_window_attn(q, store, lens, order, out, tree_sizes=sizes)
+        else:
+            E.eagle_window_attn(q, store, lens, order, out)
+        differ += (out.view(torch.int16) != want.view(torch.int16)).any()
+    torch.cuda.synchronize()
+    assert int(differ.item()) == 0
