@@ -706,7 +706,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(SampleParams p, int
     const double n = by_k ? k : p.V;
     const double tail = fmax((1.0 - static_cast<double>(top_p)) * (by_k ? 1.0 : static_cast<double>(at_least)) / n - half_unit, half_unit);
     const float depth = static_cast<float>((1e-3 - log2(tail)) * 16.0 / w.rate);
-    const float scale = (kMassBins - 1.f) / depth;
+    // (of temperatures below 1e-35 or so it would overflow in the end: the bins are wider there)
+    const float scale = fminf((kMassBins - 1.f) / depth, 1e37f);
     const float floor = cut;
     const float half_top = 0.5f * static_cast<float>(w.top_d), twice = 2.f * scale;      // (differences of halves do not overflow)
     auto bin_of = [&](float z) { return fmaf(fminf(z, 3.4028234663852886e38f), -0.5f, half_top) * twice; };
@@ -753,9 +754,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(SampleParams p, int
     } else {
       const float bin = static_cast<float>(s.bin);
       const float room = fabsf(w.top) * 1e-6f + (1.f + 1e-3f * bin) / scale;
-      rank_in_bin(w.top - (bin + 1.f) / scale - room, w.top - bin / scale + room, [&](float z) {
+      const bool last = bin == kMassBins - 1.f;             // (all that lies below belongs to it, so that a bin with a mass has members)
+      rank_in_bin(last ? -INFINITY : w.top - (bin + 1.f) / scale - room, w.top - bin / scale + room, [&](float z) {
         const float x = bin_of(z);
-        return x >= bin && x < bin + 1.f && z > floor;
+        return x >= bin && (last || x < bin + 1.f) && z > floor;
       }, std::true_type{}, s.base, target);
     }
     known = true;

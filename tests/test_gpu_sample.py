@@ -319,3 +319,28 @@ def test_small_top_k(E, bf16):
         tokens, probs, status = _run(E, z, u, **kw)
         assert status == 0
         _check(z, u, tokens, probs, **kw)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_tiny_temperatures_with_filters(E, bf16):
+    """Temperatures down to the smallest numbers of fp32: only values next to the largest one weigh anything, whatever the filters do with differences
+    of values over the temperature.  Rows of ordinary values, of equal largest ones, and of values about as far apart as the temperature is small."""
+    g = torch.Generator().manual_seed(15)
+    temperatures = torch.tensor([1e-35, 1e-36, 4e-37, 1e-37, 1.2e-38, 1e-40, 1e-45] * 3)
+    B, V = len(temperatures), 12007
+    z = torch.randn(B, 1, V, generator=g) * 3
+    z[7:14, 0, ::5] = z[7:14, 0].max(-1, keepdim=True).values   # (2402 equal ones)
+    z[14:] = torch.randn(B - 14, 1, V, generator=g) * 3 * temperatures[14:, None, None]
+    z = z.bfloat16() if bf16 else z
+    u = torch.rand(B, 1, generator=g)
+    t, p = {"temperature": temperatures}, torch.linspace(0.05, 0.999, B)
+    for kw in ({"top_p": p}, {"top_k": torch.full((B,), 3000).int(), "top_p": p}, {"top_k": torch.full((B,), 300).int(), "top_p": p},
+               {"top_k": torch.full((B,), 40).int(), "top_p": p}, {"top_p": p, "min_p": torch.full((B,), 0.05)}, {"top_k": torch.full((B,), 3000).int()}, {}):
+        for R in (1, 30):                                       # clusters of eight CTAs, and a CTA or two to a row
+            many, uu = z.expand(B, R, V).contiguous(), u.expand(B, R).contiguous()
+            tokens, probs, status = _run(E, many, uu, **kw, **t)
+            assert status == 0 and torch.equal(tokens, tokens[:, :1].expand(B, R)) and torch.equal(probs, probs[:, :1].expand(B, R, V))
+            _check(z, u, tokens[:, :1], probs[:, :1], **kw, **t)
+            only, _, _ = _run(E, many, uu, probs=False, **kw, **t)
+            _, alone, _ = _run(E, many, None, **kw, **t)
+            assert torch.equal(only, tokens) and torch.equal(alone, probs)
