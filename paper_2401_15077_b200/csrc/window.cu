@@ -721,7 +721,7 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
                 x = max3_nan(x, __uint_as_float(raw[e]), __uint_as_float(raw[e + 1]));
                 y = max3_nan(y, __uint_as_float(raw[e + 2]), __uint_as_float(raw[e + 3]));
               }
-              tmax = max3_nan(tmax, fmaf(max3_nan(x, y, -INFINITY), __uint_as_float(c.x) * up, __uint_as_float(c.y)), -INFINITY);
+              tmax = max3_nan(tmax, fmaf(max3_nan(x, y, -INFINITY), score_factor(__uint_as_float(c.x), up), __uint_as_float(c.y)), -INFINITY);
             };
             ld32(s_addr, ra);
 #pragma unroll 1
@@ -802,7 +802,7 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
           const float neg_base = m_ref == -INFINITY ? 0.f : -m_ref;
           if constexpr (CODES) {
             auto exp_group = [&](const uint32_t* raw, int group, const uint4& c) {   // 16 scores with their scales
-              const float a = __uint_as_float(c.x) * up, base = __uint_as_float(c.y) + neg_base + kHalfShift;
+              const float a = score_factor(__uint_as_float(c.x), up), base = __uint_as_float(c.y) + neg_base + kHalfShift;
               const uint64_t scale2 = pack2(a, a), base2 = pack2(base, base);
               uint64_t ls2[2] = {0ull, 0ull};
               uint32_t pk[8];

@@ -29,6 +29,11 @@ __device__ __forceinline__ float fast_rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// What scores over codes are multiplied by: a block's scale times that of the softmax times what the row was divided by.  Masked scores are -infinity, so
+// the product may not come out 0: the least normal number is added.  Factors from 2^-101 on do not change by it, and smaller ones leave scores of 2^-83
+// at the most (the products are below 2^17).
+__device__ __forceinline__ float score_factor(float a, float b) { return fmaf(a, b, 1.17549435e-38f); }
+
 // Of a row whose largest |element| has the bits `top` (bf16, without the sign): 2^e with |element| < 2^(e + 1), and 2^-e by which the row is
 // multiplied before it is rounded to fp16.  Rows of zeros and rows with infinities or NaN (whose output is NaN anyhow) stay as they are.
 struct RowFactor {

@@ -352,7 +352,7 @@ window_codes_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, co
             float x = -INFINITY;
 #pragma unroll
             for (int u = 0; u < kTiles16; ++u) {
-              const float z = fmaf(max3_nan(sc[t][u][j], sc[t][u][2 + j], -INFINITY), ks[u] * scale[t][j], fast_log2(vs[u]));
+              const float z = fmaf(max3_nan(sc[t][u][j], sc[t][u][2 + j], -INFINITY), score_factor(ks[u], scale[t][j]), fast_log2(vs[u]));
               if (!(z < INFINITY)) l[t][j] = __uint_as_float(0x7fffffffu);      // NaN or +inf makes the row NaN
               x = fmaxf(x, z);
             }
@@ -383,7 +383,7 @@ window_codes_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, co
           const float lv = fast_log2(vs[u]) + kHalfShift, iv = fast_rcp(vs[u]);
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            const float a0 = ks[u] * scale[t][0], a1 = ks[u] * scale[t][1];
+            const float a0 = score_factor(ks[u], scale[t][0]), a1 = score_factor(ks[u], scale[t][1]);
             const float c0 = lv - (m[t][0] == -INFINITY ? 0.f : m[t][0]), c1 = lv - (m[t][1] == -INFINITY ? 0.f : m[t][1]);
             const float p0 = fast_exp2(fmaf(sc[t][u][0], a0, c0)), p1 = fast_exp2(fmaf(sc[t][u][1], a1, c1));
             const float p2 = fast_exp2(fmaf(sc[t][u][2], a0, c0)), p3 = fast_exp2(fmaf(sc[t][u][3], a1, c1));

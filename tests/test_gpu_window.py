@@ -476,3 +476,53 @@ def test_tiles_over_codes_whose_copies_land_in_any_order(E, form):
         differ += (out.view(torch.int16) != want.view(torch.int16)).any()
     torch.cuda.synchronize()
     assert int(differ.item()) == 0
+
+
+@pytest.mark.parametrize("form", ["chunk", "tree", "singles", "singles_of_16_heads"])
+def test_small_queries_over_small_scales(E, form):
+    """Query rows down to the smallest numbers over blocks of zeros, whose scales are 2^-40 as the append leaves them, and over scales at the bottom of
+    their range: every score is next to 0, and a key that a row does not see has no weight all the same."""
+    n = [1, 1] if form.startswith("singles") else [40, 33]
+    hq = 16 if form == "singles_of_16_heads" else 8
+    for scale, power in ((2.0 ** -40, -100), (2.0 ** -40, -110), (2.0 ** -40, -120), (2.0 ** -40, -133), (2.0 ** -126, -21), (2.0 ** -126, -60), (2.0 ** -126, -126)):
+        c = Case(n=n, lens=[200, 333], hq=hq, hkv=1 if hq == 16 else 2, block=16, window=90, sinks=3, tree=form == "tree", seed=19, spare=0)
+        c.q = (c.q.float() * 2.0 ** power).bfloat16()
+        c.ks = torch.where(torch.isnan(c.ks), c.ks, torch.full_like(c.ks, scale))
+        c.check(E)
+        c.k = torch.where(c.k == 0x7f, c.k, torch.zeros_like(c.k))      # (what is not visible stays NaN)
+        c.check(E)
+
+
+@pytest.mark.parametrize("form", ["chunk", "tree", "singles"])
+def test_small_queries_over_appended_zeros(E, form):
+    """Keys of zeros and ordinary values through the library's own append, then queries of 2^-120: the mean of the values that a row sees."""
+    tree, hq, hkv, B = form == "tree", 8, 2, 2
+    g, lens = torch.Generator().manual_seed(20), [50, 0]
+    shape = (B, hkv, 192, 128)
+    k, v = (torch.zeros(shape, dtype=torch.uint8, device=DEV) for _ in range(2))
+    scales = [torch.ones(B, hkv, 12, device=DEV) for _ in range(2)]
+    store = E.KVStore(k, v, k_scale=scales[0], v_scale=scales[1], block_size=16)
+    freqs, _ = E.eagle_rope_frequencies(128, device=DEV)
+    for step, n in enumerate(([50, 0], [1, 1] if form == "singles" else [40, 33])):
+        last = step == 1
+        rows = (B, max(n)) if tree and last else (sum(n),)
+        q = (torch.randn(*rows, hq, 128, generator=g) * 2.0 ** -120).bfloat16().to(DEV)
+        kk, vv = torch.zeros(*rows, hkv, 128, dtype=torch.bfloat16, device=DEV), torch.randn(*rows, hkv, 128, generator=g).bfloat16().to(DEV)
+        at = _ints(lens if last else [0, 0])
+        if tree and last:
+            order = torch.zeros(B, max(n), dtype=torch.int32)
+            for i in range(max(n)):
+                order[:, i] = i // 2 - 1
+            q = E.eagle_tree_block_append(q, kk, vv, store, at.to(DEV), order.to(DEV), freqs, tree_sizes=_ints(n).to(DEV))
+        else:
+            order = _ints(np.concatenate([[0], np.cumsum(n)]).tolist())
+            q = E.eagle_block_append(q, kk, vv, store, at.to(DEV), order.to(DEV), freqs)
+    assert (scales[0][0, :, :4] == 2.0 ** -40).all()
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    kw = {"tree_parent": order, "tree_sizes": _ints(n)} if tree else {"token_start": order}
+    fn = E.eagle_tree_window_attn if tree else E.eagle_window_attn
+    got = fn(q, store, _ints(lens).to(DEV), order.to(DEV), status=status, window=70, sinks=2, **({"tree_sizes": _ints(n).to(DEV)} if tree else {}))
+    want, spread = S.window_attn(q.cpu(), k.cpu(), v.cpu(), lens, k_scale=scales[0].cpu(), v_scale=scales[1].cpu(), block=16, window=70, sinks=2, **kw)
+    rows = ~np.isnan(want[..., 0, 0])
+    err = np.abs(got.cpu().double().numpy() - want)[rows]
+    assert int(status.item()) == 0 and (err <= (2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 5e-4) * spread)[rows]).all()
