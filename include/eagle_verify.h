@@ -50,7 +50,8 @@ enum {
   EAGLE_ERR_DEVICE = -9,     /* the GPU is not an sm_100 device, or it lacks a required limit */
   EAGLE_ERR_PATH = -10,      /* device-detected: an accepted path that is not an increasing list of tree nodes whose slots exist */
   EAGLE_ERR_PAGE = -11,        /* device-detected: a block-table entry of a page in use outside [0, num_pages) */
-  EAGLE_ERR_ROW = -12          /* device-detected: a row of logits whose values are all -infinity or NaN: nothing can be drawn from it */
+  EAGLE_ERR_ROW = -12,         /* device-detected: a row of logits whose values are all -infinity or NaN: nothing can be drawn from it */
+  EAGLE_ERR_SCALE = -13        /* device-detected: a scale of values in use that the attention does not take */
 };
 
 #define EAGLE_MAX_TREE 64
@@ -687,7 +688,8 @@ typedef struct eagle_block_desc {
  * nearest e4m3 code of x / scale in fp32 (ties to the even code, magnitudes above 448 become 448, NaN stays NaN).
  * A power of two loses nothing against a finer scale, since codes are floating-point numbers, and storing older codes again costs them
  * at most the bits that leave the bottom of the range.  An old scale has to be a normal number above 0; blocks that hold no slot of a sequence
- * in use may have any.  No block may be shared by two sequences that append.
+ * in use may have any.  No block may be shared by two sequences that append.  Values above 448 * 2^60 are stored, too, but their block's scale is one that
+ * eagle_window_attn reports and does not take.
  */
 int eagle_block_append(const eagle_block_desc* desc, const void* q, const void* k, const void* v, void* q_out, const eagle_kv_store* kv,
                        const int32_t* seq_lens, const int32_t* token_start, eagle_stream_t stream);
@@ -734,7 +736,10 @@ size_t eagle_window_attn_workspace(const eagle_window_desc* desc);
  * Arithmetic: as for eagle_chunk_attn over bf16.  Over codes the products are fp16 (every e4m3 number is one exactly): a query row is
  * scaled by a power of two so that its largest magnitude is in [1, 2), then rounded to fp16 (half a step is 2^-12 of an element, and 2^-25 of the
  * row's largest for those below 2^-14 of it); scores take their block's scale in fp32; a probability times its block's value scale is
- * rounded to fp16; sums are fp32.  Scales of values have to be from 2^-60 to 2^60, those of keys normal numbers above 0.
+ * rounded to fp16; sums are fp32.  Scales of keys have to be normal numbers above 0, those of values from 2^-60 to 2^60: another one that is visible
+ * reports EAGLE_ERR_SCALE, and rows that see it may hold anything.  (The row sum drops weights below 2^-133 of the largest probability times value scale, over
+ * their own value scale.  With value scales within 2^100 of one another, as all are from 2^-40 to 2^60, no weight above 2^-33 of the largest is lost; with 2^60
+ * and 2^-60 in one row those below 2^-13 can be.)
  * A visible score that is NaN or +infinite makes its row NaN.  Slots past the chunk may hold anything; what holds for slots in use and for the size of scores is
  * as for eagle_chunk_attn (values of slots in use have to be finite), with NaN codes in the place of values that are not.
  * Device-detected errors, rows outside every sequence, time-outs, launches and the rule N <= B are those of eagle_chunk_attn, too.

@@ -755,6 +755,7 @@ const char* eagle_status_string(int code) {
     case EAGLE_ERR_PATH: return "invalid accepted path (not increasing, outside the tree, or past the cache)";
     case EAGLE_ERR_PAGE: return "block-table entry of a page in use outside the page pool";
     case EAGLE_ERR_ROW: return "a row of logits that nothing can be drawn from";
+    case EAGLE_ERR_SCALE: return "a scale of values in use outside 2^-60 .. 2^60";
     default: return "unknown status";
   }
 }

@@ -359,9 +359,8 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
         };
         auto read = [&](const Round& r, float& ks, float& vs) {
           ks = vs = 1.f;
-          if (r.row >= 0) {
-            const int page = PAGED && static_cast<uint32_t>(r.page) >= static_cast<uint32_t>(p.num_pages) ? 0 : r.page;
-            const long long place = (static_cast<long long>(page) * p.Hkv + r.g) * p.head_blocks + (r.row >> p.block_shift);
+          if (r.row >= 0 && (!PAGED || static_cast<uint32_t>(r.page) < static_cast<uint32_t>(p.num_pages))) {
+            const long long place = (static_cast<long long>(r.page) * p.Hkv + r.g) * p.head_blocks + (r.row >> p.block_shift);
             ks = __ldg(p.k_scale + place);
             vs = __ldg(p.v_scale + place);
           }
@@ -373,6 +372,7 @@ window_attn_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, con
           const Round later = look_up();
           float ks_next, vs_next;
           read(next, ks_next, vs_next);
+          if (beyond_range(vs) > kScaleRange) report_status(p.status, EAGLE_ERR_SCALE);
           const uint4 entry = make_uint4(__float_as_uint(ks * p.scale_log2), __float_as_uint(fast_log2(vs)), __float_as_uint(fast_rcp(vs)), 0u);
 #pragma unroll 1
           for (int j = 0; j < now.found && ok; ++j, ++steps) {

@@ -34,6 +34,10 @@ __device__ __forceinline__ float fast_rcp(float x) {
 // at the most (the products are below 2^17).
 __device__ __forceinline__ float score_factor(float a, float b) { return fmaf(a, b, 1.17549435e-38f); }
 
+// Value scales that the arithmetic holds for: 2^-60 to 2^60, by their bits (NaN and negative numbers are outside).
+__device__ __forceinline__ uint32_t beyond_range(float vs) { return __float_as_uint(vs) - (67u << 23); }
+constexpr uint32_t kScaleRange = 120u << 23;
+
 // Of a row whose largest |element| has the bits `top` (bf16, without the sign): 2^e with |element| < 2^(e + 1), and 2^-e by which the row is
 // multiplied before it is rounded to fp16.  Rows of zeros and rows with infinities or NaN (whose output is NaN anyhow) stay as they are.
 struct RowFactor {

@@ -88,6 +88,8 @@ __device__ __forceinline__ void arrive_with_copies(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+__device__ const float kNoScale = 1.f;                       // what stands for the scales of a page outside the pool
+
 template <int NT, bool PAGED, bool STALL>                    // (STALL: of the test hook, as in chunk.cu)
 __global__ void __launch_bounds__(kThreads, 1)
 window_codes_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
@@ -226,8 +228,8 @@ window_codes_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, co
     while (more) {
       if (!mbar_wait_warp(empty(ring.slot), ring.par ^ 1u, s_abort)) break;
       if (lane < 8) {
-        if (PAGED && static_cast<unsigned long long>(row) >= static_cast<unsigned long long>(p.num_pages)) row = 0;
-        copy_word(sbase + S::kScale + ring.slot * 32 + lane * 4, scales + (row * p.Hkv + w.it.g) * p.head_blocks + (y >> p.block_shift));
+        const bool out_of_pool = PAGED && static_cast<unsigned long long>(row) >= static_cast<unsigned long long>(p.num_pages);
+        copy_word(sbase + S::kScale + ring.slot * 32 + lane * 4, out_of_pool ? &kNoScale : scales + (row * p.Hkv + w.it.g) * p.head_blocks + (y >> p.block_shift));
         arrive_with_copies(full(ring.slot));
       }
       ring.step();
@@ -324,12 +326,15 @@ window_codes_kernel(ChunkParams p, const __grid_constant__ CUtensorMap map_k, co
         {
           const uint4 a = load_shared(sbase + S::kScale + slot * 32), b = load_shared(sbase + S::kScale + slot * 32 + 16);
           const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+          uint32_t worst = 0;
 #pragma unroll
           for (int u = 0; u < kTiles16; ++u) {
             const bool seen = key0 + u * 16 < in_use && it.span.sees_some(key0 + u * 16, 16);
             ks[u] = seen ? __uint_as_float(wa[u]) : 1.f;
             vs[u] = seen ? __uint_as_float(wb[u]) : 1.f;
+            worst = max(worst, beyond_range(vs[u]));
           }
+          if (worst > kScaleRange) report_status(p.status, EAGLE_ERR_SCALE);
         }
         if (!(key0 + kKeys - 1 <= it.L + it.first && (key0 >= low_last || key0 + kKeys <= p.sinks))) {      // a tile that some row does not see whole
 #pragma unroll

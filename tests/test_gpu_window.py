@@ -526,3 +526,56 @@ def test_small_queries_over_appended_zeros(E, form):
     rows = ~np.isnan(want[..., 0, 0])
     err = np.abs(got.cpu().double().numpy() - want)[rows]
     assert int(status.item()) == 0 and (err <= (2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 5e-4) * spread)[rows]).all()
+
+
+@pytest.mark.parametrize("form", ["chunk", "tree", "singles", "singles_of_16_heads"])
+def test_value_scales_outside_of_their_range(E, form):
+    """A visible one is reported, and the rows of other sequences are as ever; one that nothing sees may be anything."""
+    n = [1, 1, 1] if form.startswith("singles") else [40, 33, 20]
+    hq, hkv = (16, 1) if form == "singles_of_16_heads" else (4, 2)
+    for page in (0, 32):
+        c = Case(n=n, lens=[200, 333, 60], hq=hq, hkv=hkv, block=16, page=page, window=120, sinks=3, tree=form == "tree", seed=21, spare=0)
+        whole, status = c.run(E)
+        assert status == 0
+        own = slice(1, 2) if form == "tree" else slice(n[0], n[0] + n[1])
+        others = torch.ones(whole.shape[0], dtype=torch.bool)
+        others[own] = False
+        for slot, seen in ((300, True), (2, True), (100, False), (340, form != "singles" and form != "singles_of_16_heads")):
+            at, block = (int(c.table[1, slot // page]), slot % page // 16) if page else (1, slot // 16)
+            if at < 0:
+                continue                                     # (a page that nothing sees)
+            old = c.vs[at, -1, block].item()
+            for scale in (2.0 ** -60.5, 2.0 ** 60.5, 2.0 ** 120, 0.0, -1.0, float("inf"), float("nan"), 2.0 ** -60, 2.0 ** 60):
+                wrong = seen and not 2.0 ** -60 <= scale <= 2.0 ** 60
+                c.vs[at, -1, block] = scale
+                out, status = c.run(E)
+                assert status == (-13 if wrong else 0), (slot, scale, status)
+                assert torch.equal(out[others], whole[others]) and (seen or torch.equal(out, whole))
+            c.vs[at, -1, block] = old
+
+
+def test_the_largest_values_that_can_be_attended_to(E):
+    """Through the library's own append: values up to 448 * 2^60 next to zeros; a larger one is stored and reported when it is seen."""
+    g, n = torch.Generator().manual_seed(22), 80
+    for factor, want_status in ((1.0, 0), (1.1, -13)):
+        for singles in (False, True):
+            k, v = (torch.zeros(1, 1, 96, 128, dtype=torch.uint8, device=DEV) for _ in range(2))
+            ks, vs = (torch.ones(1, 1, 6, device=DEV) for _ in range(2))
+            store = E.KVStore(k, v, k_scale=ks, v_scale=vs, block_size=16)
+            freqs, _ = E.eagle_rope_frequencies(128, device=DEV)
+            q, kk, vv = torch.randn(n, 4, 128, generator=g), torch.randn(n, 1, 128, generator=g), torch.randn(n, 1, 128, generator=g)
+            vv[:16] = 0.0
+            vv[16:32] *= 2.0 ** 58
+            vv[20, 0, 5] = 448.0 * 2.0 ** 60 * factor
+            status = torch.zeros(1, dtype=torch.int32, device=DEV)
+            start = _ints([0, n]).to(DEV)
+            q = E.eagle_block_append(q.bfloat16().to(DEV), kk.bfloat16().to(DEV), vv.bfloat16().to(DEV), store, _ints([0]).to(DEV), start, freqs, status=status)
+            assert int(status.item()) == 0 and float(vs[0, 0, 0]) == 2.0 ** -40 and float(vs[0, 0, 1]) == 2.0 ** (60 if factor == 1.0 else 61)
+            lens = [0]
+            if singles:
+                q, lens, start = q[-1:].contiguous(), [n - 1], _ints([0, 1]).to(DEV)
+            got = E.eagle_window_attn(q, store, _ints(lens).to(DEV), start, status=status)
+            assert int(status.item()) == want_status
+            if want_status == 0:
+                want, spread = S.window_attn(q.cpu(), k.cpu(), v.cpu(), lens, token_start=start.cpu(), k_scale=ks.cpu(), v_scale=vs.cpu(), block=16)
+                assert (np.abs(got.cpu().double().numpy() - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 5e-4) * spread).all()

@@ -268,3 +268,8 @@ def test_stores_that_do_not_fit_are_refused(lib):
         E.eagle_window_attn_workspace(1, 10, 6, 4, 128)
     with pytest.raises(E.EagleError):
         E.eagle_sample(torch.zeros(1, 1, 8))                 # not on a GPU
+
+
+def test_the_status_of_a_scale_has_a_name(lib):
+    from paper_2401_15077_b200 import binding
+    assert len({binding.status_string(c) for c in range(-13, 1)}) == 14 and binding.status_string(-13) != "unknown status"
