@@ -219,13 +219,17 @@ __global__ void __launch_bounds__(kThreads) block_kernel(BlockParams p) {
     if (page < 0 || page >= r.num_pages) return -1;
     return static_cast<long long>(page) * r.Hkv * p.head_blocks + ((slot & (r.page_size - 1)) >> p.block_shift);
   };
-  // Codes of an older slot again, by a scale that has grown (16 of a lane).
+  // Codes of an older slot again, by a scale that has grown (16 of a lane).  The products have 28 bits: rounded to fp32, one next to a middle between two
+  // codes would be taken for the middle.  So they are cut off, with the last bit set where something is missing, and rounded once.
   auto store_again = [&](uint8_t* at, float held, float scale) {
     const float ratio = held * __uint_as_float(0x7f000000u - __float_as_uint(scale));      // 1 / 2^e
     float f[16];
     decode(*reinterpret_cast<const uint4*>(at), f);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) f[e] *= ratio;
+    for (int e = 0; e < 16; ++e) {
+      const float cut = __fmul_rz(f[e], ratio);
+      f[e] = __uint_as_float(__float_as_uint(cut) | (fmaf(f[e], ratio, -cut) != 0.f ? 1u : 0u));
+    }
     const uint2 lo = codes(f, 1.f, 1.f), hi = codes(f + 8, 1.f, 1.f);
     *reinterpret_cast<uint4*>(at) = make_uint4(lo.x, lo.y, hi.x, hi.y);
   };

@@ -307,3 +307,18 @@ def test_pages_at_the_far_end_of_a_large_pool(E, tree):
     assert int(state.item()) == 0 and torch.equal(got.cpu(), q)
     for t, want in zip(big, near):
         assert torch.equal(t[far:].cpu(), want)
+
+
+@pytest.mark.parametrize("form", ["chunks", "singles", "trees"])
+def test_older_codes_by_a_scale_that_is_no_power_of_two(E, form):
+    """Stored again, an older code is the nearest one to value(code) * old / new, also where that product lies next to a middle between two codes: old scales are
+    quotients of small numbers, rounded to fp32, so that products of codes with them do (1.7 times a code is off a middle by a rounding of 1.7)."""
+    B = 40
+    n, lens = [1 if form == "singles" else 9] * B, [37 + i % 20 for i in range(B)]
+    c = Case(n, lens, 1, 3, 64, tree="random" if form == "trees" else None, seed=10, scale=(0, 1), spare=0)
+    g = torch.Generator().manual_seed(23)
+    for s in (c.ks, c.vs):
+        num, den = (torch.randint(lo, hi, s.shape, generator=g).double() for lo, hi in ((17, 64), (8, 16)))
+        s[:] = (num / den * torch.exp2(torch.randint(-14, -8, s.shape, generator=g).double())).float()
+    c.check(E)
+    assert (c.got[2].cpu() > c.ks).float().mean() > 0.2      # (they have grown)
