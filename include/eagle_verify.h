@@ -731,7 +731,8 @@ size_t eagle_window_attn_workspace(const eagle_window_desc* desc);
  *     j <= p  and  (W = 0  or  j > p - W  or  j < S).
  * kv holds bf16 (block_size 0, no scales) or block-scaled codes.  Keys and values of slots that no token of the call sees are not used,
  * pages that hold only such slots are not read and their block-table entries may be anything: pages that a window has left behind may go back
- * to the pool.  Work is proportional to what is visible.
+ * to the pool.  Work is proportional to what is visible.  A sequence may have up to 2^31 - 256 slots in use, the new tokens' among them; a longer one reports
+ * EAGLE_ERR_SEQ.
  *
  * Arithmetic: as for eagle_chunk_attn over bf16.  Over codes the products are fp16 (every e4m3 number is one exactly): a query row is
  * scaled by a power of two so that its largest magnitude is in [1, 2), then rounded to fp16 (half a step is 2^-12 of an element, and 2^-25 of the

@@ -245,6 +245,7 @@ int window_call(const eagle_window_desc* desc, bool tree, const void* q, const e
   int rc = check_store(*kv, d.head_dim, d.num_kv_heads, &p.capacity);
   if (rc == EAGLE_OK && d.block_size) rc = check_blocks(*kv, d.block_size);
   if (rc != EAGLE_OK) return rc;
+  p.capacity = std::min(p.capacity, kMaxWindowSlots);
   if (as.batch == 0 || as.num_tokens == 0) return EAGLE_OK;
   if (!q || !kv->k || !kv->v || !seq_lens || !order || !out) return EAGLE_ERR_NULL;
   if (misaligned(q, 16) || misaligned(out, 32)) return EAGLE_ERR_SHAPE;

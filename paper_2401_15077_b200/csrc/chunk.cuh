@@ -98,6 +98,10 @@ struct ChunkParams {
   long long head_blocks;         // blocks from one KV head to the next
 };
 
+// Slots of a sequence in a windowed call: slots up to two query tiles past its end are 32-bit numbers too.  (Without a window a sequence of
+// such a length would be read whole; with one it is a table of pages whose first entries nobody looks at.)
+constexpr long long kMaxWindowSlots = 0x7fffff00ll;
+
 // What a unit whose first token is `first` sees of its sequence: slots below `sinks` and from `low` on.  K/V tiles that hold neither are
 // left out: the plan counts tiles without them, and tile t of the plan is tile(t) of the sequence.
 struct ChunkSpan {

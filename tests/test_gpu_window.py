@@ -579,3 +579,27 @@ def test_the_largest_values_that_can_be_attended_to(E):
             if want_status == 0:
                 want, spread = S.window_attn(q.cpu(), k.cpu(), v.cpu(), lens, token_start=start.cpu(), k_scale=ks.cpu(), v_scale=vs.cpu(), block=16)
                 assert (np.abs(got.cpu().double().numpy() - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 5e-4) * spread).all()
+
+
+@pytest.mark.parametrize("block", [0, 16])
+@pytest.mark.parametrize("form", ["chunk", "tree", "singles"])
+def test_sequences_that_end_where_32_bits_do(E, form, block):
+    """A window at the far end of a sequence of almost 2^31 slots (of whose pages the table holds the last few): up to 2^31 - 256 the same as anywhere else, past it refused."""
+    n = {"chunk": [150], "singles": [1], "tree": [40]}[form]
+    most, page = 2 ** 31 - 256, 256
+    near = 1024 - n[0]                                       # ends with a tile, as the far one does
+    case = Case(n, [near], 8, 2, page=page, block=block, window=300, tree=form == "tree", seed=24, spare=0)
+    want = case.check(E)
+    table = torch.full((1, 2 ** 31 // page), -1, dtype=torch.int32)
+    shift = (most - 1024) // page
+    table[0, shift:shift + 4] = case.table[0, :4]
+    table[0, shift + 4] = case.table[0, 3]
+    case.table = table
+    store = case.store(E)
+    case.lens = [most - n[0]]
+    out, status = case.run(E, store)
+    assert status == 0 and torch.equal(out, want)
+    for more in (1, 100, 255):
+        case.lens = [most - n[0] + more]
+        out, status = case.run(E, store)
+        assert status == -6 and (out == 0).all()
