@@ -737,7 +737,7 @@ size_t eagle_window_attn_workspace(const eagle_window_desc* desc);
  * Arithmetic: as for eagle_chunk_attn over bf16.  Over codes the products are fp16 (every e4m3 number is one exactly): a query row is
  * scaled by a power of two so that its largest magnitude is in [1, 2), then rounded to fp16 (half a step is 2^-12 of an element, and 2^-25 of the
  * row's largest for those below 2^-14 of it); scores take their block's scale in fp32; a probability times its block's value scale is
- * rounded to fp16; sums are fp32.  Scales of keys have to be normal numbers above 0, those of values from 2^-60 to 2^60: another one that is visible
+ * rounded to fp16 (2^-11 of it, or 2^-32 of the row's largest such product); sums are fp32.  Scales of keys have to be normal numbers above 0, those of values from 2^-60 to 2^60: another one that is visible
  * reports EAGLE_ERR_SCALE, and rows that see it may hold anything.  (The row sum drops weights below 2^-133 of the largest probability times value scale, over
  * their own value scale.  With value scales within 2^100 of one another, as all are from 2^-40 to 2^60, no weight above 2^-33 of the largest is lost; with 2^60
  * and 2^-60 in one row those below 2^-13 can be.)
@@ -791,7 +791,8 @@ typedef struct eagle_sample_desc {
  * stays, in ascending order of the id.  A greedy row keeps the first token alone.  NaN logits count as -infinity; where some are +infinity these
  * share the mass.  A row without any value above -infinity reports EAGLE_ERR_ROW: token -1, probs 0.
  *
- * Orders are exact; w is taken in fp64 (relative error below 2^-45) and summed as integers of at most 2^-46 of the largest w (V <= 2^17; 2^-43 at
+ * Orders are exact; w is taken in fp64 (relative error below 2^-45 for w of 2^-47 and more, which are those that sums see, and below 2^-41 down to 2^-980; smaller
+ * ones count as 0) and summed as integers of at most 2^-46 of the largest w (V <= 2^17; 2^-43 at
  * V = 2^20), so results do not depend on how the work is split, and a decision can differ from the definition only where a boundary is nearer than
  * 1e-9 (1e-7 at V = 2^20) of the largest w at the worst, 1e-10 as a rule.  One launch; no workspace.
  */
